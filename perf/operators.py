@@ -70,7 +70,7 @@ def draw(rng):
         C = 8 * _log(rng, 16, 3584)                     # 128 .. 28672
         T = min(_log(rng, 1, 8192), 8192 * 8192 // C)
         return dict(op=op, T=T, C=C, x=rng.choice(["f32", "bf16"]), r=rng.choice(["f32", "bf16"]),
-                    res=rng.random() < 0.7, bits=rng.choice([8, 8, 6, 4]))
+                    res=rng.random() < 0.7, bits=8)
     if op == "gemm":
         N, K = 8 * _log(rng, 32, 2752), 16 * _log(rng, 16, 864)      # 256 .. 22016, 256 .. 13824
         M = min(_log(rng, 1, 4096), max(1, 2048 * 22016 * 4096 // (N * K)))
