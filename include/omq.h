@@ -447,6 +447,96 @@ omq_status omq_adamw_update_dev(omq_stream_t stream, int64_t n, float* p, const 
 /* *step_dev += 1 on `stream` (one thread). */
 omq_status omq_step_advance(omq_stream_t stream, int32_t* step_dev);
 
+/* ------------------------------------------------------------------------------------------
+ * Serving a calibrated block in 8 bits: the codes, steps and zero points that omq_block_fold_pack
+ * writes (wbits <= 8, group 0) run as they are.  One decoder layer is
+ *   omq_rmsnorm_quant -> omq_qgemm_i8 (q|k|v) -> omq_kv_append -> omq_kv_attention ->
+ *   omq_act_quant_per_token -> omq_qgemm_i8 (o) -> omq_rmsnorm_quant -> omq_qgemm_i8 (gate|up) -> ...
+ * Codes are uint8 with a step h and a zero point z per row (Eq. 2): the value is (code - z) h.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { OMQ_F32 = 0, OMQ_BF16 = 1 } omq_dtype;
+
+/* Residual addition, RMSNorm and Q_a in one pass over the row:
+ *   t = x + r;  y = t / sqrt(mean(t^2) + rms_eps) * gain + bias;  (codes, h, z) = Q_a(y)
+ * with Q_a the per-token MinMax quantizer of omq_act_quant_per_token (cfg->abits 2..8, or 16 = off)
+ * and gain, bias the folded norm of omq_block_packed (1/s, -delta/s).
+ *   X [T, C], row stride ldx, of x_dtype (an omq_dtype: the output of a linear); R [T, C] and H [T, C],
+ *   row stride ldr, of r_dtype: the residual stream before and after (R NULL: t = x; H NULL: not
+ *   written; H may be R).  The norm takes the unrounded sum, H holds it rounded to r_dtype.
+ *   gain, bias [C] fp32 (NULL = 1, 0).
+ *   codes [T, C] uint8 (NULL = skip), h [T] fp32 and z [T] int32 (all ignored when abits = 16);
+ *   Xq [T, C] bf16: the values (q - z) h, or bf16(y) when abits = 16 (NULL = skip, but one of codes
+ *   and Xq is required).
+ * A row that holds an infinity or a NaN gets h = NaN, values NaN and codes 0.
+ * C at most 32768; C, ldx and ldr multiples of 8. */
+omq_status omq_rmsnorm_quant(omq_stream_t stream, int64_t T, int64_t C, const void* X, int32_t x_dtype,
+                             int64_t ldx, const void* R, void* H, int32_t r_dtype, int64_t ldr,
+                             const float* gain, const float* bias, float rms_eps, uint8_t* codes, void* Xq,
+                             float* h, int32_t* z, const omq_qcfg* cfg);
+
+/* Product of 8-bit codes with a step and a zero point per token and per output channel (Eq. 4 on
+ * codes):  Y[m, n] = a_h[m] b_h[n] sum_k (A[m, k] - a_z[m]) (B[n, k] - b_z[n]) + bias[n].
+ *   A [M, K] uint8, row stride lda: activation codes; B [N, K] uint8, row stride ldb: weight codes.
+ *   a_h [M], b_h [N] fp32; a_z [M], b_z [N] int32 (NULL = 128: symmetric codes); bias [N] fp32 or NULL.
+ *   Cf [M, N] fp32 and / or Cb [M, N] bf16, row stride ldc (NULL = skip; at least one).
+ * The integer sum is exact for |z| < 2^22 and rounded once to fp32; then come a_h, b_h and the bias, one
+ * rounding each.  K, lda, ldb multiples of 16; N, ldc multiples of 8; M any; K at most 65536. */
+omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A, int64_t lda,
+                        const float* a_h, const int32_t* a_z, const uint8_t* B, int64_t ldb, const float* b_h,
+                        const int32_t* b_z, const float* bias, float* Cf, void* Cb, int64_t ldc,
+                        int32_t* dev_status);
+
+/* Pages of an 8-bit key / value cache.  A page holds `page` consecutive tokens (16, 32, 64 or 128) of
+ * one sequence for every KV head, with one scale per (page, head): the value is (code - 128) scale.
+ * Sequence b holds kv_len[b] tokens (those of the current call included); token j lies in page
+ * page_table[b, j / page], slot j % page.  Tokens beyond kv_len and table entries beyond the last page are
+ * never read.  All pointers device, owned by the caller; offsets are 64-bit.  Page ids and lengths are
+ * checked on the device: one outside the pool, the table or the arguments' bounds sets
+ * OMQ_ERR_INVALID_ARG in dev_status, and the sequence (or page) is skipped: nothing of it is read or
+ * written in the pool. */
+typedef struct {
+  uint8_t* k; uint8_t* v;            /* [n_pages, n_kv, page, 128] codes */
+  float* k_scale; float* v_scale;    /* [n_pages, n_kv] */
+  const int32_t* page_table;         /* [B, max_pages] */
+  const int32_t* kv_len;             /* [B] */
+  int32_t n_pages, n_kv, page, max_pages, B;
+} omq_kv_cache;
+
+/* Interleaved (cos, sin) of t theta^(-2j/128): out [n_pos, 64, 2] fp32, 16-byte aligned. */
+omq_status omq_rope_table(omq_stream_t stream, int32_t n_pos, float theta, float* out);
+
+/* Rotary positions, the [Q, K] LET scale (Eq. 5) and the write of new tokens into the cache.
+ *   cu_q [B + 1] int32: rows cu_q[b] .. cu_q[b+1] - 1 of QKV are sequence b's new tokens, its newest
+ *        (token kv_len[b] - rows + i); at most max_q each, total_q rows in all.  NULL: max_q each.
+ *   QKV [total_q, (n_heads + 2 n_kv) 128] of `dtype`, row stride ld: q | k | v before RoPE (rotate-half
+ *        pairs i, i + 64); rope [n_pos, 64, 2] as omq_rope_table writes it; sa [n_kv*128] or NULL (= 1).
+ *   Qo [total_q, n_heads*128] bf16, row stride ldq: RoPE(q) / sa (sa of the head's KV group).
+ *   k = RoPE(k) sa and v go to the cache: per page and head, scale = max(scale before, max|new| / 127)
+ *        (before = 0 in a page that this call starts); where it grows, the codes of the tokens already
+ *        in the page become 128 + round((code - 128) before / after); new codes are
+ *        128 + clamp(round(value / scale), -127, 127), 128 for a zero scale.
+ *   Ko, Vo [total_q, n_kv*128] bf16, row stride ldkv: the values the new codes stand for, for a prompt's
+ *        own attention (both or neither NULL).
+ * A page that is written belongs to one sequence.  Every product, sum and quotient is one fp32 rounding. */
+omq_status omq_kv_append(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                         const int32_t* cu_q, int32_t n_heads, const void* QKV, int32_t dtype, int64_t ld,
+                         const float* rope, int32_t n_pos, const float* sa, void* Qo, int64_t ldq, void* Ko,
+                         void* Vo, int64_t ldkv, int32_t* dev_status);
+
+/* Causal attention of every sequence's newest tokens over its cache: O = softmax(q k^T / sqrt(128)) v.
+ *   Rows as in omq_kv_append (cu_q, max_q, total_q); row i of sequence b sees the keys
+ *   j <= kv_len[b] - rows + i; query head h reads KV head h / (n_heads / n_kv).
+ *   max_kv: host bound of kv_len.  Q [total_q, n_heads*128] bf16, row stride ldq.
+ *   Of fp32 and / or Ob bf16 [total_q, n_heads*128], row stride ldo; lse [total_q, n_heads] fp32 (NULL =
+ *   skip): log2 of the sum of 2^s, s = q.k log2(e) / sqrt(128).  A row that sees no key: O = 0, lse = -inf.
+ * workspace: omq_kv_attention_workspace_size bytes (may be 0, then NULL is allowed). */
+omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                            const int32_t* cu_q, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq,
+                            float* Of, void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,
+                            int32_t* dev_status);
+size_t omq_kv_attention_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                       int32_t n_kv);
+
 /* Reads the device status word written by kernels (synchronises `stream`).  *host_out receives
  * the word (0 = ok); the return value is OMQ_OK or OMQ_ERR_CUDA if the copy failed. */
 omq_status omq_stream_status(omq_stream_t stream, const int32_t* dev_status, int32_t* host_out);

@@ -83,6 +83,12 @@ class omq_let_stats(Structure):
     _fields_ = [(n, c_void_p) for n in LET_STATS_FIELDS]
 
 
+class omq_kv_cache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("page_table", c_void_p), ("kv_len", c_void_p), ("n_pages", c_int32), ("n_kv", c_int32),
+                ("page", c_int32), ("max_pages", c_int32), ("B", c_int32)]
+
+
 P, I64, I32, F32, SZ = c_void_p, c_int64, c_int32, c_float, c_size_t
 _SIGS = {
     "omq_let_apply": (I32, [P, I64, I64, I64, P, P, P, P, P, P, P, P, P]),
@@ -120,6 +126,12 @@ _SIGS = {
     "omq_adamw_update": (I32, [P, I64, P, P, P, P, F32, F32, F32, F32, F32, I32]),
     "omq_adamw_update_dev": (I32, [P, I64, P, P, P, P, F32, F32, F32, F32, F32, P]),
     "omq_step_advance": (I32, [P, P]),
+    "omq_rmsnorm_quant": (I32, [P, I64, I64, P, I32, I64, P, P, I32, I64, P, P, F32, P, P, P, P, P]),
+    "omq_qgemm_i8": (I32, [P, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P, P, I64, P]),
+    "omq_rope_table": (I32, [P, I32, F32, P]),
+    "omq_kv_append": (I32, [P, P, I32, I32, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
+    "omq_kv_attention": (I32, [P, P, I32, I32, P, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
+    "omq_kv_attention_workspace_size": (SZ, [I32, I32, I32, I32, I32, I32]),
     "omq_stream_status": (I32, [P, P, POINTER(c_int32)]),
     "omq_status_string": (c_char_p, [I32]),
     "omq_version": (I32, []),
@@ -166,6 +178,15 @@ def ptr(t) -> Optional[int]:
         raise ValueError("libomq takes device tensors only")
     if not t.is_contiguous():
         raise ValueError("libomq takes contiguous tensors only")
+    return t.data_ptr()
+
+
+def row_ptr(t) -> Optional[int]:
+    """Device pointer of a CUDA tensor whose rows may be strided (the entry point takes the stride)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("libomq takes device tensors only")
     return t.data_ptr()
 
 
@@ -380,6 +401,42 @@ def omq_adamw_update_dev(n, p, g, m, v, lr, beta1, beta2, eps, weight_decay, ste
 
 def omq_step_advance(step_dev, stream=None):
     check("omq_step_advance", lib().omq_step_advance(stream_handle(stream), ptr(step_dev)))
+
+
+def omq_rmsnorm_quant(T, C, X, x_dtype, ldx, R, H, r_dtype, ldr, gain, bias, rms_eps, codes, Xq, h, z, cfg,
+                      stream=None):
+    check("omq_rmsnorm_quant", lib().omq_rmsnorm_quant(
+        stream_handle(stream), T, C, row_ptr(X), x_dtype, ldx, row_ptr(R), row_ptr(H), r_dtype, ldr, ptr(gain), ptr(bias),
+        rms_eps, ptr(codes), ptr(Xq), ptr(h), ptr(z), ctypes.byref(cfg)))
+
+
+def omq_qgemm_i8(M, N, K, A, lda, a_h, a_z, B, ldb, b_h, b_z, bias, Cf, Cb, ldc, dev_status=None, stream=None):
+    check("omq_qgemm_i8", lib().omq_qgemm_i8(
+        stream_handle(stream), M, N, K, row_ptr(A), lda, ptr(a_h), ptr(a_z), row_ptr(B), ldb, ptr(b_h), ptr(b_z),
+        ptr(bias), row_ptr(Cf), row_ptr(Cb), ldc, ptr(dev_status)))
+
+
+def omq_rope_table(n_pos, theta, out, stream=None):
+    check("omq_rope_table", lib().omq_rope_table(stream_handle(stream), n_pos, theta, ptr(out)))
+
+
+def omq_kv_append(cache, total_q, max_q, cu_q, n_heads, QKV, dtype, ld, rope, n_pos, sa, Qo, ldq, Ko, Vo, ldkv,
+                  dev_status=None, stream=None):
+    check("omq_kv_append", lib().omq_kv_append(
+        stream_handle(stream), ctypes.byref(cache), total_q, max_q, ptr(cu_q), n_heads, row_ptr(QKV), dtype, ld,
+        ptr(rope), n_pos, ptr(sa), row_ptr(Qo), ldq, row_ptr(Ko), row_ptr(Vo), ldkv, ptr(dev_status)))
+
+
+def omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) -> int:
+    return lib().omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv)
+
+
+def omq_kv_attention(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
+                     dev_status=None, stream=None):
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    check("omq_kv_attention", lib().omq_kv_attention(
+        stream_handle(stream), ctypes.byref(cache), total_q, max_q, ptr(cu_q), max_kv, n_heads, row_ptr(Q), ldq,
+        row_ptr(Of), row_ptr(Ob), ldo, ptr(lse), ptr(workspace), ws_bytes, ptr(dev_status)))
 
 
 def omq_stream_status(dev_status, stream=None) -> int:
