@@ -480,11 +480,13 @@ omq_status omq_rmsnorm_quant(omq_stream_t stream, int64_t T, int64_t C, const vo
  *   a_h [M], b_h [N] fp32; a_z [M], b_z [N] int32 (NULL = 128: symmetric codes); bias [N] fp32 or NULL.
  *   Cf [M, N] fp32 and / or Cb [M, N] bf16, row stride ldc (NULL = skip; at least one).
  * The integer sum is exact for |z| < 2^22 and rounded once to fp32; then come a_h, b_h and the bias, one
- * rounding each.  K, lda, ldb multiples of 16; N, ldc multiples of 8; M any; K at most 65536. */
+ * rounding each.  K, lda, ldb multiples of 16; N, ldc multiples of 8; M below 2^22, N below 2^24; K at most 65536.
+ * workspace: omq_qgemm_i8_workspace_size bytes (may be 0, then NULL is allowed). */
 omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A, int64_t lda,
                         const float* a_h, const int32_t* a_z, const uint8_t* B, int64_t ldb, const float* b_h,
                         const int32_t* b_z, const float* bias, float* Cf, void* Cb, int64_t ldc,
-                        int32_t* dev_status);
+                        void* workspace, size_t ws_bytes, int32_t* dev_status);
+size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K);
 
 /* Pages of an 8-bit key / value cache.  A page holds `page` consecutive tokens (16, 32, 64 or 128) of
  * one sequence for every KV head, with one scale per (page, head): the value is (code - 128) scale.

@@ -127,7 +127,8 @@ _SIGS = {
     "omq_adamw_update_dev": (I32, [P, I64, P, P, P, P, F32, F32, F32, F32, F32, P]),
     "omq_step_advance": (I32, [P, P]),
     "omq_rmsnorm_quant": (I32, [P, I64, I64, P, I32, I64, P, P, I32, I64, P, P, F32, P, P, P, P, P]),
-    "omq_qgemm_i8": (I32, [P, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P, P, I64, P]),
+    "omq_qgemm_i8": (I32, [P, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P, P, I64, P, SZ, P]),
+    "omq_qgemm_i8_workspace_size": (SZ, [I64, I64, I64]),
     "omq_rope_table": (I32, [P, I32, F32, P]),
     "omq_kv_append": (I32, [P, P, I32, I32, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
     "omq_kv_attention": (I32, [P, P, I32, I32, P, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
@@ -410,10 +411,16 @@ def omq_rmsnorm_quant(T, C, X, x_dtype, ldx, R, H, r_dtype, ldr, gain, bias, rms
         rms_eps, ptr(codes), ptr(Xq), ptr(h), ptr(z), ctypes.byref(cfg)))
 
 
-def omq_qgemm_i8(M, N, K, A, lda, a_h, a_z, B, ldb, b_h, b_z, bias, Cf, Cb, ldc, dev_status=None, stream=None):
+def omq_qgemm_i8_workspace_size(M, N, K) -> int:
+    return lib().omq_qgemm_i8_workspace_size(M, N, K)
+
+
+def omq_qgemm_i8(M, N, K, A, lda, a_h, a_z, B, ldb, b_h, b_z, bias, Cf, Cb, ldc, workspace=None, dev_status=None,
+                 stream=None):
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     check("omq_qgemm_i8", lib().omq_qgemm_i8(
         stream_handle(stream), M, N, K, row_ptr(A), lda, ptr(a_h), ptr(a_z), row_ptr(B), ldb, ptr(b_h), ptr(b_z),
-        ptr(bias), row_ptr(Cf), row_ptr(Cb), ldc, ptr(dev_status)))
+        ptr(bias), row_ptr(Cf), row_ptr(Cb), ldc, ptr(workspace), ws_bytes, ptr(dev_status)))
 
 
 def omq_rope_table(n_pos, theta, out, stream=None):

@@ -1,11 +1,21 @@
 // Product of 8-bit codes with a step and zero point per token and output channel (omq_qgemm_i8).
 //
-// sum_k (a - za)(b - zb) is formed from the codes moved by 128 (a' = a - 128 fits a signed byte) as
+// sum_k (a - za)(b - zb) is formed from the codes moved by 128 (a' = a - 128, b' = b - 128) as
 //   sum a'b' - za' sum b' - zb' sum a' + K za' zb',   za' = za - 128, zb' = zb - 128,
 // each sum an exact integer; the combination is taken in 64 bits and rounded once to fp32.
+//
+// sm_103a has no integer form of tcgen05.mma and a small integer rate elsewhere, so sum a'b' runs on
+// the fp16 tensor path, exactly: |a'|, |b'| <= 128 are fp16 integers, a product is below 2^14, and fp32
+// sums of up to 1024 of them stay at or below 2^24, where every integer is an fp32 number.  Every 1024
+// steps of K the accumulator is added to 32-bit integers.
 #include "common.cuh"
+#include "tc.cuh"
+#include <cuda_fp16.h>
+#include <cstring>
 
 namespace {
+
+using namespace tc;
 
 struct QgemmArgs {
   int M, N, K;
@@ -14,82 +24,591 @@ struct QgemmArgs {
   const float* bias;
   float* Cf; __nv_bfloat16* Cb; int64_t ldc;
   int32_t* status;
+  // K split over S work items per tile (S > 1): integer partial sums, joined by qgemm_join_kernel
+  int splits, kb_per_split;
+  int32_t* part;              // [S, M, N]
+  int32_t* part_sa;           // [S, M]
+  int32_t* part_sb;           // [S, N]
+  int m_fast;
 };
 
-// 64 x 64 outputs per CTA, 4 x 4 per thread, 64 codes of K at a time through shared memory
-__global__ void __launch_bounds__(256) qgemm_tile_kernel(const QgemmArgs p) {
-  __shared__ int As[64][17], Bs[64][17];
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  int acc[4][4] = {}, sa[4] = {}, sb[4] = {};
-  const int lr = tid >> 2, lc = tid & 3;                 // row and 16-byte chunk this thread loads
-  for (int k0 = 0; k0 < p.K; k0 += 64) {
-    const int k = k0 + 16 * lc;
-    uint4 a = make_uint4(0, 0, 0, 0), b = a;             // beyond the matrix: a' = b' = 0
-    const uint32_t s = 0x80808080u;
-    if (k < p.K && m0 + lr < p.M) {
-      a = __ldg(reinterpret_cast<const uint4*>(p.A + (int64_t)(m0 + lr) * p.lda + k));
-      a.x ^= s; a.y ^= s; a.z ^= s; a.w ^= s;
+// two of the four codes of a word as fp16 integers code - 128: the byte under the exponent of 1024
+// (0x6400 | c = 1024 + c), minus 1152
+__device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
+  const uint32_t u = __byte_perm(w, 0x64646464u, sel);
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// h_a h_b (integer sum) + bias, each step one fp32 rounding
+__device__ __forceinline__ float finish(int acc, long long za, long long zb, int sa, int sb, int K, float ah, float bh,
+                                        bool zeros) {
+  float s;
+  if (zeros) s = __ll2float_rn((long long)acc - za * sb - zb * ((long long)sa - (long long)K * za));
+  else s = __int2float_rn(acc);
+  return __fmul_rn(__fmul_rn(s, ah), bh);
+}
+
+// ================================================================================================
+// many rows: CTA pairs on the tensor cores
+// ================================================================================================
+// A pair of CTAs computes a 256 x 256 tile with one tcgen05.mma of cta_group::2 per 16 steps of K;
+// each CTA holds 128 rows of A and 128 of B.  Roles of a CTA's 20 warps:
+//   0       TMA: raw code tiles [128 x 64] of A and B into a ring (64-byte swizzle)
+//   1       leader CTA: issues the MMAs; other CTA: passes its "tile ready" signals on to the leader
+//   4..11   drain: warps w and w + 4 own the 32 accumulator rows of lane quadrant w % 4, half the columns
+//           each; every 1024 steps of K they add the fp32 accumulator to integers in registers
+//   12..19  convert: one row per thread (12..15 A, 16..19 B), 64 codes to fp16 in the 128-byte swizzled
+//           layout the MMA reads; they also form the rows' code sums for the zero points
+// The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
+constexpr int BM = 128, BN = 256, BK = 64;
+constexpr int RAW = 4, CONV = 4;                  // ring depths
+constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumulation
+constexpr int TC_THREADS = 640;
+constexpr int RAW_BYTES = 2 * 128 * BK, CONV_BYTES = 2 * 128 * BK * 2;
+constexpr int SUM_OFF = RAW * RAW_BYTES + CONV * CONV_BYTES;      // [2][128] sums of A, [2][256] of B
+constexpr int BAR_OFF = SUM_OFF + 2 * (128 + 256) * 4;
+constexpr int TC_SMEM = BAR_OFF + 512 + 1024;
+static_assert(TC_SMEM <= 227 * 1024, "shared memory per CTA");
+
+struct Item { int m0, n0, kb0, nkb, split; };
+
+__device__ __forceinline__ Item item_of(const QgemmArgs& p, int i, int mt, int nt) {
+  const int tiles = mt * nt, t = i % tiles;
+  Item it;
+  it.split = i / tiles;
+  const int mi = p.m_fast ? t % mt : t / nt, ni = p.m_fast ? t / mt : t % nt;
+  it.m0 = mi * 2 * BM;
+  it.n0 = ni * BN;
+  const int all = (p.K + BK - 1) / BK;
+  it.kb0 = it.split * p.kb_per_split;
+  it.nkb = min(all, it.kb0 + p.kb_per_split) - it.kb0;
+  return it;
+}
+
+__device__ __forceinline__ void sts_cluster(uint32_t addr, int v) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+__global__ void __launch_bounds__(TC_THREADS, 1)
+    qgemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const QgemmArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* conv_ring = smem;                                     // 1024-aligned (swizzle atom)
+  uint8_t* raw_ring = smem + CONV * CONV_BYTES;
+  int* sums = reinterpret_cast<int*>(smem + SUM_OFF);            // A: [buf * 128 + row], B: 256 + [buf * 256 + col]
+  uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + BAR_OFF);
+  uint64_t* raw_empty = raw_full + RAW;
+  uint64_t* conv_full = raw_empty + RAW;                         // this CTA's tiles converted
+  uint64_t* peer_full = conv_full + CONV;                        // leader: the other CTA's tiles converted
+  uint64_t* conv_empty = peer_full + CONV;
+  uint64_t* acc_full = conv_empty + CONV;                        // [2]
+  uint64_t* acc_empty = acc_full + 2;                            // [2], leader's
+  uint64_t* sum_full = acc_empty + 2;                            // [2]
+  uint64_t* sum_empty = sum_full + 2;                            // [2]
+  uint64_t* drain = sum_empty + 2;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  const bool leader = rank == 0;
+  const int mt = (p.M + 2 * BM - 1) / (2 * BM), nt = (p.N + BN - 1) / BN;
+  const int total = mt * nt * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const bool zeros = p.az || p.bz;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < RAW; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 8); }
+    for (int s = 0; s < CONV; ++s) { mbar_init(&conv_full[s], 8); mbar_init(&peer_full[s], 1); mbar_init(&conv_empty[s], 1); }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16);
+      mbar_init(&sum_full[b], 4 + 8); mbar_init(&sum_empty[b], 16);   // A: own 4 warps; B: both CTAs' 4 warps
     }
-    if (k < p.K && n0 + lr < p.N) {
-      b = __ldg(reinterpret_cast<const uint4*>(p.B + (int64_t)(n0 + lr) * p.ldb + k));
-      b.x ^= s; b.y ^= s; b.z ^= s; b.w ^= s;
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_holder, 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();                            // both CTAs' barriers initialised before any remote use
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  auto fail = [&]() { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 0 && lane == 0) {
+      // ---------------- raw code tiles ----------------
+      uint32_t it = 0;
+      for (int i = first; i < total && !*abort_flag; i += step) {
+        const Item w = item_of(p, i, mt, nt);
+        for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+          const int s = it % RAW;
+          if (!mbar_wait(&raw_empty[s], ((it / RAW) & 1) ^ 1)) { fail(); break; }
+          uint8_t* dst = raw_ring + s * RAW_BYTES;
+          mbar_expect_tx(&raw_full[s], RAW_BYTES);
+          const int k0 = (w.kb0 + kb) * BK;
+          tma_load_3d(&tmA, &raw_full[s], dst, k0, w.m0 + rank * BM, 0);
+          tma_load_3d(&tmB, &raw_full[s], dst + 128 * BK, k0, w.n0 + rank * 128, 0);
+        }
+      }
+      if (*abort_flag) {                     // no copy may land after this CTA has left
+        const uint32_t from = it > (uint32_t)RAW ? it - RAW : 0u;
+        for (uint32_t j = from; j < it; ++j) mbar_wait(&raw_full[j % RAW], (j / RAW) & 1);
+      }
+    } else if (warp == 1 && lane == 0 && leader) {
+      // ---------------- MMA issuer ----------------
+      constexpr uint32_t idesc = idesc_f16(2 * BM, BN);
+      uint32_t it = 0, ch = 0;
+      bool issued = false;
+      for (int i = first; i < total && !*abort_flag; i += step) {
+        const Item w = item_of(p, i, mt, nt);
+        bool ok = true;
+        for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+          const uint32_t buf = ch & 1;
+          if (kb % CHUNK_KB == 0) {
+            if (!mbar_wait(&acc_empty[buf], ((ch >> 1) & 1) ^ 1)) { fail(); ok = false; break; }
+            tc_fence_after();
+          }
+          const int s = it % CONV;
+          const uint32_t ph = (it / CONV) & 1;
+          if (!mbar_wait(&conv_full[s], ph) || !mbar_wait_cluster(&peer_full[s], ph)) { fail(); ok = false; break; }
+          tc_fence_after();
+          issued = true;
+          const uint32_t sa = smem_u32(conv_ring + s * CONV_BYTES), sb = sa + 128 * BK * 2;
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            umma_bf16_pair(tmem + buf * BN, sdesc(sa + k * 32, 16, 1024), sdesc(sb + k * 32, 16, 1024), idesc,
+                           kb % CHUNK_KB != 0 || k != 0);
+          umma_commit_pair(&conv_empty[s], 0x3);
+          if (kb % CHUNK_KB == CHUNK_KB - 1 || kb == w.nkb - 1) {
+            umma_commit_pair(&acc_full[buf], 0x3);
+            ++ch;
+          }
+        }
+        if (!ok) break;
+      }
+      if (*abort_flag && issued) {           // products in flight end before the tensor memory is released
+        umma_commit_pair(drain, 0x1);
+        mbar_wait(drain, 0);
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ---------------- the other CTA's tiles: ready signals to the leader ----------------
+      uint32_t it = 0;
+      for (int i = first; i < total && !*abort_flag; i += step) {
+        const Item w = item_of(p, i, mt, nt);
+        for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+          const int s = it % CONV;
+          if (!mbar_wait(&conv_full[s], (it / CONV) & 1)) { fail(); break; }
+          mbar_arrive_cluster(mapa_shared(smem_u32(&peer_full[s]), 0));
+        }
+      }
     }
-    __syncthreads();
-    As[lr][4 * lc] = a.x; As[lr][4 * lc + 1] = a.y; As[lr][4 * lc + 2] = a.z; As[lr][4 * lc + 3] = a.w;
-    Bs[lr][4 * lc] = b.x; Bs[lr][4 * lc + 1] = b.y; Bs[lr][4 * lc + 2] = b.z; Bs[lr][4 * lc + 3] = b.w;
-    __syncthreads();
+  } else if (warp < 12) {
+    // ---------------- drain: fp32 accumulators -> integers -> outputs ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    const int q = warp & 3, c0 = warp >= 8 ? BN / 2 : 0;
+    uint32_t ch = 0, tile = 0;
+    for (int i = first; i < total; i += step, ++tile) {
+      const Item w = item_of(p, i, mt, nt);
+      int acc[BN / 2];
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      int av[4], bv[4];
+      for (int j = 0; j < BN / 2; ++j) acc[j] = 0;
+      bool ok = true;
+      for (int kb = 0; kb < w.nkb; kb += CHUNK_KB, ++ch) {
+        const uint32_t buf = ch & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (ch >> 1) & 1));
+        if (!ok) { fail(); break; }
+        tc_fence_after();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { av[i] = As[ty + 16 * i][w]; bv[i] = Bs[tx + 16 * i][w]; }
+        for (int j = 0; j < BN / 2; j += 16) {
+          float v[16];
+          tmem_ld16(tmem + buf * BN + ((uint32_t)(q * 32) << 16) + c0 + j, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sa[i] = __dp4a(av[i], 0x01010101, sa[i]);
-        sb[i] = __dp4a(bv[i], 0x01010101, sb[i]);
+          for (int e = 0; e < 16; ++e) acc[j + e] += __float2int_rn(v[e]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&acc_empty[buf]), 0));
+      }
+      if (!ok) break;
+      const uint32_t sbuf = tile & 1;
+      const int* sumA = sums + sbuf * 128;
+      const int* sumB = sums + 256 + sbuf * 256;
+      const int row_l = q * 32 + lane, m = w.m0 + rank * BM + row_l;
+      int sa = 0;
+      if (zeros) {
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_full[sbuf], (tile >> 1) & 1));
+        if (!ok) { fail(); break; }
+        sa = sumA[row_l];
+      }
+      if (p.splits > 1) {
+        if (m < p.M) {
+          int32_t* out = p.part + ((int64_t)w.split * p.M + m) * p.N + w.n0 + c0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(av[i], bv[j], acc[i][j]);
+          for (int j = 0; j < BN / 2; j += 4)
+            if (w.n0 + c0 + j < p.N) *reinterpret_cast<int4*>(out + j) = make_int4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+          if (zeros && w.n0 == 0 && c0 == 0) p.part_sa[(int64_t)w.split * p.M + m] = sa;
+        }
+        if (zeros && w.m0 == 0 && rank == 0 && q == 0) {
+#pragma unroll
+          for (int j = 0; j < BN / 2; j += 32)
+            if (w.n0 + c0 + j + lane < p.N) p.part_sb[(int64_t)w.split * p.N + w.n0 + c0 + j + lane] = sumB[c0 + j + lane];
+        }
+      } else if (m < p.M) {
+        const float ah = __ldg(p.ah + m);
+        const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0;
+#pragma unroll
+        for (int j = 0; j < BN / 2; j += 8) {
+          const int n = w.n0 + c0 + j;
+          if (n < p.N) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+              const float4 bh = __ldg(reinterpret_cast<const float4*>(p.bh + n + e));
+              int4 zb = make_int4(128, 128, 128, 128), sb = make_int4(0, 0, 0, 0);
+              if (p.bz) zb = __ldg(reinterpret_cast<const int4*>(p.bz + n + e));
+              if (zeros) sb = *reinterpret_cast<const int4*>(sumB + c0 + j + e);
+              y[e] = finish(acc[j + e], za, (long long)zb.x - 128, sa, sb.x, p.K, ah, bh.x, zeros);
+              y[e + 1] = finish(acc[j + e + 1], za, (long long)zb.y - 128, sa, sb.y, p.K, ah, bh.y, zeros);
+              y[e + 2] = finish(acc[j + e + 2], za, (long long)zb.z - 128, sa, sb.z, p.K, ah, bh.z, zeros);
+              y[e + 3] = finish(acc[j + e + 3], za, (long long)zb.w - 128, sa, sb.w, p.K, ah, bh.w, zeros);
+              if (p.bias) {
+                const float4 b = __ldg(reinterpret_cast<const float4*>(p.bias + n + e));
+                y[e] = __fadd_rn(y[e], b.x); y[e + 1] = __fadd_rn(y[e + 1], b.y);
+                y[e + 2] = __fadd_rn(y[e + 2], b.z); y[e + 3] = __fadd_rn(y[e + 3], b.w);
+              }
+            }
+            const int64_t at = (int64_t)m * p.ldc + n;
+            if (p.Cf) {
+              reinterpret_cast<float4*>(p.Cf + at)[0] = make_float4(y[0], y[1], y[2], y[3]);
+              reinterpret_cast<float4*>(p.Cf + at)[1] = make_float4(y[4], y[5], y[6], y[7]);
+            }
+            if (p.Cb) *reinterpret_cast<uint4*>(p.Cb + at) = pack_bf16x8(y);
+          }
+        }
+      }
+      if (zeros) {
+        __syncwarp();
+        if (lane < 2) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_empty[sbuf]), lane));
+      }
+    }
+  } else {
+    // ---------------- convert ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const bool is_b = warp >= 16;
+    const int r = threadIdx.x & 127;
+    const bool want_sum = zeros && (is_b ? p.az != nullptr : p.bz != nullptr);
+    uint32_t it = 0, tile = 0;
+    bool ok = true;
+    for (int i = first; i < total && ok && !*abort_flag; i += step, ++tile) {
+      const Item w = item_of(p, i, mt, nt);
+      int sum = 0;
+      for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+        const int rs = it % RAW, cs = it % CONV;
+        ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[rs], (it / RAW) & 1));
+        if (!ok) { fail(); break; }
+        const uint32_t src = smem_u32(raw_ring + rs * RAW_BYTES + (is_b ? 128 * BK : 0)) + r * BK;
+        uint4 u[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) u[c] = lds128(src + ((c ^ ((r >> 1) & 3)) << 4));
+        ok = __all_sync(0xffffffffu, mbar_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1));
+        if (!ok) { fail(); break; }
+        const uint32_t dst = smem_u32(conv_ring + cs * CONV_BYTES + (is_b ? 128 * BK * 2 : 0)) + r * 128;
+        const int k0 = (w.kb0 + kb) * BK;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;      // codes beyond K add nothing
+          if (k0 + 16 * c < p.K) {
+            if (want_sum) {
+              const uint32_t x = 0x80808080u;
+              sum = __dp4a((int)(u[c].x ^ x), 0x01010101, sum);
+              sum = __dp4a((int)(u[c].y ^ x), 0x01010101, sum);
+              sum = __dp4a((int)(u[c].z ^ x), 0x01010101, sum);
+              sum = __dp4a((int)(u[c].w ^ x), 0x01010101, sum);
+            }
+            lo = make_uint4(half_codes(u[c].x, 0x4140), half_codes(u[c].x, 0x4342), half_codes(u[c].y, 0x4140),
+                            half_codes(u[c].y, 0x4342));
+            hi = make_uint4(half_codes(u[c].z, 0x4140), half_codes(u[c].z, 0x4342), half_codes(u[c].w, 0x4140),
+                            half_codes(u[c].w, 0x4342));
+          }
+          sts128(dst + (((2 * c) ^ (r & 7)) << 4), lo);
+          sts128(dst + (((2 * c + 1) ^ (r & 7)) << 4), hi);
+        }
+        fence_async_smem();                  // the converted tile -> visible to the tensor core
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&raw_empty[rs]);
+          mbar_arrive(&conv_full[cs]);
+        }
+      }
+      if (!ok) break;
+      if (zeros) {
+        const uint32_t sbuf = tile & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_empty[sbuf], ((tile >> 1) & 1) ^ 1));
+        if (!ok) { fail(); break; }
+        if (is_b) {                          // this CTA's 128 columns of the tile, to both CTAs
+          const uint32_t at = smem_u32(sums + 256 + sbuf * 256 + rank * 128 + r);
+          sts_cluster(mapa_shared(at, 0), sum);
+          sts_cluster(mapa_shared(at, 1), sum);
+          __syncwarp();
+          if (lane < 2) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_full[sbuf]), lane));
+        } else {
+          sums[sbuf * 128 + r] = sum;
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_full[sbuf]), rank));
+        }
       }
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int m = m0 + ty + 16 * i;
-    if (m >= p.M) continue;
-    const int za = p.az ? p.az[m] - 128 : 0;
-    const float ah = p.ah[m];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + tx + 16 * j;
-      if (n >= p.N) continue;
-      const int zb = p.bz ? p.bz[n] - 128 : 0;
-      const long long s = (long long)acc[i][j] - (long long)za * sb[j] - (long long)zb * sa[i] +
-                          (long long)p.K * za * zb;
-      float y = __fmul_rn(__fmul_rn(__ll2float_rn(s), ah), p.bh[n]);
-      if (p.bias) y = __fadd_rn(y, p.bias[n]);
-      if (p.Cf) p.Cf[(int64_t)m * p.ldc + n] = y;
-      if (p.Cb) p.Cb[(int64_t)m * p.ldc + n] = f_to_bf16(y);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();                            // no CTA leaves while its peer may still signal it
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+// sums of the splits -> outputs; four columns per thread
+__global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int nv = p.N >> 2;
+  if (i >= (int64_t)p.M * nv) return;
+  const int m = (int)(i / nv), n = (int)(i % nv) * 4;
+  const bool zeros = p.az || p.bz;
+  int a[4] = {}, b[4] = {}, sa = 0;
+  for (int s = 0; s < p.splits; ++s) {
+    const int4 v = *reinterpret_cast<const int4*>(p.part + ((int64_t)s * p.M + m) * p.N + n);
+    a[0] += v.x; a[1] += v.y; a[2] += v.z; a[3] += v.w;
+    if (zeros) {
+      sa += p.part_sa[(int64_t)s * p.M + m];
+      const int4 t = *reinterpret_cast<const int4*>(p.part_sb + (int64_t)s * p.N + n);
+      b[0] += t.x; b[1] += t.y; b[2] += t.z; b[3] += t.w;
     }
   }
+  const float ah = __ldg(p.ah + m);
+  const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0;
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const long long zb = p.bz ? (long long)__ldg(p.bz + n + e) - 128 : 0;
+    y[e] = finish(a[e], za, zb, sa, b[e], p.K, ah, __ldg(p.bh + n + e), zeros);
+    if (p.bias) y[e] = __fadd_rn(y[e], __ldg(p.bias + n + e));
+  }
+  const int64_t at = (int64_t)m * p.ldc + n;
+  if (p.Cf) *reinterpret_cast<float4*>(p.Cf + at) = make_float4(y[0], y[1], y[2], y[3]);
+  if (p.Cb) {
+    uint2 u;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
+    h[0] = __floats2bfloat162_rn(y[0], y[1]);
+    h[1] = __floats2bfloat162_rn(y[2], y[3]);
+    *reinterpret_cast<uint2*>(p.Cb + at) = u;
+  }
+}
+
+// ================================================================================================
+// few rows: the weight read is the bound
+// ================================================================================================
+// A warp forms 16 output channels x 8 NT tokens by mma.sync m16n8k16: the weight rows are the M
+// dimension and are converted in registers on their way from HBM, the activation codes are the N
+// dimension.  K is split over the warps of the CTA (their integer sums are joined in shared memory),
+// so that N / 16 CTAs are enough to load every SM.  K is numbered inside the products so that each
+// thread's operand values are 16 consecutive codes of its row.
+constexpr int FEW_WARPS = 8;
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pick(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
+
+__device__ __forceinline__ int code_sum(const uint4& u, int s) {
+  const uint32_t x = 0x80808080u;
+  s = __dp4a((int)(u.x ^ x), 0x01010101, s);
+  s = __dp4a((int)(u.y ^ x), 0x01010101, s);
+  s = __dp4a((int)(u.z ^ x), 0x01010101, s);
+  return __dp4a((int)(u.w ^ x), 0x01010101, s);
+}
+
+// 16 codes 128 (value 0): what lies beyond the matrix
+__device__ __forceinline__ uint4 no_codes() { return make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u); }
+
+template <int NT>
+__global__ void __launch_bounds__(FEW_WARPS * 32) qgemm_few_kernel(const QgemmArgs p) {
+  __shared__ int red[FEW_WARPS][16][8 * NT + 1];
+  __shared__ int red_b[FEW_WARPS][16], red_a[FEW_WARPS][8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * NT;
+  const bool sum_b = p.az != nullptr, sum_a = p.bz != nullptr;
+  const int r0 = n0 + g, r1 = n0 + g + 8;
+  const uint8_t* w0 = p.B + (int64_t)min(r0, p.N - 1) * p.ldb + 16 * t;
+  const uint8_t* w1 = p.B + (int64_t)min(r1, p.N - 1) * p.ldb + 16 * t;
+  int acc[NT][4], sb0 = 0, sb1 = 0, sa[NT];
+  float d[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    sa[j] = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { acc[j][e] = 0; d[j][e] = 0.f; }
+  }
+  int pending = 0;                            // steps of 64 codes in the fp32 sums
+  // the warps take 64-code steps in turn; the next step's weights are in flight while one is used
+  int k = 64 * warp;
+  uint4 a0 = no_codes(), a1 = no_codes();
+  if (k + 16 * t < p.K) { a0 = __ldg((const uint4*)(w0 + k)); a1 = __ldg((const uint4*)(w1 + k)); }
+  while (k < p.K) {
+    const int kn = k + 64 * FEW_WARPS;
+    uint4 b0 = no_codes(), b1 = no_codes();
+    if (kn + 16 * t < p.K) { b0 = __ldg((const uint4*)(w0 + kn)); b1 = __ldg((const uint4*)(w1 + kn)); }
+    uint4 x[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int m = m0 + 8 * j + g;
+      x[j] = no_codes();
+      if (m < p.M && k + 16 * t < p.K) x[j] = __ldg(reinterpret_cast<const uint4*>(p.A + (int64_t)m * p.lda + k + 16 * t));
+      if (sum_a) sa[j] = code_sum(x[j], sa[j]);
+    }
+    if (sum_b) { sb0 = code_sum(a0, sb0); sb1 = code_sum(a1, sb1); }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = pick(a0, i), v = pick(a1, i);
+      const uint32_t f0 = half_codes(u, 0x4140), f1 = half_codes(v, 0x4140), f2 = half_codes(u, 0x4342), f3 = half_codes(v, 0x4342);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const uint32_t y = pick(x[j], i);
+        mma16816(d[j], f0, f1, f2, f3, half_codes(y, 0x4140), half_codes(y, 0x4342));
+      }
+    }
+    if (++pending == 16) {                    // 1024 codes: the fp32 sums are still exact integers
+      pending = 0;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { acc[j][e] += __float2int_rn(d[j][e]); d[j][e] = 0.f; }
+    }
+    a0 = b0; a1 = b1;
+    k = kn;
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[j][e] += __float2int_rn(d[j][e]);
+      red[warp][g + 8 * (e >> 1)][8 * j + 2 * t + (e & 1)] = acc[j][e];
+    }
+    sa[j] += __shfl_xor_sync(0xffffffffu, sa[j], 1);
+    sa[j] += __shfl_xor_sync(0xffffffffu, sa[j], 2);
+    if (t == 0) red_a[warp][8 * j + g] = sa[j];
+  }
+  sb0 += __shfl_xor_sync(0xffffffffu, sb0, 1); sb0 += __shfl_xor_sync(0xffffffffu, sb0, 2);
+  sb1 += __shfl_xor_sync(0xffffffffu, sb1, 1); sb1 += __shfl_xor_sync(0xffffffffu, sb1, 2);
+  if (t == 0) { red_b[warp][g] = sb0; red_b[warp][g + 8] = sb1; }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * 8 * NT; i += FEW_WARPS * 32) {
+    const int c = i & 15, mr = i >> 4, n = n0 + c, m = m0 + mr;
+    if (n >= p.N || m >= p.M) continue;
+    int s = 0, ta = 0, tb = 0;
+#pragma unroll
+    for (int w = 0; w < FEW_WARPS; ++w) { s += red[w][c][mr]; ta += red_a[w][mr]; tb += red_b[w][c]; }
+    const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0, zb = p.bz ? (long long)__ldg(p.bz + n) - 128 : 0;
+    float y = finish(s, za, zb, ta, tb, p.K, __ldg(p.ah + m), __ldg(p.bh + n), sum_a || sum_b);
+    if (p.bias) y = __fadd_rn(y, __ldg(p.bias + n));
+    if (p.Cf) p.Cf[(int64_t)m * p.ldc + n] = y;
+    if (p.Cb) p.Cb[(int64_t)m * p.ldc + n] = f_to_bf16(y);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+constexpr int FEW_ROWS = 32;
+
+struct QPlan { int splits, kb_per_split; };
+
+// K split of the tensor-core form: as many pieces as keep every CTA pair busy, none under 512 codes
+QPlan plan_of(int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), pairs = omq_num_sms() / 2, kbs = (K + BK - 1) / BK;
+  int64_t s = tiles < pairs ? pairs / tiles : 1;
+  const int64_t most = kbs / 8 > 0 ? kbs / 8 : 1;
+  if (s > most) s = most;
+  const int64_t per = (kbs + s - 1) / s;
+  return {(int)((kbs + per - 1) / per), (int)per};
 }
 
 }  // namespace
 
+extern "C" size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (M <= FEW_ROWS || N <= 0 || K <= 0) return 0;
+  const QPlan q = plan_of(M, N, K);
+  if (q.splits <= 1) return 0;
+  return (size_t)q.splits * ((size_t)M * N + (size_t)((M + 3) / 4 * 4) + N) * sizeof(int32_t);
+}
+
 extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A, int64_t lda,
                                    const float* a_h, const int32_t* a_z, const uint8_t* B, int64_t ldb, const float* b_h,
                                    const int32_t* b_z, const float* bias, float* Cf, void* Cb, int64_t ldc,
-                                   int32_t* dev_status) {
-  OMQ_REQUIRE(M > 0 && N > 0 && K > 0 && M < (1 << 22) && N < (1 << 30) && K <= 65536, OMQ_ERR_SHAPE);
+                                   void* workspace, size_t ws_bytes, int32_t* dev_status) {
+  OMQ_REQUIRE(M > 0 && N > 0 && K > 0 && M < (1 << 22) && N < (1 << 24) && K <= 65536, OMQ_ERR_SHAPE);
   OMQ_REQUIRE(A && B && a_h && b_h && (Cf || Cb), OMQ_ERR_INVALID_ARG);
   OMQ_REQUIRE(lda >= K && ldb >= K && ldc >= N, OMQ_ERR_SHAPE);
   OMQ_REQUIRE(K % 16 == 0 && lda % 16 == 0 && ldb % 16 == 0 && N % 8 == 0 && ldc % 8 == 0, OMQ_ERR_ALIGN);
   OMQ_REQUIRE(omq_aligned16(A) && omq_aligned16(B) && omq_aligned16(a_h) && omq_aligned16(b_h) && omq_aligned16(a_z) &&
-                  omq_aligned16(b_z) && omq_aligned16(bias) && omq_aligned16(Cf) && omq_aligned16(Cb),
+                  omq_aligned16(b_z) && omq_aligned16(bias) && omq_aligned16(Cf) && omq_aligned16(Cb) &&
+                  omq_aligned16(workspace),
               OMQ_ERR_ALIGN);
-  const QgemmArgs p{(int)M, (int)N, (int)K, A, lda, a_h, a_z, B, ldb, b_h, b_z, bias, Cf, (__nv_bfloat16*)Cb, ldc, dev_status};
-  const dim3 grid((unsigned)((N + 63) / 64), (unsigned)((M + 63) / 64));
-  qgemm_tile_kernel<<<grid, 256, 0, (cudaStream_t)stream>>>(p);
+  const size_t need = omq_qgemm_i8_workspace_size(M, N, K);
+  OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
+  cudaStream_t st = (cudaStream_t)stream;
+  QgemmArgs p{};
+  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  p.A = A; p.lda = lda; p.ah = a_h; p.az = a_z;
+  p.B = B; p.ldb = ldb; p.bh = b_h; p.bz = b_z;
+  p.bias = bias; p.Cf = Cf; p.Cb = (__nv_bfloat16*)Cb; p.ldc = ldc; p.status = dev_status;
+  if (M <= FEW_ROWS) {
+    const unsigned gx = (unsigned)((N + 15) / 16);
+    if (M <= 8) qgemm_few_kernel<1><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
+    else if (M <= 16) qgemm_few_kernel<2><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
+    else qgemm_few_kernel<4><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
+    OMQ_LAUNCH_CHECK();
+    return OMQ_OK;
+  }
+  const QPlan q = plan_of(M, N, K);
+  p.splits = q.splits; p.kb_per_split = q.kb_per_split;
+  if (q.splits > 1) {
+    p.part = (int32_t*)workspace;
+    p.part_sb = p.part + (size_t)q.splits * M * N;              // N and M N are multiples of 4: 16-byte aligned
+    p.part_sa = p.part_sb + (size_t)q.splits * N;
+  }
+  p.m_fast = (double)M > 1.5 * (double)N ? 0 : 1;               // keep the smaller operand in L2
+  CUtensorMap ta, tb;
+  if (!omq_make_map_u8(&ta, A, K, M, lda, 128) || !omq_make_map_u8(&tb, B, K, N, ldb, 128)) return OMQ_ERR_UNSUPPORTED;
+  static bool attr_set = false;
+  if (!attr_set) {
+    if (cudaFuncSetAttribute(qgemm_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM) != cudaSuccess)
+      return OMQ_ERR_CUDA;
+    attr_set = true;
+  }
+  const int64_t items = ((M + 255) / 256) * ((N + 255) / 256) * q.splits, pairs = omq_num_sms() / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * (items < pairs ? items : pairs)), 1, 1);
+  cfg.blockDim = dim3(TC_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = TC_SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, qgemm_tc_kernel, ta, tb, p) != cudaSuccess) { cudaGetLastError(); return OMQ_ERR_CUDA; }
   OMQ_LAUNCH_CHECK();
+  if (q.splits > 1) {
+    const int64_t n = M * (N / 4);
+    qgemm_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p);
+    OMQ_LAUNCH_CHECK();
+  }
   return OMQ_OK;
 }

@@ -112,8 +112,10 @@ def qgemm(a, a_h, a_z, w, w_h, w_z, bias=None, out=None, out_dtype=F32, status=N
         out = torch.empty(M, N, dtype=out_dtype, device=a.device)
     ldc = _rows(out, "out", (F32, BF16), N, M)
     f32 = out.dtype == F32
+    need = _lib.omq_qgemm_i8_workspace_size(M, N, K)
+    ws = torch.empty(need, dtype=torch.uint8, device=a.device) if need else None
     _lib.omq_qgemm_i8(M, N, K, a, lda, a_h, a_z, w, ldw, w_h, w_z, bias, out if f32 else None, None if f32 else out, ldc,
-                      status)
+                      ws, status)
     return out
 
 

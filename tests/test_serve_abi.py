@@ -30,8 +30,8 @@ def test_norm_refusals(kw, code):
 
 
 def _gemm(M=4, N=64, K=128, A=FAKE, lda=128, ah=FAKE, az=None, B=FAKE, ldb=128, bh=FAKE, bz=None, bias=None, Cf=FAKE,
-          Cb=None, ldc=64):
-    return _lib.lib().omq_qgemm_i8(None, M, N, K, A, lda, ah, az, B, ldb, bh, bz, bias, Cf, Cb, ldc, None)
+          Cb=None, ldc=64, ws=None, ws_bytes=0):
+    return _lib.lib().omq_qgemm_i8(None, M, N, K, A, lda, ah, az, B, ldb, bh, bz, bias, Cf, Cb, ldc, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -39,7 +39,9 @@ def _gemm(M=4, N=64, K=128, A=FAKE, lda=128, ah=FAKE, az=None, B=FAKE, ldb=128, 
     (dict(lda=112), SHAPE), (dict(ldb=112), SHAPE), (dict(ldc=56), SHAPE), (dict(M=1 << 22), SHAPE),
     (dict(K=120), ALIGN), (dict(lda=136), ALIGN), (dict(ldb=136), ALIGN), (dict(N=60), ALIGN), (dict(ldc=68), ALIGN),
     (dict(A=FAKE + 8), ALIGN), (dict(bias=FAKE + 4), ALIGN), (dict(az=FAKE + 4), ALIGN), (dict(A=None), INVALID),
-    (dict(B=None), INVALID), (dict(ah=None), INVALID), (dict(bh=None), INVALID), (dict(Cf=None), INVALID)])
+    (dict(B=None), INVALID), (dict(ah=None), INVALID), (dict(bh=None), INVALID), (dict(Cf=None), INVALID), (dict(ws=FAKE + 8), ALIGN),
+    (dict(M=200, K=8192, lda=8192, ldb=8192), WORKSPACE),
+    (dict(M=200, K=8192, lda=8192, ldb=8192, ws=FAKE, ws_bytes=64), WORKSPACE)])
 def test_gemm_refusals(kw, code):
     assert _gemm(**kw) == code
 

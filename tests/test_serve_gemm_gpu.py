@@ -78,8 +78,10 @@ def test_both_outputs_repeat_and_side_stream(cuda_lib, M):
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    need = _lib.omq_qgemm_i8_workspace_size(M, 776, 2064)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     torch.cuda.synchronize()
-    _lib.omq_qgemm_i8(M, 776, 2064, a, 2064, ah, az, w, 2064, wh, wz, bias, f, h, 776, status, stream=s)
+    _lib.omq_qgemm_i8(M, 776, 2064, a, 2064, ah, az, w, 2064, wh, wz, bias, f, h, 776, ws, status, stream=s)
     s.synchronize()
     want = _want(a, ah, az, w, wh, wz, bias)
     assert torch.equal(f, want) and torch.equal(h, want.to(BF16)) and int(status) == 0
