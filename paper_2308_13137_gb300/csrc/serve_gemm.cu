@@ -40,6 +40,15 @@ __device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// s + the sum of 16 codes moved by 128
+__device__ __forceinline__ int code_sum(const uint4& u, int s) {
+  const uint32_t x = 0x80808080u;
+  s = __dp4a((int)(u.x ^ x), 0x01010101, s);
+  s = __dp4a((int)(u.y ^ x), 0x01010101, s);
+  s = __dp4a((int)(u.z ^ x), 0x01010101, s);
+  return __dp4a((int)(u.w ^ x), 0x01010101, s);
+}
+
 // h_a h_b (integer sum) + bias, each step one fp32 rounding
 __device__ __forceinline__ float finish(int acc, long long za, long long zb, int sa, int sb, int K, float ah, float bh,
                                         bool zeros) {
@@ -55,19 +64,21 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 // A pair of CTAs computes a 256 x 256 tile with one tcgen05.mma of cta_group::2 per 16 steps of K;
 // each CTA holds 128 rows of A and 128 of B.  Roles of a CTA's 20 warps:
 //   0       TMA: raw code tiles [128 x 64] of A and B into a ring (64-byte swizzle)
-//   1       leader CTA: issues the MMAs; other CTA: passes its "tile ready" signals on to the leader
+//   1       leader CTA: issues the MMAs
 //   4..11   drain: warps w and w + 4 own the 32 accumulator rows of lane quadrant w % 4, half the columns
 //           each; every 1024 steps of K they add the fp32 accumulator to integers in registers
-//   12..19  convert: one row per thread (12..15 A, 16..19 B), 64 codes to fp16 in the 128-byte swizzled
-//           layout the MMA reads; they also form the rows' code sums for the zero points
+//   12..19  convert: 64 codes of a row per thread, A and B, to fp16 in the 128-byte swizzled layout the MMA
+//           reads; warps 12..15 take the even stages and 16..19 the odd ones, so that one group's waits
+//           and proxy fence overlap the other's work.  They also form the rows' code sums for the
+//           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
 constexpr int BM = 128, BN = 256, BK = 64;
 constexpr int RAW = 4, CONV = 4;                  // ring depths
 constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumulation
 constexpr int TC_THREADS = 640;
 constexpr int RAW_BYTES = 2 * 128 * BK, CONV_BYTES = 2 * 128 * BK * 2;
-constexpr int SUM_OFF = RAW * RAW_BYTES + CONV * CONV_BYTES;      // [2][128] sums of A, [2][256] of B
-constexpr int BAR_OFF = SUM_OFF + 2 * (128 + 256) * 4;
+constexpr int SUM_OFF = RAW * RAW_BYTES + CONV * CONV_BYTES;      // 2 tiles x 2 groups: [128] sums of A, [256] of B
+constexpr int BAR_OFF = SUM_OFF + 4 * (128 + 256) * 4;
 constexpr int TC_SMEM = BAR_OFF + 512 + 1024;
 static_assert(TC_SMEM <= 227 * 1024, "shared memory per CTA");
 
@@ -96,12 +107,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* conv_ring = smem;                                     // 1024-aligned (swizzle atom)
   uint8_t* raw_ring = smem + CONV * CONV_BYTES;
-  int* sums = reinterpret_cast<int*>(smem + SUM_OFF);            // A: [buf * 128 + row], B: 256 + [buf * 256 + col]
+  int* sum_a = reinterpret_cast<int*>(smem + SUM_OFF);           // [tile parity][group][row]
+  int* sum_b = sum_a + 4 * 128;                                  // [tile parity][group][column of the pair's tile]
   uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + BAR_OFF);
   uint64_t* raw_empty = raw_full + RAW;
-  uint64_t* conv_full = raw_empty + RAW;                         // this CTA's tiles converted
-  uint64_t* peer_full = conv_full + CONV;                        // leader: the other CTA's tiles converted
-  uint64_t* conv_empty = peer_full + CONV;
+  uint64_t* conv_full = raw_empty + RAW;                         // leader's: both CTAs' tiles converted
+  uint64_t* conv_empty = conv_full + CONV;
   uint64_t* acc_full = conv_empty + CONV;                        // [2]
   uint64_t* acc_empty = acc_full + 2;                            // [2], leader's
   uint64_t* sum_full = acc_empty + 2;                            // [2]
@@ -118,11 +129,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   const bool zeros = p.az || p.bz;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < RAW; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 8); }
-    for (int s = 0; s < CONV; ++s) { mbar_init(&conv_full[s], 8); mbar_init(&peer_full[s], 1); mbar_init(&conv_empty[s], 1); }
+    for (int s = 0; s < RAW; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
+    for (int s = 0; s < CONV; ++s) { mbar_init(&conv_full[s], 8); mbar_init(&conv_empty[s], 1); }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16);
-      mbar_init(&sum_full[b], 4 + 8); mbar_init(&sum_empty[b], 16);   // A: own 4 warps; B: both CTAs' 4 warps
+      mbar_init(&sum_full[b], 16); mbar_init(&sum_empty[b], 16);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -137,7 +148,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   auto fail = [&]() { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     if (warp == 0 && lane == 0) {
       // ---------------- raw code tiles ----------------
       uint32_t it = 0;
@@ -173,7 +184,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           }
           const int s = it % CONV;
           const uint32_t ph = (it / CONV) & 1;
-          if (!mbar_wait(&conv_full[s], ph) || !mbar_wait_cluster(&peer_full[s], ph)) { fail(); ok = false; break; }
+          if (!mbar_wait(&conv_full[s], ph)) { fail(); ok = false; break; }
           tc_fence_after();
           issued = true;
           const uint32_t sa = smem_u32(conv_ring + s * CONV_BYTES), sb = sa + 128 * BK * 2;
@@ -192,17 +203,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (*abort_flag && issued) {           // products in flight end before the tensor memory is released
         umma_commit_pair(drain, 0x1);
         mbar_wait(drain, 0);
-      }
-    } else if (warp == 1 && lane == 0) {
-      // ---------------- the other CTA's tiles: ready signals to the leader ----------------
-      uint32_t it = 0;
-      for (int i = first; i < total && !*abort_flag; i += step) {
-        const Item w = item_of(p, i, mt, nt);
-        for (int kb = 0; kb < w.nkb; ++kb, ++it) {
-          const int s = it % CONV;
-          if (!mbar_wait(&conv_full[s], (it / CONV) & 1)) { fail(); break; }
-          mbar_arrive_cluster(mapa_shared(smem_u32(&peer_full[s]), 0));
-        }
       }
     }
   } else if (warp < 12) {
@@ -234,14 +234,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       }
       if (!ok) break;
       const uint32_t sbuf = tile & 1;
-      const int* sumA = sums + sbuf * 128;
-      const int* sumB = sums + 256 + sbuf * 256;
+      const int* sumA = sum_a + sbuf * 256;
+      const int* sumB = sum_b + sbuf * 512;
       const int row_l = q * 32 + lane, m = w.m0 + rank * BM + row_l;
       int sa = 0;
       if (zeros) {
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_full[sbuf], (tile >> 1) & 1));
         if (!ok) { fail(); break; }
-        sa = sumA[row_l];
+        sa = sumA[row_l] + sumA[128 + row_l];
       }
       if (p.splits > 1) {
         if (m < p.M) {
@@ -254,7 +254,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (zeros && w.m0 == 0 && rank == 0 && q == 0) {
 #pragma unroll
           for (int j = 0; j < BN / 2; j += 32)
-            if (w.n0 + c0 + j + lane < p.N) p.part_sb[(int64_t)w.split * p.N + w.n0 + c0 + j + lane] = sumB[c0 + j + lane];
+            if (w.n0 + c0 + j + lane < p.N) 
+              p.part_sb[(int64_t)w.split * p.N + w.n0 + c0 + j + lane] = sumB[c0 + j + lane] + sumB[256 + c0 + j + lane];
         }
       } else if (m < p.M) {
         const float ah = __ldg(p.ah + m);
@@ -269,7 +270,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               const float4 bh = __ldg(reinterpret_cast<const float4*>(p.bh + n + e));
               int4 zb = make_int4(128, 128, 128, 128), sb = make_int4(0, 0, 0, 0);
               if (p.bz) zb = __ldg(reinterpret_cast<const int4*>(p.bz + n + e));
-              if (zeros) sb = *reinterpret_cast<const int4*>(sumB + c0 + j + e);
+              if (zeros) {
+                const int4 s0 = *reinterpret_cast<const int4*>(sumB + c0 + j + e);
+                const int4 s1 = *reinterpret_cast<const int4*>(sumB + 256 + c0 + j + e);
+                sb = make_int4(s0.x + s1.x, s0.y + s1.y, s0.z + s1.z, s0.w + s1.w);
+              }
               y[e] = finish(acc[j + e], za, (long long)zb.x - 128, sa, sb.x, p.K, ah, bh.x, zeros);
               y[e + 1] = finish(acc[j + e + 1], za, (long long)zb.y - 128, sa, sb.y, p.K, ah, bh.y, zeros);
               y[e + 2] = finish(acc[j + e + 2], za, (long long)zb.z - 128, sa, sb.z, p.K, ah, bh.z, zeros);
@@ -296,51 +301,48 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     }
   } else {
     // ---------------- convert ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    const bool is_b = warp >= 16;
-    const int r = threadIdx.x & 127;
-    const bool want_sum = zeros && (is_b ? p.az != nullptr : p.bz != nullptr);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    const int grp = (warp - 12) >> 2, r = threadIdx.x & 127;
+    const uint32_t src0 = smem_u32(raw_ring) + r * BK, dst0 = smem_u32(conv_ring) + r * 128;
+    const uint32_t rx = (r >> 1) & 3, cx = r & 7;
     uint32_t it = 0, tile = 0;
     bool ok = true;
     for (int i = first; i < total && ok && !*abort_flag; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
-      int sum = 0;
+      int sa = 0, sb = 0;
       for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+        if ((int)(it & 1) != grp) continue;
         const int rs = it % RAW, cs = it % CONV;
         ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[rs], (it / RAW) & 1));
         if (!ok) { fail(); break; }
-        const uint32_t src = smem_u32(raw_ring + rs * RAW_BYTES + (is_b ? 128 * BK : 0)) + r * BK;
-        uint4 u[4];
+        uint4 u[8];                          // A then B: 64 codes each
 #pragma unroll
-        for (int c = 0; c < 4; ++c) u[c] = lds128(src + ((c ^ ((r >> 1) & 3)) << 4));
+        for (int c = 0; c < 8; ++c) u[c] = lds128(src0 + rs * RAW_BYTES + (c >> 2) * 128 * BK + (((c & 3) ^ rx) << 4));
         ok = __all_sync(0xffffffffu, mbar_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1));
         if (!ok) { fail(); break; }
-        const uint32_t dst = smem_u32(conv_ring + cs * CONV_BYTES + (is_b ? 128 * BK * 2 : 0)) + r * 128;
         const int k0 = (w.kb0 + kb) * BK;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 8; ++c) {
           uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;      // codes beyond K add nothing
-          if (k0 + 16 * c < p.K) {
-            if (want_sum) {
-              const uint32_t x = 0x80808080u;
-              sum = __dp4a((int)(u[c].x ^ x), 0x01010101, sum);
-              sum = __dp4a((int)(u[c].y ^ x), 0x01010101, sum);
-              sum = __dp4a((int)(u[c].z ^ x), 0x01010101, sum);
-              sum = __dp4a((int)(u[c].w ^ x), 0x01010101, sum);
+          if (k0 + 16 * (c & 3) < p.K) {
+            if (zeros) {
+              if (c < 4) sa = code_sum(u[c], sa);
+              else sb = code_sum(u[c], sb);
             }
             lo = make_uint4(half_codes(u[c].x, 0x4140), half_codes(u[c].x, 0x4342), half_codes(u[c].y, 0x4140),
                             half_codes(u[c].y, 0x4342));
             hi = make_uint4(half_codes(u[c].z, 0x4140), half_codes(u[c].z, 0x4342), half_codes(u[c].w, 0x4140),
                             half_codes(u[c].w, 0x4342));
           }
-          sts128(dst + (((2 * c) ^ (r & 7)) << 4), lo);
-          sts128(dst + (((2 * c + 1) ^ (r & 7)) << 4), hi);
+          const uint32_t dst = dst0 + cs * CONV_BYTES + (c >> 2) * 128 * BK * 2;
+          sts128(dst + (((2 * (c & 3)) ^ cx) << 4), lo);
+          sts128(dst + (((2 * (c & 3) + 1) ^ cx) << 4), hi);
         }
-        fence_async_smem();                  // the converted tile -> visible to the tensor core
+        fence_async_smem();                  // the converted tile -> visible to this SM's tensor core
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&raw_empty[rs]);
-          mbar_arrive(&conv_full[cs]);
+          mbar_signal_cluster(mapa_shared(smem_u32(&conv_full[cs]), 0));
         }
       }
       if (!ok) break;
@@ -348,17 +350,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         const uint32_t sbuf = tile & 1;
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_empty[sbuf], ((tile >> 1) & 1) ^ 1));
         if (!ok) { fail(); break; }
-        if (is_b) {                          // this CTA's 128 columns of the tile, to both CTAs
-          const uint32_t at = smem_u32(sums + 256 + sbuf * 256 + rank * 128 + r);
-          sts_cluster(mapa_shared(at, 0), sum);
-          sts_cluster(mapa_shared(at, 1), sum);
-          __syncwarp();
-          if (lane < 2) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_full[sbuf]), lane));
-        } else {
-          sums[sbuf * 128 + r] = sum;
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_full[sbuf]), rank));
-        }
+        sum_a[sbuf * 256 + grp * 128 + r] = sa;
+        // this CTA's 128 columns of the tile, to both CTAs
+        const uint32_t at = smem_u32(sum_b + sbuf * 512 + grp * 256 + rank * 128 + r);
+        sts_cluster(mapa_shared(at, 0), sb);
+        sts_cluster(mapa_shared(at, 1), sb);
+        __syncwarp();
+        if (lane < 2) mbar_arrive_cluster(mapa_shared(smem_u32(&sum_full[sbuf]), lane));
       }
     }
   }
@@ -427,14 +425,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 }
 
 __device__ __forceinline__ uint32_t pick(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
-
-__device__ __forceinline__ int code_sum(const uint4& u, int s) {
-  const uint32_t x = 0x80808080u;
-  s = __dp4a((int)(u.x ^ x), 0x01010101, s);
-  s = __dp4a((int)(u.y ^ x), 0x01010101, s);
-  s = __dp4a((int)(u.z ^ x), 0x01010101, s);
-  return __dp4a((int)(u.w ^ x), 0x01010101, s);
-}
 
 // 16 codes 128 (value 0): what lies beyond the matrix
 __device__ __forceinline__ uint4 no_codes() { return make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u); }

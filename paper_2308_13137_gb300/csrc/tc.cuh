@@ -231,6 +231,11 @@ static __device__ __forceinline__ void cluster_sync() {
 static __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// the same without cluster-scope release: a signal to the peer about data that the peer's threads do
+// not read themselves
+static __device__ __forceinline__ void mbar_signal_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // TMA tile load into this CTA's shared memory, completion counted on an mbarrier of either CTA of
 // the pair (given by its shared::cluster address)
 static __device__ __forceinline__ void tma_load_3d_pair(const CUtensorMap* map, uint32_t bar_cluster, void* dst, int c0,
