@@ -78,7 +78,8 @@ constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumula
 constexpr int TC_THREADS = 640;
 constexpr int RAW_BYTES = 2 * 128 * BK, CONV_BYTES = 2 * 128 * BK * 2;
 constexpr int SUM_OFF = RAW * RAW_BYTES + CONV * CONV_BYTES;      // 2 tiles x 2 groups: [128] sums of A, [256] of B
-constexpr int BAR_OFF = SUM_OFF + 4 * (128 + 256) * 4;
+constexpr int COL_OFF = SUM_OFF + 4 * (128 + 256) * 4;             // drain warps: [8][4][128] column operands
+constexpr int BAR_OFF = COL_OFF + 8 * 4 * 128 * 4;
 constexpr int TC_SMEM = BAR_OFF + 512 + 1024;
 static_assert(TC_SMEM <= 227 * 1024, "shared memory per CTA");
 
@@ -99,6 +100,79 @@ __device__ __forceinline__ Item item_of(const QgemmArgs& p, int i, int mt, int n
 
 __device__ __forceinline__ void sts_cluster(uint32_t addr, int v) {
   asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// 32 bytes of one row, two rows of 16 where the output is only 16-byte aligned
+__device__ __forceinline__ void store32(void* at, const uint32_t (&v)[8], bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(at)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(at)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+// A drain thread's 128 integer sums (row m, columns n0 ..) to the outputs.  MODE 0: no zero points; 1: 32-bit
+// combination; 2: 64-bit.  A thread writes whole 32-byte sectors where the alignment allows it.
+template <int MODE>
+__device__ __forceinline__ void tc_store(const QgemmArgs& p, const int (&acc)[BN / 2], int m, int n0, float ah, int za, int sa,
+                                         const float* col_h, const int* col_z, const int* col_s, const float* col_b) {
+  if (m >= p.M) return;
+  const int64_t at = (int64_t)m * p.ldc + n0;
+  const bool wide_f = ((uintptr_t)p.Cf & 31) == 0;                              // ldc is a multiple of 8
+  const bool wide_b = ((uintptr_t)p.Cb & 31) == 0 && p.ldc % 16 == 0;
+  const uint32_t ta = (uint32_t)sa - (uint32_t)p.K * (uint32_t)za;               // MODE 1: modulo 2^32
+  const long long ta64 = (long long)sa - (long long)p.K * za;
+#pragma unroll
+  for (int j = 0; j < BN / 2; j += 16) {
+    if (n0 + j >= p.N) break;
+    float y[16];
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const float4 h = *reinterpret_cast<const float4*>(col_h + j + e);
+      const float hv[4] = {h.x, h.y, h.z, h.w};
+      int4 z = make_int4(0, 0, 0, 0), s = z;
+      if (MODE != 0) { z = *reinterpret_cast<const int4*>(col_z + j + e); s = *reinterpret_cast<const int4*>(col_s + j + e); }
+      const int zv[4] = {z.x, z.y, z.z, z.w}, sv[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float f;
+        if (MODE == 2) f = __ll2float_rn((long long)acc[j + e + k] - (long long)za * sv[k] - zv[k] * ta64);
+        else if (MODE == 1) f = __int2float_rn((int)((uint32_t)acc[j + e + k] - (uint32_t)za * (uint32_t)sv[k] - (uint32_t)zv[k] * ta));
+        else f = __int2float_rn(acc[j + e + k]);
+        y[e + k] = __fmul_rn(__fmul_rn(f, ah), hv[k]);
+      }
+    }
+    if (p.bias) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const float4 b = *reinterpret_cast<const float4*>(col_b + j + e);
+        y[e] = __fadd_rn(y[e], b.x); y[e + 1] = __fadd_rn(y[e + 1], b.y);
+        y[e + 2] = __fadd_rn(y[e + 2], b.z); y[e + 3] = __fadd_rn(y[e + 3], b.w);
+      }
+    }
+    const bool both = n0 + j + 8 < p.N;                      // N is a multiple of 8
+    if (p.Cf) {
+#pragma unroll
+      for (int hlf = 0; hlf < 2; ++hlf) {
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __float_as_uint(y[8 * hlf + e]);
+        if (hlf == 0 || both) store32(p.Cf + at + j + 8 * hlf, v, wide_f);
+      }
+    }
+    if (p.Cb) {
+      float lo[8], hi[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { lo[e] = y[e]; hi[e] = y[8 + e]; }
+      const uint4 a = pack_bf16x8(lo), b = pack_bf16x8(hi);
+      const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      if (both) store32(p.Cb + at + j, v, wide_b);
+      else *reinterpret_cast<uint4*>(p.Cb + at + j) = a;
+    }
+  }
 }
 
 __global__ void __launch_bounds__(TC_THREADS, 1)
@@ -209,6 +283,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // ---------------- drain: fp32 accumulators -> integers -> outputs ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int q = warp & 3, c0 = warp >= 8 ? BN / 2 : 0;
+    // this warp's copy of its 128 columns' step, zero point - 128, code sum and bias
+    float* col_h = reinterpret_cast<float*>(smem + COL_OFF) + (warp - 4) * 512;
+    int* col_z = reinterpret_cast<int*>(col_h + 128);
+    int* col_s = col_z + 128;
+    float* col_b = reinterpret_cast<float*>(col_s + 128);
     uint32_t ch = 0, tile = 0;
     for (int i = first; i < total; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
@@ -257,42 +336,32 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (w.n0 + c0 + j + lane < p.N) 
               p.part_sb[(int64_t)w.split * p.N + w.n0 + c0 + j + lane] = sumB[c0 + j + lane] + sumB[256 + c0 + j + lane];
         }
-      } else if (m < p.M) {
-        const float ah = __ldg(p.ah + m);
-        const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0;
+      } else {
+        int zmax = 0;
 #pragma unroll
-        for (int j = 0; j < BN / 2; j += 8) {
-          const int n = w.n0 + c0 + j;
-          if (n < p.N) {
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-              const float4 bh = __ldg(reinterpret_cast<const float4*>(p.bh + n + e));
-              int4 zb = make_int4(128, 128, 128, 128), sb = make_int4(0, 0, 0, 0);
-              if (p.bz) zb = __ldg(reinterpret_cast<const int4*>(p.bz + n + e));
-              if (zeros) {
-                const int4 s0 = *reinterpret_cast<const int4*>(sumB + c0 + j + e);
-                const int4 s1 = *reinterpret_cast<const int4*>(sumB + 256 + c0 + j + e);
-                sb = make_int4(s0.x + s1.x, s0.y + s1.y, s0.z + s1.z, s0.w + s1.w);
-              }
-              y[e] = finish(acc[j + e], za, (long long)zb.x - 128, sa, sb.x, p.K, ah, bh.x, zeros);
-              y[e + 1] = finish(acc[j + e + 1], za, (long long)zb.y - 128, sa, sb.y, p.K, ah, bh.y, zeros);
-              y[e + 2] = finish(acc[j + e + 2], za, (long long)zb.z - 128, sa, sb.z, p.K, ah, bh.z, zeros);
-              y[e + 3] = finish(acc[j + e + 3], za, (long long)zb.w - 128, sa, sb.w, p.K, ah, bh.w, zeros);
-              if (p.bias) {
-                const float4 b = __ldg(reinterpret_cast<const float4*>(p.bias + n + e));
-                y[e] = __fadd_rn(y[e], b.x); y[e + 1] = __fadd_rn(y[e + 1], b.y);
-                y[e + 2] = __fadd_rn(y[e + 2], b.z); y[e + 3] = __fadd_rn(y[e + 3], b.w);
-              }
-            }
-            const int64_t at = (int64_t)m * p.ldc + n;
-            if (p.Cf) {
-              reinterpret_cast<float4*>(p.Cf + at)[0] = make_float4(y[0], y[1], y[2], y[3]);
-              reinterpret_cast<float4*>(p.Cf + at)[1] = make_float4(y[4], y[5], y[6], y[7]);
-            }
-            if (p.Cb) *reinterpret_cast<uint4*>(p.Cb + at) = pack_bf16x8(y);
+        for (int k = 0; k < 4; ++k) {
+          const int c = 32 * k + lane, n = w.n0 + c0 + c;
+          const bool in = n < p.N;
+          col_h[c] = in ? __ldg(p.bh + n) : 0.f;
+          col_b[c] = in && p.bias ? __ldg(p.bias + n) : 0.f;
+          if (zeros) {
+            const int z = in && p.bz ? __ldg(p.bz + n) - 128 : 0;
+            zmax = max(zmax, abs(z));
+            col_z[c] = z;
+            col_s[c] = sumB[c0 + c] + sumB[256 + c0 + c];
           }
         }
+        zmax = (int)__reduce_max_sync(0xffffffffu, (unsigned)zmax);
+        __syncwarp();
+        const float ah = m < p.M ? __ldg(p.ah + m) : 0.f;
+        const int za = p.az && m < p.M ? __ldg(p.az + m) - 128 : 0;
+        // |sum| <= K (128 + |za'|)(128 + |zb'|): where that is below 2^31, 32-bit arithmetic (modulo 2^32)
+        // gives it, and the 64-bit form is left to rows or columns far from zero
+        const bool narrow = (unsigned long long)p.K * (128u + abs(za)) * (128u + zmax) < (1ull << 31);
+        if (!zeros) tc_store<0>(p, acc, m, w.n0 + c0, ah, za, sa, col_h, col_z, col_s, col_b);
+        else if (__all_sync(0xffffffffu, narrow)) tc_store<1>(p, acc, m, w.n0 + c0, ah, za, sa, col_h, col_z, col_s, col_b);
+        else tc_store<2>(p, acc, m, w.n0 + c0, ah, za, sa, col_h, col_z, col_s, col_b);
+        __syncwarp();                        // the column operands are rewritten by the next tile
       }
       if (zeros) {
         __syncwarp();
