@@ -879,15 +879,16 @@ bool omq_make_map_f32_out(CUtensorMap* map, float* ptr, int64_t N, int64_t M, in
   return make_map_c(map, ptr, N, M, 1, ld, 0);
 }
 
-bool omq_make_map_u8(CUtensorMap* map, const void* ptr, int64_t inner, int64_t rows, int64_t ld, int box_rows) {
+bool omq_make_map_u8(CUtensorMap* map, const void* ptr, int64_t inner, int64_t rows, int64_t ld, int box_rows,
+                     int box_inner) {
   PFN_encodeTiled_t enc = get_encode();
   if (!enc) return false;
   cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, 1u};
   cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(ld * rows)};
-  cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u};
+  cuuint32_t box[3] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows, 1u};
   cuuint32_t estr[3] = {1u, 1u, 1u};
   CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(ptr), dims, strides, box, estr,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
 }

@@ -40,13 +40,13 @@ __device__ __forceinline__ uint32_t half_codes(uint32_t w, uint32_t sel) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// s + the sum of 16 codes moved by 128
+// s + the sum of 16 codes
 __device__ __forceinline__ int code_sum(const uint4& u, int s) {
-  const uint32_t x = 0x80808080u;
-  s = __dp4a((int)(u.x ^ x), 0x01010101, s);
-  s = __dp4a((int)(u.y ^ x), 0x01010101, s);
-  s = __dp4a((int)(u.z ^ x), 0x01010101, s);
-  return __dp4a((int)(u.w ^ x), 0x01010101, s);
+  uint32_t v = (uint32_t)s;
+  v = __dp4a(u.x, 0x01010101u, v);
+  v = __dp4a(u.y, 0x01010101u, v);
+  v = __dp4a(u.z, 0x01010101u, v);
+  return (int)__dp4a(u.w, 0x01010101u, v);
 }
 
 // h_a h_b (integer sum) + bias, each step one fp32 rounding
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     bool ok = true;
     for (int i = first; i < total && ok && !*abort_flag; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
-      int sa = 0, sb = 0;
+      int sa = 0, sb = 0, codes = 0;         // sums of this group's codes and their number per row
       for (int kb = 0; kb < w.nkb; ++kb, ++it) {
         if ((int)(it & 1) != grp) continue;
         const int rs = it % RAW, cs = it % CONV;
@@ -390,6 +390,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         ok = __all_sync(0xffffffffu, mbar_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1));
         if (!ok) { fail(); break; }
         const int k0 = (w.kb0 + kb) * BK;
+        codes += min(BK, p.K - k0);
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;      // codes beyond K add nothing
@@ -419,6 +420,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         const uint32_t sbuf = tile & 1;
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_empty[sbuf], ((tile >> 1) & 1) ^ 1));
         if (!ok) { fail(); break; }
+        sa -= 128 * codes;                   // the codes moved by 128
+        sb -= 128 * codes;
         sum_a[sbuf * 256 + grp * 128 + r] = sa;
         // this CTA's 128 columns of the tile, to both CTAs
         const uint32_t at = smem_u32(sum_b + sbuf * 512 + grp * 256 + rank * 128 + r);
@@ -478,12 +481,15 @@ __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
 // ================================================================================================
 // few rows: the weight read is the bound
 // ================================================================================================
-// A warp forms 16 output channels x 8 NT tokens by mma.sync m16n8k16: the weight rows are the M
-// dimension and are converted in registers on their way from HBM, the activation codes are the N
-// dimension.  K is split over the warps of the CTA (their integer sums are joined in shared memory),
-// so that N / 16 CTAs are enough to load every SM.  K is numbered inside the products so that each
-// thread's operand values are 16 consecutive codes of its row.
-constexpr int FEW_WARPS = 8;
+// A CTA owns 128 output channels and a share of K; a cluster of 1 to 8 CTAs covers K and joins its integer
+// sums through distributed shared memory.  One thread keeps a ring of TMA tiles [128 channels x 128 codes]
+// and [8 NT tokens x 128 codes] in flight; eight warps, one per 32 channels and half of a tile's codes,
+// form 32 channels x 8 NT tokens by mma.sync m16n8k16.  The weight rows are the M dimension, so one token costs an eighth of a tile, and the codes
+// are converted in registers between the shared-memory load and the product: no converted copy is
+// written.  K is numbered inside the products so that a thread's operand values are 16 consecutive
+// codes of its row; row 8 i + g of a product is tile row 8 i + (g % 2) 4 + g / 2, so that the eight
+// lanes of a load phase hit eight distinct 16-byte bank groups of the 128-byte swizzle.
+constexpr int FEW_WARPS = 8, FEW_N = 128, FEW_K = 128;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -495,92 +501,200 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
 
 __device__ __forceinline__ uint32_t pick(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
 
-// 16 codes 128 (value 0): what lies beyond the matrix
+// 16 codes 128 (value 0): what lies beyond K
 __device__ __forceinline__ uint4 no_codes() { return make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u); }
 
+__device__ __forceinline__ int lds_cluster(uint32_t addr) {
+  int v;
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 template <int NT>
-__global__ void __launch_bounds__(FEW_WARPS * 32) qgemm_few_kernel(const QgemmArgs p) {
-  __shared__ int red[FEW_WARPS][16][8 * NT + 1];
-  __shared__ int red_b[FEW_WARPS][16], red_a[FEW_WARPS][8 * NT];
+struct Few {
+  static constexpr int TOK = 8 * NT;
+  static constexpr int STAGES = NT <= 2 ? 5 : 4;
+  static constexpr int STAGE = (FEW_N + TOK) * FEW_K;                 // bytes
+  static constexpr int RED_OFF = STAGES * STAGE;                      // [TOK][FEW_N] integer sums
+  static constexpr int SUM_OFF = RED_OFF + TOK * FEW_N * 4;           // code sums: [TOK] of A, [FEW_N] of B
+  static constexpr int BAR_OFF = SUM_OFF + (TOK + FEW_N) * 4;
+  static constexpr int BYTES = BAR_OFF + 2 * STAGES * 8 + 16 + 1024;
+};
+
+template <int NT>
+__global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
+    qgemm_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const QgemmArgs p,
+                     const int ck, const int k_share) {
+  using F = Few<NT>;
+  extern __shared__ uint8_t few_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(few_raw) + 1023) & ~uintptr_t(1023));
+  int* red = reinterpret_cast<int*>(smem + F::RED_OFF);
+  int* red_a = reinterpret_cast<int*>(smem + F::SUM_OFF);
+  int* red_b = red_a + F::TOK;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + F::BAR_OFF);
+  uint64_t* empty = full + F::STAGES;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + F::STAGES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 8 * NT;
+  const int rank = ck > 1 ? (int)cluster_ctarank() : 0;
+  const int n0 = (blockIdx.x / ck) * FEW_N;
+  const int k_begin = rank * k_share, k_end = min(p.K, k_begin + k_share);
+  const int steps = k_end > k_begin ? (k_end - k_begin + FEW_K - 1) / FEW_K : 0;
   const bool sum_b = p.az != nullptr, sum_a = p.bz != nullptr;
-  const int r0 = n0 + g, r1 = n0 + g + 8;
-  const uint8_t* w0 = p.B + (int64_t)min(r0, p.N - 1) * p.ldb + 16 * t;
-  const uint8_t* w1 = p.B + (int64_t)min(r1, p.N - 1) * p.ldb + 16 * t;
-  int acc[NT][4], sb0 = 0, sb1 = 0, sa[NT];
-  float d[NT][4];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    sa[j] = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { acc[j][e] = 0; d[j][e] = 0.f; }
+  for (int i = threadIdx.x; i < F::TOK * FEW_N + F::TOK + FEW_N; i += (FEW_WARPS + 1) * 32) red[i] = 0;   // and the code sums
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], FEW_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  int pending = 0;                            // steps of 64 codes in the fp32 sums
-  // the warps take 64-code steps in turn; the next step's weights are in flight while one is used
-  int k = 64 * warp;
-  uint4 a0 = no_codes(), a1 = no_codes();
-  if (k + 16 * t < p.K) { a0 = __ldg((const uint4*)(w0 + k)); a1 = __ldg((const uint4*)(w1 + k)); }
-  while (k < p.K) {
-    const int kn = k + 64 * FEW_WARPS;
-    uint4 b0 = no_codes(), b1 = no_codes();
-    if (kn + 16 * t < p.K) { b0 = __ldg((const uint4*)(w0 + kn)); b1 = __ldg((const uint4*)(w1 + kn)); }
-    uint4 x[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int m = m0 + 8 * j + g;
-      x[j] = no_codes();
-      if (m < p.M && k + 16 * t < p.K) x[j] = __ldg(reinterpret_cast<const uint4*>(p.A + (int64_t)m * p.lda + k + 16 * t));
-      if (sum_a) sa[j] = code_sum(x[j], sa[j]);
-    }
-    if (sum_b) { sb0 = code_sum(a0, sb0); sb1 = code_sum(a1, sb1); }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t u = pick(a0, i), v = pick(a1, i);
-      const uint32_t f0 = half_codes(u, 0x4140), f1 = half_codes(v, 0x4140), f2 = half_codes(u, 0x4342), f3 = half_codes(v, 0x4342);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const uint32_t y = pick(x[j], i);
-        mma16816(d[j], f0, f1, f2, f3, half_codes(y, 0x4140), half_codes(y, 0x4342));
+  __syncthreads();
+  if (warp == FEW_WARPS) {
+    if (lane == 0) {
+      int i = 0;
+      for (; i < steps && !*abort_flag; ++i) {
+        const int s = i % F::STAGES;
+        if (!mbar_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1)) { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
+        mbar_expect_tx(&full[s], F::STAGE);
+        uint8_t* dst = smem + s * F::STAGE;
+        tma_load_3d(&tmB, &full[s], dst, k_begin + i * FEW_K, n0, 0);
+        tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K, k_begin + i * FEW_K, 0, 0);
       }
+      if (*abort_flag)                       // no copy may land after this CTA has left
+        for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j) mbar_wait(&full[j % F::STAGES], (j / F::STAGES) & 1);
     }
-    if (++pending == 16) {                    // 1024 codes: the fp32 sums are still exact integers
-      pending = 0;
+  } else {
+    const int cw = warp & 3, c = t + 4 * (warp >> 2);   // channel group, this thread's 16-code chunk of its rows
+    int sb[4] = {0, 0, 0, 0}, sa = 0;                // code sums: of the weight rows, of the tokens of tile cw
+    float d[2][NT][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { acc[j][e] += __float2int_rn(d[j][e]); d[j][e] = 0.f; }
-    }
-    a0 = b0; a1 = b1;
-    k = kn;
-  }
+        for (int e = 0; e < 4; ++e) d[i][j][e] = 0.f;
+    const int row = (g & 1) * 4 + (g >> 1);          // tile row of product row g
+    for (int i = 0; i < steps; ++i) {
+      const int s = i % F::STAGES;
+      if (!__all_sync(0xffffffffu, mbar_wait(&full[s], (i / F::STAGES) & 1))) {
+        omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
+      }
+      const uint32_t wb = smem_u32(smem + s * F::STAGE) + (32 * cw + row) * FEW_K + ((c ^ row) << 4);
+      const uint32_t ab = smem_u32(smem + s * F::STAGE) + (FEW_N + row) * FEW_K + ((c ^ row) << 4);
+      uint4 w[4], x[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
+      for (int q = 0; q < 4; ++q) w[q] = lds128(wb + 8 * q * FEW_K);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[j][e] += __float2int_rn(d[j][e]);
-      red[warp][g + 8 * (e >> 1)][8 * j + 2 * t + (e & 1)] = acc[j][e];
+      for (int j = 0; j < NT; ++j) x[j] = lds128(ab + 8 * j * FEW_K);
+      if (i == steps - 1 && 16 * c >= k_end - (k_begin + i * FEW_K)) {   // beyond K
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = no_codes();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) x[j] = no_codes();
+      }
+      if (sum_b) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sb[q] = code_sum(w[q], sb[q]);
+      }
+      if (sum_a) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          if (j == cw) sa = code_sum(x[j], sa);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t b0[NT], b1[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) { b0[j] = half_codes(pick(x[j], q), 0x4140); b1[j] = half_codes(pick(x[j], q), 0x4342); }
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const uint32_t u = pick(w[2 * mt], q), v = pick(w[2 * mt + 1], q);
+          const uint32_t f0 = half_codes(u, 0x4140), f1 = half_codes(v, 0x4140), f2 = half_codes(u, 0x4342),
+                         f3 = half_codes(v, 0x4342);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) mma16816(d[mt][j], f0, f1, f2, f3, b0[j], b1[j]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[s]);
+      // every 1024 codes of this warp's half the fp32 sums, still exact, go to integers in shared memory
+      // (two warps add to each: integer sums do not depend on the order)
+      if (i % 16 == 15 || i == steps - 1) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              // column e & 1 of the pair is token 2 t + (e & 1) as a product column: tile row of A
+              const int col = 2 * t + (e & 1), tok = 8 * j + (col & 1) * 4 + (col >> 1);
+              atomicAdd(red + tok * FEW_N + 32 * cw + 16 * mt + 8 * (e >> 1) + row, __float2int_rn(d[mt][j][e]));
+              d[mt][j][e] = 0.f;
+            }
+      }
     }
-    sa[j] += __shfl_xor_sync(0xffffffffu, sa[j], 1);
-    sa[j] += __shfl_xor_sync(0xffffffffu, sa[j], 2);
-    if (t == 0) red_a[warp][8 * j + g] = sa[j];
+    const int moved = 128 * 16 * steps;              // the codes moved by 128: each thread summed 16 per stage
+    if (sum_b) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) atomicAdd(red_b + 32 * cw + 8 * q + row, sb[q] - moved);
+    }
+    if (sum_a && cw < NT) atomicAdd(red_a + 8 * cw + row, sa - moved);
   }
-  sb0 += __shfl_xor_sync(0xffffffffu, sb0, 1); sb0 += __shfl_xor_sync(0xffffffffu, sb0, 2);
-  sb1 += __shfl_xor_sync(0xffffffffu, sb1, 1); sb1 += __shfl_xor_sync(0xffffffffu, sb1, 2);
-  if (t == 0) { red_b[warp][g] = sb0; red_b[warp][g + 8] = sb1; }
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * 8 * NT; i += FEW_WARPS * 32) {
-    const int c = i & 15, mr = i >> 4, n = n0 + c, m = m0 + mr;
-    if (n >= p.N || m >= p.M) continue;
+  if (ck > 1) cluster_sync();                                         // release / acquire over the cluster
+  // CTA `rank` finishes its share of the channels over the cluster's sums
+  const int share = FEW_N / ck, rows = min(F::TOK, p.M);
+  for (int i = threadIdx.x; i < share * rows; i += (FEW_WARPS + 1) * 32) {
+    const int c = rank * share + i % share, m = i / share, n = n0 + c;
+    if (n >= p.N) continue;
     int s = 0, ta = 0, tb = 0;
-#pragma unroll
-    for (int w = 0; w < FEW_WARPS; ++w) { s += red[w][c][mr]; ta += red_a[w][mr]; tb += red_b[w][c]; }
+    if (ck > 1) {
+      const uint32_t ar = smem_u32(red + m * FEW_N + c), aa = smem_u32(red_a + m), ab = smem_u32(red_b + c);
+      for (int r = 0; r < ck; ++r) {
+        s += lds_cluster(mapa_shared(ar, r));
+        if (sum_a) ta += lds_cluster(mapa_shared(aa, r));
+        if (sum_b) tb += lds_cluster(mapa_shared(ab, r));
+      }
+    } else {
+      s = red[m * FEW_N + c]; ta = red_a[m]; tb = red_b[c];
+    }
     const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0, zb = p.bz ? (long long)__ldg(p.bz + n) - 128 : 0;
     float y = finish(s, za, zb, ta, tb, p.K, __ldg(p.ah + m), __ldg(p.bh + n), sum_a || sum_b);
     if (p.bias) y = __fadd_rn(y, __ldg(p.bias + n));
     if (p.Cf) p.Cf[(int64_t)m * p.ldc + n] = y;
     if (p.Cb) p.Cb[(int64_t)m * p.ldc + n] = f_to_bf16(y);
   }
+  if (ck > 1) cluster_sync();                                         // no CTA leaves while its sums may be read
+}
+
+template <int NT>
+omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
+  using F = Few<NT>;
+  auto kern = qgemm_few_kernel<NT>;
+  static bool attr_set = false;
+  if (!attr_set) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES) != cudaSuccess) return OMQ_ERR_CUDA;
+    attr_set = true;
+  }
+  CUtensorMap ta, tb;
+  if (!omq_make_map_u8(&ta, p.A, p.K, p.M, p.lda, F::TOK, FEW_K) || !omq_make_map_u8(&tb, p.B, p.K, p.N, p.ldb, FEW_N, FEW_K))
+    return OMQ_ERR_UNSUPPORTED;
+  // K over as many CTAs as give every SM two, none under 512 codes
+  const int blocks = (p.N + FEW_N - 1) / FEW_N;
+  int ck = 1;
+  while (ck < 8 && blocks * ck < 2 * omq_num_sms() && p.K / (2 * ck) >= 512) ck *= 2;
+  const int k_share = ((p.K + ck - 1) / ck + FEW_K - 1) / FEW_K * FEW_K;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(blocks * ck), 1, 1);
+  cfg.blockDim = dim3((FEW_WARPS + 1) * 32, 1, 1);
+  cfg.dynamicSmemBytes = F::BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ck; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ck > 1 ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, kern, ta, tb, p, ck, k_share) != cudaSuccess) { cudaGetLastError(); return OMQ_ERR_CUDA; }
+  OMQ_LAUNCH_CHECK();
+  return OMQ_OK;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -628,12 +742,7 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   p.B = B; p.ldb = ldb; p.bh = b_h; p.bz = b_z;
   p.bias = bias; p.Cf = Cf; p.Cb = (__nv_bfloat16*)Cb; p.ldc = ldc; p.status = dev_status;
   if (M <= FEW_ROWS) {
-    const unsigned gx = (unsigned)((N + 15) / 16);
-    if (M <= 8) qgemm_few_kernel<1><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
-    else if (M <= 16) qgemm_few_kernel<2><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
-    else qgemm_few_kernel<4><<<dim3(gx, 1), FEW_WARPS * 32, 0, st>>>(p);
-    OMQ_LAUNCH_CHECK();
-    return OMQ_OK;
+    return M <= 8 ? few_launch<1>(st, p) : (M <= 16 ? few_launch<2>(st, p) : few_launch<4>(st, p));
   }
   const QPlan q = plan_of(M, N, K);
   p.splits = q.splits; p.kb_per_split = q.kb_per_split;
@@ -644,7 +753,7 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   }
   p.m_fast = (double)M > 1.5 * (double)N ? 0 : 1;               // keep the smaller operand in L2
   CUtensorMap ta, tb;
-  if (!omq_make_map_u8(&ta, A, K, M, lda, 128) || !omq_make_map_u8(&tb, B, K, N, ldb, 128)) return OMQ_ERR_UNSUPPORTED;
+  if (!omq_make_map_u8(&ta, A, K, M, lda, 128, BK) || !omq_make_map_u8(&tb, B, K, N, ldb, 128, BK)) return OMQ_ERR_UNSUPPORTED;
   static bool attr_set = false;
   if (!attr_set) {
     if (cudaFuncSetAttribute(qgemm_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM) != cudaSuccess)

@@ -313,9 +313,11 @@ static __device__ __forceinline__ void store_block32(const CUtensorMap* map, uin
 // Host: 3-D bf16 tensor map {inner, rows, batch}, box {box_inner, box_rows, 1}, 128-byte swizzle.
 bool omq_make_map_bf16(CUtensorMap* map, const void* ptr, int64_t inner, int64_t rows, int64_t batch, int64_t ld,
                        int64_t bs, int box_inner, int box_rows);
-// Host: map of 8-bit codes {inner, rows, 1} with row stride ld (bytes), box {64, box_rows, 1}, 64-byte
-// swizzle (16-byte chunk c of row r at chunk c ^ ((r >> 1) & 3)); elements outside read as 0
-bool omq_make_map_u8(CUtensorMap* map, const void* ptr, int64_t inner, int64_t rows, int64_t ld, int box_rows);
+// Host: map of 8-bit codes {inner, rows, 1} with row stride ld (bytes), box {box_inner, box_rows, 1}; elements
+// outside read as 0.  box_inner 64: 64-byte swizzle (16-byte chunk c of row r at chunk c ^ ((r >> 1) & 3));
+// 128: 128-byte swizzle (chunk c ^ (r & 7))
+bool omq_make_map_u8(CUtensorMap* map, const void* ptr, int64_t inner, int64_t rows, int64_t ld, int box_rows,
+                     int box_inner);
 // Host: fp32 output map {N, M, 1} with row stride ld (elements), box {32, 32, 1}, 128-byte swizzle:
 // the layout of a warp's 32 x 32 staging block for tma_store_3d
 bool omq_make_map_f32_out(CUtensorMap* map, float* ptr, int64_t N, int64_t M, int64_t ld);
