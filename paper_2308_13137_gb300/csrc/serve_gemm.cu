@@ -481,15 +481,15 @@ __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
 // ================================================================================================
 // few rows: the weight read is the bound
 // ================================================================================================
-// A CTA owns 128 output channels and a share of K; a cluster of 1 to 8 CTAs covers K and joins its integer
-// sums through distributed shared memory.  One thread keeps a ring of TMA tiles [128 channels x 128 codes]
-// and [8 NT tokens x 128 codes] in flight; eight warps, one per 32 channels and half of a tile's codes,
-// form 32 channels x 8 NT tokens by mma.sync m16n8k16.  The weight rows are the M dimension, so one token costs an eighth of a tile, and the codes
+// A CTA owns BN = 64 or 128 output channels and a share of K; a cluster of 1 to 8 CTAs covers K and joins its
+// integer sums through distributed shared memory.  One thread keeps a ring of 16 KB weight tiles [BN
+// channels x 16384 / BN codes] and the matching codes of 8 NT tokens in flight (TMA); eight warps, each on
+// 32 channels and a 64-code slice of a tile, form 32 channels x 8 NT tokens by mma.sync m16n8k16.  The weight rows are the M dimension, so one token costs an eighth of a tile, and the codes
 // are converted in registers between the shared-memory load and the product: no converted copy is
 // written.  K is numbered inside the products so that a thread's operand values are 16 consecutive
 // codes of its row; row 8 i + g of a product is tile row 8 i + (g % 2) 4 + g / 2, so that the eight
 // lanes of a load phase hit eight distinct 16-byte bank groups of the 128-byte swizzle.
-constexpr int FEW_WARPS = 8, FEW_N = 128, FEW_K = 128;
+constexpr int FEW_WARPS = 8;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -510,9 +510,9 @@ __device__ __forceinline__ int lds_cluster(uint32_t addr) {
   return v;
 }
 
-template <int NT>
+template <int NT, int FEW_N>
 struct Few {
-  static constexpr int TOK = 8 * NT;
+  static constexpr int TOK = 8 * NT, FEW_K = 16384 / FEW_N;
   static constexpr int STAGES = NT <= 2 ? 5 : 4;
   static constexpr int STAGE = (FEW_N + TOK) * FEW_K;                 // bytes
   static constexpr int RED_OFF = STAGES * STAGE;                      // [TOK][FEW_N] integer sums
@@ -521,11 +521,12 @@ struct Few {
   static constexpr int BYTES = BAR_OFF + 2 * STAGES * 8 + 16 + 1024;
 };
 
-template <int NT>
+template <int NT, int FEW_N>
 __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
     qgemm_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const QgemmArgs p,
                      const int ck, const int k_share) {
-  using F = Few<NT>;
+  using F = Few<NT, FEW_N>;
+  constexpr int FEW_K = F::FEW_K, FEW_GROUPS = FEW_N / 32;
   extern __shared__ uint8_t few_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(few_raw) + 1023) & ~uintptr_t(1023));
   int* red = reinterpret_cast<int*>(smem + F::RED_OFF);
@@ -555,15 +556,19 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
         if (!mbar_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1)) { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
         mbar_expect_tx(&full[s], F::STAGE);
         uint8_t* dst = smem + s * F::STAGE;
-        tma_load_3d(&tmB, &full[s], dst, k_begin + i * FEW_K, n0, 0);
-        tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K, k_begin + i * FEW_K, 0, 0);
+#pragma unroll
+        for (int b = 0; b < FEW_K / 128; ++b) {
+          tma_load_3d(&tmB, &full[s], dst + b * FEW_N * 128, k_begin + i * FEW_K + 128 * b, n0, 0);
+          tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K + b * F::TOK * 128, k_begin + i * FEW_K + 128 * b, 0, 0);
+        }
       }
       if (*abort_flag)                       // no copy may land after this CTA has left
         for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j) mbar_wait(&full[j % F::STAGES], (j / F::STAGES) & 1);
     }
   } else {
-    const int cw = warp & 3, c = t + 4 * (warp >> 2);   // channel group, this thread's 16-code chunk of its rows
-    int sb[4] = {0, 0, 0, 0}, sa = 0;                // code sums: of the weight rows, of the tokens of tile cw
+    // channel group, 64-code slice of the tile, this thread's 16-code chunk of its rows' 128 bytes
+    const int cw = warp % FEW_GROUPS, kq = warp / FEW_GROUPS, c = t + 4 * (kq & 1);
+    int sb[4] = {0, 0, 0, 0}, sa[NT] = {};           // code sums: of the weight rows, of the token tiles that this warp counts
     float d[2][NT][4];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -577,14 +582,14 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
       if (!__all_sync(0xffffffffu, mbar_wait(&full[s], (i / F::STAGES) & 1))) {
         omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
       }
-      const uint32_t wb = smem_u32(smem + s * F::STAGE) + (32 * cw + row) * FEW_K + ((c ^ row) << 4);
-      const uint32_t ab = smem_u32(smem + s * F::STAGE) + (FEW_N + row) * FEW_K + ((c ^ row) << 4);
+      const uint32_t wb = smem_u32(smem + s * F::STAGE) + ((kq >> 1) * FEW_N + 32 * cw + row) * 128 + ((c ^ row) << 4);
+      const uint32_t ab = smem_u32(smem + s * F::STAGE) + FEW_N * FEW_K + ((kq >> 1) * F::TOK + row) * 128 + ((c ^ row) << 4);
       uint4 w[4], x[NT];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = lds128(wb + 8 * q * FEW_K);
+      for (int q = 0; q < 4; ++q) w[q] = lds128(wb + 8 * q * 128);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) x[j] = lds128(ab + 8 * j * FEW_K);
-      if (i == steps - 1 && 16 * c >= k_end - (k_begin + i * FEW_K)) {   // beyond K
+      for (int j = 0; j < NT; ++j) x[j] = lds128(ab + 8 * j * 128);
+      if (i == steps - 1 && 128 * (kq >> 1) + 16 * c >= k_end - (k_begin + i * FEW_K)) {   // beyond K
 #pragma unroll
         for (int q = 0; q < 4; ++q) w[q] = no_codes();
 #pragma unroll
@@ -597,7 +602,7 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
       if (sum_a) {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-          if (j == cw) sa = code_sum(x[j], sa);
+          if (j % FEW_GROUPS == cw) sa[j / FEW_GROUPS] = code_sum(x[j], sa[j / FEW_GROUPS]);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -615,8 +620,8 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[s]);
-      // every 1024 codes of this warp's half the fp32 sums, still exact, go to integers in shared memory
-      // (two warps add to each: integer sums do not depend on the order)
+      // every 1024 codes of this warp's slices the fp32 sums, still exact, go to integers in shared memory
+      // (several warps add to each: integer sums do not depend on the order)
       if (i % 16 == 15 || i == steps - 1) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
@@ -636,7 +641,11 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
 #pragma unroll
       for (int q = 0; q < 4; ++q) atomicAdd(red_b + 32 * cw + 8 * q + row, sb[q] - moved);
     }
-    if (sum_a && cw < NT) atomicAdd(red_a + 8 * cw + row, sa - moved);
+    if (sum_a) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        if (j % FEW_GROUPS == cw) atomicAdd(red_a + 8 * j + row, sa[j / FEW_GROUPS] - moved);
+    }
   }
   __syncthreads();
   if (ck > 1) cluster_sync();                                         // release / acquire over the cluster
@@ -665,23 +674,27 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
   if (ck > 1) cluster_sync();                                         // no CTA leaves while its sums may be read
 }
 
-template <int NT>
+template <int NT, int FEW_N>
 omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
-  using F = Few<NT>;
-  auto kern = qgemm_few_kernel<NT>;
+  using F = Few<NT, FEW_N>;
+  auto kern = qgemm_few_kernel<NT, FEW_N>;
   static bool attr_set = false;
   if (!attr_set) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES) != cudaSuccess) return OMQ_ERR_CUDA;
     attr_set = true;
   }
   CUtensorMap ta, tb;
-  if (!omq_make_map_u8(&ta, p.A, p.K, p.M, p.lda, F::TOK, FEW_K) || !omq_make_map_u8(&tb, p.B, p.K, p.N, p.ldb, FEW_N, FEW_K))
+  if (!omq_make_map_u8(&ta, p.A, p.K, p.M, p.lda, F::TOK, 128) || !omq_make_map_u8(&tb, p.B, p.K, p.N, p.ldb, FEW_N, 128))
     return OMQ_ERR_UNSUPPORTED;
-  // K over as many CTAs as give every SM two, none under 512 codes
-  const int blocks = (p.N + FEW_N - 1) / FEW_N;
+  // One wave of CTAs, two per SM: the start of a CTA (tile ring, signals, joining) costs about 4 us, so a
+  // second wave loses more than an idle SM (4096 x 4096, one row: 6.6 us on 256 CTAs, 10.9 us on 512).
+  // Within that K is split as far as it goes, no share under 512 codes; clusters of 5 and 7 fill the SMs
+  // badly (5120 x 13824: 16.7 us with 6, 24.5 us with 7).
+  const int blocks = (p.N + FEW_N - 1) / FEW_N, cand[6] = {8, 6, 4, 3, 2, 1};
   int ck = 1;
-  while (ck < 8 && blocks * ck < 2 * omq_num_sms() && p.K / (2 * ck) >= 512) ck *= 2;
-  const int k_share = ((p.K + ck - 1) / ck + FEW_K - 1) / FEW_K * FEW_K;
+  for (int c : cand)
+    if (blocks * c <= 2 * omq_num_sms() && p.K >= 512 * c) { ck = c; break; }
+  const int k_share = ((p.K + ck - 1) / ck + F::FEW_K - 1) / F::FEW_K * F::FEW_K;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks * ck), 1, 1);
   cfg.blockDim = dim3((FEW_WARPS + 1) * 32, 1, 1);
@@ -742,7 +755,12 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   p.B = B; p.ldb = ldb; p.bh = b_h; p.bz = b_z;
   p.bias = bias; p.Cf = Cf; p.Cb = (__nv_bfloat16*)Cb; p.ldc = ldc; p.status = dev_status;
   if (M <= FEW_ROWS) {
-    return M <= 8 ? few_launch<1>(st, p) : (M <= 16 ? few_launch<2>(st, p) : few_launch<4>(st, p));
+    // 64 channels per CTA while that is one wave, else 128 (22016 x 4096, one row: 22.9 against 25.8 us); with
+    // 17 rows and more the conversion of the tokens counts and 64 stays the faster (34.4 against 40.5 us)
+    const bool wide = (N + 63) / 64 > 2 * omq_num_sms();
+    if (M <= 8) return wide ? few_launch<1, 128>(st, p) : few_launch<1, 64>(st, p);
+    if (M <= 16) return wide ? few_launch<2, 128>(st, p) : few_launch<2, 64>(st, p);
+    return few_launch<4, 64>(st, p);
   }
   const QPlan q = plan_of(M, N, K);
   p.splits = q.splits; p.kb_per_split = q.kb_per_split;

@@ -25,7 +25,7 @@ def _want(a, ah, az, w, wh, wz, bias):
     return y if bias is None else y + bias
 
 
-SIZES = [(1, 8, 16), (1, 4096, 4096), (2, 264, 48), (5, 136, 1040), (8, 1024, 2048), (16, 520, 4112), (17, 4096, 11008),
+SIZES = [(1, 8, 16), (1, 4096, 4096), (2, 264, 48), (3, 20000, 160), (11, 19472, 528), (5, 136, 1040), (8, 1024, 2048), (16, 520, 4112), (17, 4096, 11008),
          (33, 1000, 1024), (64, 256, 512), (65, 2056, 1008), (127, 264, 2064), (128, 4096, 1024), (129, 512, 4096),
          (200, 1288, 208), (256, 256, 64), (300, 4104, 2064), (511, 1032, 1040), (1024, 2048, 512), (700, 6152, 1168)]
 
