@@ -6,29 +6,39 @@
 // the tokens: a CTA takes (sequence, KV head, a chunk of tokens), its warps take 16-token tiles, and
 // their partial results are joined through shared memory and, between CTAs, by a second small kernel.
 //
-// Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync m16n8k16 with
-// fp16 operands and fp32 sums.  The tokens are the M dimension of the first product and the channels
-// of the second, so a single query row costs an eighth of a tile and not a sixteenth.  tcgen05 has
-// nothing to offer here: its smallest tile is 64 or 128 rows, and the products take 0.2 of the
-// instruction issue of the loop.  A code becomes an fp16 integer in registers, exactly: the byte under
-// the exponent of 1024 (0x6400 | c = 1024 + c), minus 1152.  Channels and tokens are numbered inside
-// the products so that each thread's operand values are 16 consecutive bytes of the page.
+// One thread keeps a ring of 128-token stages of K and V in flight (TMA, one box per page and head, 128-byte
+// swizzle).  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
+// m16n8k16 with fp16 operands and fp32 sums.  The tokens are the M dimension of the first product and
+// the channels of the second, so a single query row costs an eighth of a tile and not a sixteenth.
+// tcgen05 has nothing to offer here: its smallest tile is 64 or 128 rows, and the products are a tenth
+// of the loop's instructions.  A code becomes an fp16 integer in registers, exactly: the byte under the
+// exponent of 1024 (0x6400 | c = 1024 + c), minus 1152.  Channels are numbered inside the products so
+// that a thread's operand values are 16 consecutive bytes of the page; row g of a product is token
+// g ^ ((g & 1) << 2) of its eight, which puts the eight lanes of every load phase, of K and of V, on
+// eight distinct 16-byte bank groups.
 //
 // Precision: the codes are exact; q (bf16) is exact after a power-of-two scale per row that puts
 // its largest value in [2^13, 2^14); scores, sums and accumulators are fp32.  The weight of a token,
-// p sv, is rounded to fp16 against a running reference M >= log2(p sv) with 14 bits of headroom, so
-// that a weight keeps 11 bits down to 2^-28 of the largest; p's own sum stays fp32 against its own
-// running maximum m (V's scales differ by page, so the two references differ).
+// p sv, is rounded to fp16 against a reference M near the largest log2(p sv), so that a weight keeps 11
+// bits down to 2^-22 of the largest; p's own sum stays fp32 against its own reference m (V's scales
+// differ by page, so the two references differ).  A reference moves, and the accumulator with it,
+// only when a score passes it by more than 2^7: few tiles do, and the others need no maximum across
+// lanes at all, only a vote.
 #include "serve_cache.cuh"
 #include "tc.cuh"
 #include <cuda_fp16.h>
 
 namespace {
 
+using namespace tc;
+
 constexpr int HD = 128;
 constexpr int TILE = 16;                    // tokens of a warp's tile
 constexpr int MAX_CHUNK = 16384;
-constexpr float SHIFT = 14.f;               // headroom of the fp16 weights, in powers of two
+constexpr int STAGE_TOK = 128;              // tokens of a ring stage
+constexpr int STAGE_BYTES = 2 * STAGE_TOK * HD;
+constexpr float SHIFT = 8.f, SLACK = 7.f;   // a weight is 2^SHIFT at the reference and at most 2^(SHIFT + SLACK)
+constexpr float NOTHING = -1e30f;           // a reference before the first visible token
 constexpr int OPAD = 132;                   // floats per row of the joining buffer
 
 struct AttnArgs {
@@ -74,31 +84,39 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
 
-struct Tile { uint4 k[4], v[4]; };
-
-// shared memory of a CTA: query fragments | row factors | page records | joining buffers
-template <int W, int NT>
+// shared memory of a CTA: ring (the joining buffers after the loop) | query fragments | row factors |
+// references and sums | barriers | page records
+template <int NT, int STAGES>
 struct Smem {
-  static constexpr int QF = 4 * NT * 8 * 32 * 8;              // up to 4 row groups: [rg][NT][8][32] uint2
-  static constexpr int QS = 4 * NT * 8 * 4;
+  static constexpr int W = 8;
+  static constexpr int RING = STAGES * STAGE_BYTES;
+  static constexpr int QF = (NT == 1 ? 1 : 4) * NT * 8 * 32 * 8;      // [row groups][NT][8][32] uint2
+  static constexpr int QS = (NT == 1 ? 1 : 4) * NT * 8 * 4;
   static constexpr int STAT = 3 * W * NT * 8 * 4;
-  static constexpr int JOIN = W * 8 * OPAD * 4;
-  static constexpr int PAGES_OFF = QF + QS + STAT + JOIN;
-  static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12; }
+  static constexpr int BAR_OFF = RING + QF + QS + STAT;
+  static constexpr int PAGES_OFF = BAR_OFF + 2 * STAGES * 8 + 16;
+  static_assert(W * 8 * OPAD * 4 <= RING, "the joining buffer fits the ring");
+  static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12 + 1024; }
 };
 
-template <int W, int NT, int MIN_CTAS>
-__global__ void __launch_bounds__(W * 32, MIN_CTAS) kv_attention_kernel(const AttnArgs a) {
-  using S = Smem<W, NT>;
-  extern __shared__ __align__(16) uint8_t smem[];
-  uint2* qf = reinterpret_cast<uint2*>(smem);
-  float* qs = reinterpret_cast<float*>(smem + S::QF);
-  float* st_m = reinterpret_cast<float*>(smem + S::QF + S::QS);
+template <int NT, int STAGES, int MIN_CTAS>
+__global__ void __launch_bounds__(288, MIN_CTAS)
+    kv_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
+  using S = Smem<NT, STAGES>;
+  constexpr int W = S::W;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* join = reinterpret_cast<float*>(smem);
+  uint2* qf = reinterpret_cast<uint2*>(smem + S::RING);
+  float* qs = reinterpret_cast<float*>(smem + S::RING + S::QF);
+  float* st_m = reinterpret_cast<float*>(smem + S::RING + S::QF + S::QS);
   float* st_M = st_m + W * NT * 8;
   float* st_l = st_M + W * NT * 8;
-  float* join = reinterpret_cast<float*>(smem + S::QF + S::QS + S::STAT);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
+  uint64_t* empty = full + STAGES;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + STAGES);
   int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF);
-  const int P = a.c.page, per_chunk = a.chunk / P;
+  const int P = a.c.page, per_chunk = a.chunk / P, pshift = 31 - __clz(P);
   float* pks = reinterpret_cast<float*>(pid + per_chunk);     // key scale, times log2(e) / sqrt(128)
   float* plv = pks + per_chunk;                               // log2 of the value scale
 
@@ -121,11 +139,12 @@ __global__ void __launch_bounds__(W * 32, MIN_CTAS) kv_attention_kernel(const At
   const int t_begin = split * a.chunk;
   const int t_end = min(kv_end, t_begin + a.chunk);
   if (split > 0 && t_begin >= kv_end) return;
+  const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
+  const int stages = t_end > t_begin ? (t_end - t_begin + STAGE_TOK - 1) / STAGE_TOK : 0;
 
   // ---- page records of the chunk, query fragments and row factors ----
-  const int np = t_end > t_begin ? (t_end - t_begin + P - 1) / P : 0;
-  for (int i = threadIdx.x; i < np; i += W * 32) {
-    const int pg = t_begin / P + i;
+  for (int i = threadIdx.x; i < np; i += 288) {
+    const int pg = (t_begin >> pshift) + i;
     int id = pg < a.c.max_pages ? __ldg(a.c.page_table + (int64_t)b * a.c.max_pages + pg) : -1;
     if (id < 0 || id >= a.c.n_pages) {
       omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
@@ -136,7 +155,12 @@ __global__ void __launch_bounds__(W * 32, MIN_CTAS) kv_attention_kernel(const At
     pks[i] = __ldg(a.c.k_scale + at) * 0.12751743074602467f;  // log2(e) / sqrt(128)
     plv[i] = log2f(__ldg(a.c.v_scale + at));
   }
-  for (int r = warp; r < rows_cta; r += W) {
+  if (threadIdx.x == 256) {
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int r = warp; r < rows_cta; r += 9) {
     const int row = r0 + r;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (row < R) {
@@ -160,172 +184,218 @@ __global__ void __launch_bounds__(W * 32, MIN_CTAS) kv_attention_kernel(const At
   __syncthreads();
 
   const int rgi = warp % a.rg, tw = warp / a.rg, n_tw = W / a.rg;   // row group and token group of this warp
-  const uint2* qfw = qf + rgi * NT * 8 * 32 + lane;
-  float f[NT][2], m[NT][2], M[NT][2], l[NT][2];
-  int lim[NT][2];
-  float acc[NT][8][4];
+  float m[NT][2], M[NT][2], l[NT][2], acc[NT][8][4];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int r = rgi * NT * 8 + nt * 8 + 2 * lt + e, row = r0 + r;
-      f[nt][e] = qs[r];
-      lim[nt][e] = row < R ? min(s.len, start + row / rep + 1) : 0;
-      m[nt][e] = -INFINITY; M[nt][e] = -INFINITY; l[nt][e] = 0.f;
-    }
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+    for (int e = 0; e < 2; ++e) { m[nt][e] = NOTHING; M[nt][e] = NOTHING; l[nt][e] = 0.f; }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[nt][i][e] = 0.f;
+  }
 
-  const int64_t page_bytes = (int64_t)P * HD, pool_stride = page_bytes * a.c.n_kv;
-  const uint8_t* kbase = a.c.k + g * page_bytes + lg * HD + lt * 16;
-  const uint8_t* vbase = a.c.v + g * page_bytes + 2 * lt * HD + lg * 16;
-  const int pshift = 31 - __clz(P);
-  auto load = [&](int t0, Tile& T) {
-    const int id = pid[(t0 - t_begin) >> pshift];
-    const int64_t off = (int64_t)max(id, 0) * pool_stride + (t0 & (P - 1)) * HD;
-    const uint4* k = reinterpret_cast<const uint4*>(kbase + off);
-    const uint4* v = reinterpret_cast<const uint4*>(vbase + off);
-    T.k[0] = __ldg(k); T.k[1] = __ldg(k + 4); T.k[2] = __ldg(k + 64); T.k[3] = __ldg(k + 68);
-    T.v[0] = __ldg(v); T.v[1] = __ldg(v + 8); T.v[2] = __ldg(v + 64); T.v[3] = __ldg(v + 72);
-  };
-  auto compute = [&](int t0, const Tile& T) {
-    const int pi = (t0 - t_begin) >> pshift;
-    const float ks = pks[pi], lv = plv[pi];
-    const bool there = pid[pi] >= 0;
-    float sc[NT][4];
+  if (warp == W) {
+    // ---------------- the ring ----------------
+    if (lane == 0) {
+      int i = 0;
+      for (; i < stages && !*abort_flag; ++i) {
+        const int st = i % STAGES;
+        if (!mbar_wait(&empty[st], ((i / STAGES) & 1) ^ 1)) { omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
+        const int p0 = (i * STAGE_TOK) >> pshift, p1 = min(np, ((i + 1) * STAGE_TOK + P - 1) >> pshift);
+        uint32_t bytes = 0;
+        for (int p = p0; p < p1; ++p) bytes += pid[p] >= 0 ? 2 * P * HD : 0;
+        mbar_expect_tx(&full[st], bytes);
+        for (int p = p0; p < p1; ++p) {
+          if (pid[p] < 0) continue;
+          const int row = (pid[p] * a.c.n_kv + g) * P;
+          uint8_t* dst = smem + st * STAGE_BYTES + (p - p0) * P * HD;
+          tma_load_3d(&tmK, &full[st], dst, 0, row, 0);
+          tma_load_3d(&tmV, &full[st], dst + STAGE_TOK * HD, 0, row, 0);
+        }
+      }
+      if (*abort_flag)                       // no copy may land after this CTA has left
+        for (int j = i > STAGES ? i - STAGES : 0; j < i; ++j) mbar_wait(&full[j % STAGES], (j / STAGES) & 1);
+    }
+  } else {
+    const uint2* qfw = qf + rgi * NT * 8 * 32 + lane;
+    uint2 qr[NT == 1 ? 8 : 1];               // one row tile: its fragments stay in registers
+    if (NT == 1) {
+#pragma unroll
+      for (int w = 0; w < 8; ++w) qr[NT == 1 ? w : 0] = qfw[w * 32];
+    }
+    float f[NT][2];
+    int lim[NT][2], lim_min = 0x7fffffff;    // keys seen by each row; by all of the warp's rows
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const uint32_t x = u4(T.k[w >> 2], w & 3), y = u4(T.k[2 + (w >> 2)], w & 3);
-      const uint32_t a0 = codes_lo(x), a1 = codes_lo(y), a2 = codes_hi(x), a3 = codes_hi(y);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint2 q = qfw[(nt * 8 + w) * 32];
-        mma16816(sc[nt], a0, a1, a2, a3, q.x, q.y);
-      }
-    }
-    uint32_t p0[NT], p1[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float x[4], top[2];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = t0 + lg + 8 * (e >> 1);
-        x[e] = t < lim[nt][e & 1] && there ? sc[nt][e] * (ks * f[nt][e & 1]) : -INFINITY;
-      }
-#pragma unroll
       for (int e = 0; e < 2; ++e) {
-        top[e] = fmaxf(x[e], x[e + 2]);
-        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 4));
-        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
-        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16));
+        const int r = rgi * NT * 8 + nt * 8 + 2 * lt + e, row = r0 + r;
+        f[nt][e] = qs[r];
+        lim[nt][e] = row < R ? min(s.len, start + row / rep + 1) : 0;
+        if (row < R) lim_min = min(lim_min, lim[nt][e]);
       }
-      float grow[2], pw[4];
-      bool moved = false;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[nt][e], top[e]), mr = mn == -INFINITY ? 0.f : mn;
-        l[nt][e] = l[nt][e] * tc::ex2(m[nt][e] - mr) + (tc::ex2(x[e] - mr) + tc::ex2(x[e + 2] - mr));
-        m[nt][e] = mn;
-        const float Mn = fmaxf(M[nt][e], top[e] + lv), Mr = Mn == -INFINITY ? 0.f : Mn;
-        grow[e] = tc::ex2(M[nt][e] - Mr);
-        moved = moved || Mn != M[nt][e];
-        M[nt][e] = Mn;
-        const float ref = lv - Mr + SHIFT;
-        pw[e] = tc::ex2(x[e] + ref);
-        pw[e + 2] = tc::ex2(x[e + 2] + ref);
-      }
-      if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[nt][i][e] *= grow[e & 1];
-      }
-      p0[nt] = transpose8x8(pack_half2(pw[0], pw[1]));
-      p1[nt] = transpose8x8(pack_half2(pw[2], pw[3]));
-    }
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t va = u4(T.v[0], w), vb = u4(T.v[1], w), vc = u4(T.v[2], w), vd = u4(T.v[3], w);
-      const uint32_t x0 = __byte_perm(va, vb, 0x5140), x1 = __byte_perm(vc, vd, 0x5140);
-      const uint32_t y0 = __byte_perm(va, vb, 0x7362), y1 = __byte_perm(vc, vd, 0x7362);
-      const uint32_t a0 = codes_lo(x0), a1 = codes_hi(x0), a2 = codes_lo(x1), a3 = codes_hi(x1);
-      const uint32_t c0 = codes_lo(y0), c1 = codes_hi(y0), c2 = codes_lo(y1), c3 = codes_hi(y1);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        mma16816(acc[nt][2 * w], a0, a1, a2, a3, p0[nt], p1[nt]);
-        mma16816(acc[nt][2 * w + 1], c0, c1, c2, c3, p0[nt], p1[nt]);
-      }
-    }
-  };
+    lim_min = __reduce_min_sync(0xffffffffu, lim_min);
+    const bool idle = r0 + rgi * NT * 8 >= R;                 // no row of this warp exists
+    const int row_k = lg ^ ((lg & 1) << 2);                   // token of product row lg among its eight
+    const int row_v0 = 2 * lt, row_v1 = (2 * lt + 1) ^ 4;     // tokens of the product columns 2 lt, 2 lt + 1
+    const uint32_t k_off = row_k * HD, kx0 = (uint32_t)(lt ^ row_k) << 4, kx1 = (uint32_t)((lt + 4) ^ row_k) << 4;
+    const uint32_t v_off0 = STAGE_TOK * HD + row_v0 * HD + ((uint32_t)(lg ^ row_v0) << 4);
+    const uint32_t v_off1 = STAGE_TOK * HD + row_v1 * HD + ((uint32_t)(lg ^ row_v1) << 4);
 
-  // the next tile's loads are in flight while the current one is computed
-  const int step = TILE * n_tw;
-  int t0 = t_begin + TILE * tw;
-  Tile cur, nxt;
-  if (t0 < t_end) load(t0, cur);
-  while (t0 < t_end) {
-    if (t0 + step < t_end) load(t0 + step, nxt);
-    compute(t0, cur);
-    cur = nxt;
-    t0 += step;
+    auto tile = [&](const uint32_t base, const int t0) {
+      const int pi = (t0 - t_begin) >> pshift;
+      if (pid[pi] < 0) return;
+      const float ks = pks[pi], lv = plv[pi];
+      float sc[NT][4];
+      {
+        uint4 k[4];
+        k[0] = lds128(base + k_off + kx0); k[1] = lds128(base + k_off + kx1);
+        k[2] = lds128(base + k_off + 8 * HD + kx0); k[3] = lds128(base + k_off + 8 * HD + kx1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const uint32_t x = u4(k[w >> 2], w & 3), y = u4(k[2 + (w >> 2)], w & 3);
+          const uint32_t a0 = codes_lo(x), a1 = codes_lo(y), a2 = codes_hi(x), a3 = codes_hi(y);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const uint2 q = NT == 1 ? qr[NT == 1 ? w : 0] : qfw[(nt * 8 + w) * 32];
+            mma16816(sc[nt], a0, a1, a2, a3, q.x, q.y);
+          }
+        }
+      }
+      uint4 v[4];
+      v[0] = lds128(base + v_off0); v[1] = lds128(base + v_off1);
+      v[2] = lds128(base + v_off0 + 8 * HD); v[3] = lds128(base + v_off1 + 8 * HD);
+      uint32_t p0[NT], p1[NT];
+      const bool cut = t0 + TILE > lim_min;                   // some row does not see all of the tile
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = sc[nt][e] * (ks * f[nt][e & 1]);
+        if (cut) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t0 + row_k + 8 * (e >> 1) >= lim[nt][e & 1]) x[e] = -INFINITY;
+        }
+        const float t0m = fmaxf(x[0], x[2]), t1m = fmaxf(x[1], x[3]);
+        const bool over = t0m > m[nt][0] + SLACK || t1m > m[nt][1] + SLACK || t0m + lv > M[nt][0] + SLACK ||
+                          t1m + lv > M[nt][1] + SLACK;
+        if (__any_sync(0xffffffffu, over)) {
+          float top[2] = {t0m, t1m}, grow[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 4));
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16));
+            const float mn = fmaxf(m[nt][e], top[e]), Mn = fmaxf(M[nt][e], top[e] + lv);
+            l[nt][e] *= ex2(m[nt][e] - mn);
+            grow[e] = ex2(M[nt][e] - Mn);
+            m[nt][e] = mn;
+            M[nt][e] = Mn;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[nt][i][e] *= grow[e & 1];
+        }
+        float pw[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float c = ex2(lv + (m[nt][e] - M[nt][e]) + SHIFT);
+          pw[e] = ex2(x[e] - m[nt][e]);
+          pw[e + 2] = ex2(x[e + 2] - m[nt][e]);
+          l[nt][e] += pw[e] + pw[e + 2];
+          pw[e] *= c;
+          pw[e + 2] *= c;
+        }
+        p0[nt] = transpose8x8(pack_half2(pw[0], pw[1]));
+        p1[nt] = transpose8x8(pack_half2(pw[2], pw[3]));
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t va = u4(v[0], w), vb = u4(v[1], w), vc = u4(v[2], w), vd = u4(v[3], w);
+        const uint32_t x0 = __byte_perm(va, vb, 0x5140), x1 = __byte_perm(vc, vd, 0x5140);
+        const uint32_t y0 = __byte_perm(va, vb, 0x7362), y1 = __byte_perm(vc, vd, 0x7362);
+        const uint32_t a0 = codes_lo(x0), a1 = codes_hi(x0), a2 = codes_lo(x1), a3 = codes_hi(x1);
+        const uint32_t c0 = codes_lo(y0), c1 = codes_hi(y0), c2 = codes_lo(y1), c3 = codes_hi(y1);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma16816(acc[nt][2 * w], a0, a1, a2, a3, p0[nt], p1[nt]);
+          mma16816(acc[nt][2 * w + 1], c0, c1, c2, c3, p0[nt], p1[nt]);
+        }
+      }
+    };
+
+    for (int i = 0; i < stages; ++i) {
+      const int st = i % STAGES;
+      if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (i / STAGES) & 1))) {
+        omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
+      }
+      const uint32_t base = smem_u32(smem + st * STAGE_BYTES);
+      const int ts = t_begin + i * STAGE_TOK;
+      if (!idle)
+        for (int k = tw; k < STAGE_TOK / TILE && ts + k * TILE < t_end; k += n_tw) tile(base + k * TILE * HD, ts + k * TILE);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[st]);
+    }
   }
 
   // ---- join the token groups of each row group ----
+  if (warp < W) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float v = l[nt][e];
-      v += __shfl_xor_sync(0xffffffffu, v, 4);
-      v += __shfl_xor_sync(0xffffffffu, v, 8);
-      v += __shfl_xor_sync(0xffffffffu, v, 16);
-      if (lg == 0) {
-        const int at = (warp * NT + nt) * 8 + 2 * lt + e;
-        st_m[at] = m[nt][e]; st_M[at] = M[nt][e]; st_l[at] = v;
+      for (int e = 0; e < 2; ++e) {
+        float v = l[nt][e];
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        if (lg == 0) {
+          const int at = (warp * NT + nt) * 8 + 2 * lt + e;
+          st_m[at] = m[nt][e]; st_M[at] = M[nt][e]; st_l[at] = v;
+        }
       }
-    }
+  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     __syncthreads();
+    if (warp < W) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float4* o = reinterpret_cast<float4*>(join + (warp * 8 + 2 * lt + e) * OPAD + 16 * lg);
+      for (int e = 0; e < 2; ++e) {
+        float4* o = reinterpret_cast<float4*>(join + (warp * 8 + 2 * lt + e) * OPAD + 16 * lg);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        o[i] = make_float4(acc[nt][2 * i][e], acc[nt][2 * i][e + 2], acc[nt][2 * i + 1][e], acc[nt][2 * i + 1][e + 2]);
+        for (int i = 0; i < 4; ++i)
+          o[i] = make_float4(acc[nt][2 * i][e], acc[nt][2 * i][e + 2], acc[nt][2 * i + 1][e], acc[nt][2 * i + 1][e + 2]);
+      }
     }
     __syncthreads();
-    for (int rq = warp; rq < a.rg * 8; rq += W) {             // one query row per warp, 4 channels per lane
+    for (int rq = warp; rq < a.rg * 8; rq += 9) {             // one query row per warp, 4 channels per lane
       const int gi = rq >> 3, q = rq & 7;
       const int row = r0 + gi * NT * 8 + nt * 8 + q;
       if (row >= R) continue;
-      float mm = -INFINITY, MM = -INFINITY;
+      float mm = NOTHING, MM = NOTHING;
       for (int k = 0; k < n_tw; ++k) {
         const int at = ((k * a.rg + gi) * NT + nt) * 8 + q;
         mm = fmaxf(mm, st_m[at]);
         MM = fmaxf(MM, st_M[at]);
       }
-      const float mr = mm == -INFINITY ? 0.f : mm, Mr = MM == -INFINITY ? 0.f : MM;
       float L = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = 0; k < n_tw; ++k) {
         const int wk = k * a.rg + gi, at = (wk * NT + nt) * 8 + q;
-        L += st_l[at] * tc::ex2(st_m[at] - mr);
-        const float c = tc::ex2(st_M[at] - Mr);
+        L += st_l[at] * ex2(st_m[at] - mm);
+        const float c = ex2(st_M[at] - MM);
         const float4 x = *reinterpret_cast<const float4*>(join + (wk * 8 + q) * OPAD + 4 * lane);
         o.x = fmaf(x.x, c, o.x); o.y = fmaf(x.y, c, o.y); o.z = fmaf(x.z, c, o.z); o.w = fmaf(x.w, c, o.w);
       }
-      const bool empty = mm == -INFINITY && L == 0.f;         // a NaN score is not an empty row
-      const float c = empty ? 0.f : tc::ex2(Mr - mr - SHIFT) / L;
-      const float lse = empty ? -INFINITY : mr + log2f(L);
+      const bool none = L == 0.f;                             // a NaN score is not an empty row
+      const float c = none ? 0.f : ex2(MM - mm - SHIFT) / L;
+      const float lse = none ? -INFINITY : mm + log2f(L);
       o.x *= c; o.y *= c; o.z *= c; o.w *= c;
       const int64_t tok = s.row0 + row / rep;
       const int head = g * rep + row % rep;
@@ -369,7 +439,7 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
   for (int k = 0; k < nv; ++k) {
-    const float c = tc::ex2(a.wl[at + k] - ref);
+    const float c = ex2(a.wl[at + k] - ref);
     const float4 x = *reinterpret_cast<const float4*>(a.wo + (at + k) * HD + 4 * lane);
     L += c;
     o.x = fmaf(x.x, c, o.x); o.y = fmaf(x.y, c, o.y); o.z = fmaf(x.z, c, o.z); o.w = fmaf(x.w, c, o.w);
@@ -399,7 +469,7 @@ Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   const int64_t per = 8ll * p.nt * p.rg;
   p.row_tiles = (int)((rows + per - 1) / per);
   const int64_t units = B * n_kv * p.row_tiles;
-  const int64_t slots = (int64_t)omq_num_sms() * (p.nt == 1 ? 2 : 3);
+  const int64_t slots = (int64_t)omq_num_sms() * (p.nt == 1 ? 2 : 1);
   int64_t n = (2 * slots + units - 1) / units;
   const int64_t most = (max_kv + 255) / 256;
   if (n > most) n = most;
@@ -417,18 +487,21 @@ size_t plan_workspace(const Plan& p, int64_t total_q, int64_t n_heads) {
   return parts * HD * sizeof(float) + (parts * sizeof(float) + 255) / 256 * 256;
 }
 
-template <int W, int NT, int MIN_CTAS>
+template <int NT, int STAGES, int MIN_CTAS>
 omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
-  auto kern = kv_attention_kernel<W, NT, MIN_CTAS>;
-  const int bytes = Smem<W, NT>::bytes(a.chunk, a.c.page);
+  using S = Smem<NT, STAGES>;
+  auto kern = kv_attention_kernel<NT, STAGES, MIN_CTAS>;
   static bool set = false;
   if (!set) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<W, NT>::bytes(MAX_CHUNK, 16)) !=
-        cudaSuccess)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes(MAX_CHUNK, 16)) != cudaSuccess)
       return OMQ_ERR_CUDA;
     set = true;
   }
-  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), W * 32, bytes, st>>>(a);
+  CUtensorMap tk, tv;
+  const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
+  if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, a.c.page, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, a.c.page, HD))
+    return OMQ_ERR_UNSUPPORTED;
+  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), 288, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -455,6 +528,7 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
               OMQ_ERR_ALIGN);
   const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
   OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles <= 65535, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE((int64_t)cache->n_pages * cache->n_kv * cache->page < (1ll << 31), OMQ_ERR_SHAPE);   // TMA coordinates
   const size_t need = plan_workspace(p, total_q, n_heads);
   OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
   AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
@@ -464,7 +538,7 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
     a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
   }
   cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY(p.nt == 1 ? (attn_launch<8, 1, 2>(st, a)) : (attn_launch<4, 2, 3>(st, a)));
+  OMQ_TRY(p.nt == 1 ? (attn_launch<1, 3, 2>(st, a)) : (attn_launch<2, 6, 1>(st, a)));
   if (p.n_split > 1) {
     const int64_t pairs = (int64_t)max_q * n_heads;
     kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
