@@ -6,8 +6,9 @@
 // the tokens: a CTA takes (sequence, KV head, a chunk of tokens), its warps take 16-token tiles, and
 // their partial results are joined through shared memory and, between CTAs, by a second small kernel.
 //
-// One thread keeps a ring of 128-token stages of K and V in flight (TMA, one box per page and head, 128-byte
-// swizzle).  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
+// Every token group of warps keeps its own ring of 16-token tiles in flight (TMA, 2 KB of K and of V each,
+// 128-byte swizzle): a warp that is alone on its tiles refills a slot as soon as it has used it, with no
+// barrier between warps.  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
 // m16n8k16 with fp16 operands and fp32 sums.  The tokens are the M dimension of the first product and
 // the channels of the second, so a single query row costs an eighth of a tile and not a sixteenth.
 // tcgen05 has nothing to offer here: its smallest tile is 64 or 128 rows, and the products are a tenth
@@ -35,8 +36,7 @@ using namespace tc;
 constexpr int HD = 128;
 constexpr int TILE = 16;                    // tokens of a warp's tile
 constexpr int MAX_CHUNK = 16384;
-constexpr int STAGE_TOK = 128;              // tokens of a ring stage
-constexpr int STAGE_BYTES = 2 * STAGE_TOK * HD;
+constexpr int TILE_BYTES = 2 * TILE * HD;    // K and V
 constexpr float SHIFT = 8.f, SLACK = 7.f;   // a weight is 2^SHIFT at the reference and at most 2^(SHIFT + SLACK)
 constexpr float NOTHING = -1e30f;           // a reference before the first visible token
 constexpr int OPAD = 132;                   // floats per row of the joining buffer
@@ -84,37 +84,39 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
 
-// shared memory of a CTA: ring (the joining buffers after the loop) | query fragments | row factors |
-// references and sums | barriers | page records
-template <int NT, int STAGES>
+// shared memory of a CTA: ring (the joining buffers after the loop) | query fragments | per row: factor,
+// keys seen | references and sums | barriers | page records
+constexpr int W = 8;                        // warps
+template <int NT>
 struct Smem {
-  static constexpr int W = 8;
-  static constexpr int RING = STAGES * STAGE_BYTES;
-  static constexpr int QF = (NT == 1 ? 1 : 4) * NT * 8 * 32 * 8;      // [row groups][NT][8][32] uint2
-  static constexpr int QS = (NT == 1 ? 1 : 4) * NT * 8 * 4;
-  static constexpr int STAT = 3 * W * NT * 8 * 4;
-  static constexpr int BAR_OFF = RING + QF + QS + STAT;
-  static constexpr int PAGES_OFF = BAR_OFF + 2 * STAGES * 8 + 16;
+  static constexpr int SLOTS = NT == 1 ? 24 : 16;                     // ring tiles: SLOTS / W per warp of a token group
+  static constexpr int RING = SLOTS * TILE_BYTES;
+  static constexpr int ROWS = (NT == 1 ? 1 : 4) * NT * 8;             // up to 4 row groups
+  static constexpr int QF = ROWS * HD * 2;                            // [row groups][NT][8][32] uint2
+  static constexpr int QS_OFF = RING + QF;
+  static constexpr int STAT_OFF = QS_OFF + 2 * ROWS * 4;
+  static constexpr int BAR_OFF = STAT_OFF + 3 * W * NT * 8 * 4;
+  static constexpr int PAGES_OFF = BAR_OFF + 2 * SLOTS * 8 + 16;
   static_assert(W * 8 * OPAD * 4 <= RING, "the joining buffer fits the ring");
   static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12 + 1024; }
 };
 
-template <int NT, int STAGES, int MIN_CTAS>
-__global__ void __launch_bounds__(288, MIN_CTAS)
+template <int NT>
+__global__ void __launch_bounds__(W * 32, 2)
     kv_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
-  using S = Smem<NT, STAGES>;
-  constexpr int W = S::W;
+  using S = Smem<NT>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* join = reinterpret_cast<float*>(smem);
   uint2* qf = reinterpret_cast<uint2*>(smem + S::RING);
-  float* qs = reinterpret_cast<float*>(smem + S::RING + S::QF);
-  float* st_m = reinterpret_cast<float*>(smem + S::RING + S::QF + S::QS);
+  float* qs = reinterpret_cast<float*>(smem + S::QS_OFF);
+  int* lims = reinterpret_cast<int*>(qs + S::ROWS);
+  float* st_m = reinterpret_cast<float*>(smem + S::STAT_OFF);
   float* st_M = st_m + W * NT * 8;
   float* st_l = st_M + W * NT * 8;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
-  uint64_t* empty = full + STAGES;
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + STAGES);
+  uint64_t* empty = full + S::SLOTS;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + S::SLOTS);
   int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF);
   const int P = a.c.page, per_chunk = a.chunk / P, pshift = 31 - __clz(P);
   float* pks = reinterpret_cast<float*>(pid + per_chunk);     // key scale, times log2(e) / sqrt(128)
@@ -140,10 +142,15 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
   const int t_end = min(kv_end, t_begin + a.chunk);
   if (split > 0 && t_begin >= kv_end) return;
   const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
-  const int stages = t_end > t_begin ? (t_end - t_begin + STAGE_TOK - 1) / STAGE_TOK : 0;
+  const int tiles = t_end > t_begin ? (t_end - t_begin + TILE - 1) / TILE : 0;
+
+  // row groups that the CTA's rows need: with fewer than the call's largest, more warps share the tokens
+  int rg = a.rg;
+  while (rg > 1 && R - r0 <= (rg >> 1) * NT * 8) rg >>= 1;
+  const int rows_here = rg * NT * 8;
 
   // ---- page records of the chunk, query fragments and row factors ----
-  for (int i = threadIdx.x; i < np; i += 288) {
+  for (int i = threadIdx.x; i < np; i += W * 32) {
     const int pg = (t_begin >> pshift) + i;
     int id = pg < a.c.max_pages ? __ldg(a.c.page_table + (int64_t)b * a.c.max_pages + pg) : -1;
     if (id < 0 || id >= a.c.n_pages) {
@@ -155,12 +162,13 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
     pks[i] = __ldg(a.c.k_scale + at) * 0.12751743074602467f;  // log2(e) / sqrt(128)
     plv[i] = log2f(__ldg(a.c.v_scale + at));
   }
-  if (threadIdx.x == 256) {
-    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], W); }
+  if (threadIdx.x == 0) {
+    const int sharing = min(rg, (R - r0 + NT * 8 - 1) / (NT * 8));            // warps that use each tile
+    for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], sharing); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int r = warp; r < rows_cta; r += 9) {
+  for (int r = warp; r < rows_here; r += W) {
     const int row = r0 + r;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (row < R) {
@@ -179,11 +187,14 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
     const int nt = r >> 3, q = r & 7;
     const int w = (lane & 3) + (lane < 16 ? 0 : 4), t = (lane >> 2) & 3;
     qf[(nt * 8 + w) * 32 + q * 4 + t] = make_uint2(pack_half2(v[0] * up, v[1] * up), pack_half2(v[2] * up, v[3] * up));
-    if (lane == 0) qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
+    if (lane == 0) {
+      qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
+      lims[r] = row < R ? min(s.len, start + row / rep + 1) : 0;
+    }
   }
   __syncthreads();
 
-  const int rgi = warp % a.rg, tw = warp / a.rg, n_tw = W / a.rg;   // row group and token group of this warp
+  const int rgi = warp % rg, tw = warp / rg, n_tw = W / rg;         // row group and token group of this warp
   float m[NT][2], M[NT][2], l[NT][2], acc[NT][8][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -195,53 +206,44 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
       for (int e = 0; e < 4; ++e) acc[nt][i][e] = 0.f;
   }
 
-  if (warp == W) {
-    // ---------------- the ring ----------------
-    if (lane == 0) {
-      int i = 0;
-      for (; i < stages && !*abort_flag; ++i) {
-        const int st = i % STAGES;
-        if (!mbar_wait(&empty[st], ((i / STAGES) & 1) ^ 1)) { omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
-        const int p0 = (i * STAGE_TOK) >> pshift, p1 = min(np, ((i + 1) * STAGE_TOK + P - 1) >> pshift);
-        uint32_t bytes = 0;
-        for (int p = p0; p < p1; ++p) bytes += pid[p] >= 0 ? 2 * P * HD : 0;
-        mbar_expect_tx(&full[st], bytes);
-        for (int p = p0; p < p1; ++p) {
-          if (pid[p] < 0) continue;
-          const int row = (pid[p] * a.c.n_kv + g) * P;
-          uint8_t* dst = smem + st * STAGE_BYTES + (p - p0) * P * HD;
-          tma_load_3d(&tmK, &full[st], dst, 0, row, 0);
-          tma_load_3d(&tmV, &full[st], dst + STAGE_TOK * HD, 0, row, 0);
-        }
-      }
-      if (*abort_flag)                       // no copy may land after this CTA has left
-        for (int j = i > STAGES ? i - STAGES : 0; j < i; ++j) mbar_wait(&full[j % STAGES], (j / STAGES) & 1);
-    }
-  } else {
+  // this token group's ring: its n-th tile is tile tw + n n_tw of the chunk, in slot n % depth
+  const int depth = S::SLOTS / n_tw, mine = tiles > tw ? (tiles - tw + n_tw - 1) / n_tw : 0;
+  uint64_t* gfull = full + tw * depth;
+  uint64_t* gempty = empty + tw * depth;
+  const uint32_t ring = smem_u32(smem + tw * depth * TILE_BYTES);
+  auto fill = [&](const int n, const int slot) {              // one thread
+    const int t = (tw + n * n_tw) * TILE, id = pid[t >> pshift];
+    if (id < 0) { mbar_arrive(&gfull[slot]); return; }        // its tokens read as unseen
+    uint8_t* dst = smem + (tw * depth + slot) * TILE_BYTES;
+    const int row = (id * a.c.n_kv + g) * P + (t & (P - 1));
+    mbar_expect_tx(&gfull[slot], TILE_BYTES);
+    tma_load_3d(&tmK, &gfull[slot], dst, 0, row, 0);
+    tma_load_3d(&tmV, &gfull[slot], dst + TILE * HD, 0, row, 0);
+  };
+  const bool leads = rgi == 0 && lane == 0;
+  int filled = min(depth, mine);
+  if (leads)
+    for (int n = 0; n < filled; ++n) fill(n, n);
+
+  {
     const uint2* qfw = qf + rgi * NT * 8 * 32 + lane;
     uint2 qr[NT == 1 ? 8 : 1];               // one row tile: its fragments stay in registers
     if (NT == 1) {
 #pragma unroll
       for (int w = 0; w < 8; ++w) qr[NT == 1 ? w : 0] = qfw[w * 32];
     }
-    float f[NT][2];
-    int lim[NT][2], lim_min = 0x7fffffff;    // keys seen by each row; by all of the warp's rows
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = rgi * NT * 8 + nt * 8 + 2 * lt + e, row = r0 + r;
-        f[nt][e] = qs[r];
-        lim[nt][e] = row < R ? min(s.len, start + row / rep + 1) : 0;
-        if (row < R) lim_min = min(lim_min, lim[nt][e]);
-      }
+    int lim_min = 0x7fffffff;                // keys that every row of the warp sees
+    for (int r = lane; r < NT * 8; r += 32)
+      if (r0 + rgi * NT * 8 + r < R) lim_min = lims[rgi * NT * 8 + r];
     lim_min = __reduce_min_sync(0xffffffffu, lim_min);
-    const bool idle = r0 + rgi * NT * 8 >= R;                 // no row of this warp exists
+    const int n_here = min(NT, (R - r0 - rgi * NT * 8 + 7) >> 3);   // row tiles of this warp that hold rows
+    const float2* f2 = reinterpret_cast<const float2*>(qs + rgi * NT * 8) + lt;
+    const int2* lim2 = reinterpret_cast<const int2*>(lims + rgi * NT * 8) + lt;
     const int row_k = lg ^ ((lg & 1) << 2);                   // token of product row lg among its eight
     const int row_v0 = 2 * lt, row_v1 = (2 * lt + 1) ^ 4;     // tokens of the product columns 2 lt, 2 lt + 1
     const uint32_t k_off = row_k * HD, kx0 = (uint32_t)(lt ^ row_k) << 4, kx1 = (uint32_t)((lt + 4) ^ row_k) << 4;
-    const uint32_t v_off0 = STAGE_TOK * HD + row_v0 * HD + ((uint32_t)(lg ^ row_v0) << 4);
-    const uint32_t v_off1 = STAGE_TOK * HD + row_v1 * HD + ((uint32_t)(lg ^ row_v1) << 4);
+    const uint32_t v_off0 = TILE * HD + row_v0 * HD + ((uint32_t)(lg ^ row_v0) << 4);
+    const uint32_t v_off1 = TILE * HD + row_v1 * HD + ((uint32_t)(lg ^ row_v1) << 4);
 
     auto tile = [&](const uint32_t base, const int t0) {
       const int pi = (t0 - t_begin) >> pshift;
@@ -262,6 +264,7 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
           const uint32_t a0 = codes_lo(x), a1 = codes_lo(y), a2 = codes_hi(x), a3 = codes_hi(y);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt >= n_here) break;
             const uint2 q = NT == 1 ? qr[NT == 1 ? w : 0] : qfw[(nt * 8 + w) * 32];
             mma16816(sc[nt], a0, a1, a2, a3, q.x, q.y);
           }
@@ -274,13 +277,17 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
       const bool cut = t0 + TILE > lim_min;                   // some row does not see all of the tile
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
+        if (nt > 0 && nt >= n_here) break;
+        const float2 f = f2[4 * nt];
+        const float fk[2] = {ks * f.x, ks * f.y};
         float x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = sc[nt][e] * (ks * f[nt][e & 1]);
+        for (int e = 0; e < 4; ++e) x[e] = sc[nt][e] * fk[e & 1];
         if (cut) {
+          const int2 lm = lim2[4 * nt];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t0 + row_k + 8 * (e >> 1) >= lim[nt][e & 1]) x[e] = -INFINITY;
+            if (t0 + row_k + 8 * (e >> 1) >= (e & 1 ? lm.y : lm.x)) x[e] = -INFINITY;
         }
         const float t0m = fmaxf(x[0], x[2]), t1m = fmaxf(x[1], x[3]);
         const bool over = t0m > m[nt][0] + SLACK || t1m > m[nt][1] + SLACK || t0m + lv > M[nt][0] + SLACK ||
@@ -325,69 +332,76 @@ __global__ void __launch_bounds__(288, MIN_CTAS)
         const uint32_t c0 = codes_lo(y0), c1 = codes_hi(y0), c2 = codes_lo(y1), c3 = codes_hi(y1);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          if (nt > 0 && nt >= n_here) break;
           mma16816(acc[nt][2 * w], a0, a1, a2, a3, p0[nt], p1[nt]);
           mma16816(acc[nt][2 * w + 1], c0, c1, c2, c3, p0[nt], p1[nt]);
         }
       }
     };
 
-    for (int i = 0; i < stages; ++i) {
-      const int st = i % STAGES;
-      if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (i / STAGES) & 1))) {
+    int slot = 0, turn = 0;                  // of tile n
+    for (int n = 0; n < mine && n_here > 0; ++n) {
+      if (rg > 1 && leads && n > 0 && filled < mine) {        // the slot that the group left last
+        const int ls = slot == 0 ? depth - 1 : slot - 1, lt_ = slot == 0 ? turn ^ 1 : turn;
+        if (mbar_wait(&gempty[ls], lt_)) fill(filled++, ls);
+        else *abort_flag = 1;
+      }
+      __syncwarp();
+      if (!__all_sync(0xffffffffu, !*abort_flag && mbar_wait(&gfull[slot], turn))) {
         omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
       }
-      const uint32_t base = smem_u32(smem + st * STAGE_BYTES);
-      const int ts = t_begin + i * STAGE_TOK;
-      if (!idle)
-        for (int k = tw; k < STAGE_TOK / TILE && ts + k * TILE < t_end; k += n_tw) tile(base + k * TILE * HD, ts + k * TILE);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[st]);
+      tile(ring + slot * TILE_BYTES, t_begin + (tw + n * n_tw) * TILE);
+      __syncwarp();                          // every lane has read the tile
+      if (rg > 1) {
+        if (lane == 0) mbar_arrive(&gempty[slot]);
+      } else if (leads && filled < mine) {
+        fill(filled++, slot);
+      }
+      if (++slot == depth) { slot = 0; turn ^= 1; }
     }
+    if (leads && *abort_flag)                // no copy may land after this CTA has left
+      for (int j = max(0, filled - depth); j < filled; ++j) mbar_wait(&gfull[j % depth], (j / depth) & 1);
   }
 
   // ---- join the token groups of each row group ----
-  if (warp < W) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float v = l[nt][e];
-        v += __shfl_xor_sync(0xffffffffu, v, 4);
-        v += __shfl_xor_sync(0xffffffffu, v, 8);
-        v += __shfl_xor_sync(0xffffffffu, v, 16);
-        if (lg == 0) {
-          const int at = (warp * NT + nt) * 8 + 2 * lt + e;
-          st_m[at] = m[nt][e]; st_M[at] = M[nt][e]; st_l[at] = v;
-        }
+    for (int e = 0; e < 2; ++e) {
+      float v = l[nt][e];
+      v += __shfl_xor_sync(0xffffffffu, v, 4);
+      v += __shfl_xor_sync(0xffffffffu, v, 8);
+      v += __shfl_xor_sync(0xffffffffu, v, 16);
+      if (lg == 0) {
+        const int at = (warp * NT + nt) * 8 + 2 * lt + e;
+        st_m[at] = m[nt][e]; st_M[at] = M[nt][e]; st_l[at] = v;
       }
-  }
+    }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     __syncthreads();
-    if (warp < W) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float4* o = reinterpret_cast<float4*>(join + (warp * 8 + 2 * lt + e) * OPAD + 16 * lg);
+    for (int e = 0; e < 2; ++e) {
+      float4* o = reinterpret_cast<float4*>(join + (warp * 8 + 2 * lt + e) * OPAD + 16 * lg);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          o[i] = make_float4(acc[nt][2 * i][e], acc[nt][2 * i][e + 2], acc[nt][2 * i + 1][e], acc[nt][2 * i + 1][e + 2]);
-      }
+      for (int i = 0; i < 4; ++i)
+        o[i] = make_float4(acc[nt][2 * i][e], acc[nt][2 * i][e + 2], acc[nt][2 * i + 1][e], acc[nt][2 * i + 1][e + 2]);
     }
     __syncthreads();
-    for (int rq = warp; rq < a.rg * 8; rq += 9) {             // one query row per warp, 4 channels per lane
+    for (int rq = warp; rq < rg * 8; rq += W) {             // one query row per warp, 4 channels per lane
       const int gi = rq >> 3, q = rq & 7;
       const int row = r0 + gi * NT * 8 + nt * 8 + q;
       if (row >= R) continue;
       float mm = NOTHING, MM = NOTHING;
       for (int k = 0; k < n_tw; ++k) {
-        const int at = ((k * a.rg + gi) * NT + nt) * 8 + q;
+        const int at = ((k * rg + gi) * NT + nt) * 8 + q;
         mm = fmaxf(mm, st_m[at]);
         MM = fmaxf(MM, st_M[at]);
       }
       float L = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = 0; k < n_tw; ++k) {
-        const int wk = k * a.rg + gi, at = (wk * NT + nt) * 8 + q;
+        const int wk = k * rg + gi, at = (wk * NT + nt) * 8 + q;
         L += st_l[at] * ex2(st_m[at] - mm);
         const float c = ex2(st_M[at] - MM);
         const float4 x = *reinterpret_cast<const float4*>(join + (wk * 8 + q) * OPAD + 4 * lane);
@@ -459,8 +473,11 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
 
 struct Plan { int nt, rg, row_tiles, chunk, n_split; };
 
-// How a call is cut.  Rows per CTA: 8 (one new token of up to 8 query heads per KV head), 16, 32 or 64;
-// tokens per CTA: as many chunks as give every SM two rounds of CTAs, none under 256 tokens.
+// How a call is cut.  Rows per CTA: 8 (one new token of up to 8 query heads per KV head), 16, 32 or 64.
+// Tokens per CTA: with 8 rows as many chunks as fill one wave (a second one costs more than it balances:
+// 4 x 131072 tokens 145 us on one wave, 155 us on two); with more rows, where the work of a CTA depends on its
+// sequence's rows and length, six waves (64 ragged sequences: 270 us on one, 204 us on six); none under
+// 256 tokens.
 Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   Plan p;
   const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
@@ -469,8 +486,8 @@ Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   const int64_t per = 8ll * p.nt * p.rg;
   p.row_tiles = (int)((rows + per - 1) / per);
   const int64_t units = B * n_kv * p.row_tiles;
-  const int64_t slots = (int64_t)omq_num_sms() * (p.nt == 1 ? 2 : 1);
-  int64_t n = (2 * slots + units - 1) / units;
+  const int64_t slots = 2ll * omq_num_sms();
+  int64_t n = p.nt == 1 ? slots / units : 6 * slots / units;
   const int64_t most = (max_kv + 255) / 256;
   if (n > most) n = most;
   if (n < 1) n = 1;
@@ -487,10 +504,10 @@ size_t plan_workspace(const Plan& p, int64_t total_q, int64_t n_heads) {
   return parts * HD * sizeof(float) + (parts * sizeof(float) + 255) / 256 * 256;
 }
 
-template <int NT, int STAGES, int MIN_CTAS>
+template <int NT>
 omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
-  using S = Smem<NT, STAGES>;
-  auto kern = kv_attention_kernel<NT, STAGES, MIN_CTAS>;
+  using S = Smem<NT>;
+  auto kern = kv_attention_kernel<NT>;
   static bool set = false;
   if (!set) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes(MAX_CHUNK, 16)) != cudaSuccess)
@@ -499,9 +516,9 @@ omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
   }
   CUtensorMap tk, tv;
   const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
-  if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, a.c.page, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, a.c.page, HD))
+  if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, TILE, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, TILE, HD))
     return OMQ_ERR_UNSUPPORTED;
-  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), 288, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
+  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), W * 32, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -538,7 +555,7 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
     a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
   }
   cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY(p.nt == 1 ? (attn_launch<1, 3, 2>(st, a)) : (attn_launch<2, 6, 1>(st, a)));
+  OMQ_TRY(p.nt == 1 ? attn_launch<1>(st, a) : attn_launch<2>(st, a));
   if (p.n_split > 1) {
     const int64_t pairs = (int64_t)max_q * n_heads;
     kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
