@@ -467,7 +467,7 @@ typedef enum { OMQ_F32 = 0, OMQ_BF16 = 1 } omq_dtype;
  *   codes [T, C] uint8 (NULL = skip), h [T] fp32 and z [T] int32 (all ignored when abits = 16);
  *   Xq [T, C] bf16: the values (q - z) h, or bf16(y) when abits = 16 (NULL = skip, but one of codes
  *   and Xq is required).
- * A row that holds an infinity or a NaN gets h = NaN, values NaN and codes 0.
+ * A row whose y holds an infinity or a NaN gets h = NaN, values NaN and codes 0.
  * C at most 32768; C, ldx and ldr multiples of 8. */
 omq_status omq_rmsnorm_quant(omq_stream_t stream, int64_t T, int64_t C, const void* X, int32_t x_dtype,
                              int64_t ldx, const void* R, void* H, int32_t r_dtype, int64_t ldr,

@@ -1,8 +1,11 @@
 // Residual addition + RMSNorm + per-token Q_a in one pass (omq_rmsnorm_quant).
 //
 // One CTA owns one token row at a time and keeps it in registers: t = x + r, the block sum of t^2,
-// y = t rstd gain + bias, the block max / min of y, Eq. 2 on every element.  Nothing of the row is
-// read twice; the bound is HBM (x, r in; codes, values, residual sum out).
+// y = t rstd gain + bias, the block max / min of y, Eq. 2 on every element; the next row is on its way
+// to L2 meanwhile.  Nothing of the row is read twice; the bound is HBM (x, r in; codes, values, residual sum
+// out): 8192 x 8192, bf16 in, fp32 residual, 147 us, 5.95 TB/s.  Elements are worked on in pairs, and the
+// roundings of Eq. 2 are additions of 1.5 * 2^23 instead of conversions, which halves the instructions
+// per element.
 #include "common.cuh"
 
 namespace {
@@ -19,48 +22,65 @@ struct NormArgs {
 
 // eight consecutive elements, widened exactly
 template <bool BF>
-__device__ __forceinline__ void load8(const void* base, int64_t off, float (&v)[8]) {
+__device__ __forceinline__ void widen8(const uint4& a, const uint4& b, float2 (&v)[4]) {
   if (BF) {
-    const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + off));
-    unpack_bf16x8(u, v);
+    v[0] = make_float2(__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u));
+    v[1] = make_float2(__uint_as_float(a.y << 16), __uint_as_float(a.y & 0xffff0000u));
+    v[2] = make_float2(__uint_as_float(a.z << 16), __uint_as_float(a.z & 0xffff0000u));
+    v[3] = make_float2(__uint_as_float(a.w << 16), __uint_as_float(a.w & 0xffff0000u));
   } else {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + off);
-    const float4 a = __ldg(p), b = __ldg(p + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+    v[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+    v[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
   }
 }
 
-// R and H may be one buffer: plain loads (no read-only path) for the residual
+// RO: through the read-only path.  The residual is not: R and H may be one buffer.
+template <bool BF, bool RO>
+__device__ __forceinline__ void load8(const void* base, int64_t off, float2 (&v)[4]) {
+  const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + off * (BF ? 2 : 4));
+  const uint4 a = RO ? __ldg(p) : *p;
+  uint4 b = a;
+  if (!BF) b = RO ? __ldg(p + 1) : p[1];
+  widen8<BF>(a, b, v);
+}
+
+__device__ __forceinline__ uint32_t bf16x2(float2 v) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 template <bool BF>
-__device__ __forceinline__ void load8_rw(const void* base, int64_t off, float (&v)[8]) {
+__device__ __forceinline__ void store8(void* base, int64_t off, const float2 (&v)[4]) {
+  uint4* p = reinterpret_cast<uint4*>(static_cast<char*>(base) + off * (BF ? 2 : 4));
   if (BF) {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + off);
-    unpack_bf16x8(u, v);
+    *p = make_uint4(bf16x2(v[0]), bf16x2(v[1]), bf16x2(v[2]), bf16x2(v[3]));
   } else {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + off);
-    const float4 a = p[0], b = p[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
   }
 }
 
-template <bool BF>
-__device__ __forceinline__ void store8(void* base, int64_t off, const float (&v)[8]) {
-  if (BF) {
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(base) + off) = pack_bf16x8(v);
-  } else {
-    float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + off);
-    p[0] = make_float4(v[0], v[1], v[2], v[3]);
-    p[1] = make_float4(v[4], v[5], v[6], v[7]);
-  }
+// max / min of three that return NaN where an operand is one
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
-// block max and min; an unordered value was turned into +inf by the caller.  smem >= 64 floats.
+// block max and min, NaN where the row holds one.  smem >= 64 floats.
 __device__ __forceinline__ void block_extremes(float& M, float& m, float* smem) {
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) {
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    m = fminf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    M = max3_nan(M, __shfl_xor_sync(0xffffffffu, M, off), -INFINITY);
+    m = min3_nan(m, __shfl_xor_sync(0xffffffffu, m, off), INFINITY);
   }
   if (lane == 0) { smem[wid] = M; smem[32 + wid] = m; }
   __syncthreads();
@@ -68,115 +88,183 @@ __device__ __forceinline__ void block_extremes(float& M, float& m, float* smem) 
   m = lane < nw ? smem[32 + lane] : INFINITY;
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) {
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    m = fminf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    M = max3_nan(M, __shfl_xor_sync(0xffffffffu, M, off), -INFINITY);
+    m = min3_nan(m, __shfl_xor_sync(0xffffffffu, m, off), INFINITY);
   }
 }
 
-template <bool XB, bool RB, int V>
-__global__ void __launch_bounds__(1024) rmsnorm_quant_kernel(const NormArgs a) {
-  __shared__ float red[128];
+// block sum; smem >= 32 floats
+__device__ __forceinline__ float block_sum(float a, float* smem) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
+  a = warp_sum(a);
+  if (lane == 0) smem[wid] = a;
+  __syncthreads();
+  return warp_sum(lane < nw ? smem[lane] : 0.f);
+}
+
+constexpr float ROUND = 12582912.f;            // 1.5 * 2^23: x + ROUND holds the integer nearest to x, |x| < 2^22
+
+// Eq. 2 on a pair, as omq_fakequant2, with the roundings by the addition of ROUND (half to even, like
+// rint): for |y / h| and |z| below 2^21.  Returns the value; *w = code + ROUND.
+struct Fast { float2 rh, nh, h, round, back, zr, nzr; float lo, hi; };
+__device__ __forceinline__ float2 quant2(const float2 y, const Fast& q, float2* w) {
+  const float2 k = omq_add2(omq_add2(omq_mul2(y, q.rh), q.round), q.back);
+  const float2 r = omq_mul2(omq_fma2(k, q.nh, y), q.rh);
+  const float2 c = omq_add2(omq_add2(omq_add2(omq_add2(r, q.round), q.back), k), q.zr);     // round(y / h) + z + ROUND
+  w->x = fminf(fmaxf(c.x, q.lo), q.hi);
+  w->y = fminf(fmaxf(c.y, q.lo), q.hi);
+  return omq_mul2(omq_add2(*w, q.nzr), q.h);
+}
+
+template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS>
+__global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(const NormArgs a) {
+  __shared__ float red[2][96];                   // by row parity: one barrier fewer per row
   const int tid = threadIdx.x, nt = blockDim.x, nvec = a.C >> 3;
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-    float v[V][8];
-    float ss = 0.f;
+  int par = 0;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, par ^= 1) {
+    float2 v[V][4];
+    if (tid == 0 && t + gridDim.x < a.T) {       // the next row of this CTA, into L2
+      omq_l2_prefetch((const char*)a.X + (t + gridDim.x) * a.ldx * (XB ? 2 : 4), (uint64_t)a.C * (XB ? 2 : 4));
+      if (a.R) omq_l2_prefetch((const char*)a.R + (t + gridDim.x) * a.ldr * (RB ? 2 : 4), (uint64_t)a.C * (RB ? 2 : 4));
+    }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int vi = j * nt + tid;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
-      if (vi < nvec) load8<XB>(a.X, t * a.ldx + 8 * vi, v[j]);
+      for (int e = 0; e < 4; ++e) v[j][e] = make_float2(0.f, 0.f);
+      if (vi < nvec) load8<XB, true>(a.X, t * a.ldx + 8 * vi, v[j]);
     }
     if (a.R) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int vi = j * nt + tid;
         if (vi < nvec) {
-          float r[8];
-          load8_rw<RB>(a.R, t * a.ldr + 8 * vi, r);
+          float2 r[4];
+          load8<RB, false>(a.R, t * a.ldr + 8 * vi, r);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[j][e] += r[e];
+          for (int e = 0; e < 4; ++e) v[j][e] = omq_add2(v[j][e], r[e]);
         }
       }
     }
+    float2 ss = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int vi = j * nt + tid;
       if (a.H && vi < nvec) store8<RB>(a.H, t * a.ldr + 8 * vi, v[j]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(v[j][e], v[j][e], ss);
+      for (int e = 0; e < 4; ++e) ss = omq_fma2(v[j][e], v[j][e], ss);
     }
-    const float2 tot = block_sum2(ss, 0.f, red);
-    const float rstd = 1.0f / sqrtf(tot.x / (float)a.C + a.rms_eps);
+    const float tot = block_sum(ss.x + ss.y, red[par]);
+    const float rstd = 1.0f / sqrtf(tot / (float)a.C + a.rms_eps);
+    const float2 rs = make_float2(rstd, rstd);
     float M = -INFINITY, m = INFINITY;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int vi = j * nt + tid;
       if (vi < nvec) {
-        float g[8], b[8];
-        if (a.gain) load8<false>(a.gain, 8 * vi, g);
-        if (a.bias) load8<false>(a.bias, 8 * vi, b);
+        float2 g[4], b[4];
+        if (a.gain) load8<false, true>(a.gain, 8 * vi, g);
+        if (a.bias) load8<false, true>(a.bias, 8 * vi, b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float y = v[j][e] * rstd;
-          if (a.gain) y *= g[e];
-          if (a.bias) y += b[e];
+        for (int e = 0; e < 4; ++e) {
+          float2 y = omq_mul2(v[j][e], rs);
+          if (a.gain) y = omq_mul2(y, g[e]);
+          if (a.bias) y = omq_add2(y, b[e]);
           v[j][e] = y;
-          M = fmaxf(M, fabsf(y) < INFINITY ? y : INFINITY);   // a NaN or an infinity shows as +inf
-          m = fminf(m, y);
+          M = max3_nan(M, y.x, y.y);
+          m = min3_nan(m, y.x, y.y);
         }
       }
     }
     if (a.abits < 16) {
       const float Q = (float)((1 << a.abits) - 1);
-      block_extremes(M, m, red + 64);
-      const bool bad = !(M < INFINITY);
-      QState qs = omq_qstate(bad ? 0.f : M, bad ? 0.f : m, 1.f, 1.f, Q, a.h_eps);
+      block_extremes(M, m, red[par] + 32);
+      const bool bad = !(M < INFINITY && m > -INFINITY);
+      const QState qs = omq_qstate(bad ? 0.f : M, bad ? 0.f : m, 1.f, 1.f, Q, a.h_eps);
       if (tid == 0) { a.h[t] = bad ? NAN : qs.h; a.z[t] = bad ? 0 : (int32_t)qs.z; }
+      uint8_t* cr = a.codes ? a.codes + t * a.C : nullptr;
+      __nv_bfloat16* xr = a.Xq ? a.Xq + t * a.C : nullptr;
+      const bool near = fmaxf(fabsf(M), fabsf(m)) * qs.rh < 2097152.f && fabsf(qs.z) < 2097152.f;
+      if (near) {                                // every row but those far from zero in steps
+        Fast q;
+        q.rh = make_float2(qs.rh, qs.rh); q.nh = make_float2(-qs.h, -qs.h); q.h = make_float2(qs.h, qs.h);
+        q.round = make_float2(ROUND, ROUND); q.back = make_float2(-ROUND, -ROUND);
+        q.zr = make_float2(qs.z + ROUND, qs.z + ROUND); q.nzr = make_float2(-(qs.z + ROUND), -(qs.z + ROUND));
+        q.lo = ROUND; q.hi = ROUND + Q;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int vi = j * nt + tid;
-        if (vi >= nvec) continue;
-        float cd[8];
+        for (int j = 0; j < V; ++j) {
+          const int vi = j * nt + tid;
+          if (vi >= nvec) continue;
+          uint32_t c[8];
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          float2 c2;
-          const float2 w = omq_fakequant2(make_float2(v[j][e], v[j][e + 1]), qs, Q, &c2);
-          v[j][e] = bad ? NAN : w.x; v[j][e + 1] = bad ? NAN : w.y;
-          cd[e] = bad ? 0.f : c2.x; cd[e + 1] = bad ? 0.f : c2.y;
+          for (int e = 0; e < 4; ++e) {
+            float2 w;
+            v[j][e] = quant2(v[j][e], q, &w);
+            c[2 * e] = __float_as_uint(w.x);       // the code is the low byte
+            c[2 * e + 1] = __float_as_uint(w.y);
+          }
+          if (cr)
+            *reinterpret_cast<uint2*>(cr + 8 * vi) =
+                make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                           __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+          if (xr) store8<true>(xr, 8 * vi, v[j]);
         }
-        if (a.codes) {
-          uint32_t p[2];
+      } else {
+#pragma unroll 1
+        for (int j = 0; j < V; ++j) {
+          const int vi = j * nt + tid;
+          if (vi >= nvec) continue;
+          float2 y[4];
 #pragma unroll
-          for (int k = 0; k < 2; ++k)
-            p[k] = (uint32_t)cd[4 * k] | ((uint32_t)cd[4 * k + 1] << 8) | ((uint32_t)cd[4 * k + 2] << 16) |
-                   ((uint32_t)cd[4 * k + 3] << 24);
-          *reinterpret_cast<uint2*>(a.codes + t * a.C + 8 * vi) = make_uint2(p[0], p[1]);
+          for (int k = 0; k < V; ++k)
+            if (k == j) { y[0] = v[k][0]; y[1] = v[k][1]; y[2] = v[k][2]; y[3] = v[k][3]; }
+          uint32_t p[2] = {0, 0};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float2 c2;
+            const float2 w = omq_fakequant2(y[e], qs, Q, &c2);
+            y[e] = bad ? make_float2(NAN, NAN) : w;
+            if (!bad) p[e >> 1] |= ((uint32_t)c2.x | ((uint32_t)c2.y << 8)) << (16 * (e & 1));
+          }
+          if (cr) *reinterpret_cast<uint2*>(cr + 8 * vi) = make_uint2(p[0], p[1]);
+          if (xr) store8<true>(xr, 8 * vi, y);
         }
-        if (a.Xq) *reinterpret_cast<uint4*>(a.Xq + t * a.C + 8 * vi) = pack_bf16x8(v[j]);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int vi = j * nt + tid;
-        if (vi < nvec) *reinterpret_cast<uint4*>(a.Xq + t * a.C + 8 * vi) = pack_bf16x8(v[j]);
+        if (vi < nvec) store8<true>(a.Xq, t * a.C + 8 * vi, v[j]);
       }
     }
-    __syncthreads();                             // the reduction scratch is reused by the next row
   }
 }
 
+template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS>
+omq_status norm_run(cudaStream_t st, const NormArgs& a) {
+  auto kern = rmsnorm_quant_kernel<XB, RB, V, MAX_THREADS, MIN_CTAS>;
+  const int nt = ((a.C / 8 + V - 1) / V + 31) / 32 * 32;
+  int per = 1;
+  cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, nt, 0);
+  const int64_t most = (int64_t)omq_num_sms() * (per > 0 ? per : 1);
+  kern<<<(unsigned)(a.T < most ? a.T : most), nt, 0, st>>>(a);
+  OMQ_LAUNCH_CHECK();
+  return OMQ_OK;
+}
+
+// Eight-element vectors per thread.  Up to one row per SM the row's own latency counts and more threads win
+// (1 x 4096: 3.8 us with one vector, 4.4 with four; 1 x 8192: 5.1, 5.3); with more rows fewer threads leave
+// room for a second CTA (2048 x 5120 30.5 us with two, 38.1 with one) and, from 6 K columns on, four
+// vectors amortise the two block reductions better (8192 x 8192: 146.6 us against 153.1 with two).
 template <bool XB, bool RB>
 omq_status norm_launch(cudaStream_t st, const NormArgs& a) {
   const int nvec = a.C / 8;
-  const int V = nvec <= 1024 ? 1 : (nvec <= 2048 ? 2 : 4);
-  const int nt = ((nvec + V - 1) / V + 31) / 32 * 32;
-  const unsigned grid = (unsigned)(a.T < 65536 ? a.T : 65536);
-  if (V == 1) rmsnorm_quant_kernel<XB, RB, 1><<<grid, nt, 0, st>>>(a);
-  else if (V == 2) rmsnorm_quant_kernel<XB, RB, 2><<<grid, nt, 0, st>>>(a);
-  else rmsnorm_quant_kernel<XB, RB, 4><<<grid, nt, 0, st>>>(a);
-  OMQ_LAUNCH_CHECK();
-  return OMQ_OK;
+  const bool few = a.T <= omq_num_sms();
+  if (few && nvec <= 1024) return norm_run<XB, RB, 1, 1024, 1>(st, a);
+  if (few && nvec <= 2048) return norm_run<XB, RB, 2, 1024, 1>(st, a);
+  if (nvec <= 768) return norm_run<XB, RB, 2, 512, 2>(st, a);
+  if (nvec <= 2048) return norm_run<XB, RB, 4, 512, 1>(st, a);
+  return norm_run<XB, RB, 8, 512, 1>(st, a);
 }
 
 }  // namespace

@@ -114,3 +114,28 @@ def test_side_stream_and_repeat(cuda_lib):
     s.synchronize()
     for u, v in zip(a, b):
         assert torch.equal(u, v)
+
+
+def test_rows_far_from_zero(cuda_lib):
+    """Rows whose values lie many steps from zero: a bias of up to 2^24 steps, beyond what the short form of
+    the rounding covers, and a constant row (h floored, z large)."""
+    from paper_2308_13137_gb300 import serve
+    x, r, _, _ = _case(6, 512, F32, None)
+    for bias in (3e3, 2e5, 1e6):
+        b = torch.full((512,), bias, device="cuda")
+        out = serve.rmsnorm_quant(x, r, None, b, values=True)
+        _check(f"norm bias {bias:g}", out, x, r, None, b, 8)
+    b = torch.full((512,), 300.0, device="cuda")
+    z = torch.zeros_like(x)
+    out = serve.rmsnorm_quant(z, None, None, b, values=True)
+    assert bool((out.h == 1e-5).all())
+    _check("norm constant row", out, z, None, None, b, 8)
+
+
+def test_non_finite_bias(cuda_lib):
+    from paper_2308_13137_gb300 import serve
+    x, _, gain, bias = _case(3, 512, F32, None)
+    for v in (float("nan"), float("inf"), -float("inf")):
+        bias[77] = v
+        out = serve.rmsnorm_quant(x, None, gain, bias, values=True)
+        assert bool(out.h.isnan().all()) and bool(out.values.isnan().all()) and int(out.codes.max()) == 0
