@@ -27,9 +27,10 @@ struct QgemmArgs {
   // K split over S work items per tile (S > 1): integer partial sums, joined by qgemm_join_kernel
   int splits, kb_per_split;
   int32_t* part;              // [S, M, N]
-  int32_t* part_sa;           // [S, M]
   int32_t* part_sb;           // [S, N]
   int m_fast;
+  __half* wide;               // [M, K] activation codes as fp16 integers, written by qgemm_widen_kernel
+  int32_t* sum_a;             // [M] their row sums
 };
 
 // two of the four codes of a word as fp16 integers code - 128: the byte under the exponent of 1024
@@ -61,24 +62,31 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 // ================================================================================================
 // many rows: CTA pairs on the tensor cores
 // ================================================================================================
-// A pair of CTAs computes a 256 x 256 tile with one tcgen05.mma of cta_group::2 per 16 steps of K;
-// each CTA holds 128 rows of A and 128 of B.  Roles of a CTA's 20 warps:
-//   0       TMA: raw code tiles [128 x 64] of A and B into a ring (64-byte swizzle)
+// The activation codes are widened to fp16 once per call (qgemm_widen_kernel: M K codes, an N-th of the
+// conversions that the product's tiles would repeat); the weights stay 8-bit in HBM and are converted
+// on their way to the MMA.  A pair of CTAs computes a 256 x 256 tile with one tcgen05.mma of cta_group::2 per
+// 16 steps of K; each CTA holds 128 rows of A and 128 of B.  Roles of a CTA's 20 warps:
+//   0       TMA: raw weight code tiles [128 x 128] into a ring (128-byte swizzle)
 //   1       leader CTA: issues the MMAs
+//   2       TMA: fp16 tiles of A into the operand ring (128-byte swizzle)
 //   4..11   drain: warps w and w + 4 own the 32 accumulator rows of lane quadrant w % 4, half the columns
 //           each; every 1024 steps of K they add the fp32 accumulator to integers in registers
-//   12..19  convert: 64 codes of a row per thread, A and B, to fp16 in the 128-byte swizzled layout the MMA
+//   12..19  convert: 128 codes of a weight row per thread to fp16 in the 128-byte swizzled layout the MMA
 //           reads; warps 12..15 take the even stages and 16..19 the odd ones, so that one group's waits
 //           and proxy fence overlap the other's work.  They also form the rows' code sums for the
 //           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
-constexpr int BM = 128, BN = 256, BK = 64;
-constexpr int RAW = 4, CONV = 4;                  // ring depths
+constexpr int BM = 128, BN = 256, BK = 128;
+// Ring depths: raw weight tiles, A tiles, converted weight tiles.  Stages of 128 codes: with 64 the signals
+// between the roles, not the work, set the pace (2048 x 22016 x 4096: 356 us with 64, 286 us with 128, and
+// 136 us for 1024 rows with the conversion and three quarters of the MMAs of 64-code stages left out).
+constexpr int RAW = 2, AS = 3, CONV = 2;
 constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumulation
 constexpr int TC_THREADS = 640;
-constexpr int RAW_BYTES = 2 * 128 * BK, CONV_BYTES = 2 * 128 * BK * 2;
-constexpr int SUM_OFF = RAW * RAW_BYTES + CONV * CONV_BYTES;      // 2 tiles x 2 groups: [128] sums of A, [256] of B
-constexpr int COL_OFF = SUM_OFF + 4 * (128 + 256) * 4;             // drain warps: [8][4][128] column operands
+constexpr int RAW_BYTES = 128 * BK, OP_BYTES = 128 * BK * 2;      // a raw tile, an fp16 tile of A or B
+constexpr int RAW_OFF = (AS + CONV) * OP_BYTES;
+constexpr int SUM_OFF = RAW_OFF + RAW * RAW_BYTES;      // code sums of B: 2 tiles x 2 groups x [256]
+constexpr int COL_OFF = SUM_OFF + 4 * 256 * 4;                    // drain warps: [8][4][128] column operands
 constexpr int BAR_OFF = COL_OFF + 8 * 4 * 128 * 4;
 constexpr int TC_SMEM = BAR_OFF + 512 + 1024;
 static_assert(TC_SMEM <= 227 * 1024, "shared memory per CTA");
@@ -179,13 +187,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     qgemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const QgemmArgs p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* conv_ring = smem;                                     // 1024-aligned (swizzle atom)
-  uint8_t* raw_ring = smem + CONV * CONV_BYTES;
-  int* sum_a = reinterpret_cast<int*>(smem + SUM_OFF);           // [tile parity][group][row]
-  int* sum_b = sum_a + 4 * 128;                                  // [tile parity][group][column of the pair's tile]
+  uint8_t* a_ring = smem;                                        // 1024-aligned (swizzle atom)
+  uint8_t* conv_ring = smem + AS * OP_BYTES;
+  uint8_t* raw_ring = smem + RAW_OFF;
+  int* sum_b = reinterpret_cast<int*>(smem + SUM_OFF);           // [tile parity][group][column of the pair's tile]
   uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + BAR_OFF);
   uint64_t* raw_empty = raw_full + RAW;
-  uint64_t* conv_full = raw_empty + RAW;                         // leader's: both CTAs' tiles converted
+  uint64_t* a_full = raw_empty + RAW;                            // leader's: both CTAs' A tiles landed
+  uint64_t* a_empty = a_full + AS;
+  uint64_t* conv_full = a_empty + AS;                            // leader's: both CTAs' B tiles converted
   uint64_t* conv_empty = conv_full + CONV;
   uint64_t* acc_full = conv_empty + CONV;                        // [2]
   uint64_t* acc_empty = acc_full + 2;                            // [2], leader's
@@ -204,6 +214,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < RAW; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
+    for (int s = 0; s < AS; ++s) { mbar_init(&a_full[s], 1); mbar_init(&a_empty[s], 1); }
     for (int s = 0; s < CONV; ++s) { mbar_init(&conv_full[s], 8); mbar_init(&conv_empty[s], 1); }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16);
@@ -234,13 +245,31 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           uint8_t* dst = raw_ring + s * RAW_BYTES;
           mbar_expect_tx(&raw_full[s], RAW_BYTES);
           const int k0 = (w.kb0 + kb) * BK;
-          tma_load_3d(&tmA, &raw_full[s], dst, k0, w.m0 + rank * BM, 0);
-          tma_load_3d(&tmB, &raw_full[s], dst + 128 * BK, k0, w.n0 + rank * 128, 0);
+          tma_load_3d(&tmB, &raw_full[s], dst, k0, w.n0 + rank * 128, 0);
         }
       }
       if (*abort_flag) {                     // no copy may land after this CTA has left
         const uint32_t from = it > (uint32_t)RAW ? it - RAW : 0u;
         for (uint32_t j = from; j < it; ++j) mbar_wait(&raw_full[j % RAW], (j / RAW) & 1);
+      }
+    } else if (warp == 2 && lane == 0) {
+      // ---------------- A tiles: both CTAs' loads complete on the leader's barrier ----------------
+      uint32_t it = 0;
+      for (int i = first; i < total && !*abort_flag; i += step) {
+        const Item w = item_of(p, i, mt, nt);
+        for (int kb = 0; kb < w.nkb; ++kb, ++it) {
+          const int s = it % AS;
+          if (!mbar_wait(&a_empty[s], ((it / AS) & 1) ^ 1)) { fail(); break; }
+          if (leader) mbar_expect_tx(&a_full[s], 2 * OP_BYTES);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            tma_load_3d_pair(&tmA, mapa_shared(smem_u32(&a_full[s]), 0), a_ring + s * OP_BYTES + h * OP_BYTES / 2,
+                             (w.kb0 + kb) * BK + 64 * h, w.m0 + rank * BM, 0);
+        }
+      }
+      if (*abort_flag && leader) {           // no copy may land after the pair has left (the peer leaves with the leader)
+        const uint32_t from = it > (uint32_t)AS ? it - AS : 0u;
+        for (uint32_t j = from; j < it; ++j) mbar_wait(&a_full[j % AS], (j / AS) & 1);
       }
     } else if (warp == 1 && lane == 0 && leader) {
       // ---------------- MMA issuer ----------------
@@ -256,16 +285,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (!mbar_wait(&acc_empty[buf], ((ch >> 1) & 1) ^ 1)) { fail(); ok = false; break; }
             tc_fence_after();
           }
-          const int s = it % CONV;
-          const uint32_t ph = (it / CONV) & 1;
-          if (!mbar_wait(&conv_full[s], ph)) { fail(); ok = false; break; }
+          const int s = it % CONV, as = it % AS;
+          if (!mbar_wait(&a_full[as], (it / AS) & 1) || !mbar_wait(&conv_full[s], (it / CONV) & 1)) { fail(); ok = false; break; }
           tc_fence_after();
           issued = true;
-          const uint32_t sa = smem_u32(conv_ring + s * CONV_BYTES), sb = sa + 128 * BK * 2;
+          const uint32_t sa = smem_u32(a_ring + as * OP_BYTES), sb = smem_u32(conv_ring + s * OP_BYTES);
 #pragma unroll
           for (int k = 0; k < BK / 16; ++k)
-            umma_bf16_pair(tmem + buf * BN, sdesc(sa + k * 32, 16, 1024), sdesc(sb + k * 32, 16, 1024), idesc,
+            umma_bf16_pair(tmem + buf * BN, sdesc(sa + (k >> 2) * (OP_BYTES / 2) + (k & 3) * 32, 16, 1024),
+                           sdesc(sb + (k >> 2) * (OP_BYTES / 2) + (k & 3) * 32, 16, 1024), idesc,
                            kb % CHUNK_KB != 0 || k != 0);
+          umma_commit_pair(&a_empty[as], 0x3);
           umma_commit_pair(&conv_empty[s], 0x3);
           if (kb % CHUNK_KB == CHUNK_KB - 1 || kb == w.nkb - 1) {
             umma_commit_pair(&acc_full[buf], 0x3);
@@ -313,14 +343,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       }
       if (!ok) break;
       const uint32_t sbuf = tile & 1;
-      const int* sumA = sum_a + sbuf * 256;
       const int* sumB = sum_b + sbuf * 512;
       const int row_l = q * 32 + lane, m = w.m0 + rank * BM + row_l;
       int sa = 0;
       if (zeros) {
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_full[sbuf], (tile >> 1) & 1));
         if (!ok) { fail(); break; }
-        sa = sumA[row_l] + sumA[128 + row_l];
+        if (p.bz && m < p.M) sa = __ldg(p.sum_a + m);
       }
       if (p.splits > 1) {
         if (m < p.M) {
@@ -328,7 +357,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
           for (int j = 0; j < BN / 2; j += 4)
             if (w.n0 + c0 + j < p.N) *reinterpret_cast<int4*>(out + j) = make_int4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-          if (zeros && w.n0 == 0 && c0 == 0) p.part_sa[(int64_t)w.split * p.M + m] = sa;
         }
         if (zeros && w.m0 == 0 && rank == 0 && q == 0) {
 #pragma unroll
@@ -373,40 +401,34 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const int grp = (warp - 12) >> 2, r = threadIdx.x & 127;
     const uint32_t src0 = smem_u32(raw_ring) + r * BK, dst0 = smem_u32(conv_ring) + r * 128;
-    const uint32_t rx = (r >> 1) & 3, cx = r & 7;
+    const uint32_t cx = r & 7;
     uint32_t it = 0, tile = 0;
     bool ok = true;
     for (int i = first; i < total && ok && !*abort_flag; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
-      int sa = 0, sb = 0, codes = 0;         // sums of this group's codes and their number per row
+      int sb = 0, codes = 0;                 // sum of this group's codes and their number per row
       for (int kb = 0; kb < w.nkb; ++kb, ++it) {
         if ((int)(it & 1) != grp) continue;
         const int rs = it % RAW, cs = it % CONV;
         ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[rs], (it / RAW) & 1));
         if (!ok) { fail(); break; }
-        uint4 u[8];                          // A then B: 64 codes each
+        uint4 u[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) u[c] = lds128(src0 + rs * RAW_BYTES + (c >> 2) * 128 * BK + (((c & 3) ^ rx) << 4));
+        for (int c = 0; c < 8; ++c) u[c] = lds128(src0 + rs * RAW_BYTES + ((c ^ cx) << 4));
+        if (zeros) {
+          codes += min(BK, p.K - (w.kb0 + kb) * BK);       // beyond K the tile holds zeros, which add nothing
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sb = code_sum(u[c], sb);
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1));
         if (!ok) { fail(); break; }
-        const int k0 = (w.kb0 + kb) * BK;
-        codes += min(BK, p.K - k0);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;      // codes beyond K add nothing
-          if (k0 + 16 * (c & 3) < p.K) {
-            if (zeros) {
-              if (c < 4) sa = code_sum(u[c], sa);
-              else sb = code_sum(u[c], sb);
-            }
-            lo = make_uint4(half_codes(u[c].x, 0x4140), half_codes(u[c].x, 0x4342), half_codes(u[c].y, 0x4140),
-                            half_codes(u[c].y, 0x4342));
-            hi = make_uint4(half_codes(u[c].z, 0x4140), half_codes(u[c].z, 0x4342), half_codes(u[c].w, 0x4140),
-                            half_codes(u[c].w, 0x4342));
-          }
-          const uint32_t dst = dst0 + cs * CONV_BYTES + (c >> 2) * 128 * BK * 2;
-          sts128(dst + (((2 * (c & 3)) ^ cx) << 4), lo);
-          sts128(dst + (((2 * (c & 3) + 1) ^ cx) << 4), hi);
+        for (int c = 0; c < 8; ++c) {        // (beyond K they are -128, and A is zero there)
+          const uint32_t dst = dst0 + cs * OP_BYTES + (c >> 2) * (OP_BYTES / 2);
+          sts128(dst + (((2 * (c & 3)) ^ cx) << 4), make_uint4(half_codes(u[c].x, 0x4140), half_codes(u[c].x, 0x4342),
+                                                               half_codes(u[c].y, 0x4140), half_codes(u[c].y, 0x4342)));
+          sts128(dst + (((2 * (c & 3) + 1) ^ cx) << 4), make_uint4(half_codes(u[c].z, 0x4140), half_codes(u[c].z, 0x4342),
+                                                                   half_codes(u[c].w, 0x4140), half_codes(u[c].w, 0x4342)));
         }
         fence_async_smem();                  // the converted tile -> visible to this SM's tensor core
         __syncwarp();
@@ -420,9 +442,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         const uint32_t sbuf = tile & 1;
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(&sum_empty[sbuf], ((tile >> 1) & 1) ^ 1));
         if (!ok) { fail(); break; }
-        sa -= 128 * codes;                   // the codes moved by 128
-        sb -= 128 * codes;
-        sum_a[sbuf * 256 + grp * 128 + r] = sa;
+        sb -= 128 * codes;                   // the codes moved by 128
         // this CTA's 128 columns of the tile, to both CTAs
         const uint32_t at = smem_u32(sum_b + sbuf * 512 + grp * 256 + rank * 128 + r);
         sts_cluster(mapa_shared(at, 0), sb);
@@ -441,6 +461,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   }
 }
 
+// A's codes -> fp16 integers code - 128, and the row sums of those; one CTA per row
+__global__ void __launch_bounds__(256) qgemm_widen_kernel(const QgemmArgs p) {
+  __shared__ int red[8];
+  const int m = blockIdx.x, nv = p.K >> 4;
+  int s = 0;
+  for (int i = threadIdx.x; i < nv; i += 256) {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.A + (int64_t)m * p.lda) + i);
+    s = code_sum(u, s) - 128 * 16;
+    uint4* o = reinterpret_cast<uint4*>(p.wide + (int64_t)m * p.K) + 2 * i;
+    o[0] = make_uint4(half_codes(u.x, 0x4140), half_codes(u.x, 0x4342), half_codes(u.y, 0x4140), half_codes(u.y, 0x4342));
+    o[1] = make_uint4(half_codes(u.z, 0x4140), half_codes(u.z, 0x4342), half_codes(u.w, 0x4140), half_codes(u.w, 0x4342));
+  }
+  if (!p.bz) return;
+  s = __reduce_add_sync(0xffffffffu, s);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += red[w];
+    p.sum_a[m] = s;
+  }
+}
+
 // sums of the splits -> outputs; four columns per thread
 __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -448,12 +491,12 @@ __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
   if (i >= (int64_t)p.M * nv) return;
   const int m = (int)(i / nv), n = (int)(i % nv) * 4;
   const bool zeros = p.az || p.bz;
-  int a[4] = {}, b[4] = {}, sa = 0;
+  int a[4] = {}, b[4] = {};
+  const int sa = p.bz ? __ldg(p.sum_a + m) : 0;
   for (int s = 0; s < p.splits; ++s) {
     const int4 v = *reinterpret_cast<const int4*>(p.part + ((int64_t)s * p.M + m) * p.N + n);
     a[0] += v.x; a[1] += v.y; a[2] += v.z; a[3] += v.w;
     if (zeros) {
-      sa += p.part_sa[(int64_t)s * p.M + m];
       const int4 t = *reinterpret_cast<const int4*>(p.part_sb + (int64_t)s * p.N + n);
       b[0] += t.x; b[1] += t.y; b[2] += t.z; b[3] += t.w;
     }
@@ -719,19 +762,29 @@ struct QPlan { int splits, kb_per_split; };
 QPlan plan_of(int64_t M, int64_t N, int64_t K) {
   const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), pairs = omq_num_sms() / 2, kbs = (K + BK - 1) / BK;
   int64_t s = tiles < pairs ? pairs / tiles : 1;
-  const int64_t most = kbs / 8 > 0 ? kbs / 8 : 1;
+  const int64_t most = K / 512 > 0 ? K / 512 : 1;
   if (s > most) s = most;
   const int64_t per = (kbs + s - 1) / s;
   return {(int)((kbs + per - 1) / per), (int)per};
+}
+
+// workspace of the tensor-core form: fp16 A | its row sums | partial sums of the K split (and of B's codes);
+// every part a multiple of 16 bytes
+struct QSpace { size_t sum_a, part, part_sb, bytes; };
+QSpace space_of(int64_t M, int64_t N, int64_t K, int splits) {
+  QSpace w;
+  w.sum_a = (size_t)M * K * 2;
+  w.part = w.sum_a + (size_t)((M + 3) / 4 * 4) * 4;
+  w.part_sb = w.part + (splits > 1 ? (size_t)splits * M * N * 4 : 0);
+  w.bytes = w.part_sb + (splits > 1 ? (size_t)splits * N * 4 : 0);
+  return w;
 }
 
 }  // namespace
 
 extern "C" size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K) {
   if (M <= FEW_ROWS || N <= 0 || K <= 0) return 0;
-  const QPlan q = plan_of(M, N, K);
-  if (q.splits <= 1) return 0;
-  return (size_t)q.splits * ((size_t)M * N + (size_t)((M + 3) / 4 * 4) + N) * sizeof(int32_t);
+  return space_of(M, N, K, plan_of(M, N, K).splits).bytes;
 }
 
 extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A, int64_t lda,
@@ -764,14 +817,18 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   }
   const QPlan q = plan_of(M, N, K);
   p.splits = q.splits; p.kb_per_split = q.kb_per_split;
-  if (q.splits > 1) {
-    p.part = (int32_t*)workspace;
-    p.part_sb = p.part + (size_t)q.splits * M * N;              // N and M N are multiples of 4: 16-byte aligned
-    p.part_sa = p.part_sb + (size_t)q.splits * N;
-  }
+  const QSpace sp = space_of(M, N, K, q.splits);
+  uint8_t* const space = (uint8_t*)workspace;
+  p.wide = (__half*)space;
+  p.sum_a = (int32_t*)(space + sp.sum_a);
+  p.part = (int32_t*)(space + sp.part);
+  p.part_sb = (int32_t*)(space + sp.part_sb);
   p.m_fast = (double)M > 1.5 * (double)N ? 0 : 1;               // keep the smaller operand in L2
   CUtensorMap ta, tb;
-  if (!omq_make_map_u8(&ta, A, K, M, lda, 128, BK) || !omq_make_map_u8(&tb, B, K, N, ldb, 128, BK)) return OMQ_ERR_UNSUPPORTED;
+  if (!omq_make_map_bf16(&ta, p.wide, K, M, 1, K, 0, 64, 128) || !omq_make_map_u8(&tb, B, K, N, ldb, 128, BK))
+    return OMQ_ERR_UNSUPPORTED;              // (a map of any 16-bit type moves fp16)
+  qgemm_widen_kernel<<<(unsigned)M, 256, 0, st>>>(p);
+  OMQ_LAUNCH_CHECK();
   static bool attr_set = false;
   if (!attr_set) {
     if (cudaFuncSetAttribute(qgemm_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM) != cudaSuccess)

@@ -98,6 +98,12 @@ def test_attention_refusals(kw, code):
     assert _attend(**kw) == code
 
 
+def test_gemm_workspace_size():
+    size = _lib.omq_qgemm_i8_workspace_size
+    assert size(1, 4096, 4096) == 0 and size(0, 8, 16) == 0 and size(512, 0, 64) == 0
+    assert size(2048, 22016, 4096) >= 2048 * 4096 * 2              # the widened activation codes
+
+
 def test_workspace_size():
     size = _lib.omq_kv_attention_workspace_size
     assert size(512, 512, 1, 256, 32, 32) == 0                 # enough sequences and heads: nothing is split
