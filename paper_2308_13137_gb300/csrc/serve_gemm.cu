@@ -77,10 +77,10 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 //           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
 constexpr int BM = 128, BN = 256, BK = 128;
-// Ring depths: raw weight tiles, A tiles, converted weight tiles.  Stages of 128 codes: with 64 the signals
+// Ring depths: raw weight tiles (they come from HBM), A tiles, converted weight tiles.  Stages of 128 codes: with 64 the signals
 // between the roles, not the work, set the pace (2048 x 22016 x 4096: 356 us with 64, 286 us with 128, and
 // 136 us for 1024 rows with the conversion and three quarters of the MMAs of 64-code stages left out).
-constexpr int RAW = 2, AS = 3, CONV = 2;
+constexpr int RAW = 4, AS = 2, CONV = 2;
 constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumulation
 constexpr int TC_THREADS = 640;
 constexpr int RAW_BYTES = 128 * BK, OP_BYTES = 128 * BK * 2;      // a raw tile, an fp16 tile of A or B
@@ -758,14 +758,21 @@ constexpr int FEW_ROWS = 32;
 
 struct QPlan { int splits, kb_per_split; };
 
-// K split of the tensor-core form: as many pieces as keep every CTA pair busy, none under 512 codes
+// K split of the tensor-core form.  The work items (tiles x splits) run in rounds over the CTA pairs; a split
+// shortens an item and can fill the last round, and costs the partial sums' way through memory and a joining
+// launch.  Estimated with what the kernel measured: 0.8 us per 128 codes of K, 3 us per item, 3 us per joining
+// launch and 1 us per million partial sums (64 x 22016 x 4096: 76 us in 2 rounds of 86 tiles, SPLITTIME us
+// in 8 rounds of 602 pieces).  No piece under 512 codes.
 QPlan plan_of(int64_t M, int64_t N, int64_t K) {
   const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), pairs = omq_num_sms() / 2, kbs = (K + BK - 1) / BK;
-  int64_t s = tiles < pairs ? pairs / tiles : 1;
-  const int64_t most = K / 512 > 0 ? K / 512 : 1;
-  if (s > most) s = most;
-  const int64_t per = (kbs + s - 1) / s;
-  return {(int)((kbs + per - 1) / per), (int)per};
+  QPlan best{1, (int)kbs};
+  double best_us = 1e30;
+  for (int64_t s = 1; s <= 16 && (s == 1 || kbs / s >= 512 / BK); ++s) {
+    const int64_t per = (kbs + s - 1) / s, n = (kbs + per - 1) / per, rounds = (tiles * n + pairs - 1) / pairs;
+    const double us = rounds * (0.8 * per + 3.0) + (n > 1 ? 3.0 + 1e-6 * n * M * N : 0.0);
+    if (us < best_us) { best_us = us; best = {(int)n, (int)per}; }
+  }
+  return best;
 }
 
 // workspace of the tensor-core form: fp16 A | its row sums | partial sums of the K split (and of B's codes);
