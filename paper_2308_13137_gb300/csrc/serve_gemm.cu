@@ -580,7 +580,7 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + F::STAGES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int rank = ck > 1 ? (int)cluster_ctarank() : 0;
-  const int n0 = (blockIdx.x / ck) * FEW_N;
+  const int n0 = (blockIdx.x / ck) * FEW_N, m0 = blockIdx.y * F::TOK;
   const int k_begin = rank * k_share, k_end = min(p.K, k_begin + k_share);
   const int steps = k_end > k_begin ? (k_end - k_begin + FEW_K - 1) / FEW_K : 0;
   const bool sum_b = p.az != nullptr, sum_a = p.bz != nullptr;
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
 #pragma unroll
         for (int b = 0; b < FEW_K / 128; ++b) {
           tma_load_3d(&tmB, &full[s], dst + b * FEW_N * 128, k_begin + i * FEW_K + 128 * b, n0, 0);
-          tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K + b * F::TOK * 128, k_begin + i * FEW_K + 128 * b, 0, 0);
+          tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K + b * F::TOK * 128, k_begin + i * FEW_K + 128 * b, m0, 0);
         }
       }
       if (*abort_flag)                       // no copy may land after this CTA has left
@@ -693,10 +693,10 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
   __syncthreads();
   if (ck > 1) cluster_sync();                                         // release / acquire over the cluster
   // CTA `rank` finishes its share of the channels over the cluster's sums
-  const int share = FEW_N / ck, rows = min(F::TOK, p.M);
+  const int share = (FEW_N + ck - 1) / ck, rows = min(F::TOK, p.M - m0);
   for (int i = threadIdx.x; i < share * rows; i += (FEW_WARPS + 1) * 32) {
     const int c = rank * share + i % share, m = i / share, n = n0 + c;
-    if (n >= p.N) continue;
+    if (c >= FEW_N || n >= p.N) continue;
     int s = 0, ta = 0, tb = 0;
     if (ck > 1) {
       const uint32_t ar = smem_u32(red + m * FEW_N + c), aa = smem_u32(red_a + m), ab = smem_u32(red_b + c);
@@ -708,11 +708,12 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
     } else {
       s = red[m * FEW_N + c]; ta = red_a[m]; tb = red_b[c];
     }
-    const long long za = p.az ? (long long)__ldg(p.az + m) - 128 : 0, zb = p.bz ? (long long)__ldg(p.bz + n) - 128 : 0;
-    float y = finish(s, za, zb, ta, tb, p.K, __ldg(p.ah + m), __ldg(p.bh + n), sum_a || sum_b);
+    const int mg = m0 + m;
+    const long long za = p.az ? (long long)__ldg(p.az + mg) - 128 : 0, zb = p.bz ? (long long)__ldg(p.bz + n) - 128 : 0;
+    float y = finish(s, za, zb, ta, tb, p.K, __ldg(p.ah + mg), __ldg(p.bh + n), sum_a || sum_b);
     if (p.bias) y = __fadd_rn(y, __ldg(p.bias + n));
-    if (p.Cf) p.Cf[(int64_t)m * p.ldc + n] = y;
-    if (p.Cb) p.Cb[(int64_t)m * p.ldc + n] = f_to_bf16(y);
+    if (p.Cf) p.Cf[(int64_t)mg * p.ldc + n] = y;
+    if (p.Cb) p.Cb[(int64_t)mg * p.ldc + n] = f_to_bf16(y);
   }
   if (ck > 1) cluster_sync();                                         // no CTA leaves while its sums may be read
 }
@@ -733,13 +734,13 @@ omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
   // second wave loses more than an idle SM (4096 x 4096, one row: 6.6 us on 256 CTAs, 10.9 us on 512).
   // Within that K is split as far as it goes, no share under 512 codes; clusters of 5 and 7 fill the SMs
   // badly (5120 x 13824: 16.7 us with 6, 24.5 us with 7).
-  const int blocks = (p.N + FEW_N - 1) / FEW_N, cand[6] = {8, 6, 4, 3, 2, 1};
+  const int gy = (p.M + F::TOK - 1) / F::TOK, blocks = (p.N + FEW_N - 1) / FEW_N, cand[6] = {8, 6, 4, 3, 2, 1};
   int ck = 1;
   for (int c : cand)
-    if (blocks * c <= 2 * omq_num_sms() && p.K >= 512 * c) { ck = c; break; }
+    if (blocks * gy * c <= 2 * omq_num_sms() && p.K >= 512 * c) { ck = c; break; }
   const int k_share = ((p.K + ck - 1) / ck + F::FEW_K - 1) / F::FEW_K * F::FEW_K;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * ck), 1, 1);
+  cfg.gridDim = dim3((unsigned)(blocks * ck), (unsigned)gy, 1);
   cfg.blockDim = dim3((FEW_WARPS + 1) * 32, 1, 1);
   cfg.dynamicSmemBytes = F::BYTES;
   cfg.stream = st;
@@ -754,25 +755,31 @@ omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
 }
 
 // ------------------------------------------------------------------------------------------------
-constexpr int FEW_ROWS = 32;
-
-struct QPlan { int splits, kb_per_split; };
+struct QPlan { int splits, kb_per_split; double us; };
 
 // K split of the tensor-core form.  The work items (tiles x splits) run in rounds over the CTA pairs; a split
 // shortens an item and can fill the last round, and costs the partial sums' way through memory and a joining
 // launch.  Estimated with what the kernel measured: 0.8 us per 128 codes of K, 3 us per item, 3 us per joining
-// launch and 1 us per million partial sums (64 x 22016 x 4096: 76 us in 2 rounds of 86 tiles, SPLITTIME us
-// in 8 rounds of 602 pieces).  No piece under 512 codes.
+// launch and 1 us per million partial sums (64 x 22016 x 4096: 76 us in 2 rounds of 86 tiles, 63 us
+// split).  No piece under 512 codes.
 QPlan plan_of(int64_t M, int64_t N, int64_t K) {
   const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), pairs = omq_num_sms() / 2, kbs = (K + BK - 1) / BK;
-  QPlan best{1, (int)kbs};
-  double best_us = 1e30;
+  QPlan best{1, (int)kbs, 1e30};
   for (int64_t s = 1; s <= 16 && (s == 1 || kbs / s >= 512 / BK); ++s) {
     const int64_t per = (kbs + s - 1) / s, n = (kbs + per - 1) / per, rounds = (tiles * n + pairs - 1) / pairs;
     const double us = rounds * (0.8 * per + 3.0) + (n > 1 ? 3.0 + 1e-6 * n * M * N : 0.0);
-    if (us < best_us) { best_us = us; best = {(int)n, (int)per}; }
+    if (us < best.us) best = {(int)n, (int)per, us};
   }
   return best;
+}
+
+// Which form: up to 32 rows the first; beyond, by estimates that both measured.  The tensor-core form costs its
+// plan and 7.5 us for the widening launch and its own start (64 x 4096 x 4096: 21.8 us, 64 x 12288 x 4096: 35.8);
+// the register form 6 us and, for each 32 rows, the weight codes at 3.4 TB/s (15.4 and 36.7 us; 128 rows 23.6 and
+// 64 us; 128 x 1024 x 4096: 9.8 against 22.5 us).
+bool use_few(int64_t M, int64_t N, int64_t K) {
+  if (M <= 32) return true;
+  return 6.0 + (double)((M + 31) / 32) * N * K / 3.4e6 < plan_of(M, N, K).us + 7.5;
 }
 
 // workspace of the tensor-core form: fp16 A | its row sums | partial sums of the K split (and of B's codes);
@@ -790,7 +797,7 @@ QSpace space_of(int64_t M, int64_t N, int64_t K, int splits) {
 }  // namespace
 
 extern "C" size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K) {
-  if (M <= FEW_ROWS || N <= 0 || K <= 0) return 0;
+  if (M <= 0 || N <= 0 || K <= 0 || use_few(M, N, K)) return 0;
   return space_of(M, N, K, plan_of(M, N, K).splits).bytes;
 }
 
@@ -814,7 +821,7 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   p.A = A; p.lda = lda; p.ah = a_h; p.az = a_z;
   p.B = B; p.ldb = ldb; p.bh = b_h; p.bz = b_z;
   p.bias = bias; p.Cf = Cf; p.Cb = (__nv_bfloat16*)Cb; p.ldc = ldc; p.status = dev_status;
-  if (M <= FEW_ROWS) {
+  if (use_few(M, N, K)) {
     // 64 channels per CTA while that is one wave, else 128 (22016 x 4096, one row: 22.9 against 25.8 us); with
     // 17 rows and more the conversion of the tokens counts and 64 stays the faster (34.4 against 40.5 us)
     const bool wide = (N + 63) / 64 > 2 * omq_num_sms();

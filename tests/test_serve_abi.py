@@ -40,8 +40,8 @@ def _gemm(M=4, N=64, K=128, A=FAKE, lda=128, ah=FAKE, az=None, B=FAKE, ldb=128, 
     (dict(K=120), ALIGN), (dict(lda=136), ALIGN), (dict(ldb=136), ALIGN), (dict(N=60), ALIGN), (dict(ldc=68), ALIGN),
     (dict(A=FAKE + 8), ALIGN), (dict(bias=FAKE + 4), ALIGN), (dict(az=FAKE + 4), ALIGN), (dict(A=None), INVALID),
     (dict(B=None), INVALID), (dict(ah=None), INVALID), (dict(bh=None), INVALID), (dict(Cf=None), INVALID), (dict(ws=FAKE + 8), ALIGN),
-    (dict(M=200, K=8192, lda=8192, ldb=8192), WORKSPACE),
-    (dict(M=200, K=8192, lda=8192, ldb=8192, ws=FAKE, ws_bytes=64), WORKSPACE)])
+    (dict(M=2048, N=4096, K=8192, lda=8192, ldb=8192, ldc=4096), WORKSPACE),
+    (dict(M=2048, N=4096, K=8192, lda=8192, ldb=8192, ldc=4096, ws=FAKE, ws_bytes=64), WORKSPACE)])
 def test_gemm_refusals(kw, code):
     assert _gemm(**kw) == code
 

@@ -26,8 +26,9 @@ def _want(a, ah, az, w, wh, wz, bias):
 
 
 SIZES = [(1, 8, 16), (1, 4096, 4096), (2, 264, 48), (3, 20000, 160), (11, 19472, 528), (5, 136, 1040), (8, 1024, 2048), (16, 520, 4112), (17, 4096, 11008),
-         (33, 1000, 1024), (64, 256, 512), (65, 2056, 1008), (127, 264, 2064), (128, 4096, 1024), (129, 512, 4096),
-         (200, 1288, 208), (256, 256, 64), (300, 4104, 2064), (511, 1032, 1040), (1024, 2048, 512), (700, 6152, 1168)]
+         (33, 1000, 1024), (2, 5120, 1536), (18, 5120, 13824), (5, 2560, 4096), (64, 256, 512), (65, 2056, 1008), (127, 264, 2064), (128, 4096, 1024), (129, 512, 4096),
+         (200, 1288, 208), (256, 256, 64), (300, 4104, 2064), (511, 1032, 1040), (1024, 2048, 512), (700, 6152, 1168),
+         (40, 12296, 4112), (2000, 264, 128), (513, 4104, 4096), (90, 20008, 2064)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
@@ -52,6 +53,22 @@ def test_extreme_codes(cuda_lib, M, K):
     for zs in ((None, None), (torch.full((M,), 255, dtype=torch.int32, device="cuda"), None),
                (torch.full((M,), -70000, dtype=torch.int32, device="cuda"),
                 torch.full((264,), 90001, dtype=torch.int32, device="cuda"))):
+        ops = (a, ah, zs[0], w, wh, zs[1])
+        assert torch.equal(serve.qgemm(*ops, bias=bias), _want(*ops, bias))
+
+
+@pytest.mark.parametrize("M,N,K", [(260, 4104, 1024), (260, 4104, 8192), (300, 2056, 65536), (1100, 4096, 1040)])
+def test_extreme_codes_of_many_rows(cuda_lib, M, N, K):
+    """The same on the tensor-core form, with and without a split of K."""
+    from paper_2308_13137_gb300 import serve
+    a, ah, _, w, wh, _, bias = _case(M, N, K, False, lo=0, hi=1)
+    w[::2] = 255
+    a[1::3] = 255
+    az = torch.full((M,), 255, dtype=torch.int32, device="cuda")
+    az[7::9] = -70000
+    wz = torch.full((N,), 3, dtype=torch.int32, device="cuda")
+    wz[5::300] = 90001
+    for zs in ((None, None), (az, None), (None, wz), (az, wz)):
         ops = (a, ah, zs[0], w, wh, zs[1])
         assert torch.equal(serve.qgemm(*ops, bias=bias), _want(*ops, bias))
 
