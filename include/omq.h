@@ -489,7 +489,8 @@ omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, co
 size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K);
 
 /* Pages of an 8-bit key / value cache.  A page holds `page` consecutive tokens (16, 32, 64 or 128) of
- * one sequence for every KV head, with one scale per (page, head): the value is (code - 128) scale.
+ * one sequence for every KV head, with one scale per (page, head), not negative: the value is
+ * (code - 128) scale.
  * Sequence b holds kv_len[b] tokens (those of the current call included); token j lies in page
  * page_table[b, j / page], slot j % page.  Tokens beyond kv_len and table entries beyond the last page are
  * never read.  All pointers device, owned by the caller; offsets are 64-bit.  Page ids and lengths are

@@ -6,13 +6,13 @@
 // the tokens: a CTA takes (sequence, KV head, a chunk of tokens), its warps take 16-token tiles, and
 // their partial results are joined through shared memory and, between CTAs, by a second small kernel.
 //
-// Every token group of warps keeps its own ring of 16-token tiles in flight (TMA, 2 KB of K and of V each,
-// 128-byte swizzle): a warp that is alone on its tiles refills a slot as soon as it has used it, with no
-// barrier between warps.  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
+// This file holds the form for few query rows per KV head (up to 16: decoding).  Every warp keeps its own
+// ring of 16-token tiles in flight (TMA, 2 KB of K and of V each, 128-byte swizzle) and refills a slot as soon
+// as it has used it: no barrier between warps.  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
 // m16n8k16 with fp16 operands and fp32 sums.  The tokens are the M dimension of the first product and
 // the channels of the second, so a single query row costs an eighth of a tile and not a sixteenth.
 // tcgen05 has nothing to offer here: its smallest tile is 64 or 128 rows, and the products are a tenth
-// of the loop's instructions.  A code becomes an fp16 integer in registers, exactly: the byte under the
+// of the loop's instructions (serve_attn_tc.cu has the form for more rows).  A code becomes an fp16 integer in registers, exactly: the byte under the
 // exponent of 1024 (0x6400 | c = 1024 + c), minus 1152.  Channels are numbered inside the products so
 // that a thread's operand values are 16 consecutive bytes of the page; row g of a product is token
 // g ^ ((g & 1) << 2) of its eight, which puts the eight lanes of every load phase, of K and of V, on
@@ -25,43 +25,17 @@
 // differ by page, so the two references differ).  A reference moves, and the accumulator with it,
 // only when a score passes it by more than 2^7: few tiles do, and the others need no maximum across
 // lanes at all, only a vote.
-#include "serve_cache.cuh"
-#include "tc.cuh"
-#include <cuda_fp16.h>
+#include "serve_attn.cuh"
 
 namespace {
 
 using namespace tc;
 
-constexpr int HD = 128;
+constexpr int HD = ATTN_HD;
 constexpr int TILE = 16;                    // tokens of a warp's tile
-constexpr int MAX_CHUNK = 16384;
-constexpr int TILE_BYTES = 2 * TILE * HD;    // K and V
-constexpr float SHIFT = 8.f, SLACK = 7.f;   // a weight is 2^SHIFT at the reference and at most 2^(SHIFT + SLACK)
-constexpr float NOTHING = -1e30f;           // a reference before the first visible token
+constexpr int TILE_BYTES = 2 * TILE * HD;   // K and V
+constexpr float SHIFT = ATTN_SHIFT, SLACK = ATTN_SLACK, NOTHING = ATTN_NOTHING;
 constexpr int OPAD = 132;                   // floats per row of the joining buffer
-
-struct AttnArgs {
-  omq_kv_cache c;
-  int total_q, max_q; const int32_t* cu_q; int max_kv, n_heads;
-  const __nv_bfloat16* Q; int64_t ldq;
-  float* Of; __nv_bfloat16* Ob; int64_t ldo; float* lse;
-  float* wo; float* wl;                     // partial results of the splits (n_split > 1)
-  int chunk, n_split, row_tiles, rg;        // rg: row groups of a CTA
-  int32_t* status;
-};
-
-// two codes (bytes 0, 1 or 2, 3 of w) as fp16 integers code - 128
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
-  const uint32_t u = __byte_perm(w, 0x64646464u, 0x4140);
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
-  const uint32_t u = __byte_perm(w, 0x64646464u, 0x4342);
-  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -77,26 +51,21 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   return d;
 }
 
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w)); }
 
-// shared memory of a CTA: ring (the joining buffers after the loop) | query fragments | per row: factor,
+// shared memory of a CTA: rings (the joining buffers after the loop) | query fragments | per row: factor,
 // keys seen | references and sums | barriers | page records
 constexpr int W = 8;                        // warps
 template <int NT>
 struct Smem {
-  static constexpr int SLOTS = NT == 1 ? 24 : 16;                     // ring tiles: SLOTS / W per warp of a token group
+  static constexpr int DEPTH = 3, SLOTS = DEPTH * W;                 // ring tiles, DEPTH per warp
   static constexpr int RING = SLOTS * TILE_BYTES;
-  static constexpr int ROWS = (NT == 1 ? 1 : 4) * NT * 8;             // up to 4 row groups
-  static constexpr int QF = ROWS * HD * 2;                            // [row groups][NT][8][32] uint2
+  static constexpr int ROWS = NT * 8;
+  static constexpr int QF = ROWS * HD * 2;                            // [NT][8][32] uint2
   static constexpr int QS_OFF = RING + QF;
   static constexpr int STAT_OFF = QS_OFF + 2 * ROWS * 4;
   static constexpr int BAR_OFF = STAT_OFF + 3 * W * NT * 8 * 4;
-  static constexpr int PAGES_OFF = BAR_OFF + 2 * SLOTS * 8 + 16;
+  static constexpr int PAGES_OFF = BAR_OFF + SLOTS * 8 + 16;
   static_assert(W * 8 * OPAD * 4 <= RING, "the joining buffer fits the ring");
   static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12 + 1024; }
 };
@@ -115,8 +84,7 @@ __global__ void __launch_bounds__(W * 32, 2)
   float* st_M = st_m + W * NT * 8;
   float* st_l = st_M + W * NT * 8;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
-  uint64_t* empty = full + S::SLOTS;
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(empty + S::SLOTS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(full + S::SLOTS);
   int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF);
   const int P = a.c.page, per_chunk = a.chunk / P, pshift = 31 - __clz(P);
   float* pks = reinterpret_cast<float*>(pid + per_chunk);     // key scale, times log2(e) / sqrt(128)
@@ -132,11 +100,11 @@ __global__ void __launch_bounds__(W * 32, 2)
     s.len = 0;                                                // its rows read as empty
   }
   const int R = s.nq * rep;                                   // query rows of this KV head
-  const int rows_cta = a.rg * NT * 8;
-  const int r0 = rt * rows_cta;
+  constexpr int ROWS = S::ROWS;
+  const int r0 = rt * ROWS;
   if (r0 >= R) return;
   const int start = s.len - s.nq;
-  const int r_last = min(R, r0 + rows_cta) - 1;
+  const int r_last = min(R, r0 + ROWS) - 1;
   const int kv_end = max(0, min(s.len, start + r_last / rep + 1));   // keys that some row of the CTA sees
   const int t_begin = split * a.chunk;
   const int t_end = min(kv_end, t_begin + a.chunk);
@@ -144,49 +112,23 @@ __global__ void __launch_bounds__(W * 32, 2)
   const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
   const int tiles = t_end > t_begin ? (t_end - t_begin + TILE - 1) / TILE : 0;
 
-  // row groups that the CTA's rows need: with fewer than the call's largest, more warps share the tokens
-  int rg = a.rg;
-  while (rg > 1 && R - r0 <= (rg >> 1) * NT * 8) rg >>= 1;
-  const int rows_here = rg * NT * 8;
-
   // ---- page records of the chunk, query fragments and row factors ----
   for (int i = threadIdx.x; i < np; i += W * 32) {
-    const int pg = (t_begin >> pshift) + i;
-    int id = pg < a.c.max_pages ? __ldg(a.c.page_table + (int64_t)b * a.c.max_pages + pg) : -1;
-    if (id < 0 || id >= a.c.n_pages) {
-      omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
-      id = -1;
-    }
-    pid[i] = id;
-    const int64_t at = (int64_t)(id < 0 ? 0 : id) * a.c.n_kv + g;
-    pks[i] = __ldg(a.c.k_scale + at) * 0.12751743074602467f;  // log2(e) / sqrt(128)
-    plv[i] = log2f(__ldg(a.c.v_scale + at));
+    attn_page(a, b, g, (t_begin >> pshift) + i, pid + i, pks + i, plv + i);
   }
   if (threadIdx.x == 0) {
-    const int sharing = min(rg, (R - r0 + NT * 8 - 1) / (NT * 8));            // warps that use each tile
-    for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], sharing); }
+    for (int i = 0; i < S::SLOTS; ++i) mbar_init(&full[i], 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int r = warp; r < rows_here; r += W) {
+  for (int r = warp; r < ROWS; r += W) {
     const int row = r0 + r;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (row < R) {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(
-          a.Q + (int64_t)(s.row0 + row / rep) * a.ldq + (g * rep + row % rep) * HD + 4 * lane));
-      v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-      v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
-    }
-    uint32_t big = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) big = max(big, __float_as_uint(v[e]) & 0x7fffffffu);
-    big = __reduce_max_sync(0xffffffffu, big);
-    // 2^sh puts the largest magnitude in [2^13, 2^14) (sh capped where 2^sh would overflow)
-    const int sh = big == 0 ? 0 : min(13 + 127 - (int)(big >> 23), 126);
-    const float up = __uint_as_float((uint32_t)(127 + sh) << 23);
+    float v[4];
+    int sh;
+    attn_query4(a, s, g, rep, row, R, lane, v, &sh);
     const int nt = r >> 3, q = r & 7;
     const int w = (lane & 3) + (lane < 16 ? 0 : 4), t = (lane >> 2) & 3;
-    qf[(nt * 8 + w) * 32 + q * 4 + t] = make_uint2(pack_half2(v[0] * up, v[1] * up), pack_half2(v[2] * up, v[3] * up));
+    qf[(nt * 8 + w) * 32 + q * 4 + t] = make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
     if (lane == 0) {
       qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
       lims[r] = row < R ? min(s.len, start + row / rep + 1) : 0;
@@ -194,7 +136,6 @@ __global__ void __launch_bounds__(W * 32, 2)
   }
   __syncthreads();
 
-  const int rgi = warp % rg, tw = warp / rg, n_tw = W / rg;         // row group and token group of this warp
   float m[NT][2], M[NT][2], l[NT][2], acc[NT][8][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -206,39 +147,40 @@ __global__ void __launch_bounds__(W * 32, 2)
       for (int e = 0; e < 4; ++e) acc[nt][i][e] = 0.f;
   }
 
-  // this token group's ring: its n-th tile is tile tw + n n_tw of the chunk, in slot n % depth
-  const int depth = S::SLOTS / n_tw, mine = tiles > tw ? (tiles - tw + n_tw - 1) / n_tw : 0;
-  uint64_t* gfull = full + tw * depth;
-  uint64_t* gempty = empty + tw * depth;
-  const uint32_t ring = smem_u32(smem + tw * depth * TILE_BYTES);
-  auto fill = [&](const int n, const int slot) {              // one thread
-    const int t = (tw + n * n_tw) * TILE, id = pid[t >> pshift];
-    if (id < 0) { mbar_arrive(&gfull[slot]); return; }        // its tokens read as unseen
-    uint8_t* dst = smem + (tw * depth + slot) * TILE_BYTES;
+  // this warp's ring: its n-th tile is tile warp + n W of the chunk, in slot n % DEPTH
+  constexpr int DEPTH = S::DEPTH;
+  const int mine = tiles > warp ? (tiles - warp + W - 1) / W : 0;
+  uint64_t* wfull = full + warp * DEPTH;
+  const uint32_t ring = smem_u32(smem + warp * DEPTH * TILE_BYTES);
+  auto fill = [&](const int n, const int slot) {              // the converged warp; one lane issues
+    const int t = (warp + n * W) * TILE, id = pid[t >> pshift];
+    uint8_t* dst = smem + (warp * DEPTH + slot) * TILE_BYTES;
     const int row = (id * a.c.n_kv + g) * P + (t & (P - 1));
-    mbar_expect_tx(&gfull[slot], TILE_BYTES);
-    tma_load_3d(&tmK, &gfull[slot], dst, 0, row, 0);
-    tma_load_3d(&tmV, &gfull[slot], dst + TILE * HD, 0, row, 0);
+    if (elect_one()) {
+      if (id < 0) {
+        mbar_arrive(&wfull[slot]);                            // its tokens read as unseen
+      } else {
+        mbar_expect_tx(&wfull[slot], TILE_BYTES);
+        tma_load_3d(&tmK, &wfull[slot], dst, 0, row, 0);
+        tma_load_3d(&tmV, &wfull[slot], dst + TILE * HD, 0, row, 0);
+      }
+    }
+    __syncwarp();
   };
-  const bool leads = rgi == 0 && lane == 0;
-  int filled = min(depth, mine);
-  if (leads)
-    for (int n = 0; n < filled; ++n) fill(n, n);
+  int filled = min(DEPTH, mine);
+  for (int n = 0; n < filled; ++n) fill(n, n);
 
   {
-    const uint2* qfw = qf + rgi * NT * 8 * 32 + lane;
+    const uint2* qfw = qf + lane;
     uint2 qr[NT == 1 ? 8 : 1];               // one row tile: its fragments stay in registers
     if (NT == 1) {
 #pragma unroll
       for (int w = 0; w < 8; ++w) qr[NT == 1 ? w : 0] = qfw[w * 32];
     }
-    int lim_min = 0x7fffffff;                // keys that every row of the warp sees
-    for (int r = lane; r < NT * 8; r += 32)
-      if (r0 + rgi * NT * 8 + r < R) lim_min = lims[rgi * NT * 8 + r];
-    lim_min = __reduce_min_sync(0xffffffffu, lim_min);
-    const int n_here = min(NT, (R - r0 - rgi * NT * 8 + 7) >> 3);   // row tiles of this warp that hold rows
-    const float2* f2 = reinterpret_cast<const float2*>(qs + rgi * NT * 8) + lt;
-    const int2* lim2 = reinterpret_cast<const int2*>(lims + rgi * NT * 8) + lt;
+    const int lim_min = __reduce_min_sync(0xffffffffu, lane < ROWS && r0 + lane < R ? lims[lane] : 0x7fffffff);
+    const int n_here = (min(ROWS, R - r0) + 7) >> 3;          // row tiles that hold rows
+    const float2* f2 = reinterpret_cast<const float2*>(qs) + lt;
+    const int2* lim2 = reinterpret_cast<const int2*>(lims) + lt;
     const int row_k = lg ^ ((lg & 1) << 2);                   // token of product row lg among its eight
     const int row_v0 = 2 * lt, row_v1 = (2 * lt + 1) ^ 4;     // tokens of the product columns 2 lt, 2 lt + 1
     const uint32_t k_off = row_k * HD, kx0 = (uint32_t)(lt ^ row_k) << 4, kx1 = (uint32_t)((lt + 4) ^ row_k) << 4;
@@ -340,30 +282,20 @@ __global__ void __launch_bounds__(W * 32, 2)
     };
 
     int slot = 0, turn = 0;                  // of tile n
-    for (int n = 0; n < mine && n_here > 0; ++n) {
-      if (rg > 1 && leads && n > 0 && filled < mine) {        // the slot that the group left last
-        const int ls = slot == 0 ? depth - 1 : slot - 1, lt_ = slot == 0 ? turn ^ 1 : turn;
-        if (mbar_wait(&gempty[ls], lt_)) fill(filled++, ls);
-        else *abort_flag = 1;
-      }
-      __syncwarp();
-      if (!__all_sync(0xffffffffu, !*abort_flag && mbar_wait(&gfull[slot], turn))) {
+    for (int n = 0; n < mine; ++n) {
+      if (!warp_wait(&wfull[slot], turn)) {
         omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
       }
-      tile(ring + slot * TILE_BYTES, t_begin + (tw + n * n_tw) * TILE);
+      tile(ring + slot * TILE_BYTES, t_begin + (warp + n * W) * TILE);
       __syncwarp();                          // every lane has read the tile
-      if (rg > 1) {
-        if (lane == 0) mbar_arrive(&gempty[slot]);
-      } else if (leads && filled < mine) {
-        fill(filled++, slot);
-      }
-      if (++slot == depth) { slot = 0; turn ^= 1; }
+      if (filled < mine) fill(filled++, slot);
+      if (++slot == DEPTH) { slot = 0; turn ^= 1; }
     }
-    if (leads && *abort_flag)                // no copy may land after this CTA has left
-      for (int j = max(0, filled - depth); j < filled; ++j) mbar_wait(&gfull[j % depth], (j / depth) & 1);
+    if (lane == 0 && *abort_flag)            // no copy may land after this CTA has left
+      for (int j = max(0, filled - DEPTH); j < filled; ++j) wait_phase(&wfull[j % DEPTH], (j / DEPTH) & 1);
   }
 
-  // ---- join the token groups of each row group ----
+  // ---- join the warps ----
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -388,23 +320,22 @@ __global__ void __launch_bounds__(W * 32, 2)
         o[i] = make_float4(acc[nt][2 * i][e], acc[nt][2 * i][e + 2], acc[nt][2 * i + 1][e], acc[nt][2 * i + 1][e + 2]);
     }
     __syncthreads();
-    for (int rq = warp; rq < rg * 8; rq += W) {             // one query row per warp, 4 channels per lane
-      const int gi = rq >> 3, q = rq & 7;
-      const int row = r0 + gi * NT * 8 + nt * 8 + q;
+    {                                                         // one query row per warp, 4 channels per lane
+      const int q = warp, row = r0 + nt * 8 + q;
       if (row >= R) continue;
       float mm = NOTHING, MM = NOTHING;
-      for (int k = 0; k < n_tw; ++k) {
-        const int at = ((k * rg + gi) * NT + nt) * 8 + q;
+      for (int k = 0; k < W; ++k) {
+        const int at = (k * NT + nt) * 8 + q;
         mm = fmaxf(mm, st_m[at]);
         MM = fmaxf(MM, st_M[at]);
       }
       float L = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < n_tw; ++k) {
-        const int wk = k * rg + gi, at = (wk * NT + nt) * 8 + q;
+      for (int k = 0; k < W; ++k) {
+        const int at = (k * NT + nt) * 8 + q;
         L += st_l[at] * ex2(st_m[at] - mm);
         const float c = ex2(st_M[at] - MM);
-        const float4 x = *reinterpret_cast<const float4*>(join + (wk * 8 + q) * OPAD + 4 * lane);
+        const float4 x = *reinterpret_cast<const float4*>(join + (k * 8 + q) * OPAD + 4 * lane);
         o.x = fmaf(x.x, c, o.x); o.y = fmaf(x.y, c, o.y); o.z = fmaf(x.z, c, o.z); o.w = fmaf(x.w, c, o.w);
       }
       const bool none = L == 0.f;                             // a NaN score is not an empty row
@@ -471,28 +402,25 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = L == 0.f ? -INFINITY : ref + log2f(L);
 }
 
-struct Plan { int nt, rg, row_tiles, chunk, n_split; };
+struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
 
-// How a call is cut.  Rows per CTA: 8 (one new token of up to 8 query heads per KV head), 16, 32 or 64.
-// Tokens per CTA: with 8 rows as many chunks as fill one wave (a second one costs more than it balances:
-// 4 x 131072 tokens 145 us on one wave, 155 us on two); with more rows, where the work of a CTA depends on its
-// sequence's rows and length, six waves (64 ragged sequences: 270 us on one, 204 us on six); none under
-// 256 tokens.
+// How a call is cut.  Up to 16 query rows per KV head take this file's form, more the tcgen05 tiles.  Tokens per
+// CTA: up to 8 rows as many chunks as fill one wave (a second one costs more than it balances: 4 x 131072
+// tokens 145 us on one wave, 155 us on two); with several rows, where the work of a CTA depends on its
+// sequence's rows and length, six waves; none under 256 tokens.
 Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   Plan p;
   const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
-  p.nt = rows <= 8 ? 1 : 2;
-  p.rg = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-  const int64_t per = 8ll * p.nt * p.rg;
-  p.row_tiles = (int)((rows + per - 1) / per);
+  p.form = rows <= 8 ? 8 : (rows <= 16 ? 16 : ATTN_TC_ROWS);
+  p.row_tiles = (int)((rows + p.form - 1) / p.form);
   const int64_t units = B * n_kv * p.row_tiles;
-  const int64_t slots = 2ll * omq_num_sms();
-  int64_t n = p.nt == 1 ? slots / units : 6 * slots / units;
+  const int64_t slots = omq_num_sms() * (p.form == ATTN_TC_ROWS ? 1ll : 2ll);
+  int64_t n = p.form == 8 ? slots / units : 6 * slots / units;
   const int64_t most = (max_kv + 255) / 256;
   if (n > most) n = most;
   if (n < 1) n = 1;
   int64_t chunk = ((max_kv + n - 1) / n + 127) / 128 * 128;
-  if (chunk > MAX_CHUNK) chunk = MAX_CHUNK;
+  if (chunk > ATTN_MAX_CHUNK) chunk = ATTN_MAX_CHUNK;
   p.chunk = (int)chunk;
   p.n_split = (int)((max_kv + chunk - 1) / chunk);
   return p;
@@ -510,7 +438,7 @@ omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
   auto kern = kv_attention_kernel<NT>;
   static bool set = false;
   if (!set) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes(MAX_CHUNK, 16)) != cudaSuccess)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes(ATTN_MAX_CHUNK, 16)) != cudaSuccess)
       return OMQ_ERR_CUDA;
     set = true;
   }
@@ -549,13 +477,13 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
   const size_t need = plan_workspace(p, total_q, n_heads);
   OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
   AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
-             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, p.rg, dev_status};
+             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status};
   if (p.n_split > 1) {
     a.wo = (float*)workspace;
     a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
   }
   cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY(p.nt == 1 ? attn_launch<1>(st, a) : attn_launch<2>(st, a));
+  OMQ_TRY(p.form == 8 ? attn_launch<1>(st, a) : (p.form == 16 ? attn_launch<2>(st, a) : attn_tc_launch(st, a)));
   if (p.n_split > 1) {
     const int64_t pairs = (int64_t)max_q * n_heads;
     kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);

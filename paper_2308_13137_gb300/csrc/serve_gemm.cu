@@ -234,79 +234,84 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-    if (warp == 0 && lane == 0) {
-      // ---------------- raw code tiles ----------------
+    // (each of the three: the whole warp runs the loop, one lane issues)
+    if (warp == 0) {
+      // ---------------- raw weight code tiles ----------------
       uint32_t it = 0;
-      for (int i = first; i < total && !*abort_flag; i += step) {
+      bool ok = true;
+      for (int i = first; i < total && ok; i += step) {
         const Item w = item_of(p, i, mt, nt);
         for (int kb = 0; kb < w.nkb; ++kb, ++it) {
           const int s = it % RAW;
-          if (!mbar_wait(&raw_empty[s], ((it / RAW) & 1) ^ 1)) { fail(); break; }
-          uint8_t* dst = raw_ring + s * RAW_BYTES;
-          mbar_expect_tx(&raw_full[s], RAW_BYTES);
-          const int k0 = (w.kb0 + kb) * BK;
-          tma_load_3d(&tmB, &raw_full[s], dst, k0, w.n0 + rank * 128, 0);
+          ok = warp_wait(&raw_empty[s], ((it / RAW) & 1) ^ 1);
+          if (!ok) { fail(); break; }
+          if (elect_one()) {
+            mbar_expect_tx(&raw_full[s], RAW_BYTES);
+            tma_load_3d(&tmB, &raw_full[s], raw_ring + s * RAW_BYTES, (w.kb0 + kb) * BK, w.n0 + rank * 128, 0);
+          }
+          __syncwarp();
         }
       }
-      if (*abort_flag) {                     // no copy may land after this CTA has left
+      if (__any_sync(0xffffffffu, *abort_flag)) {    // no copy may land after this CTA has left
         const uint32_t from = it > (uint32_t)RAW ? it - RAW : 0u;
-        for (uint32_t j = from; j < it; ++j) mbar_wait(&raw_full[j % RAW], (j / RAW) & 1);
+        for (uint32_t j = from; j < it; ++j) wait_phase(&raw_full[j % RAW], (j / RAW) & 1);
       }
-    } else if (warp == 2 && lane == 0) {
+    } else if (warp == 2) {
       // ---------------- A tiles: both CTAs' loads complete on the leader's barrier ----------------
       uint32_t it = 0;
-      for (int i = first; i < total && !*abort_flag; i += step) {
+      bool ok = true;
+      for (int i = first; i < total && ok; i += step) {
         const Item w = item_of(p, i, mt, nt);
         for (int kb = 0; kb < w.nkb; ++kb, ++it) {
           const int s = it % AS;
-          if (!mbar_wait(&a_empty[s], ((it / AS) & 1) ^ 1)) { fail(); break; }
-          if (leader) mbar_expect_tx(&a_full[s], 2 * OP_BYTES);
+          ok = warp_wait(&a_empty[s], ((it / AS) & 1) ^ 1);
+          if (!ok) { fail(); break; }
+          if (elect_one()) {
+            if (leader) mbar_expect_tx(&a_full[s], 2 * OP_BYTES);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            tma_load_3d_pair(&tmA, mapa_shared(smem_u32(&a_full[s]), 0), a_ring + s * OP_BYTES + h * OP_BYTES / 2,
-                             (w.kb0 + kb) * BK + 64 * h, w.m0 + rank * BM, 0);
+            for (int h = 0; h < 2; ++h)
+              tma_load_3d_pair(&tmA, mapa_shared(smem_u32(&a_full[s]), 0), a_ring + s * OP_BYTES + h * OP_BYTES / 2,
+                               (w.kb0 + kb) * BK + 64 * h, w.m0 + rank * BM, 0);
+          }
+          __syncwarp();
         }
       }
-      if (*abort_flag && leader) {           // no copy may land after the pair has left (the peer leaves with the leader)
+      if (__any_sync(0xffffffffu, *abort_flag) && leader) {   // (the peer leaves with the leader)
         const uint32_t from = it > (uint32_t)AS ? it - AS : 0u;
-        for (uint32_t j = from; j < it; ++j) mbar_wait(&a_full[j % AS], (j / AS) & 1);
+        for (uint32_t j = from; j < it; ++j) wait_phase(&a_full[j % AS], (j / AS) & 1);
       }
-    } else if (warp == 1 && lane == 0 && leader) {
-      // ---------------- MMA issuer ----------------
+    } else if (warp == 1 && leader) {
+      // ---------------- MMA issuer: the whole warp runs the loop, one lane issues ----------------
       constexpr uint32_t idesc = idesc_f16(2 * BM, BN);
+      const uint64_t da = sdesc(smem_u32(a_ring), 16, 1024), db = sdesc(smem_u32(conv_ring), 16, 1024);
       uint32_t it = 0, ch = 0;
-      bool issued = false;
-      for (int i = first; i < total && !*abort_flag; i += step) {
+      bool ok = true;
+      for (int i = first; i < total && ok; i += step) {
         const Item w = item_of(p, i, mt, nt);
-        bool ok = true;
         for (int kb = 0; kb < w.nkb; ++kb, ++it) {
-          const uint32_t buf = ch & 1;
-          if (kb % CHUNK_KB == 0) {
-            if (!mbar_wait(&acc_empty[buf], ((ch >> 1) & 1) ^ 1)) { fail(); ok = false; break; }
-            tc_fence_after();
-          }
-          const int s = it % CONV, as = it % AS;
-          if (!mbar_wait(&a_full[as], (it / AS) & 1) || !mbar_wait(&conv_full[s], (it / CONV) & 1)) { fail(); ok = false; break; }
+          const uint32_t buf = ch & 1, s = it % CONV, as = it % AS;
+          ok = (kb % CHUNK_KB != 0 || warp_wait(&acc_empty[buf], ((ch >> 1) & 1) ^ 1)) &&
+               warp_wait(&a_full[as], (it / AS) & 1) && warp_wait(&conv_full[s], (it / CONV) & 1);
+          if (!ok) { fail(); break; }
           tc_fence_after();
-          issued = true;
-          const uint32_t sa = smem_u32(a_ring + as * OP_BYTES), sb = smem_u32(conv_ring + s * OP_BYTES);
+          const bool last = kb % CHUNK_KB == CHUNK_KB - 1 || kb == w.nkb - 1;
+          if (elect_one()) {
+            const uint64_t a0 = da + (uint64_t)(as * (OP_BYTES >> 4)), b0 = db + (uint64_t)(s * (OP_BYTES >> 4));
 #pragma unroll
-          for (int k = 0; k < BK / 16; ++k)
-            umma_bf16_pair(tmem + buf * BN, sdesc(sa + (k >> 2) * (OP_BYTES / 2) + (k & 3) * 32, 16, 1024),
-                           sdesc(sb + (k >> 2) * (OP_BYTES / 2) + (k & 3) * 32, 16, 1024), idesc,
-                           kb % CHUNK_KB != 0 || k != 0);
-          umma_commit_pair(&a_empty[as], 0x3);
-          umma_commit_pair(&conv_empty[s], 0x3);
-          if (kb % CHUNK_KB == CHUNK_KB - 1 || kb == w.nkb - 1) {
-            umma_commit_pair(&acc_full[buf], 0x3);
-            ++ch;
+            for (int k = 0; k < BK / 16; ++k)
+              umma_bf16_pair(tmem + buf * BN, a0 + (((k >> 2) * (OP_BYTES / 2) + (k & 3) * 32) >> 4),
+                             b0 + (((k >> 2) * (OP_BYTES / 2) + (k & 3) * 32) >> 4), idesc, kb % CHUNK_KB != 0 || k != 0);
+            umma_commit_pair(&a_empty[as], 0x3);
+            umma_commit_pair(&conv_empty[s], 0x3);
+            if (last) umma_commit_pair(&acc_full[buf], 0x3);
           }
+          __syncwarp();
+          if (last) ++ch;
         }
-        if (!ok) break;
       }
-      if (*abort_flag && issued) {           // products in flight end before the tensor memory is released
-        umma_commit_pair(drain, 0x1);
-        mbar_wait(drain, 0);
+      if (__any_sync(0xffffffffu, *abort_flag)) {   // products in flight end before the tensor memory is released
+        if (elect_one()) umma_commit_pair(drain, 0x1);
+        wait_phase(drain, 0);
       }
     }
   } else if (warp < 12) {
@@ -327,7 +332,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       bool ok = true;
       for (int kb = 0; kb < w.nkb; kb += CHUNK_KB, ++ch) {
         const uint32_t buf = ch & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (ch >> 1) & 1));
+        ok = warp_wait(&acc_full[buf], (ch >> 1) & 1);
         if (!ok) { fail(); break; }
         tc_fence_after();
 #pragma unroll
@@ -404,13 +409,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t cx = r & 7;
     uint32_t it = 0, tile = 0;
     bool ok = true;
-    for (int i = first; i < total && ok && !*abort_flag; i += step, ++tile) {
+    for (int i = first; i < total && ok; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
       int sb = 0, codes = 0;                 // sum of this group's codes and their number per row
       for (int kb = 0; kb < w.nkb; ++kb, ++it) {
         if ((int)(it & 1) != grp) continue;
         const int rs = it % RAW, cs = it % CONV;
-        ok = __all_sync(0xffffffffu, mbar_wait(&raw_full[rs], (it / RAW) & 1));
+        ok = warp_wait(&raw_full[rs], (it / RAW) & 1);
         if (!ok) { fail(); break; }
         uint4 u[8];
 #pragma unroll
@@ -420,7 +425,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
           for (int c = 0; c < 8; ++c) sb = code_sum(u[c], sb);
         }
-        ok = __all_sync(0xffffffffu, mbar_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1));
+        ok = warp_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1);
         if (!ok) { fail(); break; }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {        // (beyond K they are -128, and A is zero there)
@@ -592,22 +597,23 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
   }
   __syncthreads();
   if (warp == FEW_WARPS) {
-    if (lane == 0) {
-      int i = 0;
-      for (; i < steps && !*abort_flag; ++i) {
-        const int s = i % F::STAGES;
-        if (!mbar_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1)) { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
+    int i = 0;                               // the whole warp runs the loop, one lane issues
+    for (; i < steps; ++i) {
+      const int s = i % F::STAGES;
+      if (!warp_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1)) { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
+      uint8_t* dst = smem + s * F::STAGE;
+      if (elect_one()) {
         mbar_expect_tx(&full[s], F::STAGE);
-        uint8_t* dst = smem + s * F::STAGE;
 #pragma unroll
         for (int b = 0; b < FEW_K / 128; ++b) {
           tma_load_3d(&tmB, &full[s], dst + b * FEW_N * 128, k_begin + i * FEW_K + 128 * b, n0, 0);
           tma_load_3d(&tmA, &full[s], dst + FEW_N * FEW_K + b * F::TOK * 128, k_begin + i * FEW_K + 128 * b, m0, 0);
         }
       }
-      if (*abort_flag)                       // no copy may land after this CTA has left
-        for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j) mbar_wait(&full[j % F::STAGES], (j / F::STAGES) & 1);
+      __syncwarp();
     }
+    if (__any_sync(0xffffffffu, *abort_flag))        // no copy may land after this CTA has left
+      for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j) wait_phase(&full[j % F::STAGES], (j / F::STAGES) & 1);
   } else {
     // channel group, 64-code slice of the tile, this thread's 16-code chunk of its rows' 128 bytes
     const int cw = warp % FEW_GROUPS, kq = warp / FEW_GROUPS, c = t + 4 * (kq & 1);
@@ -622,7 +628,7 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
     const int row = (g & 1) * 4 + (g >> 1);          // tile row of product row g
     for (int i = 0; i < steps; ++i) {
       const int s = i % F::STAGES;
-      if (!__all_sync(0xffffffffu, mbar_wait(&full[s], (i / F::STAGES) & 1))) {
+      if (!warp_wait(&full[s], (i / F::STAGES) & 1)) {
         omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
       }
       const uint32_t wb = smem_u32(smem + s * F::STAGE) + ((kq >> 1) * FEW_N + 32 * cw + row) * 128 + ((c ^ row) << 4);

@@ -53,6 +53,27 @@ static __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity,
   }
 }
 
+// The same bounded wait counted in tries instead of nanoseconds, for pipelines whose hand-offs set their
+// pace: a read of the global timer delays a waiting warp by more than the phase it waits for.  Each try
+// suspends the thread until the phase completes or the hint (one millisecond) has passed; a try that
+// returns at once still leaves a limit of tens of milliseconds.
+static __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
+  const uint32_t at = smem_u32(bar);
+#pragma unroll 1
+  for (uint32_t i = 0; i < (1u << 20); ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity), "r"(1000000u)
+        : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+
 // 16-byte shared-memory load / store by shared-window address (explicit state space: the access
 // is scoreboarded as a shared-memory one, and loads can be issued ahead of stores to other chunks)
 static __device__ __forceinline__ uint4 lds128(uint32_t addr) {
@@ -177,6 +198,25 @@ static __device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, u
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
   return d;
+}
+
+// one lane of a converged warp, the same one at every call: the loop around it stays warp-uniform, so
+// that descriptors and addresses live in uniform registers and an MMA is issued in a few cycles (in a
+// branch of one lane each operand is moved there for every MMA, about 100 cycles)
+static __device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+
+// A converged warp waits for a phase.  Every lane polls: with one polling lane the vote after it came out
+// slower (integer product of 2048 rows 372 us instead of 267).
+static __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, wait_phase(bar, parity));
 }
 
 // Instruction descriptor of kind::f16: fp32 accumulator, bf16 A and B, major-ness, N, M.
