@@ -404,10 +404,11 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
 
 struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
 
-// How a call is cut.  Up to 16 query rows per KV head take this file's form, more the tcgen05 tiles.  Tokens per
-// CTA: up to 8 rows as many chunks as fill one wave (a second one costs more than it balances: 4 x 131072
-// tokens 145 us on one wave, 155 us on two); with several rows, where the work of a CTA depends on its
-// sequence's rows and length, six waves; none under 256 tokens.
+// How a call is cut.  Up to 16 query rows per KV head take this file's form, more the tcgen05 tiles (16 rows,
+// 16 x 4096 tokens: 36 us here, 52 us there).  Tokens per CTA: as many chunks as fill one wave, none under 256
+// tokens; a second wave costs more than it balances (4 x 131072 tokens of 8 rows 145 us on one wave, 155 us on
+// two; 8 x 8192 tokens of 128 rows 65 and 77 us; 64 ragged sequences of up to 40 rows 144 us on 3.4 rounds of
+// whole sequences, 162 us split in two).
 Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   Plan p;
   const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
@@ -415,7 +416,7 @@ Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   p.row_tiles = (int)((rows + p.form - 1) / p.form);
   const int64_t units = B * n_kv * p.row_tiles;
   const int64_t slots = omq_num_sms() * (p.form == ATTN_TC_ROWS ? 1ll : 2ll);
-  int64_t n = p.form == 8 ? slots / units : 6 * slots / units;
+  int64_t n = slots / units;
   const int64_t most = (max_kv + 255) / 256;
   if (n > most) n = most;
   if (n < 1) n = 1;
