@@ -5,7 +5,10 @@
 // takes their largest magnitude over the block, settles the scale, rounds the older codes of the page
 // again where the scale grew, and writes the new ones; so no value is read twice and no two CTAs
 // touch one scale.  The other CTAs of the launch turn the q rows.  The bound is HBM for prompts
-// (rows in, q / k / v values and codes out) and the launch for single tokens.
+// (rows in, q / k / v values and codes out): 2048 rows of 32 + 2 x 32 bf16 heads 38.5 us, 4.4 TB/s; 64 single
+// tokens of 32 + 2 x 8 heads 7.6 us, of which 4 us are the launch and the chain length -> page -> scale -> rows.
+// Eight threads to a token: with sixteen, of half the channels and 8-byte stores, the rotary loads and the
+// addresses were a larger part of the instructions (44.0 us; fp32 pages of 128 tokens 63.0 against 53.1 us).
 //
 // Every operation is one fp32 rounding (no fused multiply-add), so that the codes and scales are
 // the same as those of any implementation that rounds in the stated order.
@@ -15,8 +18,9 @@
 namespace {
 
 constexpr int HD = 128;
-constexpr int NT = 256;              // 16 threads per token or q head, 4 + 4 channels (j, j + 64) each
-constexpr int QPASS = 4;             // q heads per 16-thread group
+constexpr int NT = 256;              // eight threads per token or q head, 8 + 8 channels (j, j + 64) each
+constexpr int GRP = NT / 8;          // tokens or heads per pass
+constexpr int QPASS = 2;             // q heads per eight threads
 
 struct AppendArgs {
   omq_kv_cache c;
@@ -29,61 +33,55 @@ struct AppendArgs {
 };
 
 template <bool BF>
-__device__ __forceinline__ void load4(const void* base, int64_t off, float (&v)[4]) {
+__device__ __forceinline__ void load8(const void* base, int64_t off, float (&v)[8]) {
   if (BF) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(base) + off));
-    v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-    v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
+    unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) + off)), v);
   } else {
-    const float4 f = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(base) + off));
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + off);
+    const float4 a = __ldg(p), b = __ldg(p + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
 }
 
-__device__ __forceinline__ void store_bf4(__nv_bfloat16* p, const float (&v)[4]) {
-  uint2 u;
-  __nv_bfloat162* q = reinterpret_cast<__nv_bfloat162*>(&u);
-  q[0] = __floats2bfloat162_rn(v[0], v[1]);
-  q[1] = __floats2bfloat162_rn(v[2], v[3]);
-  *reinterpret_cast<uint2*>(p) = u;
-}
-
-// rotate-half pair of channels j .. j+3 and j+64 .. j+67 at position pos
-__device__ __forceinline__ void turn(const float2* rope, int pos, int j, float (&a)[4], float (&b)[4]) {
+// rotate-half pair of channels j .. j+7 and j+64 .. j+71 at position pos
+__device__ __forceinline__ void turn(const float2* rope, int pos, int j, float (&a)[8], float (&b)[8]) {
   const float4* p = reinterpret_cast<const float4*>(rope + (int64_t)pos * 64 + j);
-  const float4 u = __ldg(p), w = __ldg(p + 1);
-  const float cs[4] = {u.x, u.z, w.x, w.z}, sn[4] = {u.y, u.w, w.y, w.w};
+  float4 u[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int i = 0; i < 4; ++i) u[i] = __ldg(p + i);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float c = e & 1 ? u[e >> 1].z : u[e >> 1].x, s = e & 1 ? u[e >> 1].w : u[e >> 1].y;
     const float x = a[e], y = b[e];
-    a[e] = __fsub_rn(__fmul_rn(x, cs[e]), __fmul_rn(y, sn[e]));
-    b[e] = __fadd_rn(__fmul_rn(y, cs[e]), __fmul_rn(x, sn[e]));
+    a[e] = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
+    b[e] = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
   }
 }
 
 template <bool BF>
 __device__ __forceinline__ void q_unit(const AppendArgs& a, const SeqRows& s, int unit) {
-  const int grp = threadIdx.x >> 4, j = 4 * (threadIdx.x & 15);
+  const int grp = threadIdx.x >> 3, j = 8 * (threadIdx.x & 7);
   const int rep = a.n_heads / a.c.n_kv;
 #pragma unroll
   for (int p = 0; p < QPASS; ++p) {
-    const int idx = (unit * QPASS + p) * (NT / 16) + grp;
+    const int idx = (unit * QPASS + p) * GRP + grp;
     const int i = idx / a.n_heads, h = idx - i * a.n_heads;
     if (i >= s.nq) return;
     const int64_t row = s.row0 + i;
-    float x[4], y[4];
-    load4<BF>(a.QKV, row * a.ld + h * HD + j, x);
-    load4<BF>(a.QKV, row * a.ld + h * HD + j + 64, y);
+    float x[8], y[8];
+    load8<BF>(a.QKV, row * a.ld + h * HD + j, x);
+    load8<BF>(a.QKV, row * a.ld + h * HD + j + 64, y);
     turn(a.rope, s.len - s.nq + i, j, x, y);
     if (a.sa) {
-      float u[4], w[4];
-      load4<false>(a.sa, (h / rep) * HD + j, u);
-      load4<false>(a.sa, (h / rep) * HD + j + 64, w);
+      float u[8], w[8];
+      load8<false>(a.sa, (h / rep) * HD + j, u);
+      load8<false>(a.sa, (h / rep) * HD + j + 64, w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { x[e] = __fdiv_rn(x[e], u[e]); y[e] = __fdiv_rn(y[e], w[e]); }
+      for (int e = 0; e < 8; ++e) { x[e] = __fdiv_rn(x[e], u[e]); y[e] = __fdiv_rn(y[e], w[e]); }
     }
-    store_bf4(a.Qo + row * a.ldq + h * HD + j, x);
-    store_bf4(a.Qo + row * a.ldq + h * HD + j + 64, y);
+    __nv_bfloat16* o = a.Qo + row * a.ldq + h * HD + j;
+    *reinterpret_cast<uint4*>(o) = pack_bf16x8(x);
+    *reinterpret_cast<uint4*>(o + 64) = pack_bf16x8(y);
   }
 }
 
@@ -119,35 +117,35 @@ __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
   }
   const int kept = max(start - pg * P, 0);             // the page's tokens from before this call
   const int n_new = min(s.len, (pg + 1) * P) - pg * P - kept;
-  const int grp = threadIdx.x >> 4, j = 4 * (threadIdx.x & 15);
+  const int grp = threadIdx.x >> 3, j = 8 * (threadIdx.x & 7);
   const int64_t head = (int64_t)id * G + g;
   float* scale_at = (is_v ? a.c.v_scale : a.c.k_scale) + head;
   uint8_t* codes = (is_v ? a.c.v : a.c.k) + head * P * HD;
   const float before = kept > 0 ? *scale_at : 0.f;
   const int64_t col = (int64_t)(a.n_heads + (is_v ? G : 0) + g) * HD + j;
 
-  float x[NP][4], y[NP][4];
+  float x[NP][8], y[NP][8];
   uint32_t big = 0;              // largest magnitude as its bits: ordered as the values, a NaN on top
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    const int i = p * (NT / 16) + grp;                 // new token of the page
+    const int i = p * GRP + grp;                 // new token of the page
     if (i < n_new) {
       const int pos = pg * P + kept + i;
       const int64_t row = s.row0 + (pos - start);
-      load4<BF>(a.QKV, row * a.ld + col, x[p]);
-      load4<BF>(a.QKV, row * a.ld + col + 64, y[p]);
+      load8<BF>(a.QKV, row * a.ld + col, x[p]);
+      load8<BF>(a.QKV, row * a.ld + col + 64, y[p]);
       if (!is_v) {
         turn(a.rope, pos, j, x[p], y[p]);
         if (a.sa) {
-          float u[4], w[4];
-          load4<false>(a.sa, g * HD + j, u);
-          load4<false>(a.sa, g * HD + j + 64, w);
+          float u[8], w[8];
+          load8<false>(a.sa, g * HD + j, u);
+          load8<false>(a.sa, g * HD + j + 64, w);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { x[p][e] = __fmul_rn(x[p][e], u[e]); y[p][e] = __fmul_rn(y[p][e], w[e]); }
+          for (int e = 0; e < 8; ++e) { x[p][e] = __fmul_rn(x[p][e], u[e]); y[p][e] = __fmul_rn(y[p][e], w[e]); }
         }
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 8; ++e)
         big = max(big, max(__float_as_uint(x[p][e]) & 0x7fffffffu, __float_as_uint(y[p][e]) & 0x7fffffffu));
     }
   }
@@ -182,25 +180,25 @@ __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
   __nv_bfloat16* out = is_v ? a.Vo : a.Ko;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    const int i = p * (NT / 16) + grp;
+    const int i = p * GRP + grp;
     if (i < n_new) {
-      uint32_t lo = 0, hi = 0;
+      uint32_t lo[2] = {0, 0}, hi[2] = {0, 0};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 8; ++e) {
         const float cx = after > 0.f ? code_of(x[p][e], after) : 0.f;
         const float cy = after > 0.f ? code_of(y[p][e], after) : 0.f;
-        lo |= (uint32_t)((int)cx + 128) << (8 * e);
-        hi |= (uint32_t)((int)cy + 128) << (8 * e);
+        lo[e >> 2] |= (uint32_t)((int)cx + 128) << (8 * (e & 3));
+        hi[e >> 2] |= (uint32_t)((int)cy + 128) << (8 * (e & 3));
         x[p][e] = __fmul_rn(cx, after);
         y[p][e] = __fmul_rn(cy, after);
       }
       uint8_t* at = codes + (kept + i) * HD + j;
-      *reinterpret_cast<uint32_t*>(at) = lo;
-      *reinterpret_cast<uint32_t*>(at + 64) = hi;
+      *reinterpret_cast<uint2*>(at) = make_uint2(lo[0], lo[1]);
+      *reinterpret_cast<uint2*>(at + 64) = make_uint2(hi[0], hi[1]);
       if (out) {
         __nv_bfloat16* o = out + (int64_t)(s.row0 + pg * P + kept + i - start) * a.ldkv + g * HD + j;
-        store_bf4(o, x[p]);
-        store_bf4(o + 64, y[p]);
+        *reinterpret_cast<uint4*>(o) = pack_bf16x8(x[p]);
+        *reinterpret_cast<uint4*>(o + 64) = pack_bf16x8(y[p]);
       }
     }
   }
@@ -208,10 +206,9 @@ __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
 
 template <bool BF>
 omq_status append_launch(cudaStream_t st, const AppendArgs& a, const dim3& grid) {
-  if (a.c.page == 16) kv_append_kernel<BF, 1><<<grid, NT, 0, st>>>(a);
-  else if (a.c.page == 32) kv_append_kernel<BF, 2><<<grid, NT, 0, st>>>(a);
-  else if (a.c.page == 64) kv_append_kernel<BF, 4><<<grid, NT, 0, st>>>(a);
-  else kv_append_kernel<BF, 8><<<grid, NT, 0, st>>>(a);
+  if (a.c.page <= 32) kv_append_kernel<BF, 1><<<grid, NT, 0, st>>>(a);
+  else if (a.c.page == 64) kv_append_kernel<BF, 2><<<grid, NT, 0, st>>>(a);
+  else kv_append_kernel<BF, 4><<<grid, NT, 0, st>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -244,7 +241,7 @@ omq_status omq_kv_append(omq_stream_t stream, const omq_kv_cache* cache, int32_t
                (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, 0, dev_status};
   a.npg = (max_q + cache->page - 2) / cache->page + 1;       // pages that max_q tokens can touch
   const int64_t kv_units = 2ll * a.npg * cache->n_kv;
-  const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * (NT / 16) - 1) / (QPASS * (NT / 16));
+  const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * GRP - 1) / (QPASS * GRP);
   OMQ_REQUIRE(kv_units + q_units < (1ll << 31), OMQ_ERR_SHAPE);
   a.kv_units = (int)kv_units;
   const dim3 grid((unsigned)(kv_units + q_units), (unsigned)cache->B);
