@@ -77,14 +77,14 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 //           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
 constexpr int BM = 128, BN = 256, BK = 128;
-// Ring depths: raw weight tiles (they come from HBM), A tiles, converted weight tiles.  Stages of 128 codes: with 64 the signals
-// between the roles, not the work, set the pace (2048 x 22016 x 4096: 356 us with 64, 286 us with 128, and
-// 136 us for 1024 rows with the conversion and three quarters of the MMAs of 64-code stages left out).
-constexpr int RAW = 4, AS = 2, CONV = 2;
+// Ring depths: raw weight tiles (they come from HBM), operand stages (A | converted B).  Stages of 128
+// codes: the signals between the roles, not the work, set the pace (2048 x 22016 x 4096: 356 us with 64 and 277
+// with 128; 273 with one barrier for both operands of a stage).
+constexpr int RAW = 4, OPS = 2;
 constexpr int CHUNK_KB = 1024 / BK;               // k blocks per exact accumulation
 constexpr int TC_THREADS = 640;
 constexpr int RAW_BYTES = 128 * BK, OP_BYTES = 128 * BK * 2;      // a raw tile, an fp16 tile of A or B
-constexpr int RAW_OFF = (AS + CONV) * OP_BYTES;
+constexpr int RAW_OFF = 2 * OPS * OP_BYTES;
 constexpr int SUM_OFF = RAW_OFF + RAW * RAW_BYTES;      // code sums of B: 2 tiles x 2 groups x [256]
 constexpr int COL_OFF = SUM_OFF + 4 * 256 * 4;                    // drain warps: [8][4][128] column operands
 constexpr int BAR_OFF = COL_OFF + 8 * 4 * 128 * 4;
@@ -188,16 +188,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* a_ring = smem;                                        // 1024-aligned (swizzle atom)
-  uint8_t* conv_ring = smem + AS * OP_BYTES;
+  uint8_t* conv_ring = smem + OPS * OP_BYTES;
   uint8_t* raw_ring = smem + RAW_OFF;
   int* sum_b = reinterpret_cast<int*>(smem + SUM_OFF);           // [tile parity][group][column of the pair's tile]
   uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + BAR_OFF);
   uint64_t* raw_empty = raw_full + RAW;
-  uint64_t* a_full = raw_empty + RAW;                            // leader's: both CTAs' A tiles landed
-  uint64_t* a_empty = a_full + AS;
-  uint64_t* conv_full = a_empty + AS;                            // leader's: both CTAs' B tiles converted
-  uint64_t* conv_empty = conv_full + CONV;
-  uint64_t* acc_full = conv_empty + CONV;                        // [2]
+  uint64_t* ready = raw_empty + RAW;                             // leader's: both CTAs' A landed and B converted
+  uint64_t* freed = ready + OPS;                                 // the stage's products are formed
+  uint64_t* acc_full = freed + OPS;                              // [2]
   uint64_t* acc_empty = acc_full + 2;                            // [2], leader's
   uint64_t* sum_full = acc_empty + 2;                            // [2]
   uint64_t* sum_empty = sum_full + 2;                            // [2]
@@ -214,8 +212,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < RAW; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
-    for (int s = 0; s < AS; ++s) { mbar_init(&a_full[s], 1); mbar_init(&a_empty[s], 1); }
-    for (int s = 0; s < CONV; ++s) { mbar_init(&conv_full[s], 8); mbar_init(&conv_empty[s], 1); }
+    // one barrier tells the issuing warp everything about a stage, and one commit frees it: each wait and
+    // each commit costs that warp 150 cycles and more
+    for (int s = 0; s < OPS; ++s) { mbar_init(&ready[s], 1 + 8); mbar_init(&freed[s], 1); }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 16);
       mbar_init(&sum_full[b], 16); mbar_init(&sum_empty[b], 16);
@@ -263,22 +262,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int i = first; i < total && ok; i += step) {
         const Item w = item_of(p, i, mt, nt);
         for (int kb = 0; kb < w.nkb; ++kb, ++it) {
-          const int s = it % AS;
-          ok = warp_wait(&a_empty[s], ((it / AS) & 1) ^ 1);
+          const int s = it % OPS;
+          ok = warp_wait(&freed[s], ((it / OPS) & 1) ^ 1);
           if (!ok) { fail(); break; }
           if (elect_one()) {
-            if (leader) mbar_expect_tx(&a_full[s], 2 * OP_BYTES);
+            if (leader) mbar_expect_tx(&ready[s], 2 * OP_BYTES);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              tma_load_3d_pair(&tmA, mapa_shared(smem_u32(&a_full[s]), 0), a_ring + s * OP_BYTES + h * OP_BYTES / 2,
+              tma_load_3d_pair(&tmA, mapa_shared(smem_u32(&ready[s]), 0), a_ring + s * OP_BYTES + h * OP_BYTES / 2,
                                (w.kb0 + kb) * BK + 64 * h, w.m0 + rank * BM, 0);
           }
           __syncwarp();
         }
       }
       if (__any_sync(0xffffffffu, *abort_flag) && leader) {   // (the peer leaves with the leader)
-        const uint32_t from = it > (uint32_t)AS ? it - AS : 0u;
-        for (uint32_t j = from; j < it; ++j) wait_phase(&a_full[j % AS], (j / AS) & 1);
+        const uint32_t from = it > (uint32_t)OPS ? it - OPS : 0u;
+        for (uint32_t j = from; j < it; ++j) wait_phase(&ready[j % OPS], (j / OPS) & 1);
       }
     } else if (warp == 1 && leader) {
       // ---------------- MMA issuer: the whole warp runs the loop, one lane issues ----------------
@@ -289,20 +288,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int i = first; i < total && ok; i += step) {
         const Item w = item_of(p, i, mt, nt);
         for (int kb = 0; kb < w.nkb; ++kb, ++it) {
-          const uint32_t buf = ch & 1, s = it % CONV, as = it % AS;
+          const uint32_t buf = ch & 1, s = it % OPS;
           ok = (kb % CHUNK_KB != 0 || warp_wait(&acc_empty[buf], ((ch >> 1) & 1) ^ 1)) &&
-               warp_wait(&a_full[as], (it / AS) & 1) && warp_wait(&conv_full[s], (it / CONV) & 1);
+               warp_wait(&ready[s], (it / OPS) & 1);
           if (!ok) { fail(); break; }
           tc_fence_after();
           const bool last = kb % CHUNK_KB == CHUNK_KB - 1 || kb == w.nkb - 1;
           if (elect_one()) {
-            const uint64_t a0 = da + (uint64_t)(as * (OP_BYTES >> 4)), b0 = db + (uint64_t)(s * (OP_BYTES >> 4));
+            const uint64_t a0 = da + (uint64_t)(s * (OP_BYTES >> 4)), b0 = db + (uint64_t)(s * (OP_BYTES >> 4));
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k)
               umma_bf16_pair(tmem + buf * BN, a0 + (((k >> 2) * (OP_BYTES / 2) + (k & 3) * 32) >> 4),
                              b0 + (((k >> 2) * (OP_BYTES / 2) + (k & 3) * 32) >> 4), idesc, kb % CHUNK_KB != 0 || k != 0);
-            umma_commit_pair(&a_empty[as], 0x3);
-            umma_commit_pair(&conv_empty[s], 0x3);
+            umma_commit_pair(&freed[s], 0x3);
             if (last) umma_commit_pair(&acc_full[buf], 0x3);
           }
           __syncwarp();
@@ -414,7 +412,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       int sb = 0, codes = 0;                 // sum of this group's codes and their number per row
       for (int kb = 0; kb < w.nkb; ++kb, ++it) {
         if ((int)(it & 1) != grp) continue;
-        const int rs = it % RAW, cs = it % CONV;
+        const int rs = it % RAW, cs = it % OPS;
         ok = warp_wait(&raw_full[rs], (it / RAW) & 1);
         if (!ok) { fail(); break; }
         uint4 u[8];
@@ -425,7 +423,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
           for (int c = 0; c < 8; ++c) sb = code_sum(u[c], sb);
         }
-        ok = warp_wait(&conv_empty[cs], ((it / CONV) & 1) ^ 1);
+        ok = warp_wait(&freed[cs], ((it / OPS) & 1) ^ 1);
         if (!ok) { fail(); break; }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {        // (beyond K they are -128, and A is zero there)
@@ -439,7 +437,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&raw_empty[rs]);
-          mbar_signal_cluster(mapa_shared(smem_u32(&conv_full[cs]), 0));
+          mbar_signal_cluster(mapa_shared(smem_u32(&ready[cs]), 0));
         }
       }
       if (!ok) break;
