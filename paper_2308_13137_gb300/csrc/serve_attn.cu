@@ -7,16 +7,18 @@
 // their partial results are joined through shared memory and, between CTAs, by a second small kernel.
 //
 // This file holds the form for few query rows per KV head (up to 16: decoding).  Every warp keeps its own
-// ring of 16-token tiles in flight (TMA, 2 KB of K and of V each, 128-byte swizzle) and refills a slot as soon
-// as it has used it: no barrier between warps.  Per tile a warp forms S^T = K q^T (16 tokens x 8 query rows) and O^T += V^T P by mma.sync
-// m16n8k16 with fp16 operands and fp32 sums.  The tokens are the M dimension of the first product and
-// the channels of the second, so a single query row costs an eighth of a tile and not a sixteenth.
-// tcgen05 has nothing to offer here: its smallest tile is 64 or 128 rows, and the products are a tenth
-// of the loop's instructions (serve_attn_tc.cu has the form for more rows).  A code becomes an fp16 integer in registers, exactly: the byte under the
-// exponent of 1024 (0x6400 | c = 1024 + c), minus 1152.  Channels are numbered inside the products so
-// that a thread's operand values are 16 consecutive bytes of the page; row g of a product is token
-// g ^ ((g & 1) << 2) of its eight, which puts the eight lanes of every load phase, of K and of V, on
-// eight distinct 16-byte bank groups.
+// ring of 16-token tiles in flight (TMA, 2 KB of K and of V each, 128-byte swizzle) and refills a slot as
+// soon as it has used it: no barrier between warps.  Per tile a warp forms S^T = K q^T (16 tokens x 8 query
+// rows) and O^T += V^T P by mma.sync m16n8k16 with fp16 operands and fp32 sums.  The tokens are the M
+// dimension of the first product and the channels of the second, so a single query row costs an eighth of
+// a tile and not a sixteenth.  tcgen05 has nothing to offer here: its smallest tile is 64 or 128 rows, and
+// the products are a tenth of the loop's instructions (serve_attn_tc.cu has the form for more rows).  A code
+// becomes an fp16 integer in registers, exactly: the byte under the exponent of 1024 (0x6400 | c = 1024 + c),
+// minus 1152.  Channels are numbered inside the products so that a thread's operand values are 16 consecutive
+// bytes of the page; row g of a product is token g ^ ((g & 1) << 2) of its eight, which puts the eight
+// lanes of every load phase, of K and of V, on eight distinct 16-byte bank groups.
+// Measured: 4 x 131072 tokens, 8 rows on each of 8 KV heads, 136 us, 6.0 TB/s; 16 x 4096 tokens, one row on each of
+// 32 heads, 65 us, 5.3 TB/s; one sequence of 2048 tokens 11 us, of which 7 are the two launches and the first loads.
 //
 // Precision: the codes are exact; q (bf16) is exact after a power-of-two scale per row that puts
 // its largest value in [2^13, 2^14); scores, sums and accumulators are fp32.  The weight of a token,
@@ -262,6 +264,12 @@ __global__ void __launch_bounds__(W * 32, 2)
           pw[e] *= c;
           pw[e + 2] *= c;
         }
+        if (cut) {                            // nothing unseen weighs, even where the page's scale is not finite
+          const int2 lm = lim2[4 * nt];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t0 + row_k + 8 * (e >> 1) >= (e & 1 ? lm.y : lm.x)) pw[e] = 0.f;
+        }
         p0[nt] = transpose8x8(pack_half2(pw[0], pw[1]));
         p1[nt] = transpose8x8(pack_half2(pw[2], pw[3]));
       }
@@ -405,7 +413,7 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
 struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
 
 // How a call is cut.  Up to 16 query rows per KV head take this file's form, more the tcgen05 tiles (16 rows,
-// 16 x 4096 tokens: 36 us here, 52 us there).  Tokens per CTA: as many chunks as fill one wave, none under 256
+// 16 x 4096 tokens: 37 us here, 42 us there).  Tokens per CTA: as many chunks as fill one wave, none under 256
 // tokens; a second wave costs more than it balances (4 x 131072 tokens of 8 rows 145 us on one wave, 155 us on
 // two; 8 x 8192 tokens of 128 rows 65 and 77 us; 64 ragged sequences of up to 40 rows 144 us on 3.4 rounds of
 // whole sequences, 162 us split in two).

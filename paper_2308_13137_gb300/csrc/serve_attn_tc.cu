@@ -16,7 +16,9 @@
 //   8..15   convert: K (8..11) and V (12..15) to fp16, one half row of 64 codes per thread; K is read K-major, V
 //           MN-major, both from [half][64 tokens][128 bytes] swizzled tiles
 // Warps without a row of the call do not take part.  Bound: the latency of a tile's way through the
-// softmax threads (64 exponentials each) and the converters; the tile's 16 KB come from HBM in 700 cycles.
+// softmax threads, 1700 cycles per tile and group with 64 exponentials each (half of them in the waits and the
+// fences around the exponentials), where the tile's 16 KB come from HBM in 700: 8 x 8192 tokens, 128 rows on
+// each of 8 KV heads, 64 us, 0.54 PFLOP/s, 1.5 TB/s.
 #include "serve_attn.cuh"
 
 namespace {
@@ -47,6 +49,9 @@ __device__ __forceinline__ void put16(uint32_t row, int c, uint32_t x, const uin
   sts128(row + (((2 * c + 1) ^ x) << 4), make_uint4(codes_lo(u.z), codes_hi(u.z), codes_lo(u.w), codes_hi(u.w)));
 }
 
+// CP: copies of a row.  Rows that fit a half or a quarter of the tile's 128 are held two or four times, each copy
+// with its own half or quarter of every tile's tokens: a softmax thread's 64 exponentials become 32 or 16.
+template <int CP>
 __global__ void __launch_bounds__(THREADS, 1)
     kv_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -86,7 +91,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
   const int tiles = t_end > t_begin ? (t_end - t_begin + TT - 1) / TT : 0;
 
-  const int row_warps = min(4, (R - r0 + 31) >> 5);           // softmax warps of a group that hold rows
+  constexpr int SPAN = BMR / CP, TW = TT / CP;                // rows held, tokens of a softmax thread
+  const int row_warps = CP > 1 ? 4 : min(4, (R - r0 + 31) >> 5);     // softmax warps of a group that hold rows
 
   // ---- page records, the query operand (fp16, K-major, 128-byte swizzle, two halves of 64 channels) ----
   for (int i = threadIdx.x; i < np; i += THREADS) attn_page(a, b, g, (t_begin >> pshift) + i, pid + i, pks + i, plv + i);
@@ -101,16 +107,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc(tmem_holder, 512);
-  for (int r = warp; r < BMR; r += THREADS / 32) {
+  for (int i = warp; i < SPAN; i += THREADS / 32) {
     float v[4];
     int sh;
-    attn_query4(a, s, g, rep, r0 + r, R, lane, v, &sh);
-    uint8_t* row = smem + Q_OFF + (lane >> 4) * (BMR * 128) + r * 128;
-    *reinterpret_cast<uint2*>(row + (((lane & 15) >> 1 ^ (r & 7)) << 4) + (lane & 1) * 8) =
-        make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
-    if (lane == 0) {
-      qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
-      lims[r] = r0 + r < R ? min(s.len, start + (r0 + r) / rep + 1) : 0;
+    attn_query4(a, s, g, rep, r0 + i, R, lane, v, &sh);
+    const uint2 u = make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
+    for (int r = i; r < BMR; r += SPAN) {
+      uint8_t* row = smem + Q_OFF + (lane >> 4) * (BMR * 128) + r * 128;
+      *reinterpret_cast<uint2*>(row + (((lane & 15) >> 1 ^ (r & 7)) << 4) + (lane & 1) * 8) = u;
+      if (lane == 0) {
+        qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
+        lims[r] = r0 + i < R ? min(s.len, start + (r0 + i) / rep + 1) : 0;
+      }
     }
   }
   fence_async_smem();                                         // the query tile -> visible to the tensor core
@@ -121,7 +129,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   constexpr uint32_t O_COL = 128;                             // S: columns 0 and 64; O: 128 and 256
   auto fail = [&]() { omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; };
 
-  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  // registers: 128 x 48 + 256 x 64 + 256 x 144 of the launch's 640 x 96
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
   if (warp == 0 || warp == 3) {
     // ---------------- the raw ring, K and V: the whole warp runs the loop, one lane issues ----------------
     const bool is_v = warp == 3;
@@ -179,7 +188,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   } else if (warp >= 8 && warp < 16) {
     // ---------------- convert ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     const bool is_v = warp >= 12;
     const int t = threadIdx.x & 127, r = t & 63, h = t >> 6;  // token, half of its channels
     const uint32_t x = r & 7, src0 = smem_u32(smem + RAW_OFF) + (is_v ? TT * HD : 0) + r * HD;
@@ -203,46 +212,56 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     const int sg = warp >= 16, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_col = lanes + O_COL + sg * HD;
-    const float f = qs[r];
-    const int lim = lims[r], lim_min = __reduce_min_sync(0xffffffffu, r0 + r < R ? lim : 0x7fffffff);
-    const bool holds = (warp & 3) < row_warps;
+    const bool holds = (warp & 3) < row_warps, mine = r0 + (r & (SPAN - 1)) < R;
     const uint32_t prow = smem_u32(smem + P_OFF + sg * P_BYTES) + r * 128;
     float m = ATTN_NOTHING, M = ATTN_NOTHING, l = 0.f;
     bool ok = true;
-    uint32_t turn = 0;
+    if (CP > 1)                                               // the weights of the other copies' tokens
+      for (int c = 0; c < 8; ++c) sts128(prow + (c << 4), make_uint4(0, 0, 0, 0));
     if (holds && lane == 0) mbar_arrive(&s_ready[sg]);        // the first scores overwrite nothing
+    const int w0 = r / SPAN * TW;                             // this copy's tokens of a tile
+    const float f = qs[r];
+    const int lim = lims[r], lim_min = __reduce_min_sync(0xffffffffu, mine ? lim : 0x7fffffff);
+    uint32_t turn = 0;
     for (int j = sg; j < tiles && holds; j += 2, turn ^= 1) {
-      // the tile's four 16-token quarters, each of one page: score factor, log2 of the value scale; the
-      // tokens that this row sees, as bits
-      const int t0 = t_begin + j * TT;
-      float fk[4], lv[4];
-      uint64_t seen = lim - t0 >= TT ? ~0ull : (lim <= t0 ? 0ull : (1ull << (lim - t0)) - 1);
-      bool whole = t0 + TT <= min(t_end, lim_min);
+      // the 16-token quarters, each of one page: score factor, log2 of the value scale; the tokens that
+      // this row sees, as bits
+      const int t0 = t_begin + j * TT + w0;
+      float fk[TW / 16], lv[TW / 16];
+      uint64_t seen = lim - t0 >= TW ? ~0ull : (lim <= t0 ? 0ull : (1ull << (lim - t0)) - 1);
+      bool whole = t0 + TW <= min(t_end, lim_min);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int pi = min((j * TT + 16 * q) >> pshift, np - 1);
+      for (int q = 0; q < TW / 16; ++q) {
+        const int pi = min((j * TT + w0 + 16 * q) >> pshift, np - 1);
         fk[q] = pks[pi] * f;
         lv[q] = plv[pi];
         if (pid[pi] < 0) {
           whole = false;
           seen &= ~(0xffffull << (16 * q));
-          fk[q] = 0.f;
-          lv[q] = -INFINITY;
         }
+      }
+      if (!whole) {                          // a page that the row does not see weighs nothing, whatever its scale
+#pragma unroll
+        for (int q = 0; q < TW / 16; ++q)
+          if (((uint32_t)(seen >> (16 * q)) & 0xffffu) == 0) { fk[q] = 0.f; lv[q] = -INFINITY; }
       }
       ok = warp_wait(&s_full[sg], turn);
       if (!ok) { fail(); break; }
       tc_fence_after();
-      float x[TT];
-      tmem_ld32(lanes + sg * TT, x);
-      tmem_ld32(lanes + sg * TT + 32, x + 32);
+      float x[TW];
+      if (TW == 16) {
+        tmem_ld16(lanes + sg * TT + w0, x);
+      } else {
+#pragma unroll
+        for (int c = 0; c < TW; c += 32) tmem_ld32(lanes + sg * TT + w0 + c, x + c);
+      }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_ready[sg]);
       // the row's largest score (factors are not negative), and with the value scale
       float top = -INFINITY, topv = -INFINITY;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < TW / 16; ++q) {
         float mx[4];
         if (whole) {
 #pragma unroll
@@ -286,10 +305,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       float2 ls = make_float2(0.f, 0.f), lt = ls;
       const float2 nm = make_float2(-m, -m);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < TW / 16; ++q) {
+        const uint32_t sb = (uint32_t)(seen >> (16 * q));
         const float c = ex2(lv[q] + (m - M) + ATTN_SHIFT);
         const float2 c2 = make_float2(c, c), f2 = make_float2(fk[q], fk[q]);
-        const uint32_t sb = (uint32_t)(seen >> (16 * q));
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           uint32_t w[4];
@@ -307,7 +326,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             const float2 e = omq_mul2(p, c2);
             w[i] = pack_half2(e.x, e.y);
           }
-          sts128(prow + (((2 * q + hf) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+          sts128(prow + (((w0 / 8 + 2 * q + hf) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
         }
       }
       ls = omq_add2(ls, lt);
@@ -317,7 +336,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&p_ready[sg]);
     }
-    // ---- join the two groups: each takes half of the channels ----
+    // ---- join the two groups and the copies: the sums go through the converted tiles' buffers ----
     refs[(sg * 3 + 0) * BMR + r] = m;
     refs[(sg * 3 + 1) * BMR + r] = M;
     refs[(sg * 3 + 2) * BMR + r] = l;
@@ -331,21 +350,32 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (!ok) fail();
       tc_fence_after();
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");            // the two groups' references are written
+    asm volatile("bar.sync 1, 256;" ::: "memory");            // the references are written, the operands read
+    const uint32_t sums = smem_u32(smem + CONV_OFF);          // [128][32] chunks of four channels, moved by the row
     if (ok && holds) {
-      const int row = r0 + r, og = sg ^ 1;
-      const float m1 = refs[(og * 3) * BMR + r], M1 = refs[(og * 3 + 1) * BMR + r], l1 = refs[(og * 3 + 2) * BMR + r];
-      const float mm = fmaxf(m, m1), MM = fmaxf(M, M1), L = l * ex2(m - mm) + l1 * ex2(m1 - mm);
+      float mm = ATTN_NOTHING, MM = ATTN_NOTHING, L = 0.f;
+      for (int c = 0; c < CP; ++c)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int at = k * 3 * BMR + c * SPAN + (r & (SPAN - 1));
+          mm = fmaxf(mm, refs[at]);
+          MM = fmaxf(MM, refs[at + BMR]);
+        }
+      for (int c = 0; c < CP; ++c)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int at = k * 3 * BMR + c * SPAN + (r & (SPAN - 1));
+          L += refs[at + 2 * BMR] * ex2(refs[at] - mm);
+        }
       const bool none = L == 0.f;                             // a NaN score is not an empty row
       const float c = none ? 0.f : ex2(MM - mm - ATTN_SHIFT) / L;
-      const float c0 = c * ex2((sg ? M1 : M) - MM), c1 = c * ex2((sg ? M : M1) - MM);
-      const int64_t tok = s.row0 + row / rep;
-      const int head = g * rep + row % rep;
-      const int64_t part = (tok * a.n_heads + head) * a.n_split + split;
-      if (row < R && sg == 0) {
+      const float c0 = c * ex2(refs[BMR + r] - MM), c1 = c * ex2(refs[4 * BMR + r] - MM);
+      if (mine && sg == 0 && r < SPAN) {
+        const int row = r0 + r;
+        const int64_t at = (s.row0 + row / rep) * a.n_heads + g * rep + row % rep;
         const float lse = none ? -INFINITY : mm + log2f(L);
-        if (a.n_split > 1) a.wl[part] = lse;
-        else if (a.lse) a.lse[tok * a.n_heads + head] = lse;
+        if (a.n_split > 1) a.wl[at * a.n_split + split] = lse;
+        else if (a.lse) a.lse[at] = lse;
       }
 #pragma unroll 1
       for (int d = sg * 64; d < sg * 64 + 64; d += 32) {
@@ -357,16 +387,33 @@ __global__ void __launch_bounds__(THREADS, 1)
           const float o = none ? 0.f : v[i] * c0;
           v[i] = none || tiles < 2 ? o : fmaf(u[i], c1, o);
         }
-        if (row >= R) continue;
-        float* of = a.n_split > 1 ? a.wo + part * HD + d : (a.Of ? a.Of + tok * a.ldo + head * HD + d : nullptr);
-        if (of) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(of + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        }
-        if (a.n_split == 1 && a.Ob) {
-          __nv_bfloat16* ob = a.Ob + tok * a.ldo + head * HD + d;
-#pragma unroll
-          for (int i = 0; i < 32; i += 8) *reinterpret_cast<uint4*>(ob + i) = pack_bf16x8(v + i);
+        for (int i = 0; i < 32; i += 4)
+          sts128(sums + r * 512 + ((((d + i) >> 2) ^ (r & 7)) << 4), make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]),
+                                                                             __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
+      }
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    const int n_rows = *abort_flag ? 0 : min(SPAN, R - r0);
+    for (int q = (warp & 3) + 4 * sg; q < n_rows; q += 8) {   // a row per warp, four channels per lane
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < CP; ++c) {
+        const int at = c * SPAN + q;
+        const uint4 w = lds128(sums + at * 512 + ((lane ^ (at & 7)) << 4));
+        o.x += __uint_as_float(w.x); o.y += __uint_as_float(w.y); o.z += __uint_as_float(w.z); o.w += __uint_as_float(w.w);
+      }
+      const int row = r0 + q, head = g * rep + row % rep;
+      const int64_t tok = s.row0 + row / rep;
+      if (a.n_split > 1) {
+        *reinterpret_cast<float4*>(a.wo + ((tok * a.n_heads + head) * a.n_split + split) * HD + 4 * lane) = o;
+      } else {
+        if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
+        if (a.Ob) {
+          uint2 w;
+          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+          h[0] = __floats2bfloat162_rn(o.x, o.y);
+          h[1] = __floats2bfloat162_rn(o.z, o.w);
+          *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = w;
         }
       }
     }
@@ -381,11 +428,12 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 }  // namespace
 
-omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a) {
+template <int CP>
+static omq_status launch(cudaStream_t st, const AttnArgs& a) {
+  auto kern = kv_attention_tc_kernel<CP>;
   static bool set = false;
   if (!set) {
-    if (cudaFuncSetAttribute(kv_attention_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             tc_smem(ATTN_MAX_CHUNK, 16)) != cudaSuccess)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem(ATTN_MAX_CHUNK, 16)) != cudaSuccess)
       return OMQ_ERR_CUDA;
     set = true;
   }
@@ -394,7 +442,16 @@ omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a) {
   const int box = a.c.page < TT ? a.c.page : TT;
   if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, box, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, box, HD))
     return OMQ_ERR_UNSUPPORTED;
-  kv_attention_tc_kernel<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), THREADS, tc_smem(a.chunk, a.c.page), st>>>(tk, tv, a);
+  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), THREADS, tc_smem(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
+}
+
+// By the most rows that a KV head has in the call (16 x 4096 tokens of 24 rows 42 us with four copies, 53 with
+// one; 64 ragged sequences of up to 40 rows 133 us with two, 144 with one).
+omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a) {
+  const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.c.n_kv);
+  if (rows <= BMR / 4) return launch<4>(st, a);
+  if (rows <= BMR / 2) return launch<2>(st, a);
+  return launch<1>(st, a);
 }

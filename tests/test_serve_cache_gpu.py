@@ -128,6 +128,27 @@ def test_scales_of_very_different_size(cuda_lib):
     assert bool(((out.double().view_as(O) - O).abs() <= 1.5 * 2.0 ** -11 * top).all())
 
 
+@pytest.mark.parametrize("heads,n_q", [(2, 3), (4, 4), (8, 3), (16, 3), (16, 7)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_a_page_that_a_row_does_not_see(cuda_lib, heads, n_q, page):
+    """The newest token lies alone on its page, whose scales are not finite: only its own rows may show it."""
+    c = _cache([3 * page + 1, 9 * page + 1], 1, page, seed=heads + n_q + page)
+    q, out, lse = _attend(c, [n_q] * 2, heads)
+    _check(c, [n_q] * 2, heads, q, out, lse)
+    O, _, top = REF.attention(c, q, heads, [(0, n_q), (n_q, n_q)])
+    last = c.table.long()[[0, 1], [3, 9]]
+    old = [i for i in range(2 * n_q) if i % n_q != n_q - 1]
+    for which in ("k_scale", "v_scale"):
+        for bad in (float("inf"), float("nan")):
+            keep = getattr(c, which).clone()
+            getattr(c, which)[last] = bad
+            _, out, lse2 = _attend(c, [n_q] * 2, heads, q=q)
+            err = (out.double().view(O.shape) - O).abs()[old]
+            assert bool((err <= 1.5 * 2.0 ** -11 * top[old][..., None]).all())
+            assert bool(((lse2 - lse).abs()[old] <= 2e-4).all())
+            getattr(c, which).copy_(keep)
+
+
 def test_queries_of_extreme_size(cuda_lib):
     c = _cache([100, 100, 100, 100], 1, 16, seed=2)
     c.k_scale *= 1e-30
