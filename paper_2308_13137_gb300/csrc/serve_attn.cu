@@ -414,9 +414,8 @@ struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8
 
 // How a call is cut.  Up to 16 query rows per KV head take this file's form, more the tcgen05 tiles (16 rows,
 // 16 x 4096 tokens: 37 us here, 42 us there).  Tokens per CTA: as many chunks as fill one wave, none under 256
-// tokens; a second wave costs more than it balances (4 x 131072 tokens of 8 rows 145 us on one wave, 155 us on
-// two; 8 x 8192 tokens of 128 rows 65 and 77 us; 64 ragged sequences of up to 40 rows 144 us on 3.4 rounds of
-// whole sequences, 162 us split in two).
+// tokens; a second wave costs more than it balances (4 x 131072 tokens of 8 rows 136 us on one wave, 148 us on
+// two; 8 x 8192 tokens of 128 rows 65 and 77 us; 16 x 4096 tokens of 24 rows 43 and 54 us).
 Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   Plan p;
   const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
