@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
 // products so that a thread's operand values are 16 consecutive codes of its row; row 8 i + g of a product
 // is tile row 8 i + (g % 2) 4 + g / 2, so that the eight lanes of a load phase hit eight distinct 16-byte
 // bank groups of the 128-byte swizzle.
-// Measured: 1 x 12288 x 4096 13.4 us, 17 x 5120 x 13824 25 us, 3.8 and 2.8 TB/s of weight codes; about 6 us are
+// Measured: 1 x 12288 x 4096 13.4 us, 17 x 5120 x 13824 22 us, 3.8 and 3.2 TB/s of weight codes; about 6 us are
 // the launch, the first tiles and the joining, the rest the read and, from 17 rows on, the conversion.
 constexpr int FEW_WARPS = 8;
 
@@ -790,10 +790,15 @@ QPlan plan_of(int64_t M, int64_t N, int64_t K) {
   return best;
 }
 
+// Rows of a block of the register form: 24 where that makes no more blocks than 32 (17 x 5120 x 13824: 22.0
+// against 25.0 us, 48 x 22016 x 4096: 48.4 against 53.8).
+bool blocks_of_24(int64_t M) { return (M + 23) / 24 == (M + 31) / 32; }
+
 // Which form: up to 32 rows the first; beyond, by estimates that both measured.  The tensor-core form costs its
 // plan and 7.5 us for the widening launch and its own start (64 x 4096 x 4096: 21.8 us, 64 x 12288 x 4096: 35.8);
-// the register form 6 us and, for each 32 rows, the weight codes at 3.4 TB/s (15.4 and 36.7 us; 128 rows 23.6 and
-// 64 us; 128 x 1024 x 4096: 9.8 against 22.5 us).
+// the register form 6 us and, for each block of rows, the weight codes at 3.4 TB/s (15.4 and 36.7 us; 128 rows
+// 23.6 and 64 us; 128 x 1024 x 4096: 9.8 against 22.5 us).  (Blocks of 24 reach 3.9 TB/s where K is split, but
+// 33 x 5120 x 13824 takes 48.3 us in them, unsplit, and 38.8 in the tensor-core form.)
 bool use_few(int64_t M, int64_t N, int64_t K) {
   if (M <= 32) return true;
   return 6.0 + (double)((M + 31) / 32) * N * K / 3.4e6 < plan_of(M, N, K).us + 7.5;
@@ -844,7 +849,7 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
     const bool wide = (N + 63) / 64 > 2 * omq_num_sms();
     if (M <= 8) return wide ? few_launch<1, 128>(st, p) : few_launch<1, 64>(st, p);
     if (M <= 16) return wide ? few_launch<2, 128>(st, p) : few_launch<2, 64>(st, p);
-    return few_launch<4, 64>(st, p);
+    return blocks_of_24(M) ? few_launch<3, 64>(st, p) : few_launch<4, 64>(st, p);
   }
   const QPlan q = plan_of(M, N, K);
   p.splits = q.splits; p.kb_per_split = q.kb_per_split;

@@ -41,6 +41,15 @@ def test_exact(cuda_lib, M, N, K, zero):
     assert torch.equal(serve.qgemm(*ops, out_dtype=BF16), _want(*ops, None).to(BF16))
 
 
+@pytest.mark.parametrize("M", [17, 23, 24, 25, 33, 41, 48, 49, 65, 72, 73])
+@pytest.mark.parametrize("N,K", [(520, 2064), (4104, 1040)])
+def test_rows_around_the_blocks(cuda_lib, M, N, K):
+    """Blocks of 24 and 32 rows, full and with a few rows in the last."""
+    from paper_2308_13137_gb300 import serve
+    *ops, bias = _case(M, N, K, True)
+    assert torch.equal(serve.qgemm(*ops, bias=bias), _want(*ops, bias))
+
+
 @pytest.mark.parametrize("M", [1, 12, 40, 100, 300])
 @pytest.mark.parametrize("K", [1024, 8192, 65536])
 def test_extreme_codes(cuda_lib, M, K):
