@@ -2,13 +2,16 @@
 //
 // One CTA owns one token row at a time and keeps it in registers: t = x + r, the block sum of t^2,
 // y = t rstd gain + bias, the block max / min of y, Eq. 2 on every element; the next row is on its way
-// to L2 meanwhile.  Nothing of the row is read twice; the bound is HBM (x, r in; codes, values, residual sum
+// to L2, or to shared memory, meanwhile.  Nothing of the row is read twice; the bound is HBM (x, r in; codes, values, residual sum
 // out): 8192 x 8192, bf16 in, fp32 residual, 147 us, 5.95 TB/s.  Elements are worked on in pairs, and the
 // roundings of Eq. 2 are additions of 1.5 * 2^23 instead of conversions, which halves the instructions
 // per element.
 #include "common.cuh"
+#include "tc.cuh"
 
 namespace {
+
+using namespace tc;
 
 struct NormArgs {
   const void* X; int64_t ldx;
@@ -34,6 +37,15 @@ __device__ __forceinline__ void widen8(const uint4& a, const uint4& b, float2 (&
     v[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
     v[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
   }
+}
+
+template <bool BF>
+__device__ __forceinline__ void staged8(uint32_t base, int i, float2 (&v)[4]) {
+  const uint32_t at = base + i * (BF ? 2 : 4);
+  const uint4 a = lds128(at);
+  uint4 b = a;
+  if (!BF) b = lds128(at + 16);
+  widen8<BF>(a, b, v);
 }
 
 // RO: through the read-only path.  The residual is not: R and H may be one buffer.
@@ -116,14 +128,38 @@ __device__ __forceinline__ float2 quant2(const float2 y, const Fast& q, float2* 
   return omq_mul2(omq_add2(*w, q.nzr), q.h);
 }
 
-template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS>
+// ST: the next row's x and r come by bulk copy into shared memory, not by prefetch into L2
+template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS, bool ST>
 __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(const NormArgs a) {
   __shared__ float red[2][96];                   // by row parity: one barrier fewer per row
+  __shared__ uint64_t landed;
+  __shared__ int late;
+  extern __shared__ __align__(16) uint8_t stage[];         // the raw row of x and of r
   const int tid = threadIdx.x, nt = blockDim.x, nvec = a.C >> 3;
+  const uint32_t x_bytes = a.C * (XB ? 2 : 4), r_bytes = a.R ? a.C * (RB ? 2 : 4) : 0;
+  bool staged = ST;
+  auto fetch = [&](int64_t t) {                  // one thread
+    mbar_expect_tx(&landed, x_bytes + r_bytes);
+    bulk_g2s(stage, (const char*)a.X + t * a.ldx * (XB ? 2 : 4), x_bytes, &landed);
+    if (a.R) bulk_g2s(stage + x_bytes, (const char*)a.R + t * a.ldr * (RB ? 2 : 4), r_bytes, &landed);
+  };
+  if (ST) {
+    if (tid == 0) {
+      late = 0;
+      mbar_init(&landed, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      fetch(blockIdx.x);
+    }
+    __syncthreads();
+  }
   int par = 0;
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x, par ^= 1) {
     float2 v[V][4];
-    if (tid == 0 && t + gridDim.x < a.T) {       // the next row of this CTA, into L2
+    // a copy that has not come within the limit: this row and the rest without staging; the CTA leaves only
+    // after another wait for the copy
+    const bool here = staged && wait_phase(&landed, par);
+    if (staged && !here) { late = 1; wait_phase(&landed, par); }
+    if (!ST && tid == 0 && t + gridDim.x < a.T) {       // the next row of this CTA, into L2
       omq_l2_prefetch((const char*)a.X + (t + gridDim.x) * a.ldx * (XB ? 2 : 4), (uint64_t)a.C * (XB ? 2 : 4));
       if (a.R) omq_l2_prefetch((const char*)a.R + (t + gridDim.x) * a.ldr * (RB ? 2 : 4), (uint64_t)a.C * (RB ? 2 : 4));
     }
@@ -132,7 +168,10 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(co
       const int vi = j * nt + tid;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[j][e] = make_float2(0.f, 0.f);
-      if (vi < nvec) load8<XB, true>(a.X, t * a.ldx + 8 * vi, v[j]);
+      if (vi < nvec) {
+        if (here) staged8<XB>(smem_u32(stage), 8 * vi, v[j]);
+        else load8<XB, true>(a.X, t * a.ldx + 8 * vi, v[j]);
+      }
     }
     if (a.R) {
 #pragma unroll
@@ -140,7 +179,8 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(co
         const int vi = j * nt + tid;
         if (vi < nvec) {
           float2 r[4];
-          load8<RB, false>(a.R, t * a.ldr + 8 * vi, r);
+          if (here) staged8<RB>(smem_u32(stage) + x_bytes, 8 * vi, r);
+          else load8<RB, false>(a.R, t * a.ldr + 8 * vi, r);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[j][e] = omq_add2(v[j][e], r[e]);
         }
@@ -155,6 +195,10 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(co
       for (int e = 0; e < 4; ++e) ss = omq_fma2(v[j][e], v[j][e], ss);
     }
     const float tot = block_sum(ss.x + ss.y, red[par]);
+    if (ST) {                                    // the row is in registers: its buffer takes the next one
+      staged = staged && *(volatile int*)&late == 0;
+      if (staged && tid == 0 && t + gridDim.x < a.T) fetch(t + gridDim.x);
+    }
     const float rstd = 1.0f / sqrtf(tot / (float)a.C + a.rms_eps);
     const float2 rs = make_float2(rstd, rstd);
     float M = -INFINITY, m = INFINITY;
@@ -240,14 +284,23 @@ __global__ void __launch_bounds__(MAX_THREADS, MIN_CTAS) rmsnorm_quant_kernel(co
   }
 }
 
-template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS>
+template <bool XB, bool RB, int V, int MAX_THREADS, int MIN_CTAS, bool ST = false>
 omq_status norm_run(cudaStream_t st, const NormArgs& a) {
-  auto kern = rmsnorm_quant_kernel<XB, RB, V, MAX_THREADS, MIN_CTAS>;
+  auto kern = rmsnorm_quant_kernel<XB, RB, V, MAX_THREADS, MIN_CTAS, ST>;
+  const int smem = ST ? a.C * ((XB ? 2 : 4) + (a.R ? (RB ? 2 : 4) : 0)) : 0;
+  if (ST) {
+    static bool set = false;
+    if (!set) {
+      if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * V * MAX_THREADS * 8) != cudaSuccess)
+        return OMQ_ERR_CUDA;
+      set = true;
+    }
+  }
   const int nt = ((a.C / 8 + V - 1) / V + 31) / 32 * 32;
   int per = 1;
-  cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, nt, 0);
+  cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, nt, smem);
   const int64_t most = (int64_t)omq_num_sms() * (per > 0 ? per : 1);
-  kern<<<(unsigned)(a.T < most ? a.T : most), nt, 0, st>>>(a);
+  kern<<<(unsigned)(a.T < most ? a.T : most), nt, smem, st>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -255,13 +308,16 @@ omq_status norm_run(cudaStream_t st, const NormArgs& a) {
 // Eight-element vectors per thread.  Up to one row per SM the row's own latency counts and more threads win
 // (1 x 4096: 3.8 us with one vector, 4.4 with four; 1 x 8192: 5.1, 5.3); with more rows fewer threads leave
 // room for a second CTA (2048 x 5120 30.5 us with two, 38.1 with one) and, from 6 K columns on, four
-// vectors amortise the two block reductions better (8192 x 8192: 146.6 us against 153.1 with two).
+// vectors amortise the two block reductions better (8192 x 8192: 146.6 us against 153.1 with two).  From six rows per
+// SM on the shorter rows are staged (2048 x 4096, bf16 with fp32 residual: 22.4 against 25.4 us; 8192 x 4096: 70.9,
+// 77.6; 700 x 4096: 13.2, 11.9); longer ones lose more than they gain (8192 x 8192: 182 us staged).
 template <bool XB, bool RB>
 omq_status norm_launch(cudaStream_t st, const NormArgs& a) {
   const int nvec = a.C / 8;
   const bool few = a.T <= omq_num_sms();
   if (few && nvec <= 1024) return norm_run<XB, RB, 1, 1024, 1>(st, a);
   if (few && nvec <= 2048) return norm_run<XB, RB, 2, 1024, 1>(st, a);
+  if (nvec <= 768 && a.T > 6 * omq_num_sms()) return norm_run<XB, RB, 2, 512, 2, true>(st, a);
   if (nvec <= 768) return norm_run<XB, RB, 2, 512, 2>(st, a);
   if (nvec <= 2048) return norm_run<XB, RB, 4, 512, 1>(st, a);
   return norm_run<XB, RB, 8, 512, 1>(st, a);

@@ -71,7 +71,7 @@ def rmsnorm_quant(x, r=None, gain=None, bias=None, bits: int = 8, rms_eps: float
         quant = bits < 16
         out = QuantRows(new(torch.uint8, T, C) if quant else None, new(F32, T) if quant else None,
                         new(torch.int32, T) if quant else None, new(BF16, T, C) if values or not quant else None,
-                        torch.empty(T, C, dtype=r.dtype, device=x.device) if r is not None else None)
+                        torch.empty_strided(r.shape, r.stride(), dtype=r.dtype, device=x.device) if r is not None else None)
     codes, h, z, vals, res = out
     code = _calls.rmsnorm_quant(x, r, gain, bias, bits, rms_eps, h_eps, codes, h, z, vals, res)
     if code:

@@ -139,3 +139,22 @@ def test_non_finite_bias(cuda_lib):
         bias[77] = v
         out = serve.rmsnorm_quant(x, None, gain, bias, values=True)
         assert bool(out.h.isnan().all()) and bool(out.values.isnan().all()) and int(out.codes.max()) == 0
+
+
+@pytest.mark.parametrize("C,ld", [(8, 16), (1032, 1040), (4096, 4096), (6144, 6152)])
+@pytest.mark.parametrize("xd", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rd", [None, torch.float32, torch.bfloat16])
+def test_many_rows_equal_few_at_a_time(cuda_lib, C, ld, xd, rd):
+    """The form for many rows gives what 500 rows at a time give, bit for bit."""
+    from paper_2308_13137_gb300 import serve
+    g = torch.Generator(device="cuda").manual_seed(C)
+    T = 2000
+    x = torch.randn(T, ld, generator=g, device="cuda").to(xd)[:, :C]
+    r = None if rd is None else torch.randn(T, ld, generator=g, device="cuda").to(rd)[:, :C]
+    gain, bias = torch.randn(C, generator=g, device="cuda"), torch.randn(C, generator=g, device="cuda")
+    whole = serve.rmsnorm_quant(x, r=r, gain=gain, bias=bias)
+    for i in range(0, T, 500):
+        part = serve.rmsnorm_quant(x[i:i + 500], r=None if r is None else r[i:i + 500], gain=gain, bias=bias)
+        for w, p in zip(whole, part):
+            if torch.is_tensor(p):
+                assert torch.equal(w[i:i + 500], p)
