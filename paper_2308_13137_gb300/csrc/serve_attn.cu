@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(W * 32, 2)
         float pw[4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float c = ex2(lv + (m[nt][e] - M[nt][e]) + SHIFT);
+          const float c = attn_factor(lv + (m[nt][e] - M[nt][e]) + SHIFT);
           pw[e] = ex2(x[e] - m[nt][e]);
           pw[e + 2] = ex2(x[e + 2] - m[nt][e]);
           l[nt][e] += pw[e] + pw[e + 2];

@@ -12,6 +12,15 @@ constexpr float ATTN_SHIFT = 8.f, ATTN_SLACK = 7.f;
 constexpr float ATTN_NOTHING = -1e30f;      // a reference before the first visible token
 constexpr float ATTN_SCALE = 0.12751743074602467f;   // log2(e) / sqrt(128)
 
+// The part 2^e of a weight that its token's page and the references give.  e passes CAP only where the row's top
+// score lies on pages whose values vanish beside this one's; a token's own part is 2^-105 or less there, and
+// its weight counts for nothing, but infinity times zero would make the row NaN.  (A NaN of e passes through.)
+constexpr float ATTN_CAP = 120.f;
+__device__ __forceinline__ float attn_factor(float e) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(e) : "f"(ATTN_CAP));
+  return tc::ex2(e);
+}
+
 struct AttnArgs {
   omq_kv_cache c;
   int total_q, max_q; const int32_t* cu_q; int max_kv, n_heads;

@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
       for (int q = 0; q < TW / 16; ++q) {
         const uint32_t sb = (uint32_t)(seen >> (16 * q));
-        const float c = ex2(lv[q] + (m - M) + ATTN_SHIFT);
+        const float c = attn_factor(lv[q] + (m - M) + ATTN_SHIFT);
         const float2 c2 = make_float2(c, c), f2 = make_float2(fk[q], fk[q]);
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
