@@ -22,7 +22,7 @@
 //
 // Precision: the codes are exact; q (bf16) is exact after a power-of-two scale per row that puts
 // its largest value in [2^13, 2^14); scores, sums and accumulators are fp32.  The weight of a token,
-// p sv, is rounded to fp16 against a reference M near the largest log2(p sv), so that a weight keeps 11
+// p sv, is rounded to fp16 against a reference m + d near the largest log2(p sv), so that a weight keeps 11
 // bits down to 2^-22 of the largest; p's own sum stays fp32 against its own reference m (V's scales
 // differ by page, so the two references differ).  A reference moves, and the accumulator with it,
 // only when a score passes it by more than 2^7: few tiles do, and the others need no maximum across
@@ -36,7 +36,7 @@ using namespace tc;
 constexpr int HD = ATTN_HD;
 constexpr int TILE = 16;                    // tokens of a warp's tile
 constexpr int TILE_BYTES = 2 * TILE * HD;   // K and V
-constexpr float SHIFT = ATTN_SHIFT, SLACK = ATTN_SLACK, NOTHING = ATTN_NOTHING;
+constexpr float SHIFT = ATTN_SHIFT, SLACK = ATTN_SLACK, NOTHING = ATTN_NOTHING, NO_VALUE = ATTN_NO_VALUE;
 constexpr int OPAD = 132;                   // floats per row of the joining buffer
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -83,8 +83,8 @@ __global__ void __launch_bounds__(W * 32, 2)
   float* qs = reinterpret_cast<float*>(smem + S::QS_OFF);
   int* lims = reinterpret_cast<int*>(qs + S::ROWS);
   float* st_m = reinterpret_cast<float*>(smem + S::STAT_OFF);
-  float* st_M = st_m + W * NT * 8;
-  float* st_l = st_M + W * NT * 8;
+  float* st_d = st_m + W * NT * 8;
+  float* st_l = st_d + W * NT * 8;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(full + S::SLOTS);
   int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF);
@@ -138,11 +138,11 @@ __global__ void __launch_bounds__(W * 32, 2)
   }
   __syncthreads();
 
-  float m[NT][2], M[NT][2], l[NT][2], acc[NT][8][4];
+  float m[NT][2], d[NT][2], l[NT][2], acc[NT][8][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) { m[nt][e] = NOTHING; M[nt][e] = NOTHING; l[nt][e] = 0.f; }
+    for (int e = 0; e < 2; ++e) { m[nt][e] = NOTHING; d[nt][e] = NO_VALUE; l[nt][e] = 0.f; }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -215,8 +215,11 @@ __global__ void __launch_bounds__(W * 32, 2)
         }
       }
       uint4 v[4];
-      v[0] = lds128(base + v_off0); v[1] = lds128(base + v_off1);
-      v[2] = lds128(base + v_off0 + 8 * HD); v[3] = lds128(base + v_off1 + 8 * HD);
+      auto values = [&]() {
+        v[0] = lds128(base + v_off0); v[1] = lds128(base + v_off1);
+        v[2] = lds128(base + v_off0 + 8 * HD); v[3] = lds128(base + v_off1 + 8 * HD);
+      };
+      if (NT == 1) values();                 // (two row tiles have no registers for them before the weights)
       uint32_t p0[NT], p1[NT];
       const bool cut = t0 + TILE > lim_min;                   // some row does not see all of the tile
 #pragma unroll
@@ -234,8 +237,8 @@ __global__ void __launch_bounds__(W * 32, 2)
             if (t0 + row_k + 8 * (e >> 1) >= (e & 1 ? lm.y : lm.x)) x[e] = -INFINITY;
         }
         const float t0m = fmaxf(x[0], x[2]), t1m = fmaxf(x[1], x[3]);
-        const bool over = t0m > m[nt][0] + SLACK || t1m > m[nt][1] + SLACK || t0m + lv > M[nt][0] + SLACK ||
-                          t1m + lv > M[nt][1] + SLACK;
+        const float u0 = t0m - m[nt][0], u1 = t1m - m[nt][1];
+        const bool over = u0 > SLACK || u1 > SLACK || u0 + (lv - d[nt][0]) > SLACK || u1 + (lv - d[nt][1]) > SLACK;
         if (__any_sync(0xffffffffu, over)) {
           float top[2] = {t0m, t1m}, grow[2];
 #pragma unroll
@@ -243,11 +246,12 @@ __global__ void __launch_bounds__(W * 32, 2)
             top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 4));
             top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
             top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16));
-            const float mn = fmaxf(m[nt][e], top[e]), Mn = fmaxf(M[nt][e], top[e] + lv);
-            l[nt][e] *= ex2(m[nt][e] - mn);
-            grow[e] = ex2(M[nt][e] - Mn);
+            const float mn = fmaxf(m[nt][e], top[e]), drop = m[nt][e] - mn;
+            const float dn = fmaxf(fmaxf(d[nt][e] + drop, (top[e] - mn) + lv), NO_VALUE);
+            l[nt][e] *= ex2(drop);
+            grow[e] = ex2((d[nt][e] - dn) + drop);
             m[nt][e] = mn;
-            M[nt][e] = Mn;
+            d[nt][e] = dn;
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i)
@@ -257,7 +261,7 @@ __global__ void __launch_bounds__(W * 32, 2)
         float pw[4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float c = attn_factor(lv + (m[nt][e] - M[nt][e]) + SHIFT);
+          const float c = attn_factor(lv - d[nt][e] + SHIFT);
           pw[e] = ex2(x[e] - m[nt][e]);
           pw[e + 2] = ex2(x[e + 2] - m[nt][e]);
           l[nt][e] += pw[e] + pw[e + 2];
@@ -273,6 +277,7 @@ __global__ void __launch_bounds__(W * 32, 2)
         p0[nt] = transpose8x8(pack_half2(pw[0], pw[1]));
         p1[nt] = transpose8x8(pack_half2(pw[2], pw[3]));
       }
+      if (NT > 1) values();
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const uint32_t va = u4(v[0], w), vb = u4(v[1], w), vc = u4(v[2], w), vd = u4(v[3], w);
@@ -314,7 +319,7 @@ __global__ void __launch_bounds__(W * 32, 2)
       v += __shfl_xor_sync(0xffffffffu, v, 16);
       if (lg == 0) {
         const int at = (warp * NT + nt) * 8 + 2 * lt + e;
-        st_m[at] = m[nt][e]; st_M[at] = M[nt][e]; st_l[at] = v;
+        st_m[at] = m[nt][e]; st_d[at] = d[nt][e]; st_l[at] = v;
       }
     }
 #pragma unroll
@@ -331,23 +336,23 @@ __global__ void __launch_bounds__(W * 32, 2)
     {                                                         // one query row per warp, 4 channels per lane
       const int q = warp, row = r0 + nt * 8 + q;
       if (row >= R) continue;
-      float mm = NOTHING, MM = NOTHING;
+      float mm = NOTHING, dd = NO_VALUE;
+      for (int k = 0; k < W; ++k) mm = fmaxf(mm, st_m[(k * NT + nt) * 8 + q]);
       for (int k = 0; k < W; ++k) {
         const int at = (k * NT + nt) * 8 + q;
-        mm = fmaxf(mm, st_m[at]);
-        MM = fmaxf(MM, st_M[at]);
+        dd = fmaxf(dd, (st_m[at] - mm) + st_d[at]);
       }
       float L = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = 0; k < W; ++k) {
         const int at = (k * NT + nt) * 8 + q;
         L += st_l[at] * ex2(st_m[at] - mm);
-        const float c = ex2(st_M[at] - MM);
+        const float c = ex2((st_m[at] - mm) + st_d[at] - dd);
         const float4 x = *reinterpret_cast<const float4*>(join + (k * 8 + q) * OPAD + 4 * lane);
         o.x = fmaf(x.x, c, o.x); o.y = fmaf(x.y, c, o.y); o.z = fmaf(x.z, c, o.z); o.w = fmaf(x.w, c, o.w);
       }
       const bool none = L == 0.f;                             // a NaN score is not an empty row
-      const float c = none ? 0.f : ex2(MM - mm - SHIFT) / L;
+      const float c = none ? 0.f : ex2(dd - SHIFT) / L;
       const float lse = none ? -INFINITY : mm + log2f(L);
       o.x *= c; o.y *= c; o.z *= c; o.w *= c;
       const int64_t tok = s.row0 + row / rep;

@@ -7,9 +7,12 @@
 
 constexpr int ATTN_HD = 128;
 constexpr int ATTN_MAX_CHUNK = 16384;       // tokens of a CTA
-// A weight is 2^SHIFT at the reference M and at most 2^(SHIFT + SLACK), below the largest fp16
+// References of a row: m near its largest score, and d near the largest score - m + log2 of the value scale.  d is
+// held relative to m, so that scores whose size leaves no bits for the value scale's log2 do not lose it.
+// A weight is 2^SHIFT at the reference m + d and at most 2^(SHIFT + SLACK), below the largest fp16.
 constexpr float ATTN_SHIFT = 8.f, ATTN_SLACK = 7.f;
-constexpr float ATTN_NOTHING = -1e30f;      // a reference before the first visible token
+constexpr float ATTN_NOTHING = -3.402823466e38f;   // m before the first visible token: no score is lower
+constexpr float ATTN_NO_VALUE = -1e30f;     // d before the first visible token whose page has values, and its floor
 constexpr float ATTN_SCALE = 0.12751743074602467f;   // log2(e) / sqrt(128)
 
 // The part 2^e of a weight that its token's page and the references give.  e passes CAP only where the row's top

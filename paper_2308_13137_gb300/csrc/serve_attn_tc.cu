@@ -18,7 +18,7 @@
 // Warps without a row of the call do not take part.  Bound: the latency of a tile's way through the
 // softmax threads, 1700 cycles per tile and group with 64 exponentials each (half of them in the waits and the
 // fences around the exponentials), where the tile's 16 KB come from HBM in 700: 8 x 8192 tokens, 128 rows on
-// each of 8 KV heads, 64 us, 0.54 PFLOP/s, 1.5 TB/s.
+// each of 8 KV heads, 67 us, 0.52 PFLOP/s, 1.4 TB/s.
 #include "serve_attn.cuh"
 
 namespace {
@@ -36,7 +36,7 @@ constexpr int CONV_OFF = Q_OFF + Q_BYTES;
 constexpr int P_OFF = CONV_OFF + 4 * OP_BYTES;       // converted: K K | V V
 constexpr int RAW_OFF = P_OFF + 2 * P_BYTES;
 constexpr int ROW_OFF = RAW_OFF + RAW * RAW_BYTES;   // per row: factor, keys seen
-constexpr int REF_OFF = ROW_OFF + 2 * BMR * 4;      // per group and row: m, M, l
+constexpr int REF_OFF = ROW_OFF + 2 * BMR * 4;      // per group and row: m, d, l
 constexpr int BAR_OFF = REF_OFF + 2 * 3 * BMR * 4;
 constexpr int PAGES_OFF = BAR_OFF + 256;
 constexpr int THREADS = 640;
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_col = lanes + O_COL + sg * HD;
     const bool holds = (warp & 3) < row_warps, mine = r0 + (r & (SPAN - 1)) < R;
     const uint32_t prow = smem_u32(smem + P_OFF + sg * P_BYTES) + r * 128;
-    float m = ATTN_NOTHING, M = ATTN_NOTHING, l = 0.f;
+    float m = ATTN_NOTHING, d = ATTN_NO_VALUE, l = 0.f;
     bool ok = true;
     if (CP > 1)                                               // the weights of the other copies' tokens
       for (int c = 0; c < 8; ++c) sts128(prow + (c << 4), make_uint4(0, 0, 0, 0));
@@ -258,8 +258,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_ready[sg]);
-      // the row's largest score (factors are not negative), and with the value scale
-      float top = -INFINITY, topv = -INFINITY;
+      // the row's largest score (factors are not negative), and how far it passes m + d with the value scale
+      float top = -INFINITY, far = -INFINITY, xm[TW / 16];
 #pragma unroll
       for (int q = 0; q < TW / 16; ++q) {
         float mx[4];
@@ -277,20 +277,24 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
         const float mq = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        const float xq = mq == -INFINITY ? -INFINITY : mq * fk[q];
-        top = fmaxf(top, xq);
-        topv = fmaxf(topv, xq + lv[q]);
+        xm[q] = mq == -INFINITY ? -INFINITY : mq * fk[q];
+        top = fmaxf(top, xm[q]);
+        far = fmaxf(far, (xm[q] - m) + (lv[q] - d));
       }
       if (j > 1) {                                            // this group's last product: it has read P and written O
         ok = warp_wait(&p_done[sg], turn ^ 1);
         if (!ok) { fail(); break; }
         tc_fence_after();
       }
-      if (__any_sync(0xffffffffu, top > m + ATTN_SLACK || topv > M + ATTN_SLACK)) {
-        const float mn = fmaxf(m, top), Mn = fmaxf(M, topv), grow = ex2(M - Mn);
-        l *= ex2(m - mn);
+      if (__any_sync(0xffffffffu, top - m > ATTN_SLACK || far > ATTN_SLACK)) {
+        const float mn = fmaxf(m, top), drop = m - mn;
+        float dn = fmaxf(d + drop, ATTN_NO_VALUE);
+#pragma unroll
+        for (int q = 0; q < TW / 16; ++q) dn = fmaxf(dn, (xm[q] - mn) + lv[q]);
+        const float grow = ex2((d - dn) + drop);
+        l *= ex2(drop);
         m = mn;
-        M = Mn;
+        d = dn;
         if (j > 1) {
 #pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
@@ -302,12 +306,22 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
       }
+      // x fk - m below is one operation, whose exact product differs from the rounded one in m by up to
+      // 2^-25 |m|: scores of such size are rounded first
+      if (fabsf(m) > 1048576.f) {
+#pragma unroll
+        for (int q = 0; q < TW / 16; ++q) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[16 * q + i] *= fk[q];
+          fk[q] = 1.f;
+        }
+      }
       float2 ls = make_float2(0.f, 0.f), lt = ls;
       const float2 nm = make_float2(-m, -m);
 #pragma unroll
       for (int q = 0; q < TW / 16; ++q) {
         const uint32_t sb = (uint32_t)(seen >> (16 * q));
-        const float c = attn_factor(lv[q] + (m - M) + ATTN_SHIFT);
+        const float c = attn_factor(lv[q] - d + ATTN_SHIFT);
         const float2 c2 = make_float2(c, c), f2 = make_float2(fk[q], fk[q]);
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -315,8 +329,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int k = 8 * hf + 2 * i;
-            const float2 d = omq_fma2(make_float2(x[16 * q + k], x[16 * q + k + 1]), f2, nm);
-            float2 p = make_float2(ex2(d.x), ex2(d.y));
+            const float2 u = omq_fma2(make_float2(x[16 * q + k], x[16 * q + k + 1]), f2, nm);
+            float2 p = make_float2(ex2(u.x), ex2(u.y));
             if (!whole) {
               if (!((sb >> k) & 1)) p.x = 0.f;
               if (!((sb >> (k + 1)) & 1)) p.y = 0.f;
@@ -338,7 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     // ---- join the two groups and the copies: the sums go through the converted tiles' buffers ----
     refs[(sg * 3 + 0) * BMR + r] = m;
-    refs[(sg * 3 + 1) * BMR + r] = M;
+    refs[(sg * 3 + 1) * BMR + r] = d;
     refs[(sg * 3 + 2) * BMR + r] = l;
     if (ok && holds) {
 #pragma unroll
@@ -353,23 +367,20 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("bar.sync 1, 256;" ::: "memory");            // the references are written, the operands read
     const uint32_t sums = smem_u32(smem + CONV_OFF);          // [128][32] chunks of four channels, moved by the row
     if (ok && holds) {
-      float mm = ATTN_NOTHING, MM = ATTN_NOTHING, L = 0.f;
+      float mm = ATTN_NOTHING, dd = ATTN_NO_VALUE, L = 0.f;
+      for (int c = 0; c < CP; ++c)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) mm = fmaxf(mm, refs[k * 3 * BMR + c * SPAN + (r & (SPAN - 1))]);
       for (int c = 0; c < CP; ++c)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int at = k * 3 * BMR + c * SPAN + (r & (SPAN - 1));
-          mm = fmaxf(mm, refs[at]);
-          MM = fmaxf(MM, refs[at + BMR]);
-        }
-      for (int c = 0; c < CP; ++c)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int at = k * 3 * BMR + c * SPAN + (r & (SPAN - 1));
+          dd = fmaxf(dd, (refs[at] - mm) + refs[at + BMR]);
           L += refs[at + 2 * BMR] * ex2(refs[at] - mm);
         }
       const bool none = L == 0.f;                             // a NaN score is not an empty row
-      const float c = none ? 0.f : ex2(MM - mm - ATTN_SHIFT) / L;
-      const float c0 = c * ex2(refs[BMR + r] - MM), c1 = c * ex2(refs[4 * BMR + r] - MM);
+      const float c = none ? 0.f : ex2(dd - ATTN_SHIFT) / L;
+      const float c0 = c * ex2((refs[r] - mm) + refs[BMR + r] - dd), c1 = c * ex2((refs[3 * BMR + r] - mm) + refs[4 * BMR + r] - dd);
       if (mine && sg == 0 && r < SPAN) {
         const int row = r0 + r;
         const int64_t at = (s.row0 + row / rep) * a.n_heads + g * rep + row % rep;
@@ -378,10 +389,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         else if (a.lse) a.lse[at] = lse;
       }
 #pragma unroll 1
-      for (int d = sg * 64; d < sg * 64 + 64; d += 32) {
+      for (int ch = sg * 64; ch < sg * 64 + 64; ch += 32) {
         float v[32], u[32];
-        if (tiles > 0) tmem_ld32(lanes + O_COL + d, v);
-        if (tiles > 1) tmem_ld32(lanes + O_COL + HD + d, u);
+        if (tiles > 0) tmem_ld32(lanes + O_COL + ch, v);
+        if (tiles > 1) tmem_ld32(lanes + O_COL + HD + ch, u);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           const float o = none ? 0.f : v[i] * c0;
@@ -389,7 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
 #pragma unroll
         for (int i = 0; i < 32; i += 4)
-          sts128(sums + r * 512 + ((((d + i) >> 2) ^ (r & 7)) << 4), make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]),
+          sts128(sums + r * 512 + ((((ch + i) >> 2) ^ (r & 7)) << 4), make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]),
                                                                              __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
       }
     }

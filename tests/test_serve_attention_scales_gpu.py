@@ -71,3 +71,24 @@ def test_top_score_on_a_page_of_vanishing_values(cuda_lib, heads, n_q, page, n_p
         c.k_scale[_at(c, where)] = gap / unit
         c.v_scale[_at(c, where)] = v_scale
         _check(c, heads, n_q, q)
+
+
+@pytest.mark.parametrize("heads,n_q", ROWS)
+@pytest.mark.parametrize("v_scale", [0.04, 4096.0])
+@pytest.mark.parametrize("size", [2.0 ** 24, -2.0 ** 24, -2.0 ** 99, -2.0 ** 110, 2.0 ** 99, 2.0 ** 110])
+def test_scores_of_any_size(cuda_lib, heads, n_q, v_scale, size):
+    """Scores of one sign and any size below the largest fp32 number, no visible score near zero: the row is
+    not empty.  Keys differ between tokens by whole codes, so scores that are not equal are far apart."""
+    page = 16
+    c = _cache(20, page, seed=heads, tail=5)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    level = torch.randint(20, 120, c.k.shape[:3], generator=g, device="cuda")
+    c.k.copy_((128 + level)[..., None].expand(c.k.shape))
+    c.v_scale.fill_(v_scale)
+    c.v_scale[_at(c, 7)] = v_scale / 512
+    q = torch.full((n_q, heads * 128), size, device="cuda").to(BF16)
+    out, O = _check(c, heads, n_q, q)
+    assert float(O.abs().max()) > 0
+    # and beside ordinary scores: half of the pages have keys next to zero
+    c.k_scale[: 10] = 2.0 ** -100
+    _check(c, heads, n_q, q)
