@@ -169,6 +169,7 @@ struct Rows { int32_t total, max_q; const int32_t* cu; };
 
 // cu_q and max_q of a call on `rows` rows: without cu_q every sequence has the same number
 Rows row_map(Call& c, const omq_kv_cache* kv, int64_t rows, PyObject* cu, PyObject* max_q) {
+  if (kv->B <= 0) throw Bad{"cache: at least one sequence"};
   if (rows > INT32_MAX) throw Bad{"rows: too many"};
   Rows r{(int32_t)rows, 0, nullptr};
   if (cu == Py_None) {

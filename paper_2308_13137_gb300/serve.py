@@ -106,7 +106,8 @@ class KVCache:
                             (v_scale, "v_scale", F32), (table, "table", torch.int32), (kv_len, "kv_len", torch.int32)):
             _need(t.is_cuda and t.is_contiguous() and t.dtype == dt, f"{name}: contiguous device tensor of {dt}")
         _need(k_scale.shape == (n_pages, n_kv) and v_scale.shape == (n_pages, n_kv), "scales: [n_pages, n_kv]")
-        _need(table.dim() == 2 and kv_len.dim() == 1 and kv_len.shape[0] == table.shape[0], "table [B, n], kv_len [B]")
+        _need(table.dim() == 2 and kv_len.dim() == 1 and kv_len.shape[0] == table.shape[0] and table.shape[0] > 0,
+              "table [B, n], kv_len [B], B at least 1")
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.kv_len = k, v, k_scale, v_scale, table, kv_len
         self.n_kv, self.page, self.B = n_kv, page, table.shape[0]
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
