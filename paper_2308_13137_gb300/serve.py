@@ -81,7 +81,9 @@ def rmsnorm_quant(x, r=None, gain=None, bias=None, bits: int = 8, rms_eps: float
 
 def qgemm(a, a_h, a_z, w, w_h, w_z, bias=None, out=None, out_dtype=F32, status=None):
     """Y[m, n] = a_h[m] w_h[n] sum_k (a[m, k] - a_z[m]) (w[n, k] - w_z[n]) + bias[n] (omq_qgemm_i8).
-    a [M, K], w [N, K] uint8 codes; steps fp32; zero points int32 or None (= 128)."""
+    a [M, K], w [N, K] uint8 codes; steps fp32; zero points int32 or None (= 128).  status: an int32 device word
+    that is set when a wait of the kernel ran out and the output is unfinished (a KVCache's serves: its check
+    raises then)."""
     if out is None:
         out = torch.empty(a.shape[0], w.shape[0], dtype=out_dtype, device=a.device)
     code = _calls.qgemm(a, a_h, a_z, w, w_h, w_z, bias, out, status)
@@ -124,7 +126,8 @@ class KVCache:
                    new(torch.int32, B))
 
     def check(self, stream=None):
-        """Raises when a call met a page id or length out of range (waits for the stream)."""
+        """Raises when a call that reports to this cache met a page id or length out of range, or a wait of its
+        kernels ran out (waits for the stream)."""
         code = _lib.omq_stream_status(self.status, stream)
         if code:
             self.status.zero_()

@@ -64,9 +64,9 @@ class ServedBlock:
         c.table.copy_(torch.arange(B * per, dtype=I32).view(B, per))
         return c
 
-    def _product(self, name: str, rows: serve.QuantRows, out_dtype=F32):
+    def _product(self, name: str, rows: serve.QuantRows, status, out_dtype=F32):
         w, h, z = self.w[name]
-        return serve.qgemm(rows.codes, rows.h, rows.z, w, h, z, bias=self.bias[name], out_dtype=out_dtype)
+        return serve.qgemm(rows.codes, rows.h, rows.z, w, h, z, bias=self.bias[name], out_dtype=out_dtype, status=status)
 
     def _norm(self, i: int, x, r=None) -> serve.QuantRows:
         g, b = self.ln[i]
@@ -83,18 +83,20 @@ class ServedBlock:
                 max_kv: Optional[int] = None):
         """h [rows, d] fp32: the residual stream of the new tokens; delta [rows, d]: the previous block's
         output still to be added to it (fused into this block's first norm).  Returns (h, delta) for the next
-        block; the block's output is their sum.  cache.kv_len counts the new tokens already."""
+        block; the block's output is their sum.  cache.kv_len counts the new tokens already.  cache.check() raises
+        when a call met a page id or length out of range, or a wait of any kernel ran out."""
         sh = self.shape
+        self.cfg.dev_status = cache.status.data_ptr()    # the quantizer's waits
         n1 = self._norm(0, h) if delta is None else self._norm(0, delta, h)
         if delta is not None:
             h = n1.residual
-        qkv = self._product("qkv", n1)
+        qkv = self._product("qkv", n1, cache.status)
         q = serve.kv_append(cache, qkv, rope, sh.n_heads, cu_q=cu_q, max_q=max_q, sa=self.sa)
         o = serve.kv_attention(cache, q, sh.n_heads, cu_q=cu_q, max_q=max_q, max_kv=max_kv, out_dtype=F32)
-        n2 = self._norm(1, self._product("o", self._codes(o)), h)
-        gu = self._product("gu", n2)
+        n2 = self._norm(1, self._product("o", self._codes(o), cache.status), h)
+        gu = self._product("gu", n2, cache.status)
         m = torch.nn.functional.silu(gu[:, :sh.ffn]) * gu[:, sh.ffn:]
-        return n2.residual, self._product("d", self._codes(m))
+        return n2.residual, self._product("d", self._codes(m), cache.status)
 
 
 def main():
