@@ -56,31 +56,6 @@ __device__ __forceinline__ void omq_l2_prefetch(const void* p, uint64_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"((uint32_t)bytes) : "memory");
 }
 
-// Two launches of one call, the second beside the end of the first (launch_beside): the first lets it start, the
-// second waits, before it touches anything the first writes, until the first has finished and its writes
-// are visible.  What the first writes is not read through the read-only path.
-__device__ __forceinline__ void omq_release_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void omq_wait_prior() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-template <class... P, class... A>
-static inline omq_status launch_beside(void (*kern)(P...), dim3 grid, dim3 block, int smem, int cluster, cudaStream_t st,
-                                       const A&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) { cudaGetLastError(); return OMQ_ERR_CUDA; }
-  return OMQ_OK;
-}
-
 __device__ __forceinline__ uint64_t omq_globaltimer() {
   uint64_t t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));

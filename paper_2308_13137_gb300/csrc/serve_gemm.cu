@@ -76,8 +76,6 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 //           and proxy fence overlap the other's work.  They also form the rows' code sums for the
 //           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
-// The product starts beside the widening launch and fills its weight ring meanwhile, the joining launch beside
-// the product (256 x 5120 x 13824: 53.8 us, 56.1 one after another; 2048 x 4096 x 4096: 66.2, 68.2).
 // What bounds it is the hand-offs between the roles, then the tensor rate: 2048 x 22016 x 4096 in 274 us,
 // 1.35 PFLOP/s; the drain's last stores, about a tenth, are not covered.
 constexpr int BM = 128, BN = 256, BK = 128;
@@ -187,10 +185,9 @@ __device__ __forceinline__ void tc_store(const QgemmArgs& p, const int (&acc)[BN
   }
 }
 
-__global__ void __launch_bounds__(TC_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
     qgemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const QgemmArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  omq_release_next();                                            // the joining launch, where there is one
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* a_ring = smem;                                        // 1024-aligned (swizzle atom)
   uint8_t* conv_ring = smem + OPS * OP_BYTES;
@@ -262,8 +259,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       }
     } else if (warp == 2) {
       // ---------------- A tiles: both CTAs' loads complete on the leader's barrier ----------------
-      omq_wait_prior();                      // the widened codes (the weights are under way meanwhile)
-      asm volatile("fence.proxy.async;" ::: "memory");
       uint32_t it = 0;
       bool ok = true;
       for (int i = first; i < total && ok; i += step) {
@@ -329,7 +324,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     int* col_s = col_z + 128;
     float* col_b = reinterpret_cast<float*>(col_s + 128);
     uint32_t ch = 0, tile = 0;
-    omq_wait_prior();                        // the row sums
     for (int i = first; i < total; i += step, ++tile) {
       const Item w = item_of(p, i, mt, nt);
       int acc[BN / 2];
@@ -475,7 +469,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 // A's codes -> fp16 integers code - 128, and the row sums of those; one CTA per row
 __global__ void __launch_bounds__(256) qgemm_widen_kernel(const QgemmArgs p) {
   __shared__ int red[8];
-  omq_release_next();
   const int m = blockIdx.x, nv = p.K >> 4;
   int s = 0;
   for (int i = threadIdx.x; i < nv; i += 256) {
@@ -500,7 +493,6 @@ __global__ void __launch_bounds__(256) qgemm_widen_kernel(const QgemmArgs p) {
 __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int nv = p.N >> 2;
-  omq_wait_prior();
   if (i >= (int64_t)p.M * nv) return;
   const int m = (int)(i / nv), n = (int)(i % nv) * 4;
   const bool zeros = p.az || p.bz;
@@ -872,11 +864,12 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
     attr_set = true;
   }
   const int64_t items = ((M + 255) / 256) * ((N + 255) / 256) * q.splits, pairs = omq_num_sms() / 2;
-  OMQ_TRY(launch_beside(qgemm_tc_kernel, dim3((unsigned)(2 * (items < pairs ? items : pairs))), dim3(TC_THREADS), TC_SMEM, 2,
-                        st, ta, tb, p));
+  qgemm_tc_kernel<<<(unsigned)(2 * (items < pairs ? items : pairs)), TC_THREADS, TC_SMEM, st>>>(ta, tb, p);
+  OMQ_LAUNCH_CHECK();
   if (q.splits > 1) {
     const int64_t n = M * (N / 4);
-    OMQ_TRY(launch_beside(qgemm_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, 1, st, p));
+    qgemm_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p);
+    OMQ_LAUNCH_CHECK();
   }
   return OMQ_OK;
 }

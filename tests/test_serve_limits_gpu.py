@@ -30,3 +30,17 @@ def test_empty_batch_is_refused(cuda_lib):
                 bind.kv_append(at, qkv, rope, 4, cu, most, None, q, None, None, c.status)
             with pytest.raises(ValueError):
                 bind.kv_attention(at, q, 4, cu, most, 32, q, None, c.status)
+
+
+@pytest.mark.parametrize("M,N,K", [(400, 776, 2064), (2048, 4096, 4096), (300, 2056, 8192)])
+def test_every_launch_of_a_product_is_counted(cuda_lib, M, N, K):
+    """omq_launch_count: the widening launch, the product, and the joining launch where K is split: the workspace has room for
+    partial sums then, beyond the widened codes and their sums.  (Few rows: one launch, no workspace.)"""
+    from paper_2308_13137_gb300 import _lib, serve
+    a, w = _new(U8, M, K), _new(U8, N, K)
+    ah, wh = _new(F32, M), _new(F32, N)
+    need = _lib.omq_qgemm_i8_workspace_size(M, N, K)
+    want = 1 if need == 0 else (3 if need > 2 * M * K + 4 * (M + 3) else 2)      # the register form: one
+    before = _lib.omq_launch_count()
+    serve.qgemm(a, ah, None, w, wh, None)
+    assert _lib.omq_launch_count() - before == want
