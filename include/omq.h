@@ -488,6 +488,14 @@ omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, int64_t K, co
                         void* workspace, size_t ws_bytes, int32_t* dev_status);
 size_t omq_qgemm_i8_workspace_size(int64_t M, int64_t N, int64_t K);
 
+/* Failure-detection self-test of that product's form for few rows, as omq_selftest_bounded_wait: C [M, N] fp32 of
+ * packed codes A [M, K], B [N, K] without zero points (M at most 32, N and K at most 65536), every wait
+ * bounded by wait_limit_ns (1e3 .. 1e9; counted in tries of about 4 us).  withhold = 1: the first tile is never
+ * loaded, the wait for it runs out, *dev_status becomes OMQ_ERR_TIMEOUT and C is unspecified. */
+omq_status omq_selftest_qgemm_wait(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A,
+                                   const float* a_h, const uint8_t* B, const float* b_h, float* C,
+                                   uint64_t wait_limit_ns, int32_t withhold, int32_t* dev_status);
+
 /* Pages of an 8-bit key / value cache.  A page holds `page` consecutive tokens (16, 32, 64 or 128) of
  * one sequence for every KV head, with one scale per (page, head), not negative: the value is
  * (code - 128) scale.

@@ -129,6 +129,7 @@ _SIGS = {
     "omq_rmsnorm_quant": (I32, [P, I64, I64, P, I32, I64, P, P, I32, I64, P, P, F32, P, P, P, P, P]),
     "omq_qgemm_i8": (I32, [P, I64, I64, I64, P, I64, P, P, P, I64, P, P, P, P, P, I64, P, SZ, P]),
     "omq_qgemm_i8_workspace_size": (SZ, [I64, I64, I64]),
+    "omq_selftest_qgemm_wait": (I32, [P, I64, I64, I64, P, P, P, P, P, ctypes.c_uint64, I32, P]),
     "omq_rope_table": (I32, [P, I32, F32, P]),
     "omq_kv_append": (I32, [P, P, I32, I32, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
     "omq_kv_attention": (I32, [P, P, I32, I32, P, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
@@ -421,6 +422,12 @@ def omq_qgemm_i8(M, N, K, A, lda, a_h, a_z, B, ldb, b_h, b_z, bias, Cf, Cb, ldc,
     check("omq_qgemm_i8", lib().omq_qgemm_i8(
         stream_handle(stream), M, N, K, row_ptr(A), lda, ptr(a_h), ptr(a_z), row_ptr(B), ldb, ptr(b_h), ptr(b_z),
         ptr(bias), row_ptr(Cf), row_ptr(Cb), ldc, ptr(workspace), ws_bytes, ptr(dev_status)))
+
+
+def omq_selftest_qgemm_wait(M, N, K, A, a_h, B, b_h, C, wait_limit_ns, withhold, dev_status, stream=None):
+    check("omq_selftest_qgemm_wait", lib().omq_selftest_qgemm_wait(
+        stream_handle(stream), M, N, K, ptr(A), ptr(a_h), ptr(B), ptr(b_h), ptr(C), int(wait_limit_ns), int(withhold),
+        ptr(dev_status)))
 
 
 def omq_rope_table(n_pos, theta, out, stream=None):

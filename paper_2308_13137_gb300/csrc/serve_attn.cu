@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(W * 32, 2)
       if (++slot == DEPTH) { slot = 0; turn ^= 1; }
     }
     if (lane == 0 && *abort_flag)            // no copy may land after this CTA has left
-      for (int j = max(0, filled - DEPTH); j < filled; ++j) wait_phase(&wfull[j % DEPTH], (j / DEPTH) & 1);
+      for (int j = max(0, filled - DEPTH); j < filled; ++j)
+        if (!wait_phase(&wfull[j % DEPTH], (j / DEPTH) & 1)) break;
   }
 
   // ---- join the warps ----

@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
     }
     if (__any_sync(0xffffffffu, *abort_flag))        // no copy may land after this CTA has left
-      for (int j = i > RAW ? i - RAW : 0; j < i; ++j) wait_phase(&raw_full[j % RAW], (j / RAW) & 1);
+      for (int j = i > RAW ? i - RAW : 0; j < i; ++j)
+        if (!wait_phase(&raw_full[j % RAW], (j / RAW) & 1)) break;
   } else if (warp == 1 || warp == 2) {
     // ---------------- issue: the whole warp runs the loop, one lane issues ----------------
     const bool scores = warp == 1;

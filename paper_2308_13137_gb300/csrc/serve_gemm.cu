@@ -31,6 +31,8 @@ struct QgemmArgs {
   int m_fast;
   __half* wide;               // [M, K] activation codes as fp16 integers, written by qgemm_widen_kernel
   int32_t* sum_a;             // [M] their row sums
+  uint32_t wait_ns;           // limit of a wait of the register form
+  int withhold;               // self-test only: its first tile is never loaded, so the wait for it runs out
 };
 
 // two of the four codes of a word as fp16 integers code - 128: the byte under the exponent of 1024
@@ -255,7 +257,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       }
       if (__any_sync(0xffffffffu, *abort_flag)) {    // no copy may land after this CTA has left
         const uint32_t from = it > (uint32_t)RAW ? it - RAW : 0u;
-        for (uint32_t j = from; j < it; ++j) wait_phase(&raw_full[j % RAW], (j / RAW) & 1);
+        for (uint32_t j = from; j < it; ++j)
+          if (!wait_phase(&raw_full[j % RAW], (j / RAW) & 1)) break;
       }
     } else if (warp == 2) {
       // ---------------- A tiles: both CTAs' loads complete on the leader's barrier ----------------
@@ -279,7 +282,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TC_THREADS, 1)
       }
       if (__any_sync(0xffffffffu, *abort_flag) && leader) {   // (the peer leaves with the leader)
         const uint32_t from = it > (uint32_t)OPS ? it - OPS : 0u;
-        for (uint32_t j = from; j < it; ++j) wait_phase(&ready[j % OPS], (j / OPS) & 1);
+        for (uint32_t j = from; j < it; ++j)
+          if (!wait_phase(&ready[j % OPS], (j / OPS) & 1)) break;
       }
     } else if (warp == 1 && leader) {
       // ---------------- MMA issuer: the whole warp runs the loop, one lane issues ----------------
@@ -603,7 +607,10 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
     int i = 0;                               // the whole warp runs the loop, one lane issues
     for (; i < steps; ++i) {
       const int s = i % F::STAGES;
-      if (!warp_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1)) { omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break; }
+      if (p.withhold && i == 0) continue;            // self-test: the first tile never comes
+      if (!warp_wait(&empty[s], ((i / F::STAGES) & 1) ^ 1, p.wait_ns)) {
+        omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
+      }
       uint8_t* dst = smem + s * F::STAGE;
       if (elect_one()) {
         mbar_expect_tx(&full[s], F::STAGE);
@@ -616,7 +623,8 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
       __syncwarp();
     }
     if (__any_sync(0xffffffffu, *abort_flag))        // no copy may land after this CTA has left
-      for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j) wait_phase(&full[j % F::STAGES], (j / F::STAGES) & 1);
+      for (int j = i > F::STAGES ? i - F::STAGES : 0; j < i; ++j)
+        if (!(p.withhold && j == 0) && !wait_phase(&full[j % F::STAGES], (j / F::STAGES) & 1, p.wait_ns)) break;
   } else {
     // channel group, 64-code slice of the tile, this thread's 16-code chunk of its rows' 128 bytes
     const int cw = warp % FEW_GROUPS, kq = warp / FEW_GROUPS, c = t + 4 * (kq & 1);
@@ -631,7 +639,7 @@ __global__ void __launch_bounds__((FEW_WARPS + 1) * 32, 2)
     const int row = (g & 1) * 4 + (g >> 1);          // tile row of product row g
     for (int i = 0; i < steps; ++i) {
       const int s = i % F::STAGES;
-      if (!warp_wait(&full[s], (i / F::STAGES) & 1)) {
+      if (!warp_wait(&full[s], (i / F::STAGES) & 1, p.wait_ns)) {
         omq_set_status(p.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
       }
       const uint32_t wb = smem_u32(smem + s * F::STAGE) + ((kq >> 1) * FEW_N + 32 * cw + row) * 128 + ((c ^ row) << 4);
@@ -764,6 +772,18 @@ omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
 }
 
 // ------------------------------------------------------------------------------------------------
+// The register form.  64 channels per CTA while that is one wave, else 128 (22016 x 4096, one row: 22.9 against 25.8
+// us); with 17 rows and more the conversion of the tokens counts and 64 stays the faster (34.4 against 40.5 us).
+// Rows of a block from 17 on: 24 where that makes no more blocks than 32 (17 x 5120 x 13824: 22.0 against 25.0 us,
+// 48 x 22016 x 4096: 48.4 against 53.8).
+omq_status few_rows(cudaStream_t st, const QgemmArgs& p) {
+  const bool wide = (p.N + 63) / 64 > 2 * omq_num_sms();
+  if (p.M <= 8) return wide ? few_launch<1, 128>(st, p) : few_launch<1, 64>(st, p);
+  if (p.M <= 16) return wide ? few_launch<2, 128>(st, p) : few_launch<2, 64>(st, p);
+  return (p.M + 23) / 24 == (p.M + 31) / 32 ? few_launch<3, 64>(st, p) : few_launch<4, 64>(st, p);
+}
+
+// ------------------------------------------------------------------------------------------------
 struct QPlan { int splits, kb_per_split; double us; };
 
 // K split of the tensor-core form.  The work items (tiles x splits) run in rounds over the CTA pairs; a split
@@ -781,10 +801,6 @@ QPlan plan_of(int64_t M, int64_t N, int64_t K) {
   }
   return best;
 }
-
-// Rows of a block of the register form: 24 where that makes no more blocks than 32 (17 x 5120 x 13824: 22.0
-// against 25.0 us, 48 x 22016 x 4096: 48.4 against 53.8).
-bool blocks_of_24(int64_t M) { return (M + 23) / 24 == (M + 31) / 32; }
 
 // Which form: up to 32 rows the first; beyond, by estimates that both measured.  The tensor-core form costs its
 // plan and 7.5 us for the widening launch and its own start (64 x 4096 x 4096: 21.8 us, 64 x 12288 x 4096: 35.8);
@@ -835,14 +851,8 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   p.A = A; p.lda = lda; p.ah = a_h; p.az = a_z;
   p.B = B; p.ldb = ldb; p.bh = b_h; p.bz = b_z;
   p.bias = bias; p.Cf = Cf; p.Cb = (__nv_bfloat16*)Cb; p.ldc = ldc; p.status = dev_status;
-  if (use_few(M, N, K)) {
-    // 64 channels per CTA while that is one wave, else 128 (22016 x 4096, one row: 22.9 against 25.8 us); with
-    // 17 rows and more the conversion of the tokens counts and 64 stays the faster (34.4 against 40.5 us)
-    const bool wide = (N + 63) / 64 > 2 * omq_num_sms();
-    if (M <= 8) return wide ? few_launch<1, 128>(st, p) : few_launch<1, 64>(st, p);
-    if (M <= 16) return wide ? few_launch<2, 128>(st, p) : few_launch<2, 64>(st, p);
-    return blocks_of_24(M) ? few_launch<3, 64>(st, p) : few_launch<4, 64>(st, p);
-  }
+  p.wait_ns = (uint32_t)OMQ_WAIT_LIMIT_NS;
+  if (use_few(M, N, K)) return few_rows(st, p);
   const QPlan q = plan_of(M, N, K);
   p.splits = q.splits; p.kb_per_split = q.kb_per_split;
   const QSpace sp = space_of(M, N, K, q.splits);
@@ -872,4 +882,25 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
     OMQ_LAUNCH_CHECK();
   }
   return OMQ_OK;
+}
+
+// Failure-detection self-test: the register form with every wait bounded by wait_limit_ns, and optionally
+// without its first tile, so that the wait for it runs out.
+extern "C" omq_status omq_selftest_qgemm_wait(omq_stream_t stream, int64_t M, int64_t N, int64_t K, const uint8_t* A,
+                                              const float* a_h, const uint8_t* B, const float* b_h, float* C,
+                                              uint64_t wait_limit_ns, int32_t withhold, int32_t* dev_status) {
+  OMQ_REQUIRE(M > 0 && M <= 32 && N > 0 && N <= 65536 && K > 0 && K <= 65536, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(A && a_h && B && b_h && C, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(withhold == 0 || withhold == 1, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(wait_limit_ns >= 1000ull && wait_limit_ns <= OMQ_WAIT_LIMIT_NS, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(K % 16 == 0 && N % 8 == 0, OMQ_ERR_ALIGN);
+  OMQ_REQUIRE(omq_aligned16(A) && omq_aligned16(B) && omq_aligned16(a_h) && omq_aligned16(b_h) && omq_aligned16(C),
+              OMQ_ERR_ALIGN);
+  QgemmArgs p{};
+  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  p.A = A; p.lda = K; p.ah = a_h; p.B = B; p.ldb = K; p.bh = b_h; p.Cf = C; p.ldc = N;
+  p.status = dev_status;
+  p.wait_ns = (uint32_t)wait_limit_ns;
+  p.withhold = withhold;
+  return few_rows((cudaStream_t)stream, p);
 }
