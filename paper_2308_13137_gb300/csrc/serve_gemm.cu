@@ -809,6 +809,7 @@ QPlan plan_of(int64_t M, int64_t N, int64_t K) {
 // 33 x 5120 x 13824 takes 48.3 us in them, unsplit, and 38.8 in the tensor-core form.)
 bool use_few(int64_t M, int64_t N, int64_t K) {
   if (M <= 32) return true;
+  if ((M + 31) / 32 > 65535) return false;       // its row blocks are the grid's second axis
   return 6.0 + (double)((M + 31) / 32) * N * K / 3.4e6 < plan_of(M, N, K).us + 7.5;
 }
 

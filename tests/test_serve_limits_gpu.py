@@ -4,6 +4,8 @@ import ctypes
 import pytest
 import torch
 
+import _serve_ref as REF
+
 pytestmark = pytest.mark.gpu
 F32, BF16, U8, I32 = torch.float32, torch.bfloat16, torch.uint8, torch.int32
 
@@ -44,3 +46,21 @@ def test_every_launch_of_a_product_is_counted(cuda_lib, M, N, K):
     before = _lib.omq_launch_count()
     serve.qgemm(a, ah, None, w, wh, None)
     assert _lib.omq_launch_count() - before == want
+
+
+@pytest.mark.parametrize("M,N,K", [(65535 * 32, 8, 16), (65535 * 32 + 40, 8, 16), (2200000, 128, 128), (3000000, 64, 256)])
+def test_many_rows_of_a_small_product(cuda_lib, M, N, K):
+    """More rows than the register form's grid has room for; every output equals the exact one."""
+    from paper_2308_13137_gb300 import serve
+    g = torch.Generator(device="cuda").manual_seed(M % 1000)
+    a = torch.randint(0, 256, (M, K), generator=g, device="cuda", dtype=torch.int32).to(U8)
+    w = torch.randint(0, 256, (N, K), generator=g, device="cuda", dtype=torch.int32).to(U8)
+    ah, wh = torch.rand(M, generator=g, device="cuda") + 0.5, torch.rand(N, generator=g, device="cuda") + 0.5
+    az = torch.randint(0, 256, (M,), generator=g, device="cuda", dtype=torch.int32)
+    wz = torch.randint(0, 256, (N,), generator=g, device="cuda", dtype=torch.int32)
+    status = _new(I32, 1)
+    got = serve.qgemm(a, ah, az, w, wh, wz, status=status)
+    assert int(status) == 0
+    for lo in range(0, M, 1 << 19):
+        s = slice(lo, lo + (1 << 19))
+        assert torch.equal(got[s], REF.int_product(a[s], az[s], w, wz).float() * ah[s, None] * wh)
