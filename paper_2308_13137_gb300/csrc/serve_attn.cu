@@ -92,8 +92,8 @@ __global__ void __launch_bounds__(W * 32, 2)
   float* pks = reinterpret_cast<float*>(pid + per_chunk);     // key scale, times log2(e) / sqrt(128)
   float* plv = pks + per_chunk;                               // log2 of the value scale
 
-  const int b = blockIdx.z, split = blockIdx.x;
-  const int g = blockIdx.y / a.row_tiles, rt = blockIdx.y % a.row_tiles;
+  const int b = blockIdx.y, split = blockIdx.x % a.n_split, gr = blockIdx.x / a.n_split;
+  const int g = gr / a.row_tiles, rt = gr % a.row_tiles;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lg = lane >> 2, lt = lane & 3;
   const int rep = a.n_heads / a.c.n_kv;
   SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
@@ -460,7 +460,7 @@ omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
   const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
   if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, TILE, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, TILE, HD))
     return OMQ_ERR_UNSUPPORTED;
-  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), W * 32, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
+  kern<<<dim3(a.n_split * a.c.n_kv * a.row_tiles, a.c.B), W * 32, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -486,7 +486,7 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
                   omq_aligned16(workspace),
               OMQ_ERR_ALIGN);
   const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
-  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles <= 65535, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles * p.n_split < (1ll << 31), OMQ_ERR_SHAPE);
   OMQ_REQUIRE((int64_t)cache->n_pages * cache->n_kv * cache->page < (1ll << 31), OMQ_ERR_SHAPE);   // TMA coordinates
   const size_t need = plan_workspace(p, total_q, n_heads);
   OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);

@@ -73,8 +73,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   float* pks = reinterpret_cast<float*>(pid + per_chunk);
   float* plv = pks + per_chunk;
 
-  const int b = blockIdx.z, split = blockIdx.x;
-  const int g = blockIdx.y / a.row_tiles, rt = blockIdx.y % a.row_tiles;
+  const int b = blockIdx.y, split = blockIdx.x % a.n_split, gr = blockIdx.x / a.n_split;
+  const int g = gr / a.row_tiles, rt = gr % a.row_tiles;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rep = a.n_heads / a.c.n_kv;
   SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
@@ -454,7 +454,7 @@ static omq_status launch(cudaStream_t st, const AttnArgs& a) {
   const int box = a.c.page < TT ? a.c.page : TT;
   if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, box, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, box, HD))
     return OMQ_ERR_UNSUPPORTED;
-  kern<<<dim3(a.n_split, a.c.n_kv * a.row_tiles, a.c.B), THREADS, tc_smem(a.chunk, a.c.page), st>>>(tk, tv, a);
+  kern<<<dim3(a.n_split * a.c.n_kv * a.row_tiles, a.c.B), THREADS, tc_smem(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }

@@ -64,3 +64,29 @@ def test_many_rows_of_a_small_product(cuda_lib, M, N, K):
     for lo in range(0, M, 1 << 19):
         s = slice(lo, lo + (1 << 19))
         assert torch.equal(got[s], REF.int_product(a[s], az[s], w, wz).float() * ah[s, None] * wh)
+
+
+def test_a_prompt_of_many_row_tiles(cuda_lib):
+    """1024 query heads on one KV head, 8200 new tokens: 65600 tiles of 128 rows.  Only the newest 40 tokens are in
+    the cache, so the rows before them are empty."""
+    from paper_2308_13137_gb300 import serve
+    heads, rows, held = 1024, 8200, 40
+    g = torch.Generator(device="cuda").manual_seed(1)
+    c = serve.KVCache.empty(4, 1, 16, 1, 4)
+    c.table.copy_(torch.tensor([[2, 0, 3, 1]], dtype=I32))
+    c.kv_len.fill_(held)
+    for t in (c.k, c.v):
+        t.copy_((torch.randn(t.shape, generator=g, device="cuda") * 35 + 128).round().clamp(1, 255))
+    c.k_scale.fill_(0.03)
+    c.v_scale.fill_(0.03)
+    q = _new(BF16, rows, heads * 128)
+    q[-held - 1:] = torch.randn(held + 1, heads * 128, generator=g, device="cuda").to(BF16)
+    lse = torch.zeros(rows, heads, device="cuda")
+    out = serve.kv_attention(c, q, heads, lse=lse)
+    c.check()
+    assert bool((out[:-held] == 0).all()) and bool((lse[:-held] == -float("inf")).all())
+    O, L, top = REF.attention(c, q[-held:], heads, [(0, held)])
+    got = out[-held:].double().view(O.shape)
+    # weights in fp16, the output in bf16
+    assert bool(((got - O).abs() <= 1.5 * 2.0 ** -11 * top[..., None] + 2.0 ** -8 * O.abs()).all())
+    assert bool(((lse[-held:].double() - L).abs() <= 1e-4).all())
