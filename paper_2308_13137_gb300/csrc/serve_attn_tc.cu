@@ -355,17 +355,16 @@ __global__ void __launch_bounds__(THREADS, 1)
     refs[(sg * 3 + 0) * BMR + r] = m;
     refs[(sg * 3 + 1) * BMR + r] = d;
     refs[(sg * 3 + 2) * BMR + r] = l;
-    if (ok && holds) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (tiles > k) {                                      // the last product into O of group k
-          const int n = (tiles - k + 1) / 2;                  // its tiles
-          ok = ok && warp_wait(&p_done[k], (n - 1) & 1);
-        }
+    // each group waits for the last product into its own O, whose phases it has followed (the other's barrier may
+    // be two phases behind for it); the barrier of the two orders both against what follows
+    if (ok && holds && tiles > sg) {
+      ok = warp_wait(&p_done[sg], ((tiles - sg + 1) / 2 - 1) & 1);
       if (!ok) fail();
       tc_fence_after();
     }
+    tc_fence_before();
     asm volatile("bar.sync 1, 256;" ::: "memory");            // the references are written, the operands read
+    tc_fence_after();
     const uint32_t sums = smem_u32(smem + CONV_OFF);          // [128][32] chunks of four channels, moved by the row
     if (ok && holds) {
       float mm = ATTN_NOTHING, dd = ATTN_NO_VALUE, L = 0.f;
