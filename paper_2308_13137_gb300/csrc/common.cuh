@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "omq.h"
+#include "per_device.h"
 
 #define OMQ_VERSION 1
 
@@ -31,15 +32,30 @@ static inline omq_status omq_check_cfg(const omq_qcfg* cfg) {
   return OMQ_OK;
 }
 
+static inline int omq_device() {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  return dev;
+}
+
+// SMs of the current device
 static inline int omq_num_sms() {
-  static int n = 0;
-  if (n == 0) {
-    int dev = 0;
-    cudaGetDevice(&dev);
+  static std::atomic<int> known[64];
+  const int dev = omq_device();
+  return omq_value_per_device(known, dev, [dev] {
+    int n = 0;
     cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (n <= 0) n = 148;
-  }
-  return n;
+    return n > 0 ? n : 148;
+  });
+}
+
+// Raises a kernel's limit of dynamic shared memory on the current device; `done` is the kernel's own flag.
+template <class K>
+static inline omq_status omq_allow_smem(std::atomic<uint64_t>& done, K kern, int bytes) {
+  const bool ok = omq_once_per_device(done, omq_device(), [&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+  });
+  return ok ? OMQ_OK : OMQ_ERR_CUDA;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -450,12 +450,8 @@ template <int NT>
 omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
   using S = Smem<NT>;
   auto kern = kv_attention_kernel<NT>;
-  static bool set = false;
-  if (!set) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes(ATTN_MAX_CHUNK, 16)) != cudaSuccess)
-      return OMQ_ERR_CUDA;
-    set = true;
-  }
+  static std::atomic<uint64_t> allowed{0};
+  OMQ_TRY(omq_allow_smem(allowed, kern, S::bytes(ATTN_MAX_CHUNK, 16)));
   CUtensorMap tk, tv;
   const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
   if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, TILE, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, TILE, HD))

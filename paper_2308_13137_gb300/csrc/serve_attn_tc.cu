@@ -442,12 +442,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 template <int CP>
 static omq_status launch(cudaStream_t st, const AttnArgs& a) {
   auto kern = kv_attention_tc_kernel<CP>;
-  static bool set = false;
-  if (!set) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem(ATTN_MAX_CHUNK, 16)) != cudaSuccess)
-      return OMQ_ERR_CUDA;
-    set = true;
-  }
+  static std::atomic<uint64_t> allowed{0};
+  OMQ_TRY(omq_allow_smem(allowed, kern, tc_smem(ATTN_MAX_CHUNK, 16)));
   CUtensorMap tk, tv;
   const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
   const int box = a.c.page < TT ? a.c.page : TT;

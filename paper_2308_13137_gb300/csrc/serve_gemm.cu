@@ -739,11 +739,8 @@ template <int NT, int FEW_N>
 omq_status few_launch(cudaStream_t st, const QgemmArgs& p) {
   using F = Few<NT, FEW_N>;
   auto kern = qgemm_few_kernel<NT, FEW_N>;
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES) != cudaSuccess) return OMQ_ERR_CUDA;
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> allowed{0};
+  OMQ_TRY(omq_allow_smem(allowed, kern, F::BYTES));
   CUtensorMap ta, tb;
   if (!omq_make_map_u8(&ta, p.A, p.K, p.M, p.lda, F::TOK, 128) || !omq_make_map_u8(&tb, p.B, p.K, p.N, p.ldb, FEW_N, 128))
     return OMQ_ERR_UNSUPPORTED;
@@ -866,14 +863,10 @@ extern "C" omq_status omq_qgemm_i8(omq_stream_t stream, int64_t M, int64_t N, in
   CUtensorMap ta, tb;
   if (!omq_make_map_bf16(&ta, p.wide, K, M, 1, K, 0, 64, 128) || !omq_make_map_u8(&tb, B, K, N, ldb, 128, BK))
     return OMQ_ERR_UNSUPPORTED;              // (a map of any 16-bit type moves fp16)
+  static std::atomic<uint64_t> allowed{0};
+  OMQ_TRY(omq_allow_smem(allowed, qgemm_tc_kernel, TC_SMEM));
   qgemm_widen_kernel<<<(unsigned)M, 256, 0, st>>>(p);
   OMQ_LAUNCH_CHECK();
-  static bool attr_set = false;
-  if (!attr_set) {
-    if (cudaFuncSetAttribute(qgemm_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM) != cudaSuccess)
-      return OMQ_ERR_CUDA;
-    attr_set = true;
-  }
   const int64_t items = ((M + 255) / 256) * ((N + 255) / 256) * q.splits, pairs = omq_num_sms() / 2;
   qgemm_tc_kernel<<<(unsigned)(2 * (items < pairs ? items : pairs)), TC_THREADS, TC_SMEM, st>>>(ta, tb, p);
   OMQ_LAUNCH_CHECK();

@@ -289,12 +289,8 @@ omq_status norm_run(cudaStream_t st, const NormArgs& a) {
   auto kern = rmsnorm_quant_kernel<XB, RB, V, MAX_THREADS, MIN_CTAS, ST>;
   const int smem = ST ? a.C * ((XB ? 2 : 4) + (a.R ? (RB ? 2 : 4) : 0)) : 0;
   if (ST) {
-    static bool set = false;
-    if (!set) {
-      if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * V * MAX_THREADS * 8) != cudaSuccess)
-        return OMQ_ERR_CUDA;
-      set = true;
-    }
+    static std::atomic<uint64_t> allowed{0};
+    OMQ_TRY(omq_allow_smem(allowed, kern, 8 * V * MAX_THREADS * 8));
   }
   const int nt = ((a.C / 8 + V - 1) / V + 31) / 32 * 32;
   int per = 1;
