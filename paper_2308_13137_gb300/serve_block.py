@@ -38,7 +38,7 @@ class ServedBlock:
     def __init__(self, shape, packed, wbits: int, abits: int = 8, device: str = "cuda"):
         if not 2 <= wbits <= 8 or not 2 <= abits <= 8:
             raise ValueError("wbits, abits: 2 to 8")
-        self.shape, self.abits = shape, abits
+        self.shape, self.abits, self.device = shape, abits, device
         dev = lambda t: t.to(device).contiguous()  # noqa: E731
         self.w = {}
         for k in ("qkv", "o", "gu", "d"):
@@ -58,9 +58,9 @@ class ServedBlock:
         return cls(st.shape, st.fold_pack(), st.wbits, abits, st.device)
 
     def cache(self, B: int, max_tokens: int, page: int = 64) -> serve.KVCache:
-        """A cache of B sequences of up to max_tokens tokens, its pages in order."""
+        """A cache of B sequences of up to max_tokens tokens on the block's device, its pages in order."""
         per = -(-max_tokens // page)
-        c = serve.KVCache.empty(B * per, self.shape.n_kv, page, B, per)
+        c = serve.KVCache.empty(B * per, self.shape.n_kv, page, B, per, device=self.device)
         c.table.copy_(torch.arange(B * per, dtype=I32).view(B, per))
         return c
 

@@ -42,3 +42,15 @@ def test_every_kernel_reports_to_the_cache(monkeypatch):
     _block().forward(torch.zeros(3, 256), cache, None)
     assert len(seen) == 4 and all(s is status for s in seen)
     assert words == [status.data_ptr()] * 2
+
+
+def test_the_cache_lies_on_the_blocks_device(monkeypatch):
+    asked = []
+
+    def empty(n_pages, n_kv, page, B, max_pages, device="cuda"):
+        asked.append(device)
+        return types.SimpleNamespace(table=torch.zeros(B, max_pages, dtype=I32))
+
+    monkeypatch.setattr(serve.KVCache, "empty", empty)
+    _block("cpu").cache(2, 100)
+    assert [str(d) for d in asked] == ["cpu"]
