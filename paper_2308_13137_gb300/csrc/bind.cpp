@@ -3,9 +3,9 @@
 // A decode step makes a handful of these calls per layer, each a few microseconds of GPU time, so the
 // checks and the marshalling of one call have to cost about one: here they do (a ctypes call with the same
 // checks in Python takes 10 to 15).  Every function returns the omq_status; a tensor that does not fit is a
-// ValueError and nothing is launched.  Work goes to the current stream of the tensors' device; a
-// workspace comes from torch's caching allocator on that stream and is handed back when the call
-// returns, in stream order.
+// ValueError, a workspace for which there is no room a torch.OutOfMemoryError, and nothing is launched.  Work
+// goes to the current stream of the tensors' device; a workspace comes from torch's caching allocator on that
+// stream and is handed back when the call returns, in stream order.
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -253,6 +253,12 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong((long)s);
   } catch (const Bad& e) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, e.what.c_str());
+  } catch (const c10::OutOfMemoryError& e) {       // as torch's own allocations report it
+    PyObject* torch = PyImport_ImportModule("torch");
+    PyObject* kind = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+    if (kind) PyErr_SetString(kind, e.what_without_backtrace());
+    Py_XDECREF(kind);
+    Py_XDECREF(torch);
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   }

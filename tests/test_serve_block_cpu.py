@@ -1,6 +1,8 @@
 """ServedBlock's host side, without a GPU: which arguments its calls receive."""
+import os
 import types
 
+import pytest
 import torch
 
 from paper_2308_13137_gb300 import _lib, serve
@@ -54,3 +56,14 @@ def test_the_cache_lies_on_the_blocks_device(monkeypatch):
     monkeypatch.setattr(serve.KVCache, "empty", empty)
     _block("cpu").cache(2, 100)
     assert [str(d) for d in asked] == ["cpu"]
+
+
+@pytest.mark.skipif(not os.path.exists(_lib.LIB_PATH), reason="libomq.so not built")
+def test_the_module_of_the_calls_loads():
+    """Every symbol that the compiled module needs is exported by what it links (no device is touched)."""
+    bind = serve._load_bind()
+    assert all(hasattr(bind, f) for f in ("rmsnorm_quant", "qgemm", "kv_append", "kv_attention"))
+    with pytest.raises(TypeError):
+        bind.qgemm(None)
+    with pytest.raises(ValueError):
+        bind.qgemm(*[None] * 9)

@@ -90,3 +90,25 @@ def test_a_prompt_of_many_row_tiles(cuda_lib):
     # weights in fp16, the output in bf16
     assert bool(((got - O).abs() <= 1.5 * 2.0 ** -11 * top[..., None] + 2.0 ** -8 * O.abs()).all())
     assert bool(((lse[-held:].double() - L).abs() <= 1e-4).all())
+
+
+def test_a_workspace_that_does_not_fit(cuda_lib):
+    """A torch.OutOfMemoryError, which a serving loop catches to make room; nothing is launched."""
+    from paper_2308_13137_gb300 import _lib, serve
+    M, N, K = 2048, 264, 65536
+    a, w, ah, wh, out = _new(U8, M, K), _new(U8, N, K), _new(F32, M), _new(F32, N), _new(F32, M, N)
+    assert _lib.omq_qgemm_i8_workspace_size(M, N, K) >= 2 * M * K
+    serve._load_bind()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    before = _lib.omq_launch_count()
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + M * K) / total)
+    try:
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            serve.qgemm(a, ah, None, w, wh, None, out=out)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert _lib.omq_launch_count() == before
+    serve.qgemm(a, ah, None, w, wh, None, out=out)
+    assert bool((out == 0).all())
