@@ -405,13 +405,6 @@ def omq_step_advance(step_dev, stream=None):
     check("omq_step_advance", lib().omq_step_advance(stream_handle(stream), ptr(step_dev)))
 
 
-def omq_rmsnorm_quant(T, C, X, x_dtype, ldx, R, H, r_dtype, ldr, gain, bias, rms_eps, codes, Xq, h, z, cfg,
-                      stream=None):
-    check("omq_rmsnorm_quant", lib().omq_rmsnorm_quant(
-        stream_handle(stream), T, C, row_ptr(X), x_dtype, ldx, row_ptr(R), row_ptr(H), r_dtype, ldr, ptr(gain), ptr(bias),
-        rms_eps, ptr(codes), ptr(Xq), ptr(h), ptr(z), ctypes.byref(cfg)))
-
-
 def omq_qgemm_i8_workspace_size(M, N, K) -> int:
     return lib().omq_qgemm_i8_workspace_size(M, N, K)
 
@@ -434,23 +427,8 @@ def omq_rope_table(n_pos, theta, out, stream=None):
     check("omq_rope_table", lib().omq_rope_table(stream_handle(stream), n_pos, theta, ptr(out)))
 
 
-def omq_kv_append(cache, total_q, max_q, cu_q, n_heads, QKV, dtype, ld, rope, n_pos, sa, Qo, ldq, Ko, Vo, ldkv,
-                  dev_status=None, stream=None):
-    check("omq_kv_append", lib().omq_kv_append(
-        stream_handle(stream), ctypes.byref(cache), total_q, max_q, ptr(cu_q), n_heads, row_ptr(QKV), dtype, ld,
-        ptr(rope), n_pos, ptr(sa), row_ptr(Qo), ldq, row_ptr(Ko), row_ptr(Vo), ldkv, ptr(dev_status)))
-
-
 def omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) -> int:
     return lib().omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv)
-
-
-def omq_kv_attention(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
-                     dev_status=None, stream=None):
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    check("omq_kv_attention", lib().omq_kv_attention(
-        stream_handle(stream), ctypes.byref(cache), total_q, max_q, ptr(cu_q), max_kv, n_heads, row_ptr(Q), ldq,
-        row_ptr(Of), row_ptr(Ob), ldo, ptr(lse), ptr(workspace), ws_bytes, ptr(dev_status)))
 
 
 def omq_stream_status(dev_status, stream=None) -> int:

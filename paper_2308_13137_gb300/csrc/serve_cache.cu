@@ -28,7 +28,7 @@ struct AppendArgs {
   const void* QKV; int64_t ld;
   const float2* rope; int n_pos; const float* sa;
   __nv_bfloat16* Qo; int64_t ldq; __nv_bfloat16 *Ko, *Vo; int64_t ldkv;
-  int kv_units, npg;
+  int kv_units;
   int32_t* status;
 };
 
@@ -238,9 +238,9 @@ omq_status omq_kv_append(omq_stream_t stream, const omq_kv_cache* cache, int32_t
                   omq_aligned16(Vo),
               OMQ_ERR_ALIGN);
   AppendArgs a{*cache, total_q, max_q, cu_q, n_heads, QKV, ld, (const float2*)rope, n_pos, sa, (__nv_bfloat16*)Qo, ldq,
-               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, 0, dev_status};
-  a.npg = (max_q + cache->page - 2) / cache->page + 1;       // pages that max_q tokens can touch
-  const int64_t kv_units = 2ll * a.npg * cache->n_kv;
+               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, dev_status};
+  const int64_t pages = ((int64_t)max_q + cache->page - 2) / cache->page + 1;    // that max_q tokens can touch
+  const int64_t kv_units = 2 * pages * cache->n_kv;
   const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * GRP - 1) / (QPASS * GRP);
   OMQ_REQUIRE(kv_units + q_units < (1ll << 31), OMQ_ERR_SHAPE);
   a.kv_units = (int)kv_units;
