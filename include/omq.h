@@ -500,11 +500,11 @@ omq_status omq_selftest_qgemm_wait(omq_stream_t stream, int64_t M, int64_t N, in
  * one sequence for every KV head, with one scale per (page, head), not negative: the value is
  * (code - 128) scale.
  * Sequence b holds kv_len[b] tokens (those of the current call included); token j lies in page
- * page_table[b, j / page], slot j % page.  Tokens beyond kv_len and table entries beyond the last page are
- * never read.  All pointers device, owned by the caller; offsets are 64-bit.  Page ids and lengths are
- * checked on the device: one outside the pool, the table or the arguments' bounds sets
- * OMQ_ERR_INVALID_ARG in dev_status, and the sequence (or page) is skipped: nothing of it is read or
- * written in the pool. */
+ * page_table[b, j / page], slot j % page.  Table entries beyond the last page are never read; slots beyond
+ * kv_len may be copied with the tokens of their page (whole groups of 16 or 64 slots), and have no effect.
+ * All pointers device, owned by the caller; offsets are 64-bit.  Page ids and lengths are checked on the
+ * device: one outside the pool, the table or the arguments' bounds sets OMQ_ERR_INVALID_ARG in
+ * dev_status, and the sequence (or page) is skipped: nothing of it is read or written in the pool. */
 typedef struct {
   uint8_t* k; uint8_t* v;            /* [n_pages, n_kv, page, 128] codes */
   float* k_scale; float* v_scale;    /* [n_pages, n_kv] */
@@ -537,9 +537,11 @@ omq_status omq_kv_append(omq_stream_t stream, const omq_kv_cache* cache, int32_t
 /* Causal attention of every sequence's newest tokens over its cache: O = softmax(q k^T / sqrt(128)) v.
  *   Rows as in omq_kv_append (cu_q, max_q, total_q); row i of sequence b sees the keys
  *   j <= kv_len[b] - rows + i; query head h reads KV head h / (n_heads / n_kv).
- *   max_kv: host bound of kv_len.  Q [total_q, n_heads*128] bf16, row stride ldq.
+ *   max_kv: host bound of kv_len; the work is cut by it, so a bound far above the lengths costs time.  Q [total_q, n_heads*128] bf16, row stride ldq.
  *   Of fp32 and / or Ob bf16 [total_q, n_heads*128], row stride ldo; lse [total_q, n_heads] fp32 (NULL =
  *   skip): log2 of the sum of 2^s, s = q.k log2(e) / sqrt(128).  A row that sees no key: O = 0, lse = -inf.
+ *   The weights 2^(s - lse) times a page's V scale are rounded to fp16, 2^-11 relative, also for fp32 output: an
+ *   output is within 2^-11 of the largest |v| that the row sees; all else is fp32.
  * workspace: omq_kv_attention_workspace_size bytes (may be 0, then NULL is allowed). */
 omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
                             const int32_t* cu_q, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq,

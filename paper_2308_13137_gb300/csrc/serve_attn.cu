@@ -17,12 +17,14 @@
 // minus 1152.  Channels are numbered inside the products so that a thread's operand values are 16 consecutive
 // bytes of the page; row g of a product is token g ^ ((g & 1) << 2) of its eight, which puts the eight
 // lanes of every load phase, of K and of V, on eight distinct 16-byte bank groups.
-// Measured: 4 x 131072 tokens, 8 rows on each of 8 KV heads, 136 us, 6.0 TB/s; 16 x 4096 tokens, one row on each of
-// 32 heads, 65 us, 5.3 TB/s; one sequence of 2048 tokens 11 us, of which 7 are the two launches and the first loads.
+// Measured: 4 sequences of 62108 to 131072 tokens (400 K in all), 8 rows on each of 8 KV heads, 136 us, 6.0 TB/s; 16
+// of up to 4096 tokens, one row on each of 32 heads, 66 us, 5.2 TB/s; one sequence of 2048 tokens 11 us, of which 7
+// are the two launches and the first loads.  (Here and below "n x t tokens" are n sequences between t / 4 and t long.)
 //
-// Precision: the codes are exact; q (bf16) is exact after a power-of-two scale per row that puts
-// its largest value in [2^13, 2^14); scores, sums and accumulators are fp32.  The weight of a token,
-// p sv, is rounded to fp16 against a reference m + d near the largest log2(p sv), so that a weight keeps 11
+// Precision: the codes are exact; q (bf16) is fp16 after a power-of-two scale per row that puts
+// its largest value in [2^13, 2^14): exact but for elements 2^-30 of that and less, whose last bits go; scores,
+// sums and accumulators are fp32.  The weight of a token, p sv, is rounded to fp16 (the products' operand, 2^-11
+// relative, whatever the output's type) against a reference m + d near the largest log2(p sv), so that a weight keeps 11
 // bits down to 2^-22 of the largest; p's own sum stays fp32 against its own reference m (V's scales
 // differ by page, so the two references differ).  A reference moves, and the accumulator with it,
 // only when a score passes it by more than 2^7: few tiles do, and the others need no maximum across

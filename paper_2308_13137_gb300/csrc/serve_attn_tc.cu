@@ -17,7 +17,7 @@
 //           MN-major, both from [half][64 tokens][128 bytes] swizzled tiles
 // Warps without a row of the call do not take part.  Bound: the latency of a tile's way through the
 // softmax threads, 1700 cycles per tile and group with 64 exponentials each (half of them in the waits and the
-// fences around the exponentials), where the tile's 16 KB come from HBM in 700: 8 x 8192 tokens, 128 rows on
+// fences around the exponentials), where the tile's 16 KB come from HBM in 700: 8 sequences of up to 8192 tokens, 128 rows on
 // each of 8 KV heads, 67 us, 0.52 PFLOP/s, 1.4 TB/s.
 #include "serve_attn.cuh"
 

@@ -5,7 +5,7 @@
 // takes their largest magnitude over the block, settles the scale, rounds the older codes of the page
 // again where the scale grew, and writes the new ones; so no value is read twice and no two CTAs
 // touch one scale.  The other CTAs of the launch turn the q rows.  The bound is HBM for prompts
-// (rows in, q / k / v values and codes out): 2048 rows of 32 + 2 x 32 bf16 heads 38.5 us, 4.4 TB/s; 64 single
+// (rows in, q / k / v values and codes out): 2048 rows of 32 + 2 x 32 fp32 heads 38.5 us, 4.4 TB/s; 64 single
 // tokens of 32 + 2 x 8 heads 7.6 us, of which 4 us are the launch and the chain length -> page -> scale -> rows.
 // Eight threads to a token: with sixteen, of half the channels and 8-byte stores, the rotary loads and the
 // addresses were a larger part of the instructions (44.0 us; fp32 pages of 128 tokens 63.0 against 53.1 us).

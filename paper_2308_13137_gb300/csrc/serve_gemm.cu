@@ -78,8 +78,8 @@ __device__ __forceinline__ float finish(int acc, long long za, long long zb, int
 //           and proxy fence overlap the other's work.  They also form the rows' code sums for the
 //           zero points
 // The tensor memory holds two accumulators, so the drain overlaps the MMAs of the next 1024 steps.
-// What bounds it is the hand-offs between the roles, then the tensor rate: 2048 x 22016 x 4096 in 274 us,
-// 1.35 PFLOP/s; the drain's last stores, about a tenth, are not covered.
+// What bounds it is the hand-offs between the roles, then the tensor rate: 2048 x 22016 x 4096 in 255 to 260 us,
+// 1.43 PFLOP/s; its 688 tiles are nine rounds of the 76 pairs and four tiles, which take a tenth round.
 constexpr int BM = 128, BN = 256, BK = 128;
 // Ring depths: raw weight tiles (they come from HBM), operand stages (A | converted B).  Stages of 128
 // codes: the signals between the roles, not the work, set the pace (2048 x 22016 x 4096: 356 us with 64 and 277
@@ -542,8 +542,9 @@ __global__ void __launch_bounds__(256) qgemm_join_kernel(const QgemmArgs p) {
 // products so that a thread's operand values are 16 consecutive codes of its row; row 8 i + g of a product
 // is tile row 8 i + (g % 2) 4 + g / 2, so that the eight lanes of a load phase hit eight distinct 16-byte
 // bank groups of the 128-byte swizzle.
-// Measured: 1 x 12288 x 4096 13.4 us, 17 x 5120 x 13824 22 us, 3.8 and 3.2 TB/s of weight codes; about 6 us are
-// the launch, the first tiles and the joining, the rest the read and, from 17 rows on, the conversion.
+// Measured: 1 x 12288 x 4096 (192 CTAs, no cluster) 13.4 us, 17 x 5120 x 13824 (clusters of 3) 22 us, 3.8 and 3.2 TB/s
+// of weight codes.  What is not the read is the start, the first tiles and the epilogue, about 6 us, and, from 17
+// rows on, the conversion.
 constexpr int FEW_WARPS = 8;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,

@@ -158,7 +158,7 @@ def kv_attention(cache: KVCache, q, n_heads: int, cu_q=None, max_q: Optional[int
                  out=None, out_dtype=BF16, lse=None):
     """Causal attention of the rows q [rows, n_heads*128] bf16 over the cache (omq_kv_attention): row i of a
     sequence sees every key up to its own token.  max_kv: a bound of kv_len (default: what the table can
-    hold).  lse [rows, n_heads] fp32 receives the base-2 log-sum-exp."""
+    hold); the work is cut by it, so give one near the lengths where the table is much longer.  lse [rows, n_heads] fp32 receives the base-2 log-sum-exp."""
     if out is None:
         out = torch.empty(q.shape[0], n_heads * HEAD_DIM, dtype=out_dtype, device=q.device)
     code = _calls.kv_attention(cache.address, q, n_heads, cu_q, max_q, cache.capacity if max_kv is None else max_kv, out, lse,
