@@ -93,22 +93,24 @@ def test_a_prompt_of_many_row_tiles(cuda_lib):
 
 
 def test_a_workspace_that_does_not_fit(cuda_lib):
-    """A torch.OutOfMemoryError, which a serving loop catches to make room; nothing is launched."""
+    """A torch.OutOfMemoryError, which a serving loop catches to make room; nothing is launched.  Partial results for
+    a bound of 2^30 tokens and 1024 heads are 34 GB, the process is held to 14."""
     from paper_2308_13137_gb300 import _lib, serve
-    M, N, K = 2048, 264, 65536
-    a, w, ah, wh, out = _new(U8, M, K), _new(U8, N, K), _new(F32, M), _new(F32, N), _new(F32, M, N)
-    assert _lib.omq_qgemm_i8_workspace_size(M, N, K) >= 2 * M * K
+    heads, most = 1024, 1 << 30
+    c = serve.KVCache.empty(1, heads, 16, 1, 1)
+    c.kv_len.fill_(1)
+    q, out = _new(BF16, 1, heads * 128), _new(BF16, 1, heads * 128)
+    assert _lib.omq_kv_attention_workspace_size(1, 1, 1, most, heads, heads) > 30e9
     serve._load_bind()
-    torch.cuda.synchronize()
-    torch.cuda.empty_cache()
-    total = torch.cuda.get_device_properties(0).total_memory
     before = _lib.omq_launch_count()
-    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + M * K) / total)
+    torch.cuda.set_per_process_memory_fraction(14e9 / torch.cuda.get_device_properties(0).total_memory)
     try:
         with pytest.raises(torch.cuda.OutOfMemoryError):
-            serve.qgemm(a, ah, None, w, wh, None, out=out)
+            serve.kv_attention(c, q, heads, max_kv=most, out=out)
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert _lib.omq_launch_count() == before
-    serve.qgemm(a, ah, None, w, wh, None, out=out)
+    out.fill_(1)
+    serve.kv_attention(c, q, heads, max_kv=16, out=out)
+    c.check()
     assert bool((out == 0).all())
