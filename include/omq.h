@@ -550,6 +550,74 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
 size_t omq_kv_attention_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                        int32_t n_kv);
 
+/* ------------------------------------------------------------------------------------------
+ * Drafted tokens.  A step that checks drafts gives every sequence a tree of new rows: row 0 is the newest
+ * accepted token (its keys and values are not in the cache yet), every other row a drafted token below its
+ * parent.  One step is
+ *   omq_draft_tree -> (per layer) omq_kv_append_tree -> omq_kv_attention_tree -> ... -> omq_verify_drafts ->
+ *   omq_kv_keep (every layer's cache in one call)
+ * and the sequence's length is then kv_len - rows + count.  Rows of a sequence as in omq_kv_append (cu_q, max_q,
+ * total_q); at most 1024 rows of a sequence in omq_draft_tree and omq_verify_drafts.  Rows that belong to no sequence
+ * are left as they are.
+ * ------------------------------------------------------------------------------------------ */
+
+/* What the nodes of the trees see.  parent [total_q] int32: row within the sequence, before the child's own; -1 at a
+ * root.  depth [total_q] int32: number of ancestors.  seen [total_q, words]: bit j (of word j / 32) of a row is set
+ * where row j of the sequence is the row itself or an ancestor; words >= ceil(max_q / 32), the rest zero.  A
+ * parent outside [-1, row) sets OMQ_ERR_INVALID_ARG in dev_status and the row counts as a root. */
+omq_status omq_draft_tree(omq_stream_t stream, int32_t B, int32_t total_q, int32_t max_q, const int32_t* cu_q,
+                          const int32_t* parent, int32_t* depth, uint32_t* seen, int32_t words, int32_t* dev_status);
+
+/* omq_kv_append for rows that are a tree: row i lies in slot kv_len - rows + i as there, its rotary position is
+ * kv_len - rows + depth[i].  A position outside the rope table sets OMQ_ERR_INVALID_ARG and the root's is taken. */
+omq_status omq_kv_append_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                              const int32_t* cu_q, const int32_t* depth, int32_t n_heads, const void* QKV, int32_t dtype,
+                              int64_t ld, const float* rope, int32_t n_pos, const float* sa, void* Qo, int64_t ldq, void* Ko,
+                              void* Vo, int64_t ldkv, int32_t* dev_status);
+
+/* omq_kv_attention with other visible keys: row i of a sequence sees every key j < kv_len - rows, and key
+ * kv_len - rows + k where bit k of its words in seen [total_q, words] is set (any bits, not only a tree's; those from
+ * the sequence's number of rows on count for nothing).  All else as there. */
+omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                                 const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
+                                 const void* Q, int64_t ldq, float* Of, void* Ob, int64_t ldo, float* lse, void* workspace,
+                                 size_t ws_bytes, int32_t* dev_status);
+size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                            int32_t n_kv);
+
+/* Drafted tokens against the target's probabilities, from given random numbers; the outcome is distributed as
+ * tokens drawn from the target.  The walk starts at row 0.  At a row with weights R (first its row of P) and T = 1,
+ * its children are tested in order: child c with token x = tokens[c] is accepted, and the walk goes on there, when
+ *   u[c] T q(x) < R(x),
+ * else R becomes max(R - T q, 0) and T its sum.  q is the row's row of Q, from which its children were drawn one by
+ * one.  Q NULL: the children were chosen, not drawn; then q(x) = 1, and a rejection sets R(x) to 0 and takes it
+ * from T.  Where no child is left (or the path has `steps` rows, whose last is not tested further) the new token is the first
+ * whose running sum of R passes u[row 0] times the whole (of P where R is zero throughout).
+ *   P, Q [total_q, V] of `dtype`, row strides ldp, ldq: rows that sum to one (the target's as if they did: T starts as 1);
+ *   values below 0 and NaN count as 0, above 1 as 1.  tokens [total_q] (row 0's is not read), u [total_q] fp32 in
+ *   [0, 1) (outside: the nearest; NaN 0).
+ *   out_path [B, steps]: the accepted rows within the sequence, row 0 first, -1 behind; out_count [B]: their number (0
+ *   for a sequence without rows); out_tokens [B, steps]: the accepted tokens and, at count - 1, the new one, -1 behind.
+ * Sums are exact (64-bit fixed point, terms truncated to 2^-60): the same numbers on every run and split.
+ * A parent or token out of range sets OMQ_ERR_INVALID_ARG in dev_status, and that row is nobody's child; a new token for
+ * which no weight is left in P either sets it and is 0.  V at most 2^20. */
+omq_status omq_verify_drafts(omq_stream_t stream, int32_t B, int32_t total_q, int32_t max_q, const int32_t* cu_q,
+                             const int32_t* parent, const int32_t* tokens, int64_t V, const void* P, const void* Q,
+                             int32_t dtype, int64_t ldp, int64_t ldq, const float* u, int32_t steps, int32_t* out_tokens,
+                             int32_t* out_path, int32_t* out_count, int32_t* dev_status);
+
+/* The accepted rows to the front of a sequence's newest tokens: token kv_len - rows + path[b, j] goes to place
+ * kv_len - rows + j, for j < count[b]; path strictly increasing (as omq_verify_drafts gives it).  kv_len itself is not
+ * changed.  Per page and head: scale = max(scale before, max |incoming value| / 127) over the tokens that come from
+ * other pages; where it grows, all codes of the page become 128 + round((code - 128) before / after); a token that
+ * moves gets 128 + round((code - 128) scale of its old page / scale) (one fp32 rounding each), clamped to 127 steps.
+ *   caches: n_caches handles (host array), one per layer, of equal B, n_kv and page, each named once; path [B, steps] and
+ *   count [B] int32, the same for all.  dev_status: n_caches status words (host array of device pointers; may be NULL).
+ * A count or path out of range sets OMQ_ERR_INVALID_ARG and the sequence is skipped, a page id out of range its page. */
+omq_status omq_kv_keep(omq_stream_t stream, const omq_kv_cache* const* caches, int32_t* const* dev_status, int32_t n_caches,
+                       int32_t total_q, int32_t max_q, const int32_t* cu_q, const int32_t* path, int32_t steps,
+                       const int32_t* count);
+
 /* Reads the device status word written by kernels (synchronises `stream`).  *host_out receives
  * the word (0 = ok); the return value is OMQ_OK or OMQ_ERR_CUDA if the copy failed. */
 omq_status omq_stream_status(omq_stream_t stream, const int32_t* dev_status, int32_t* host_out);

@@ -134,6 +134,12 @@ _SIGS = {
     "omq_kv_append": (I32, [P, P, I32, I32, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
     "omq_kv_attention": (I32, [P, P, I32, I32, P, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
     "omq_kv_attention_workspace_size": (SZ, [I32, I32, I32, I32, I32, I32]),
+    "omq_draft_tree": (I32, [P, I32, I32, I32, P, P, P, P, I32, P]),
+    "omq_kv_append_tree": (I32, [P, P, I32, I32, P, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
+    "omq_kv_attention_tree": (I32, [P, P, I32, I32, P, P, I32, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
+    "omq_kv_attention_tree_workspace_size": (SZ, [I32, I32, I32, I32, I32, I32]),
+    "omq_verify_drafts": (I32, [P, I32, I32, I32, P, P, P, I64, P, P, I32, I64, I64, P, I32, P, P, P, P]),
+    "omq_kv_keep": (I32, [P, P, P, I32, I32, I32, P, P, I32, P]),
     "omq_stream_status": (I32, [P, P, POINTER(c_int32)]),
     "omq_status_string": (c_char_p, [I32]),
     "omq_version": (I32, []),
@@ -429,6 +435,10 @@ def omq_rope_table(n_pos, theta, out, stream=None):
 
 def omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) -> int:
     return lib().omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv)
+
+
+def omq_kv_attention_tree_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) -> int:
+    return lib().omq_kv_attention_tree_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv)
 
 
 def omq_stream_status(dev_status, stream=None) -> int:

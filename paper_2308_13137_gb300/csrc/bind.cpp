@@ -13,6 +13,7 @@
 
 #include <exception>
 #include <string>
+#include <vector>
 
 #include "omq.h"
 
@@ -184,8 +185,9 @@ Rows row_map(Call& c, const omq_kv_cache* kv, int64_t rows, PyObject* cu, PyObje
   return r;
 }
 
-// address of the omq_kv_cache, qkv, rope, n_heads, cu_q, max_q, sa, q_out, k_out, v_out, status
-omq_status kv_append(PyObject* const* a) {
+// address of the omq_kv_cache, qkv, rope, n_heads, cu_q, max_q, sa, q_out, k_out, v_out, status; with a tree: depth
+template <bool TREE>
+omq_status append(PyObject* const* a) {
   Call c;
   const omq_kv_cache* kv = (const omq_kv_cache*)PyLong_AsVoidPtr(a[0]);
   if (!kv) throw Bad{PyErr_Occurred() ? "" : "cache: required"};
@@ -210,14 +212,31 @@ omq_status kv_append(PyObject* const* a) {
   if (q->scalar_type() != at::kBFloat16 || (k && (k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16)))
     throw Bad{"q_out, k_out, v_out: bfloat16"};
   int32_t* status = word(a[10], "status", c);
+  const int32_t* depth = TREE ? (const int32_t*)c.vec(a[11], "depth", at::kInt, n, true) : nullptr;
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+  if (TREE)
+    return omq_kv_append_tree(c.stream(), kv, r.total, r.max_q, r.cu, depth, heads, x->data_ptr(), c.float_type(*x, "qkv"), ld,
+                              (const float*)rope->data_ptr(), (int32_t)rope->size(0), sa, q->data_ptr(), ldq,
+                              k ? k->data_ptr() : nullptr, v ? v->data_ptr() : nullptr, ldk, status);
   return omq_kv_append(c.stream(), kv, r.total, r.max_q, r.cu, heads, x->data_ptr(), c.float_type(*x, "qkv"), ld,
                        (const float*)rope->data_ptr(), (int32_t)rope->size(0), sa, q->data_ptr(), ldq,
                        k ? k->data_ptr() : nullptr, v ? v->data_ptr() : nullptr, ldk, status);
 }
 
-// address of the omq_kv_cache, q, n_heads, cu_q, max_q, max_kv, out, lse, status
-omq_status kv_attention(PyObject* const* a) {
+// rows of draft trees: [n, words], words enough for max_q bits
+const uint32_t* bit_rows(Call& c, PyObject* o, int64_t n, int64_t max_q, int32_t* words) {
+  const at::Tensor* t = tensor(o, "seen");
+  if (!t) throw Bad{"seen: required"};
+  c.place(*t, "seen");
+  if (t->dim() != 2 || t->size(0) != n || t->size(1) * 32 < max_q || t->size(1) > 1024 || t->scalar_type() != at::kInt || !t->is_contiguous())
+    throw Bad{"seen: contiguous int32 [rows, words] with a bit for each of max_q rows"};
+  *words = (int32_t)t->size(1);
+  return (const uint32_t*)t->data_ptr();
+}
+
+// address of the omq_kv_cache, q, n_heads, cu_q, max_q, max_kv, out, lse, status; with a tree: seen
+template <bool TREE>
+omq_status attention(PyObject* const* a) {
   Call c;
   const omq_kv_cache* kv = (const omq_kv_cache*)PyLong_AsVoidPtr(a[0]);
   if (!kv) throw Bad{PyErr_Occurred() ? "" : "cache: required"};
@@ -236,10 +255,97 @@ omq_status kv_attention(PyObject* const* a) {
   int32_t* status = word(a[8], "status", c);
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
   const omq_stream_t s = c.stream();
-  const size_t need = omq_kv_attention_workspace_size(kv->B, r.total, r.max_q, max_kv, heads, kv->n_kv);
+  int32_t words = 0;
+  const uint32_t* seen = TREE ? bit_rows(c, a[9], n, r.max_q, &words) : nullptr;
+  const size_t need = (TREE ? omq_kv_attention_tree_workspace_size : omq_kv_attention_workspace_size)(kv->B, r.total, r.max_q, max_kv,
+                                                                                                       heads, kv->n_kv);
   const Scratch ws(need, s);
+  if (TREE)
+    return omq_kv_attention_tree(s, kv, r.total, r.max_q, r.cu, seen, words, max_kv, heads, q->data_ptr(), ldq,
+                                 f32 ? (float*)o->data_ptr() : nullptr, f32 ? nullptr : o->data_ptr(), ldo, lse, ws.p, need, status);
   return omq_kv_attention(s, kv, r.total, r.max_q, r.cu, max_kv, heads, q->data_ptr(), ldq,
                           f32 ? (float*)o->data_ptr() : nullptr, f32 ? nullptr : o->data_ptr(), ldo, lse, ws.p, need, status);
+}
+
+// B of a call on trees: cu_q has it, else the rows are max_q each
+int32_t sequences(PyObject* cu, int64_t rows, int64_t max_q) {
+  if (max_q <= 0 || max_q > INT32_MAX || rows > INT32_MAX) throw Bad{"max_q, rows: out of range"};
+  if (cu == Py_None) {
+    if (rows % max_q != 0) throw Bad{"rows: max_q for every sequence without cu_q"};
+    return (int32_t)(rows / max_q);
+  }
+  const at::Tensor* t = tensor(cu, "cu_q");
+  if (t->numel() < 2 || t->numel() > INT32_MAX) throw Bad{"cu_q: [sequences + 1]"};
+  return (int32_t)(t->numel() - 1);
+}
+
+// parent, cu_q, max_q, depth, seen, status
+omq_status draft_tree(PyObject* const* a) {
+  Call c;
+  const at::Tensor* p = tensor(a[0], "parent");
+  if (!p) throw Bad{"parent: required"};
+  const int64_t n = p->numel();
+  const int32_t max_q = integer32(a[2], "max_q"), B = sequences(a[1], n, max_q);
+  const int32_t* parent = (const int32_t*)c.vec(a[0], "parent", at::kInt, n);
+  const int32_t* cu = (const int32_t*)c.vec(a[1], "cu_q", at::kInt, (int64_t)B + 1);
+  int32_t* depth = (int32_t*)c.vec(a[3], "depth", at::kInt, n, true);
+  int32_t words = 0;
+  uint32_t* seen = (uint32_t*)bit_rows(c, a[4], n, max_q, &words);
+  int32_t* status = word(a[5], "status", c);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+  return omq_draft_tree(c.stream(), B, (int32_t)n, max_q, cu, parent, depth, seen, words, status);
+}
+
+// parent, cu_q, max_q, tokens, probs, draft_probs, u, tokens out, path, count, status
+omq_status verify_drafts(PyObject* const* a) {
+  Call c;
+  int64_t ldp = 0, ldq = 0, ldt = 0, ldo = 0;
+  const at::Tensor* P = c.rows(a[4], "probs", -1, -1, &ldp);
+  if (!P) throw Bad{"probs: required"};
+  const int64_t n = P->size(0), V = P->size(1);
+  const int32_t type = c.float_type(*P, "probs");
+  const at::Tensor* Q = c.rows(a[5], "draft_probs", n, V, &ldq);
+  if (Q && c.float_type(*Q, "draft_probs") != type) throw Bad{"draft_probs: the type of probs"};
+  const int32_t max_q = integer32(a[2], "max_q"), B = sequences(a[1], n, max_q);
+  const int32_t* cu = (const int32_t*)c.vec(a[1], "cu_q", at::kInt, (int64_t)B + 1);
+  const int32_t* parent = (const int32_t*)c.vec(a[0], "parent", at::kInt, n, true);
+  const int32_t* tokens = (const int32_t*)c.vec(a[3], "tokens", at::kInt, n, true);
+  const float* u = (const float*)c.vec(a[6], "u", at::kFloat, n, true);
+  const at::Tensor* t = c.rows(a[7], "out.tokens", B, -1, &ldt);
+  if (!t || t->size(1) < 1 || t->size(1) > 1024) throw Bad{"out.tokens, out.path: int32 [sequences, steps], steps 1 to 1024"};
+  const int64_t steps = t->size(1);
+  const at::Tensor* path = c.rows(a[8], "out.path", B, steps, &ldo);
+  if (!path || t->scalar_type() != at::kInt || path->scalar_type() != at::kInt || !t->is_contiguous() || !path->is_contiguous())
+    throw Bad{"out.tokens, out.path: contiguous int32"};
+  int32_t* count = (int32_t*)c.vec(a[9], "out.count", at::kInt, B, true);
+  int32_t* status = word(a[10], "status", c);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+  return omq_verify_drafts(c.stream(), B, (int32_t)n, max_q, cu, parent, tokens, V, P->data_ptr(), Q ? Q->data_ptr() : nullptr, type,
+                           ldp, ldq, u, (int32_t)steps, (int32_t*)t->data_ptr(), (int32_t*)path->data_ptr(), count, status);
+}
+
+// tuple of cache addresses, tuple of their status words, rows, cu_q, max_q, path, count
+omq_status kv_keep(PyObject* const* a) {
+  Call c;
+  if (!PyTuple_Check(a[0]) || !PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[0]) != PyTuple_GET_SIZE(a[1]) || PyTuple_GET_SIZE(a[0]) < 1)
+    throw Bad{"caches: at least one"};
+  std::vector<const omq_kv_cache*> kv;
+  std::vector<int32_t*> status;
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[0]); ++i) {
+    kv.push_back((const omq_kv_cache*)PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[0], i)));
+    if (!kv.back()) throw Bad{PyErr_Occurred() ? "" : "cache: required"};
+    status.push_back(word(PyTuple_GET_ITEM(a[1], i), "status", c));
+  }
+  const int64_t n = integer(a[2]);
+  const Rows r = row_map(c, kv[0], n, a[3], a[4]);
+  const at::Tensor* path = tensor(a[5], "path");
+  if (!path || path->dim() != 2 || path->size(0) != kv[0]->B || path->size(1) > 1024 || path->scalar_type() != at::kInt || !path->is_contiguous())
+    throw Bad{"path: contiguous int32 [sequences, steps], steps at most 1024"};
+  c.place(*path, "path");
+  const int32_t* count = (const int32_t*)c.vec(a[6], "count", at::kInt, kv[0]->B, true);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+  return omq_kv_keep(c.stream(), kv.data(), status.data(), (int32_t)kv.size(), r.total, r.max_q, r.cu, (const int32_t*)path->data_ptr(),
+                     (int32_t)path->size(1), count);
 }
 
 template <omq_status (*F)(PyObject* const*), int N>
@@ -265,8 +371,16 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return nullptr;
 }
 
-#define ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ENTRY(rmsnorm_quant, 12), ENTRY(qgemm, 9), ENTRY(kv_append, 11), ENTRY(kv_attention, 9),
+#define ENTRY(name, f, n) {name, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {ENTRY("rmsnorm_quant", rmsnorm_quant, 12),
+                         ENTRY("qgemm", qgemm, 9),
+                         ENTRY("kv_append", append<false>, 11),
+                         ENTRY("kv_attention", attention<false>, 9),
+                         ENTRY("draft_tree", draft_tree, 6),
+                         ENTRY("kv_append_tree", append<true>, 12),
+                         ENTRY("kv_attention_tree", attention<true>, 10),
+                         ENTRY("verify_drafts", verify_drafts, 11),
+                         ENTRY("kv_keep", kv_keep, 7),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -74,7 +74,7 @@ struct Smem {
   static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12 + 1024; }
 };
 
-template <int NT>
+template <int NT, bool TREE>
 __global__ void __launch_bounds__(W * 32, 2)
     kv_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
   using S = Smem<NT>;
@@ -109,7 +109,8 @@ __global__ void __launch_bounds__(W * 32, 2)
   if (r0 >= R) return;
   const int start = s.len - s.nq;
   const int r_last = min(R, r0 + ROWS) - 1;
-  const int kv_end = max(0, min(s.len, start + r_last / rep + 1));   // keys that some row of the CTA sees
+  // keys that some row of the CTA sees
+  const int kv_end = TREE ? s.len : max(0, min(s.len, start + r_last / rep + 1));
   const int t_begin = split * a.chunk;
   const int t_end = min(kv_end, t_begin + a.chunk);
   if (split > 0 && t_begin >= kv_end) return;
@@ -135,7 +136,10 @@ __global__ void __launch_bounds__(W * 32, 2)
     qf[(nt * 8 + w) * 32 + q * 4 + t] = make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
     if (lane == 0) {
       qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
-      lims[r] = row < R ? min(s.len, start + row / rep + 1) : 0;
+      if (TREE)                              // at most 16 nodes: one word
+        lims[r] = row < R ? (int)attn_window(a.seen + (int64_t)(s.row0 + row / rep) * a.words, a.words, s.nq, 0) : 0;
+      else
+        lims[r] = row < R ? min(s.len, start + row / rep + 1) : 0;
     }
   }
   __syncthreads();
@@ -181,7 +185,13 @@ __global__ void __launch_bounds__(W * 32, 2)
 #pragma unroll
       for (int w = 0; w < 8; ++w) qr[NT == 1 ? w : 0] = qfw[w * 32];
     }
-    const int lim_min = __reduce_min_sync(0xffffffffu, lane < ROWS && r0 + lane < R ? lims[lane] : 0x7fffffff);
+    const int lim_min = TREE ? start : __reduce_min_sync(0xffffffffu, lane < ROWS && r0 + lane < R ? lims[lane] : 0x7fffffff);
+    // does a row see token t?  lim: its number of visible keys, or its nodes' bits
+    auto hidden = [&](int t, int lim) {
+      if (!TREE) return t >= lim;
+      const int node = t - start;
+      return node >= 0 && (node >= 32 || !(((uint32_t)lim >> node) & 1u));
+    };
     const int n_here = (min(ROWS, R - r0) + 7) >> 3;          // row tiles that hold rows
     const float2* f2 = reinterpret_cast<const float2*>(qs) + lt;
     const int2* lim2 = reinterpret_cast<const int2*>(lims) + lt;
@@ -236,7 +246,7 @@ __global__ void __launch_bounds__(W * 32, 2)
           const int2 lm = lim2[4 * nt];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t0 + row_k + 8 * (e >> 1) >= (e & 1 ? lm.y : lm.x)) x[e] = -INFINITY;
+            if (hidden(t0 + row_k + 8 * (e >> 1), e & 1 ? lm.y : lm.x)) x[e] = -INFINITY;
         }
         const float t0m = fmaxf(x[0], x[2]), t1m = fmaxf(x[1], x[3]);
         const float u0 = t0m - m[nt][0], u1 = t1m - m[nt][1];
@@ -274,7 +284,7 @@ __global__ void __launch_bounds__(W * 32, 2)
           const int2 lm = lim2[4 * nt];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t0 + row_k + 8 * (e >> 1) >= (e & 1 ? lm.y : lm.x)) pw[e] = 0.f;
+            if (hidden(t0 + row_k + 8 * (e >> 1), e & 1 ? lm.y : lm.x)) pw[e] = 0.f;
         }
         p0[nt] = transpose8x8(pack_half2(pw[0], pw[1]));
         p1[nt] = transpose8x8(pack_half2(pw[2], pw[3]));
@@ -388,7 +398,7 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   if (!s.ok || s.len > a.max_kv) s.len = 0;
   const int i = idx / a.n_heads, head = idx % a.n_heads;
   if (i >= s.nq) return;
-  const int seen = max(0, min(s.len, s.len - s.nq + i + 1));
+  const int seen = a.seen ? s.len : max(0, min(s.len, s.len - s.nq + i + 1));
   const int nv = (seen + a.chunk - 1) / a.chunk;
   const int64_t tok = s.row0 + i, at = (tok * a.n_heads + head) * a.n_split;
   float top = -INFINITY;
@@ -448,10 +458,10 @@ size_t plan_workspace(const Plan& p, int64_t total_q, int64_t n_heads) {
   return parts * HD * sizeof(float) + (parts * sizeof(float) + 255) / 256 * 256;
 }
 
-template <int NT>
+template <int NT, bool TREE>
 omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
   using S = Smem<NT>;
-  auto kern = kv_attention_kernel<NT>;
+  auto kern = kv_attention_kernel<NT, TREE>;
   static std::atomic<uint64_t> allowed{0};
   OMQ_TRY(omq_allow_smem(allowed, kern, S::bytes(ATTN_MAX_CHUNK, 16)));
   CUtensorMap tk, tv;
@@ -460,6 +470,39 @@ omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
     return OMQ_ERR_UNSUPPORTED;
   kern<<<dim3(a.n_split * a.c.n_kv * a.row_tiles, a.c.B), W * 32, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
   OMQ_LAUNCH_CHECK();
+  return OMQ_OK;
+}
+
+omq_status attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q,
+                     const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq, float* Of,
+                     void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes, int32_t* dev_status) {
+  OMQ_TRY(kv_check(cache, total_q, max_q, cu_q, n_heads));
+  OMQ_REQUIRE(Q && (Of || Ob), OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(max_kv > 0 && ldq >= (int64_t)n_heads * HD && ldo >= (int64_t)n_heads * HD, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(ldq % 8 == 0 && ldo % 8 == 0, OMQ_ERR_ALIGN);
+  OMQ_REQUIRE(omq_aligned16(Q) && omq_aligned16(Of) && omq_aligned16(Ob) && omq_aligned16(lse) &&
+                  omq_aligned16(workspace),
+              OMQ_ERR_ALIGN);
+  const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
+  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles * p.n_split < (1ll << 31), OMQ_ERR_SHAPE);
+  OMQ_REQUIRE((int64_t)cache->n_pages * cache->n_kv * cache->page < (1ll << 31), OMQ_ERR_SHAPE);   // TMA coordinates
+  const size_t need = plan_workspace(p, total_q, n_heads);
+  OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
+  AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
+             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status, seen, words};
+  if (p.n_split > 1) {
+    a.wo = (float*)workspace;
+    a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
+  }
+  cudaStream_t st = (cudaStream_t)stream;
+  OMQ_TRY(p.form == 8    ? (seen ? attn_launch<1, true>(st, a) : attn_launch<1, false>(st, a))
+          : p.form == 16 ? (seen ? attn_launch<2, true>(st, a) : attn_launch<2, false>(st, a))
+                         : attn_tc_launch(st, a));
+  if (p.n_split > 1) {
+    const int64_t pairs = (int64_t)max_q * n_heads;
+    kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
+    OMQ_LAUNCH_CHECK();
+  }
   return OMQ_OK;
 }
 
@@ -476,32 +519,24 @@ size_t omq_kv_attention_workspace_size(int32_t B, int32_t total_q, int32_t max_q
 omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
                             const int32_t* cu_q, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq, float* Of,
                             void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes, int32_t* dev_status) {
-  OMQ_TRY(kv_check(cache, total_q, max_q, cu_q, n_heads));
-  OMQ_REQUIRE(Q && (Of || Ob), OMQ_ERR_INVALID_ARG);
-  OMQ_REQUIRE(max_kv > 0 && ldq >= (int64_t)n_heads * HD && ldo >= (int64_t)n_heads * HD, OMQ_ERR_SHAPE);
-  OMQ_REQUIRE(ldq % 8 == 0 && ldo % 8 == 0, OMQ_ERR_ALIGN);
-  OMQ_REQUIRE(omq_aligned16(Q) && omq_aligned16(Of) && omq_aligned16(Ob) && omq_aligned16(lse) &&
-                  omq_aligned16(workspace),
-              OMQ_ERR_ALIGN);
-  const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
-  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles * p.n_split < (1ll << 31), OMQ_ERR_SHAPE);
-  OMQ_REQUIRE((int64_t)cache->n_pages * cache->n_kv * cache->page < (1ll << 31), OMQ_ERR_SHAPE);   // TMA coordinates
-  const size_t need = plan_workspace(p, total_q, n_heads);
-  OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
-  AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
-             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status};
-  if (p.n_split > 1) {
-    a.wo = (float*)workspace;
-    a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
-  }
-  cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY(p.form == 8 ? attn_launch<1>(st, a) : (p.form == 16 ? attn_launch<2>(st, a) : attn_tc_launch(st, a)));
-  if (p.n_split > 1) {
-    const int64_t pairs = (int64_t)max_q * n_heads;
-    kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
-    OMQ_LAUNCH_CHECK();
-  }
-  return OMQ_OK;
+  return attention(stream, cache, total_q, max_q, cu_q, nullptr, 0, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
+                   ws_bytes, dev_status);
+}
+
+size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
+                                            int32_t n_kv) {
+  return omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv);
+}
+
+omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                                 const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
+                                 const void* Q, int64_t ldq, float* Of, void* Ob, int64_t ldo, float* lse, void* workspace,
+                                 size_t ws_bytes, int32_t* dev_status) {
+  OMQ_REQUIRE(seen, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(max_q > 0 && words >= (max_q - 1) / 32 + 1, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(omq_aligned4(seen), OMQ_ERR_ALIGN);
+  return attention(stream, cache, total_q, max_q, cu_q, seen, words, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
+                   ws_bytes, dev_status);
 }
 
 }  // extern "C"

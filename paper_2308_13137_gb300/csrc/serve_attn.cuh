@@ -32,7 +32,23 @@ struct AttnArgs {
   float* wo; float* wl;                     // partial results of the splits (n_split > 1)
   int chunk, n_split, row_tiles;
   int32_t* status;
+  const uint32_t* seen; int words;          // draft trees: bits of the newest tokens that each row sees
 };
+
+// Draft trees: the newest tokens that a row sees, from node d of its sequence (d below zero: context, which every row
+// sees) on, as 64 bits.  bits: the row's words.
+__device__ __forceinline__ uint64_t attn_window(const uint32_t* bits, int words, int nq, int d) {
+  if (d <= -64) return ~0ull;
+  if (d >= nq) return 0ull;
+  auto word = [&](int w) { return w < words ? (uint64_t)__ldg(bits + w) : 0ull; };
+  uint64_t x;
+  const int w = max(d, 0) >> 5, s = max(d, 0) & 31;
+  x = (word(w) | word(w + 1) << 32) >> s;
+  if (s) x |= word(w + 2) << (64 - s);
+  const int left = nq - max(d, 0);                            // nodes from there on
+  if (left < 64) x &= (1ull << left) - 1;
+  return d < 0 ? x << -d | ((1ull << -d) - 1) : x;
+}
 
 
 // two codes (bytes 0, 1 or 2, 3 of w) as fp16 integers code - 128
@@ -87,6 +103,6 @@ __device__ __forceinline__ void attn_page(const AttnArgs& a, int b, int g, int p
   *lv = log2f(__ldg(a.c.v_scale + at));
 }
 
-// the launch for many query rows per KV head
+// the launch for many query rows per KV head (a tree where a.seen is given)
 omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a);
 constexpr int ATTN_TC_ROWS = 128;           // its query rows per CTA

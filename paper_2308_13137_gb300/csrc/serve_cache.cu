@@ -30,7 +30,20 @@ struct AppendArgs {
   __nv_bfloat16* Qo; int64_t ldq; __nv_bfloat16 *Ko, *Vo; int64_t ldkv;
   int kv_units;
   int32_t* status;
+  const int32_t* depth;                // of the rows in their draft trees (TREE), or NULL
 };
+
+// rotary position of new token i of a sequence: its slot, or its depth below the tree's root.  One outside the table is
+// reported, and the root's taken.
+template <bool TREE>
+__device__ __forceinline__ int position(const AppendArgs& a, const SeqRows& s, int i) {
+  const int start = s.len - s.nq;
+  if (!TREE) return start + i;
+  const int d = __ldg(a.depth + s.row0 + i);
+  if (d >= 0 && d < a.n_pos - start) return start + d;
+  omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
+  return start;
+}
 
 template <bool BF>
 __device__ __forceinline__ void load8(const void* base, int64_t off, float (&v)[8]) {
@@ -58,7 +71,7 @@ __device__ __forceinline__ void turn(const float2* rope, int pos, int j, float (
   }
 }
 
-template <bool BF>
+template <bool BF, bool TREE>
 __device__ __forceinline__ void q_unit(const AppendArgs& a, const SeqRows& s, int unit) {
   const int grp = threadIdx.x >> 3, j = 8 * (threadIdx.x & 7);
   const int rep = a.n_heads / a.c.n_kv;
@@ -71,7 +84,7 @@ __device__ __forceinline__ void q_unit(const AppendArgs& a, const SeqRows& s, in
     float x[8], y[8];
     load8<BF>(a.QKV, row * a.ld + h * HD + j, x);
     load8<BF>(a.QKV, row * a.ld + h * HD + j + 64, y);
-    turn(a.rope, s.len - s.nq + i, j, x, y);
+    turn(a.rope, position<TREE>(a, s, i), j, x, y);
     if (a.sa) {
       float u[8], w[8];
       load8<false>(a.sa, (h / rep) * HD + j, u);
@@ -90,19 +103,19 @@ __device__ __forceinline__ float code_of(float v, float scale) {
   return fminf(fmaxf(rintf(__fdiv_rn(v, scale)), -127.f), 127.f);
 }
 
-template <bool BF, int NP>
+template <bool BF, int NP, bool TREE>
 __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
   __shared__ uint32_t red[NT / 32];
   const int b = blockIdx.y;
   const SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
   const int start = s.len - s.nq;                      // position of the first new token
-  if (!s.ok || (s.nq > 0 && (start < 0 || s.len > a.n_pos))) {
+  if (!s.ok || (s.nq > 0 && (start < 0 || (TREE ? start >= a.n_pos : s.len > a.n_pos)))) {
     if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
     return;
   }
   if (s.nq == 0) return;
   if ((int)blockIdx.x >= a.kv_units) {
-    q_unit<BF>(a, s, blockIdx.x - a.kv_units);
+    q_unit<BF, TREE>(a, s, blockIdx.x - a.kv_units);
     return;
   }
   const int G = a.c.n_kv, P = a.c.page;
@@ -135,7 +148,7 @@ __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
       load8<BF>(a.QKV, row * a.ld + col, x[p]);
       load8<BF>(a.QKV, row * a.ld + col + 64, y[p]);
       if (!is_v) {
-        turn(a.rope, pos, j, x[p], y[p]);
+        turn(a.rope, TREE ? position<TREE>(a, s, pos - start) : pos, j, x[p], y[p]);
         if (a.sa) {
           float u[8], w[8];
           load8<false>(a.sa, g * HD + j, u);
@@ -204,13 +217,42 @@ __global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
   }
 }
 
-template <bool BF>
+template <bool BF, bool TREE>
 omq_status append_launch(cudaStream_t st, const AppendArgs& a, const dim3& grid) {
-  if (a.c.page <= 32) kv_append_kernel<BF, 1><<<grid, NT, 0, st>>>(a);
-  else if (a.c.page == 64) kv_append_kernel<BF, 2><<<grid, NT, 0, st>>>(a);
-  else kv_append_kernel<BF, 4><<<grid, NT, 0, st>>>(a);
+  if (a.c.page <= 32) kv_append_kernel<BF, 1, TREE><<<grid, NT, 0, st>>>(a);
+  else if (a.c.page == 64) kv_append_kernel<BF, 2, TREE><<<grid, NT, 0, st>>>(a);
+  else kv_append_kernel<BF, 4, TREE><<<grid, NT, 0, st>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
+}
+
+template <bool TREE>
+omq_status append(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q,
+                  int32_t n_heads, const void* QKV, int32_t dtype, int64_t ld, const float* rope, int32_t n_pos,
+                  const float* sa, void* Qo, int64_t ldq, void* Ko, void* Vo, int64_t ldkv, int32_t* dev_status,
+                  const int32_t* depth) {
+  OMQ_TRY(kv_check(cache, total_q, max_q, cu_q, n_heads));
+  OMQ_REQUIRE(QKV && rope && Qo && !Ko == !Vo, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(dtype == OMQ_F32 || dtype == OMQ_BF16, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(n_pos > 0 && ld >= (int64_t)(n_heads + 2 * cache->n_kv) * HD && ldq >= (int64_t)n_heads * HD &&
+                  (!Ko || ldkv >= (int64_t)cache->n_kv * HD),
+              OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(ld % 8 == 0 && ldq % 8 == 0 && (!Ko || ldkv % 8 == 0), OMQ_ERR_ALIGN);
+  OMQ_REQUIRE(omq_aligned16(QKV) && omq_aligned16(rope) && omq_aligned16(sa) && omq_aligned16(Qo) && omq_aligned16(Ko) &&
+                  omq_aligned16(Vo),
+              OMQ_ERR_ALIGN);
+  OMQ_REQUIRE(!TREE || depth, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(omq_aligned4(depth), OMQ_ERR_ALIGN);
+  AppendArgs a{*cache, total_q, max_q, cu_q, n_heads, QKV, ld, (const float2*)rope, n_pos, sa, (__nv_bfloat16*)Qo, ldq,
+               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, dev_status, depth};
+  const int64_t pages = ((int64_t)max_q + cache->page - 2) / cache->page + 1;    // that max_q tokens can touch
+  const int64_t kv_units = 2 * pages * cache->n_kv;
+  const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * GRP - 1) / (QPASS * GRP);
+  OMQ_REQUIRE(kv_units + q_units < (1ll << 31), OMQ_ERR_SHAPE);
+  a.kv_units = (int)kv_units;
+  const dim3 grid((unsigned)(kv_units + q_units), (unsigned)cache->B);
+  return dtype == OMQ_BF16 ? append_launch<true, TREE>((cudaStream_t)stream, a, grid)
+                           : append_launch<false, TREE>((cudaStream_t)stream, a, grid);
 }
 
 }  // namespace
@@ -227,26 +269,16 @@ omq_status omq_kv_append(omq_stream_t stream, const omq_kv_cache* cache, int32_t
                          const int32_t* cu_q, int32_t n_heads, const void* QKV, int32_t dtype, int64_t ld,
                          const float* rope, int32_t n_pos, const float* sa, void* Qo, int64_t ldq, void* Ko, void* Vo,
                          int64_t ldkv, int32_t* dev_status) {
-  OMQ_TRY(kv_check(cache, total_q, max_q, cu_q, n_heads));
-  OMQ_REQUIRE(QKV && rope && Qo && !Ko == !Vo, OMQ_ERR_INVALID_ARG);
-  OMQ_REQUIRE(dtype == OMQ_F32 || dtype == OMQ_BF16, OMQ_ERR_INVALID_ARG);
-  OMQ_REQUIRE(n_pos > 0 && ld >= (int64_t)(n_heads + 2 * cache->n_kv) * HD && ldq >= (int64_t)n_heads * HD &&
-                  (!Ko || ldkv >= (int64_t)cache->n_kv * HD),
-              OMQ_ERR_SHAPE);
-  OMQ_REQUIRE(ld % 8 == 0 && ldq % 8 == 0 && (!Ko || ldkv % 8 == 0), OMQ_ERR_ALIGN);
-  OMQ_REQUIRE(omq_aligned16(QKV) && omq_aligned16(rope) && omq_aligned16(sa) && omq_aligned16(Qo) && omq_aligned16(Ko) &&
-                  omq_aligned16(Vo),
-              OMQ_ERR_ALIGN);
-  AppendArgs a{*cache, total_q, max_q, cu_q, n_heads, QKV, ld, (const float2*)rope, n_pos, sa, (__nv_bfloat16*)Qo, ldq,
-               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, dev_status};
-  const int64_t pages = ((int64_t)max_q + cache->page - 2) / cache->page + 1;    // that max_q tokens can touch
-  const int64_t kv_units = 2 * pages * cache->n_kv;
-  const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * GRP - 1) / (QPASS * GRP);
-  OMQ_REQUIRE(kv_units + q_units < (1ll << 31), OMQ_ERR_SHAPE);
-  a.kv_units = (int)kv_units;
-  const dim3 grid((unsigned)(kv_units + q_units), (unsigned)cache->B);
-  return dtype == OMQ_BF16 ? append_launch<true>((cudaStream_t)stream, a, grid)
-                           : append_launch<false>((cudaStream_t)stream, a, grid);
+  return append<false>(stream, cache, total_q, max_q, cu_q, n_heads, QKV, dtype, ld, rope, n_pos, sa, Qo, ldq, Ko, Vo, ldkv,
+                       dev_status, nullptr);
+}
+
+omq_status omq_kv_append_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                              const int32_t* cu_q, const int32_t* depth, int32_t n_heads, const void* QKV, int32_t dtype,
+                              int64_t ld, const float* rope, int32_t n_pos, const float* sa, void* Qo, int64_t ldq, void* Ko,
+                              void* Vo, int64_t ldkv, int32_t* dev_status) {
+  return append<true>(stream, cache, total_q, max_q, cu_q, n_heads, QKV, dtype, ld, rope, n_pos, sa, Qo, ldq, Ko, Vo, ldkv,
+                      dev_status, depth);
 }
 
 }  // extern "C"

@@ -22,6 +22,8 @@ __device__ __forceinline__ SeqRows seq_rows(const omq_kv_cache& c, const int32_t
   return s;
 }
 
+static inline bool omq_aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
 // checks shared by the calls that take a cache
 static inline omq_status kv_check(const omq_kv_cache* c, int32_t total_q, int32_t max_q, const int32_t* cu_q,
                                   int32_t n_heads) {

@@ -9,11 +9,17 @@ strided views (the last dimension contiguous).
 * kv_append      rotary positions, the [Q, K] scale, and the write into an 8-bit paged cache
 * kv_attention   attention of every sequence's newest tokens over that cache
 * KVCache        the cache's tensors and the handle the calls take
+
+Tokens that a smaller model has drafted are checked as a tree of new rows in one step:
+
+* draft_tree     depths and visible rows of the trees, for kv_append and kv_attention (tree=...)
+* verify_drafts  the walk that accepts drafted tokens against the target's probabilities, and the new token
+* kv_keep        the accepted rows to the front of the newest tokens in every layer's cache
 """
 from __future__ import annotations
 
 import ctypes
-from typing import NamedTuple, Optional
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -35,7 +41,8 @@ class _Calls:
 
     def __getattr__(self, name):
         b = _load_bind()
-        for f in ("rmsnorm_quant", "qgemm", "kv_append", "kv_attention"):
+        for f in ("rmsnorm_quant", "qgemm", "kv_append", "kv_attention", "draft_tree", "kv_append_tree", "kv_attention_tree",
+                  "verify_drafts", "kv_keep"):
             setattr(self, f, getattr(b, f))
         return self.__dict__[name]
 
@@ -141,13 +148,66 @@ def rope_table(n_pos: int, theta: float = 10000.0, device="cuda"):
     return out
 
 
+class DraftTree(NamedTuple):
+    """The trees of a step's rows: parent [rows] int32, and what draft_tree makes of it, depth [rows] and the bits of
+    the visible rows, seen [rows, words] (int32 words).  cu_q and max_q as in kv_append.  For attention alone the bits may
+    be any."""
+    parent: torch.Tensor
+    depth: torch.Tensor
+    seen: torch.Tensor
+    cu_q: Optional[torch.Tensor]
+    max_q: int
+
+
+class Verified(NamedTuple):
+    """tokens [B, steps] int32: every sequence's accepted tokens and the new one, -1 behind; path [B, steps]: the
+    accepted rows (row 0 first), -1 behind; count [B]: how many."""
+    tokens: torch.Tensor
+    path: torch.Tensor
+    count: torch.Tensor
+
+
+def draft_tree(parent, cu_q=None, max_q: Optional[int] = None, out: Optional[DraftTree] = None, status=None) -> DraftTree:
+    """Depths and visible rows of trees of drafted tokens (omq_draft_tree), once per step for all layers.  parent: int32,
+    the row of every row's parent within its sequence (before its own; -1 at row 0); [rows] with cu_q and max_q, or
+    [B, n] for n rows of every sequence.  out: a DraftTree whose depth and seen are filled.  status: an int32 device word
+    that is set where a parent is out of range (a KVCache's serves)."""
+    if cu_q is None:
+        _need(parent.dim() == 2 and (max_q is None or max_q == parent.shape[1]), "parent: [B, n] without cu_q")
+        max_q, parent = parent.shape[1], parent.reshape(-1)
+    else:
+        _need(parent.dim() == 1 and max_q is not None, "parent: [rows], and max_q, with cu_q")
+    if out is None:
+        new = lambda *s: torch.empty(*s, dtype=torch.int32, device=parent.device)  # noqa: E731
+        out = DraftTree(parent, new(parent.shape[0]), new(parent.shape[0], (max_q + 31) // 32), cu_q, max_q)
+    code = _calls.draft_tree(parent, cu_q, max_q, out.depth, out.seen, status)
+    if code:
+        _lib.check("omq_draft_tree", code)
+    return out
+
+
+def _rows_of(tree: Optional[DraftTree], cu_q, max_q):
+    if tree is None:
+        return cu_q, max_q
+    _need(cu_q is None and max_q is None, "cu_q, max_q: the tree's")
+    return tree.cu_q, tree.max_q
+
+
 def kv_append(cache: KVCache, qkv, rope, n_heads: int, cu_q=None, max_q: Optional[int] = None, sa=None, q_out=None,
-              k_out=None, v_out=None):
+              k_out=None, v_out=None, tree: Optional[DraftTree] = None):
     """Turns the new rows' q and k, scales them by 1 / sa and sa, writes k and v into the cache and returns q
     in bf16 (omq_kv_append).  qkv [rows, (n_heads + 2 n_kv) 128] fp32 or bf16.  k_out, v_out [rows, n_kv*128]
-    bf16 receive the values that the new codes stand for."""
+    bf16 receive the values that the new codes stand for.  tree: the rows are drafted tokens, at the positions of
+    their depths (omq_kv_append_tree); cu_q and max_q are its own then."""
     if q_out is None:
         q_out = torch.empty(qkv.shape[0], n_heads * HEAD_DIM, dtype=BF16, device=qkv.device)
+    cu_q, max_q = _rows_of(tree, cu_q, max_q)
+    if tree is not None:
+        code = _calls.kv_append_tree(cache.address, qkv, rope, n_heads, cu_q, max_q, sa, q_out, k_out, v_out, cache.status,
+                                     tree.depth)
+        if code:
+            _lib.check("omq_kv_append_tree", code)
+        return q_out
     code = _calls.kv_append(cache.address, qkv, rope, n_heads, cu_q, max_q, sa, q_out, k_out, v_out, cache.status)
     if code:
         _lib.check("omq_kv_append", code)
@@ -155,14 +215,55 @@ def kv_append(cache: KVCache, qkv, rope, n_heads: int, cu_q=None, max_q: Optiona
 
 
 def kv_attention(cache: KVCache, q, n_heads: int, cu_q=None, max_q: Optional[int] = None, max_kv: Optional[int] = None,
-                 out=None, out_dtype=BF16, lse=None):
+                 out=None, out_dtype=BF16, lse=None, tree: Optional[DraftTree] = None):
     """Causal attention of the rows q [rows, n_heads*128] bf16 over the cache (omq_kv_attention): row i of a
     sequence sees every key up to its own token.  max_kv: a bound of kv_len (default: what the table can
-    hold); the work is cut by it, so give one near the lengths where the table is much longer.  lse [rows, n_heads] fp32 receives the base-2 log-sum-exp."""
+    hold); the work is cut by it, so give one near the lengths where the table is much longer.  lse [rows, n_heads] fp32 receives the base-2 log-sum-exp.
+    tree: row i sees the tokens before its sequence's rows, and of the rows those that its bits name
+    (omq_kv_attention_tree); cu_q and max_q are the tree's own then."""
     if out is None:
         out = torch.empty(q.shape[0], n_heads * HEAD_DIM, dtype=out_dtype, device=q.device)
+    cu_q, max_q = _rows_of(tree, cu_q, max_q)
+    if tree is not None:
+        code = _calls.kv_attention_tree(cache.address, q, n_heads, cu_q, max_q, cache.capacity if max_kv is None else max_kv, out,
+                                        lse, cache.status, tree.seen)
+        if code:
+            _lib.check("omq_kv_attention_tree", code)
+        return out
     code = _calls.kv_attention(cache.address, q, n_heads, cu_q, max_q, cache.capacity if max_kv is None else max_kv, out, lse,
                                cache.status)
     if code:
         _lib.check("omq_kv_attention", code)
     return out
+
+
+def verify_drafts(tree: DraftTree, tokens, probs, u, draft_probs=None, steps: Optional[int] = None,
+                  out: Optional[Verified] = None, status=None) -> Verified:
+    """Walks every sequence's tree from row 0 and accepts drafted tokens so that what comes out is distributed as if drawn
+    from the target (omq_verify_drafts).  tokens [rows] int32; probs [rows, V] fp32 or bf16: the target's
+    distribution after every row; draft_probs, of the same type: the one from which a row's children were drawn, or
+    None where they were chosen (the likeliest, say); u [rows] fp32: uniform numbers in [0, 1), a drafted row's for its test
+    and row 0's for the new token.  steps: columns of the outputs, the most rows of a path (default: max_q).
+    status: an int32 device word that is set where a parent or token is out of range (a KVCache's serves)."""
+    if out is None:
+        B = tree.cu_q.shape[0] - 1 if tree.cu_q is not None else tree.parent.shape[0] // tree.max_q
+        n = tree.max_q if steps is None else steps
+        new = lambda *s: torch.empty(*s, dtype=torch.int32, device=probs.device)  # noqa: E731
+        out = Verified(new(B, n), new(B, n), new(B))
+    _need(steps is None or out.path.shape[1] == steps, "steps: the columns of out")
+    code = _calls.verify_drafts(tree.parent, tree.cu_q, tree.max_q, tokens, probs, draft_probs, u, out.tokens, out.path, out.count,
+                                status)
+    if code:
+        _lib.check("omq_verify_drafts", code)
+    return out
+
+
+def kv_keep(caches: Union[KVCache, Sequence[KVCache]], tree: DraftTree, path, count):
+    """Moves the accepted rows of every sequence to the front of its newest tokens, in one cache or every layer's
+    (omq_kv_keep): row path[b, j] to place j, for j < count[b], as verify_drafts gives them.  The lengths stay: what follows
+    sets kv_len to kv_len - rows + count."""
+    caches = (caches,) if isinstance(caches, KVCache) else caches
+    code = _calls.kv_keep(tuple(c.address for c in caches), tuple(c.status for c in caches), tree.parent.shape[0], tree.cu_q,
+                          tree.max_q, path, count)
+    if code:
+        _lib.check("omq_kv_keep", code)

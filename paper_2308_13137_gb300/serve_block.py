@@ -80,19 +80,22 @@ class ServedBlock:
         return q
 
     def forward(self, h, cache: serve.KVCache, rope, delta=None, cu_q=None, max_q: Optional[int] = None,
-                max_kv: Optional[int] = None):
+                max_kv: Optional[int] = None, tree: Optional[serve.DraftTree] = None):
         """h [rows, d] fp32: the residual stream of the new tokens; delta [rows, d]: the previous block's
         output still to be added to it (fused into this block's first norm).  Returns (h, delta) for the next
         block; the block's output is their sum.  cache.kv_len counts the new tokens already.  cache.check() raises
-        when a call met a page id or length out of range, or a wait of any kernel ran out."""
+        when a call met a page id or length out of range, or a wait of any kernel ran out.
+        tree: the new tokens are drafted ones, at their depths' positions, each seeing the context and its ancestors
+        (cu_q and max_q are the tree's then); serve.verify_drafts and serve.kv_keep follow."""
         sh = self.shape
         self.cfg.dev_status = cache.status.data_ptr()    # the quantizer's waits
         n1 = self._norm(0, h) if delta is None else self._norm(0, delta, h)
         if delta is not None:
             h = n1.residual
         qkv = self._product("qkv", n1, cache.status)
-        q = serve.kv_append(cache, qkv, rope, sh.n_heads, cu_q=cu_q, max_q=max_q, sa=self.sa)
-        o = serve.kv_attention(cache, q, sh.n_heads, cu_q=cu_q, max_q=max_q, max_kv=max_kv, out_dtype=F32)
+        q = serve.kv_append(cache, qkv, rope, sh.n_heads, cu_q=cu_q, max_q=max_q, sa=self.sa, tree=tree)
+        o = serve.kv_attention(cache, q, sh.n_heads, cu_q=cu_q, max_q=max_q, max_kv=max_kv, out_dtype=F32,
+                               tree=tree)
         n2 = self._norm(1, self._product("o", self._codes(o), cache.status), h)
         gu = self._product("gu", n2, cache.status)
         m = torch.nn.functional.silu(gu[:, :sh.ffn]) * gu[:, sh.ffn:]
