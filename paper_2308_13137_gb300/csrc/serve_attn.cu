@@ -29,7 +29,9 @@
 // differ by page, so the two references differ).  A reference moves, and the accumulator with it,
 // only when a score passes it by more than 2^7: few tiles do, and the others need no maximum across
 // lanes at all, only a vote.
-#include "serve_attn.cuh"
+#include <type_traits>
+
+#include "serve_tree.cuh"
 
 namespace {
 
@@ -74,9 +76,24 @@ struct Smem {
   static int bytes(int chunk, int page) { return PAGES_OFF + chunk / page * 12 + 1024; }
 };
 
-template <int NT, bool TREE>
+// draft trees: the pieces of the CTA's share, the next one made while a piece is set up; pages whose records are held
+struct Pieces {
+  TreeWalk walk;
+  TreePiece piece[2];
+  int more[2];
+};
+constexpr int PIECES_BYTES = (sizeof(Pieces) + 15) / 16 * 16, WIN = 256;
+
+__host__ __device__ __forceinline__ const AttnArgs& attn_args(const AttnArgs& a) { return a; }
+__host__ __device__ __forceinline__ const AttnArgs& attn_args(const TreeArgs& t) { return t.a; }
+
+// A = TreeArgs: the rows of draft trees, on CTAs that share all sequences' tokens (serve_tree.cuh); else a CTA has one chunk of
+// one sequence's tokens
+template <int NT, class A>
 __global__ void __launch_bounds__(W * 32, 2)
-    kv_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
+    kv_attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const A args) {
+  constexpr bool TREE = std::is_same<A, TreeArgs>::value;
+  const AttnArgs& a = attn_args(args);
   using S = Smem<NT>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -89,43 +106,68 @@ __global__ void __launch_bounds__(W * 32, 2)
   float* st_l = st_d + W * NT * 8;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(full + S::SLOTS);
-  int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF);
-  const int P = a.c.page, per_chunk = a.chunk / P, pshift = 31 - __clz(P);
+  int* pid = reinterpret_cast<int*>(smem + S::PAGES_OFF + (TREE ? PIECES_BYTES : 0));
+  const int P = a.c.page, per_chunk = TREE ? WIN : a.chunk / P, pshift = 31 - __clz(P);
   float* pks = reinterpret_cast<float*>(pid + per_chunk);     // key scale, times log2(e) / sqrt(128)
   float* plv = pks + per_chunk;                               // log2 of the value scale
+  Pieces* const pieces = reinterpret_cast<Pieces*>(smem + S::PAGES_OFF);
 
-  const int b = blockIdx.y, split = blockIdx.x % a.n_split, gr = blockIdx.x / a.n_split;
-  const int g = gr / a.row_tiles, rt = gr % a.row_tiles;
+  const int split = TREE ? 0 : blockIdx.x % a.n_split, gr = TREE ? 0 : blockIdx.x / a.n_split;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lg = lane >> 2, lt = lane & 3;
   const int rep = a.n_heads / a.c.n_kv;
-  SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
-  if (!s.ok || s.len > a.max_kv) {
-    if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
-    s.len = 0;                                                // its rows read as empty
-  }
-  const int R = s.nq * rep;                                   // query rows of this KV head
   constexpr int ROWS = S::ROWS;
-  const int r0 = rt * ROWS;
-  if (r0 >= R) return;
-  const int start = s.len - s.nq;
-  const int r_last = min(R, r0 + ROWS) - 1;
-  // keys that some row of the CTA sees
-  const int kv_end = TREE ? s.len : max(0, min(s.len, start + r_last / rep + 1));
-  const int t_begin = split * a.chunk;
-  const int t_end = min(kv_end, t_begin + a.chunk);
-  if (split > 0 && t_begin >= kv_end) return;
-  const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
-  const int tiles = t_end > t_begin ? (t_end - t_begin + TILE - 1) / TILE : 0;
-
-  // ---- page records of the chunk, query fragments and row factors ----
-  for (int i = threadIdx.x; i < np; i += W * 32) {
-    attn_page(a, b, g, (t_begin >> pshift) + i, pid + i, pks + i, plv + i);
+  int b = blockIdx.y, g = TREE ? 0 : gr / a.row_tiles, r0 = TREE ? 0 : gr % a.row_tiles * ROWS, R, start, t_begin, t_end, part = -1;
+  SeqRows s;
+  if constexpr (TREE) {
+    const TreeShare share = tree_share<W * 32>(args, reinterpret_cast<int64_t*>(smem + S::STAT_OFF));
+    if (share.hi <= share.lo) return;
+    if (threadIdx.x == 0) {
+      TreeWalk walk;
+      walk.start(args, share);
+      pieces->more[0] = walk.next(args, &pieces->piece[0]);
+      pieces->walk = walk;
+    }
+    __syncthreads();
+  } else {
+    s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
+    if (!s.ok || s.len > a.max_kv) {
+      if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
+      s.len = 0;                                              // its rows read as empty
+    }
+    R = s.nq * rep;                                           // query rows of this KV head
+    if (r0 >= R) return;
+    start = s.len - s.nq;
+    const int r_last = min(R, r0 + ROWS) - 1;
+    const int kv_end = max(0, min(s.len, start + r_last / rep + 1));   // keys that some row of the CTA sees
+    t_begin = split * a.chunk;
+    t_end = min(kv_end, t_begin + a.chunk);
+    if (split > 0 && t_begin >= kv_end) return;
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::SLOTS; ++i) mbar_init(&full[i], 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  int slot = 0, turn = 0;                                     // of this warp's next tile in its ring
+
+  for (int piece = 0;; piece ^= 1) {
+  if constexpr (TREE) {
+    if (!pieces->more[piece]) break;
+    const TreePiece p = pieces->piece[piece];
+    s = SeqRows{p.row0, p.nq, p.len, true};
+    b = p.b; g = p.g; r0 = p.r0; R = p.R; part = p.part;
+    start = p.len - p.nq;
+    t_begin = p.t0; t_end = p.t1;
+    if (threadIdx.x == 0) pieces->more[piece ^ 1] = pieces->walk.next(args, &pieces->piece[piece ^ 1]);
+  }
+
+  // ---- query fragments and row factors; page records of the tokens (of WIN pages at a time) ----
+  auto records = [&](int from, int to) {
+    const int np = to > from ? (to - from + P - 1) >> pshift : 0;
+    for (int i = threadIdx.x; i < np; i += W * 32) attn_page(a, b, g, (from >> pshift) + i, pid + i, pks + i, plv + i);
+  };
+  const int first_end = TREE ? min(t_end, t_begin + WIN * P) : t_end;
+  records(t_begin, first_end);
   for (int r = warp; r < ROWS; r += W) {
     const int row = r0 + r;
     float v[4];
@@ -155,9 +197,8 @@ __global__ void __launch_bounds__(W * 32, 2)
       for (int e = 0; e < 4; ++e) acc[nt][i][e] = 0.f;
   }
 
-  // this warp's ring: its n-th tile is tile warp + n W of the chunk, in slot n % DEPTH
+  // this warp's ring: its n-th tile of a window is tile warp + n W, in the slots one after another
   constexpr int DEPTH = S::DEPTH;
-  const int mine = tiles > warp ? (tiles - warp + W - 1) / W : 0;
   uint64_t* wfull = full + warp * DEPTH;
   const uint32_t ring = smem_u32(smem + warp * DEPTH * TILE_BYTES);
   auto fill = [&](const int n, const int slot) {              // the converged warp; one lane issues
@@ -175,8 +216,6 @@ __global__ void __launch_bounds__(W * 32, 2)
     }
     __syncwarp();
   };
-  int filled = min(DEPTH, mine);
-  for (int n = 0; n < filled; ++n) fill(n, n);
 
   {
     const uint2* qfw = qf + lane;
@@ -201,8 +240,8 @@ __global__ void __launch_bounds__(W * 32, 2)
     const uint32_t v_off0 = TILE * HD + row_v0 * HD + ((uint32_t)(lg ^ row_v0) << 4);
     const uint32_t v_off1 = TILE * HD + row_v1 * HD + ((uint32_t)(lg ^ row_v1) << 4);
 
-    auto tile = [&](const uint32_t base, const int t0) {
-      const int pi = (t0 - t_begin) >> pshift;
+    auto tile = [&](const uint32_t base, const int t0, const int from) {
+      const int pi = (t0 - from) >> pshift;
       if (pid[pi] < 0) return;
       const float ks = pks[pi], lv = plv[pi];
       float sc[NT][4];
@@ -306,19 +345,32 @@ __global__ void __launch_bounds__(W * 32, 2)
       }
     };
 
-    int slot = 0, turn = 0;                  // of tile n
-    for (int n = 0; n < mine; ++n) {
-      if (!warp_wait(&wfull[slot], turn)) {
-        omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
+    for (int from = t_begin, to = first_end;;) {
+      const int tiles = to > from ? (to - from + TILE - 1) / TILE : 0, mine = tiles > warp ? (tiles - warp + W - 1) / W : 0;
+      int filled = min(DEPTH, mine);
+      for (int n = 0; n < filled; ++n) fill(n, slot + n < DEPTH ? slot + n : slot + n - DEPTH);
+      int n = 0;
+      for (; n < mine; ++n) {
+        if (!warp_wait(&wfull[slot], turn)) {
+          omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; break;
+        }
+        tile(ring + slot * TILE_BYTES, from + (warp + n * W) * TILE, from);
+        __syncwarp();                        // every lane has read the tile
+        if (filled < mine) fill(filled++, slot);
+        if (++slot == DEPTH) { slot = 0; turn ^= 1; }
       }
-      tile(ring + slot * TILE_BYTES, t_begin + (warp + n * W) * TILE);
-      __syncwarp();                          // every lane has read the tile
-      if (filled < mine) fill(filled++, slot);
-      if (++slot == DEPTH) { slot = 0; turn ^= 1; }
+      for (; n < filled; ++n) {              // a wait ran out: no copy may land after this CTA has left
+        if (!warp_wait(&wfull[slot], turn)) break;
+        if (++slot == DEPTH) { slot = 0; turn ^= 1; }
+      }
+      if (!TREE || to >= t_end) break;
+      __syncthreads();                       // the records have been read
+      if (*abort_flag) break;
+      from = to;
+      to = min(t_end, from + WIN * P);
+      records(from, to);
+      __syncthreads();
     }
-    if (lane == 0 && *abort_flag)            // no copy may land after this CTA has left
-      for (int j = max(0, filled - DEPTH); j < filled; ++j)
-        if (!wait_phase(&wfull[j % DEPTH], (j / DEPTH) & 1)) break;
   }
 
   // ---- join the warps ----
@@ -370,7 +422,15 @@ __global__ void __launch_bounds__(W * 32, 2)
       o.x *= c; o.y *= c; o.z *= c; o.w *= c;
       const int64_t tok = s.row0 + row / rep;
       const int head = g * rep + row % rep;
-      if (a.n_split > 1) {
+      if constexpr (TREE) {
+        if (part >= 0) {
+          const int64_t at = (int64_t)part * ROWS + row - r0;
+          *reinterpret_cast<float4*>(args.po + at * HD + 4 * lane) = o;
+          if (lane == 0) args.pl[at] = lse;
+          continue;
+        }
+      }
+      if (!TREE && a.n_split > 1) {
         const int64_t at = (tok * a.n_heads + head) * a.n_split + split;
         *reinterpret_cast<float4*>(a.wo + at * HD + 4 * lane) = o;
         if (lane == 0) a.wl[at] = lse;
@@ -387,6 +447,24 @@ __global__ void __launch_bounds__(W * 32, 2)
       }
     }
   }
+  if (!TREE) break;
+  fence_async_smem();                                         // the joining buffer's writes before the ring's copies
+  __syncthreads();
+  if (*abort_flag) break;
+  }
+}
+
+// a row of the outputs, four channels per lane
+__device__ __forceinline__ void write_row(const AttnArgs& a, int64_t tok, int head, int lane, const float4& o, float lse) {
+  if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
+  if (a.Ob) {
+    uint2 u;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
+    h[0] = __floats2bfloat162_rn(o.x, o.y);
+    h[1] = __floats2bfloat162_rn(o.z, o.w);
+    *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
+  }
+  if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = lse;
 }
 
 // O = sum_s O_s 2^(lse_s - lse) over the splits that hold keys of the row, in split order; one warp per
@@ -398,7 +476,7 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   if (!s.ok || s.len > a.max_kv) s.len = 0;
   const int i = idx / a.n_heads, head = idx % a.n_heads;
   if (i >= s.nq) return;
-  const int seen = a.seen ? s.len : max(0, min(s.len, s.len - s.nq + i + 1));
+  const int seen = max(0, min(s.len, s.len - s.nq + i + 1));
   const int nv = (seen + a.chunk - 1) / a.chunk;
   const int64_t tok = s.row0 + i, at = (tok * a.n_heads + head) * a.n_split;
   float top = -INFINITY;
@@ -426,6 +504,43 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
     *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
   }
   if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = L == 0.f ? -INFINITY : ref + log2f(L);
+}
+
+// The same for the cut units of draft trees: partial results of the CTAs whose shares hold tokens of the row's unit, in
+// order of tokens
+__global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeArgs t) {
+  const AttnArgs& a = t.a;
+  const int b = blockIdx.y, lane = threadIdx.x & 31, rep = a.n_heads / a.c.n_kv;
+  const int idx = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const TreeSeq q = tree_seq(t, b);
+  const int i = idx / a.n_heads, head = idx % a.n_heads;
+  if (i >= q.nq || q.slots == 0) return;
+  const int row = i * rep + head % rep, tile = row / t.cost.rows, w = tree_weight(t, q, tile);
+  const int64_t at = t.before[b] + (head / rep) * q.head + tile * q.full, end = at + t.cost.start + (int64_t)q.slots * w;
+  const int64_t total = t.work->total, n = t.work->n;
+  int c0 = (int)(((at + 1) * n - 1) / total), c1 = (int)((end * n - 1) / total);       // CTAs of its two ends
+  // the first ones may have no more than the unit's start
+  while (c0 < c1 && tree_slots(t, q, w, at, tree_border(total, n, c0 + 1)) == 0) ++c0;
+  if (c0 == c1) return;                                       // whole
+  const int64_t lo0 = tree_border(total, n, c0);
+  auto place = [&](int c) { return (int64_t)(2 * c + (c > c0 ? 0 : at >= lo0)) * t.cost.rows + row % t.cost.rows; };
+  float top = -INFINITY;
+  for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, t.pl[place(c)]);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int c = c0; c <= c1; ++c) {
+    const int64_t k = place(c);
+    const float f = ex2(t.pl[k] - ref);
+    const float4 x = *reinterpret_cast<const float4*>(t.po + k * HD + 4 * lane);
+    L += f;
+    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+  }
+  const float f = L == 0.f ? 0.f : 1.f / L;
+  write_row(a, q.row0 + i, head, lane, make_float4(o.x * f, o.y * f, o.z * f, o.w * f), L == 0.f ? -INFINITY : ref + log2f(L));
 }
 
 struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
@@ -458,24 +573,55 @@ size_t plan_workspace(const Plan& p, int64_t total_q, int64_t n_heads) {
   return parts * HD * sizeof(float) + (parts * sizeof(float) + 255) / 256 * 256;
 }
 
-template <int NT, bool TREE>
-omq_status attn_launch(cudaStream_t st, const AttnArgs& a) {
+template <int NT, class A>
+omq_status attn_launch(cudaStream_t st, const A& args, dim3 grid) {
   using S = Smem<NT>;
-  auto kern = kv_attention_kernel<NT, TREE>;
+  constexpr bool TREE = std::is_same<A, TreeArgs>::value;
+  const AttnArgs& a = attn_args(args);
+  auto kern = kv_attention_kernel<NT, A>;
   static std::atomic<uint64_t> allowed{0};
-  OMQ_TRY(omq_allow_smem(allowed, kern, S::bytes(ATTN_MAX_CHUNK, 16)));
+  OMQ_TRY(omq_allow_smem(allowed, kern, TREE ? S::PAGES_OFF + PIECES_BYTES + WIN * 12 + 1024 : S::bytes(ATTN_MAX_CHUNK, 16)));
   CUtensorMap tk, tv;
   const int64_t rows = (int64_t)a.c.n_pages * a.c.n_kv * a.c.page;
   if (!omq_make_map_u8(&tk, a.c.k, HD, rows, HD, TILE, HD) || !omq_make_map_u8(&tv, a.c.v, HD, rows, HD, TILE, HD))
     return OMQ_ERR_UNSUPPORTED;
-  kern<<<dim3(a.n_split * a.c.n_kv * a.row_tiles, a.c.B), W * 32, S::bytes(a.chunk, a.c.page), st>>>(tk, tv, a);
+  const int bytes = TREE ? S::PAGES_OFF + PIECES_BYTES + WIN * 12 + 1024 : S::bytes(a.chunk, a.c.page);
+  kern<<<grid, W * 32, bytes, st>>>(tk, tv, args);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
 
-omq_status attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q,
-                     const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq, float* Of,
-                     void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes, int32_t* dev_status) {
+// Draft trees: rows of a unit, CTAs, and what the units cost (serve_tree.cuh)
+struct TreePlan { TreeCost cost; int64_t min_share; int ctas; };
+TreePlan tree_plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
+  const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
+  TreePlan p;
+  if (rows <= 16) {
+    const int r = rows <= 8 ? 8 : 16;
+    p.cost = TreeCost{r, r, 2, 1, 1};
+  } else {
+    p.cost = rows <= ATTN_TC_ROWS ? TreeCost{ATTN_TC_ROWS, ATTN_TC_ROWS, 12, 2, 2} : TreeCost{2 * ATTN_TC_ROWS, ATTN_TC_ROWS, 12, 3, 2};
+  }
+  p.min_share = p.cost.start + 2 * p.cost.weight;             // 256 tokens
+  // no more CTAs than there is work for by the bounds
+  const int64_t units = B * n_kv * ((rows + p.cost.rows - 1) / p.cost.rows), slots = ((int64_t)max_kv + TREE_SLOT - 1) / TREE_SLOT;
+  const int64_t most = units * (p.cost.start + slots * p.cost.weight) / p.min_share + 1;
+  const int64_t ctas = omq_num_sms() * (rows <= 16 ? 2ll : 1ll);
+  p.ctas = (int)(most < ctas ? most : ctas);
+  return p;
+}
+
+// partial results, the sequences' places, the whole
+size_t tree_workspace(const TreePlan& p, int64_t B, size_t* pl, size_t* before) {
+  const size_t parts = (size_t)2 * p.ctas * p.cost.rows;
+  *pl = parts * HD * sizeof(float);
+  *before = *pl + (parts * sizeof(float) + 255) / 256 * 256;
+  return *before + ((size_t)B * 8 + sizeof(TreeWork) + 255) / 256 * 256;
+}
+
+omq_status attention_check(const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q, int32_t max_kv,
+                           int32_t n_heads, const void* Q, int64_t ldq, const float* Of, const void* Ob, int64_t ldo,
+                           const float* lse, const void* workspace) {
   OMQ_TRY(kv_check(cache, total_q, max_q, cu_q, n_heads));
   OMQ_REQUIRE(Q && (Of || Ob), OMQ_ERR_INVALID_ARG);
   OMQ_REQUIRE(max_kv > 0 && ldq >= (int64_t)n_heads * HD && ldo >= (int64_t)n_heads * HD, OMQ_ERR_SHAPE);
@@ -483,26 +629,7 @@ omq_status attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t tot
   OMQ_REQUIRE(omq_aligned16(Q) && omq_aligned16(Of) && omq_aligned16(Ob) && omq_aligned16(lse) &&
                   omq_aligned16(workspace),
               OMQ_ERR_ALIGN);
-  const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
-  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles * p.n_split < (1ll << 31), OMQ_ERR_SHAPE);
   OMQ_REQUIRE((int64_t)cache->n_pages * cache->n_kv * cache->page < (1ll << 31), OMQ_ERR_SHAPE);   // TMA coordinates
-  const size_t need = plan_workspace(p, total_q, n_heads);
-  OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
-  AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
-             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status, seen, words};
-  if (p.n_split > 1) {
-    a.wo = (float*)workspace;
-    a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
-  }
-  cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY(p.form == 8    ? (seen ? attn_launch<1, true>(st, a) : attn_launch<1, false>(st, a))
-          : p.form == 16 ? (seen ? attn_launch<2, true>(st, a) : attn_launch<2, false>(st, a))
-                         : attn_tc_launch(st, a));
-  if (p.n_split > 1) {
-    const int64_t pairs = (int64_t)max_q * n_heads;
-    kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
-    OMQ_LAUNCH_CHECK();
-  }
   return OMQ_OK;
 }
 
@@ -519,13 +646,34 @@ size_t omq_kv_attention_workspace_size(int32_t B, int32_t total_q, int32_t max_q
 omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
                             const int32_t* cu_q, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq, float* Of,
                             void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes, int32_t* dev_status) {
-  return attention(stream, cache, total_q, max_q, cu_q, nullptr, 0, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
-                   ws_bytes, dev_status);
+  OMQ_TRY(attention_check(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace));
+  const Plan p = plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
+  OMQ_REQUIRE((int64_t)cache->n_kv * p.row_tiles * p.n_split < (1ll << 31), OMQ_ERR_SHAPE);
+  const size_t need = plan_workspace(p, total_q, n_heads);
+  OMQ_REQUIRE(need == 0 || (workspace && ws_bytes >= need), OMQ_ERR_WORKSPACE);
+  AttnArgs a{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
+             lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status, nullptr, 0};
+  if (p.n_split > 1) {
+    a.wo = (float*)workspace;
+    a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
+  }
+  cudaStream_t st = (cudaStream_t)stream;
+  const dim3 grid(p.n_split * cache->n_kv * p.row_tiles, cache->B);
+  OMQ_TRY((p.form == 8 ? attn_launch<1>(st, a, grid)
+                       : (p.form == 16 ? attn_launch<2>(st, a, grid) : attn_tc_launch(st, a))));
+  if (p.n_split > 1) {
+    const int64_t pairs = (int64_t)max_q * n_heads;
+    kv_attention_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(a);
+    OMQ_LAUNCH_CHECK();
+  }
+  return OMQ_OK;
 }
 
 size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                             int32_t n_kv) {
-  return omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv);
+  if (B <= 0 || total_q <= 0 || max_q <= 0 || max_kv <= 0 || n_kv <= 0 || n_heads <= 0 || n_heads % n_kv) return 0;
+  size_t pl, before;
+  return tree_workspace(tree_plan_of(B, max_q, max_kv, n_heads, n_kv), B, &pl, &before);
 }
 
 omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
@@ -535,8 +683,23 @@ omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache,
   OMQ_REQUIRE(seen, OMQ_ERR_INVALID_ARG);
   OMQ_REQUIRE(max_q > 0 && words >= (max_q - 1) / 32 + 1, OMQ_ERR_SHAPE);
   OMQ_REQUIRE(omq_aligned4(seen), OMQ_ERR_ALIGN);
-  return attention(stream, cache, total_q, max_q, cu_q, seen, words, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
-                   ws_bytes, dev_status);
+  OMQ_TRY(attention_check(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace));
+  const TreePlan p = tree_plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
+  const int64_t pairs = (int64_t)max_q * n_heads;
+  OMQ_REQUIRE(pairs < (1ll << 31), OMQ_ERR_SHAPE);
+  size_t pl, before;
+  OMQ_REQUIRE(workspace && ws_bytes >= tree_workspace(p, cache->B, &pl, &before), OMQ_ERR_WORKSPACE);
+  char* const ws = (char*)workspace;
+  const TreeArgs t{AttnArgs{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
+                            lse, nullptr, nullptr, 0, 1, 1, dev_status, seen, words},
+                   p.cost, p.min_share, (TreeWork*)(ws + before), (int64_t*)(ws + before + sizeof(TreeWork)), (float*)ws,
+                   (float*)(ws + pl)};
+  cudaStream_t st = (cudaStream_t)stream;
+  OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
+                            : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));
+  kv_attention_tree_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(t);
+  OMQ_LAUNCH_CHECK();
+  return OMQ_OK;
 }
 
 }  // extern "C"

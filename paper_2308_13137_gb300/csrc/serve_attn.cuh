@@ -32,7 +32,7 @@ struct AttnArgs {
   float* wo; float* wl;                     // partial results of the splits (n_split > 1)
   int chunk, n_split, row_tiles;
   int32_t* status;
-  const uint32_t* seen; int words;          // draft trees: bits of the newest tokens that each row sees
+  const uint32_t* seen; int words;          // draft trees (serve_tree.cuh): bits of the newest tokens that each row sees
 };
 
 // Draft trees: the newest tokens that a row sees, from node d of its sequence (d below zero: context, which every row
@@ -68,17 +68,17 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Four channels (4 lane ..) of query row `row` of KV head g, or zeros; *sh: the power of two that puts the row's
-// largest magnitude in [2^13, 2^14) (capped where 2^sh would overflow).  Warp-collective.
-__device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane,
-                                            float (&v)[4], int* sh) {
-  v[0] = v[1] = v[2] = v[3] = 0.f;
-  if (row < rows) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2*>(a.Q + (int64_t)(s.row0 + row / rep) * a.ldq +
-                                                         (g * rep + row % rep) * ATTN_HD + 4 * lane));
-    v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-    v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
-  }
+// Four channels (4 lane ..) of query row `row` of KV head g as bf16, or zeros
+__device__ __forceinline__ uint2 attn_query_raw(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane) {
+  if (row >= rows) return make_uint2(0, 0);
+  return __ldg(reinterpret_cast<const uint2*>(a.Q + (int64_t)(s.row0 + row / rep) * a.ldq + (g * rep + row % rep) * ATTN_HD + 4 * lane));
+}
+
+// The same times 2^*sh: the power of two that puts the row's largest magnitude in [2^13, 2^14) (capped where 2^sh
+// would overflow).  Warp-collective.
+__device__ __forceinline__ void attn_query_scaled(const uint2& u, float (&v)[4], int* sh) {
+  v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
+  v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
   uint32_t big = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) big = max(big, __float_as_uint(v[e]) & 0x7fffffffu);
@@ -87,6 +87,11 @@ __device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s,
   const float up = __uint_as_float((uint32_t)(127 + *sh) << 23);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= up;
+}
+
+__device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane,
+                                            float (&v)[4], int* sh) {
+  attn_query_scaled(attn_query_raw(a, s, g, rep, row, rows, lane), v, sh);
 }
 
 // page record i of a chunk that starts at page `first`: id (-1 and the status word where it is out of range),
@@ -103,6 +108,6 @@ __device__ __forceinline__ void attn_page(const AttnArgs& a, int b, int g, int p
   *lv = log2f(__ldg(a.c.v_scale + at));
 }
 
-// the launch for many query rows per KV head (a tree where a.seen is given)
+// the launch for many query rows per KV head
 omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a);
 constexpr int ATTN_TC_ROWS = 128;           // its query rows per CTA

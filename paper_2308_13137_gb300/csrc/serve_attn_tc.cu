@@ -51,7 +51,7 @@ __device__ __forceinline__ void put16(uint32_t row, int c, uint32_t x, const uin
 
 // CP: copies of a row.  Rows that fit a half or a quarter of the tile's 128 are held two or four times, each copy
 // with its own half or quarter of every tile's tokens: a softmax thread's 64 exponentials become 32 or 16.
-template <int CP, bool TREE>
+template <int CP>
 __global__ void __launch_bounds__(THREADS, 1)
     kv_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int R = s.nq * rep, r0 = rt * BMR;
   if (r0 >= R) return;
   const int start = s.len - s.nq, r_last = min(R, r0 + BMR) - 1;
-  const int kv_end = TREE ? s.len : max(0, min(s.len, start + r_last / rep + 1));
+  const int kv_end = max(0, min(s.len, start + r_last / rep + 1));
   const int t_begin = split * a.chunk, t_end = min(kv_end, t_begin + a.chunk);
   if (split > 0 && t_begin >= kv_end) return;
   const int np = t_end > t_begin ? (t_end - t_begin + P - 1) >> pshift : 0;
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       *reinterpret_cast<uint2*>(row + (((lane & 15) >> 1 ^ (r & 7)) << 4) + (lane & 1) * 8) = u;
       if (lane == 0) {
         qs[r] = __uint_as_float((uint32_t)(127 - sh) << 23);
-        lims[r] = r0 + i < R ? (TREE ? s.row0 + (r0 + i) / rep : min(s.len, start + (r0 + i) / rep + 1)) : 0;
+        lims[r] = r0 + i < R ? min(s.len, start + (r0 + i) / rep + 1) : 0;
       }
     }
   }
@@ -222,18 +222,14 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (holds && lane == 0) mbar_arrive(&s_ready[sg]);        // the first scores overwrite nothing
     const int w0 = r / SPAN * TW;                             // this copy's tokens of a tile
     const float f = qs[r];
-    // keys that the row sees, or (trees) its row among all, whose bits tell which nodes it sees
-    const int lim = lims[r], lim_min = TREE ? start : __reduce_min_sync(0xffffffffu, mine ? lim : 0x7fffffff);
-    const uint32_t* const bits = TREE ? a.seen + (int64_t)lim * a.words : nullptr;
+    const int lim = lims[r], lim_min = __reduce_min_sync(0xffffffffu, mine ? lim : 0x7fffffff);
     uint32_t turn = 0;
     for (int j = sg; j < tiles && holds; j += 2, turn ^= 1) {
       // the 16-token quarters, each of one page: score factor, log2 of the value scale; the tokens that
       // this row sees, as bits
       const int t0 = t_begin + j * TT + w0;
       float fk[TW / 16], lv[TW / 16];
-      uint64_t seen;
-      if (TREE) seen = attn_window(bits, mine ? a.words : 0, s.nq, t0 - start);
-      else seen = lim - t0 >= TW ? ~0ull : (lim <= t0 ? 0ull : (1ull << (lim - t0)) - 1);
+      uint64_t seen = lim - t0 >= TW ? ~0ull : (lim <= t0 ? 0ull : (1ull << (lim - t0)) - 1);
       bool whole = t0 + TW <= min(t_end, lim_min);
 #pragma unroll
       for (int q = 0; q < TW / 16; ++q) {
@@ -443,9 +439,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 }  // namespace
 
-template <int CP, bool TREE>
+template <int CP>
 static omq_status launch(cudaStream_t st, const AttnArgs& a) {
-  auto kern = kv_attention_tc_kernel<CP, TREE>;
+  auto kern = kv_attention_tc_kernel<CP>;
   static std::atomic<uint64_t> allowed{0};
   OMQ_TRY(omq_allow_smem(allowed, kern, tc_smem(ATTN_MAX_CHUNK, 16)));
   CUtensorMap tk, tv;
@@ -462,7 +458,7 @@ static omq_status launch(cudaStream_t st, const AttnArgs& a) {
 // one; 64 ragged sequences of up to 40 rows 133 us with two, 144 with one).
 omq_status attn_tc_launch(cudaStream_t st, const AttnArgs& a) {
   const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.c.n_kv);
-  if (rows <= BMR / 4) return a.seen ? launch<4, true>(st, a) : launch<4, false>(st, a);
-  if (rows <= BMR / 2) return a.seen ? launch<2, true>(st, a) : launch<2, false>(st, a);
-  return a.seen ? launch<1, true>(st, a) : launch<1, false>(st, a);
+  if (rows <= BMR / 4) return launch<4>(st, a);
+  if (rows <= BMR / 2) return launch<2>(st, a);
+  return launch<1>(st, a);
 }

@@ -14,7 +14,7 @@ namespace {
 // ------------------------------------------------------------------------------------------------
 constexpr int MAX_NODES = 1024;
 
-struct TreeArgs {
+struct NodeArgs {
   int total_q, max_q; const int32_t* cu_q; const int32_t* parent; int32_t* depth; uint32_t* seen; int words;
   int32_t* status;
 };
@@ -27,7 +27,7 @@ __device__ __forceinline__ bool node_rows(const int32_t* cu_q, int max_q, int to
   return lo >= 0 && hi >= lo && hi <= total_q && hi - lo <= max_q;
 }
 
-__global__ void __launch_bounds__(MAX_NODES) draft_tree_kernel(const TreeArgs a) {
+__global__ void __launch_bounds__(MAX_NODES) draft_tree_kernel(const NodeArgs a) {
   extern __shared__ uint32_t tree_smem[];
   int row0, n;
   if (!node_rows(a.cu_q, a.max_q, a.total_q, blockIdx.x, &row0, &n)) {
@@ -550,7 +550,7 @@ omq_status omq_draft_tree(omq_stream_t stream, int32_t B, int32_t total_q, int32
   OMQ_REQUIRE(omq_aligned4(cu_q) && omq_aligned4(parent) && omq_aligned4(depth) && omq_aligned4(seen), OMQ_ERR_ALIGN);
   static std::atomic<uint64_t> allowed{0};
   OMQ_TRY(omq_allow_smem(allowed, draft_tree_kernel, (int)tree_smem_bytes(MAX_NODES)));
-  const TreeArgs a{total_q, max_q, cu_q, parent, depth, seen, words, dev_status};
+  const NodeArgs a{total_q, max_q, cu_q, parent, depth, seen, words, dev_status};
   draft_tree_kernel<<<B, (max_q + 31) / 32 * 32, tree_smem_bytes(max_q), (cudaStream_t)stream>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
