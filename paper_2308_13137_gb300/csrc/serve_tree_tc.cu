@@ -1,17 +1,23 @@
 // Attention of draft trees over an 8-bit paged cache for more than 16 query rows per KV head: tcgen05 tiles of 128 rows x
 // 64 tokens, on CTAs that share the tokens of all sequences evenly (serve_tree.cuh).
 //
-// The mathematics and the precision are those of serve_attn.cu.  A CTA holds one tile of 128 query rows, whose even and odd
-// token tiles go to its two groups of softmax warps, or two tiles of rows, one for each group, which read the same
-// converted token tiles (a unit of more than 128 rows).  Roles of the 20 warps:
-//   0        TMA: raw code tiles of K and V (128-byte swizzle); it also walks the CTA's share
-//   1, 2     issue S = Q K^T (128 x 64 x 128), one group each
-//   3        issues O += P V (128 x 128 x 64) of both groups
-//   4..7, 16..19   softmax, a row per thread: scores from tensor memory, weights in fp16 back to the columns that
-//            the scores had, from where the second product reads them as its A operand
-//   8..15    convert: K (8..11) and V (12..15) to fp16, one half row of 64 codes per thread; K is read K-major, V MN-major
-// A group's scores have two buffers, so the product of its next tile runs while it works, and a tile costs it one
-// wait.  Every barrier belongs to one group, and the groups differ only in which tiles they take.
+// The mathematics and the precision are those of serve_attn.cu.  Shared memory sets the layout: its 128 bytes a cycle carry the
+// converted tiles in and the products' operands out.  So the queries and the weights, the A operands, lie in tensor
+// memory, and a tile of 64 tokens costs 768 cycles there (codes in and out, converted in and out), 517 on the tensor
+// cores, and its 16 KB of codes 725 from HBM.  Roles of the 28 warps:
+//   0, 1     issue S = Q K^T (128 x 64 x 128) and O += P V (128 x 128 x 64)
+//   2        walks the CTA's share: chunks of up to 1024 tokens, with the records of their pages
+//   4..11    softmax, a row per thread, two groups (even and odd tiles) with their own references, sums and accumulators:
+//            scores from tensor memory, weights in fp16 to columns of their own, so that the group's next scores are
+//            formed meanwhile
+//   12..27   convert K and V to fp16, two sets (even and odd tiles), from rings of their own that bulk copies fill.  K is
+//            read K-major, V MN-major, both from [half][64 tokens][128 bytes] swizzled tiles
+// Tile j's converted K and V lie in the places j % 3, its scores and weights in its group's.  Nothing stops between chunks or
+// pieces: the next piece's queries are written, and its scores formed, before the last one's output is.
+// No role may spill: local memory passes the small rest of the L1 here, and a tile whose softmax reloads a dozen registers takes
+// half again as long.
+#include <type_traits>
+
 #include "serve_tree.cuh"
 
 namespace {
@@ -19,39 +25,28 @@ namespace {
 using namespace tc;
 
 constexpr int HD = ATTN_HD, BMR = 128, TT = 64;
-constexpr int RAW = 4;                               // ring depth of raw tiles (K | V); converted tiles: two of each
-constexpr int RAW_BYTES = 2 * TT * HD;
 constexpr int HALF = TT * HD;                        // one 64-channel half of a converted tile: 64 rows x 128 bytes
 constexpr int OP_BYTES = 2 * HALF;
-constexpr int Q_BYTES = BMR * HD * 2;
-constexpr int WIN = 1024;                            // pages whose records are held at a time
-constexpr int THREADS = 640;
-constexpr int FIRST = 1, LAST = 2, DUAL = 4, DONE = 8;
+constexpr int BUF = 3;                               // places of tiles
+constexpr int CHUNK = 1024, PAGES = CHUNK / 16, RING = 8;      // tokens, pages at most of a chunk; chunks in flight
+constexpr int RAW_BYTES = 16 * HD, DEPTH = 2;        // a warp's share of a tile's codes, its two slots
+constexpr int THREADS = 896;
+constexpr int FIRST = 1, LAST = 2, DONE = 4;         // of a piece; the share's end
+constexpr uint32_t Q_COL = 0, S_COL = 64, P_COL = 192, O_COL = 256;       // tensor memory: Q | of the two groups: scores | weights | O
 
-struct Window {                                      // what warp 0 posts: tokens [t0, t1) of a piece
+struct __align__(16) Chunk {                         // tokens [t0, t1) of a piece
   TreePiece p;
   int t0, t1, flags;
+  float4 page[PAGES];                                // score factor, log2 of the value scale, place of its rows in the pool (-1: none)
 };
 
-template <int TILES>
-struct Smem {
-  static constexpr int CONV = TILES * Q_BYTES;       // K K | V V
-  static constexpr int RAWS = CONV + 4 * OP_BYTES;
-  static constexpr int ROW = RAWS + RAW * RAW_BYTES; // per row: factor, row among all
-  static constexpr int REF = ROW + 2 * TILES * BMR * 4;                 // per group and row: m, d, l
-  static constexpr int BAR = REF + 2 * 3 * BMR * 4;
-  static constexpr int WINDOW = BAR + 256;
-  static constexpr int SCAN = WINDOW + 2 * 64;
-  static constexpr int PAGES = SCAN + (THREADS / 32 + 4) * 8;
-  static constexpr int BYTES = PAGES + WIN * 12 + 1024;
-};
-static_assert(sizeof(Window) <= 64 && Smem<2>::BYTES <= 232448, "shared memory");
-
-// 16 codes to fp16, into two swizzled 16-byte chunks of a 128-byte row
-__device__ __forceinline__ void put16(uint32_t row, int c, uint32_t x, const uint4& u) {
-  sts128(row + (((2 * c) ^ x) << 4), make_uint4(codes_lo(u.x), codes_hi(u.x), codes_lo(u.y), codes_hi(u.y)));
-  sts128(row + (((2 * c + 1) ^ x) << 4), make_uint4(codes_lo(u.z), codes_hi(u.z), codes_lo(u.w), codes_hi(u.w)));
-}
+constexpr int K_CONV = 0, V_CONV = K_CONV + BUF * OP_BYTES, STAGE = V_CONV + BUF * OP_BYTES;
+constexpr int RAW = STAGE + BMR * HD * 2;            // the stage: queries in fp16, or 32 channels of O from each group
+constexpr int ROW = RAW + 16 * DEPTH * RAW_BYTES;    // factor of each row
+constexpr int REF = ROW + BMR * 4;                   // [group][m, d, l]
+constexpr int BAR = REF + 2 * 3 * BMR * 4, SCAN = BAR + 768, CHUNKS = SCAN + (THREADS / 32 + 4) * 8;
+constexpr int SMEM = CHUNKS + RING * (int)sizeof(Chunk) + 1024;
+static_assert(SMEM <= 232448 && CHUNKS % 16 == 0, "shared memory");
 
 // D += A B with A (fp16, K-major: a 32-bit column holds two steps of K) in tensor memory
 __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
@@ -63,6 +58,74 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       : "memory");
 }
 
+// mbarriers by their shared addresses (32 bits: the roles here have few registers)
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// A converged warp's bounded wait.  The phase is mostly over already: a test costs 50 cycles, a wait 120.  A try without a time
+// hint suspends the warp for 1.3 us at most and costs one instruction; with a hint it is a loop of polls, and those of
+// this kernel's 28 warps were more than half of all its instructions.
+__device__ __forceinline__ bool soon(uint32_t bar, uint32_t parity) {
+  bool ok = bar_test(bar, parity);
+  for (uint32_t i = 0; !__all_sync(0xffffffffu, ok); ++i) {
+    if (i == (uint32_t)(OMQ_WAIT_LIMIT_NS / 1300u)) return false;
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(p)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    ok = p != 0;
+  }
+  return true;
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive(uint32_t bar, int lane) {          // of a warp
+  __syncwarp();
+  if (lane == 0) bar_arrive(bar);
+}
+__device__ __forceinline__ void commit(uint32_t bar) {                    // tcgen05 products so far
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// bytes of global memory on their way to shared memory, counted on bar (16-byte aligned)
+__device__ __forceinline__ void fetch_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// 32 lanes x 32 consecutive 32-bit columns into registers (warp-collective; not waited for)
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // eight 32-bit columns from registers into tensor memory (warp-collective; not waited for)
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
@@ -70,546 +133,640 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8])
                : "memory");
 }
 
-__device__ __forceinline__ void cta_sync() { asm volatile("bar.sync 0, 640;" ::: "memory"); }
-__device__ __forceinline__ void group_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+// place j % 3 of a tile and the parity of j / 3
+struct Place {
+  int b; uint32_t ph;
+  __device__ __forceinline__ void move(int n) {      // n <= 3
+    b += n;
+    if (b >= BUF) { b -= BUF; ph ^= 1; }
+  }
+  __device__ __forceinline__ Place before() const { return b >= 2 ? Place{b - 2, ph} : Place{b + BUF - 2, ph ^ 1}; }      // of tile j - 2
+};
 
-// CP: copies of a row (serve_attn_tc.cu); TILES: tiles of 128 rows that a CTA has room for
-template <int CP, int TILES>
-__global__ void __launch_bounds__(THREADS, 1)
-    kv_attention_tree_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const TreeArgs t) {
-  using S = Smem<TILES>;
+// CP: copies of a row (serve_attn_tc.cu); NQ: pages (at most) that a softmax thread's 64 / CP tokens of a tile lie on
+template <int CP, int NQ>
+__global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const TreeArgs t) {
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* const smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
   const AttnArgs& a = t.a;
-  float* qs = reinterpret_cast<float*>(smem + S::ROW);
-  int* token = reinterpret_cast<int*>(qs + TILES * BMR);
-  float* refs = reinterpret_cast<float*>(smem + S::REF);
-  uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + S::BAR);
-  uint64_t* raw_empty = raw_full + RAW;
-  uint64_t* k_ready = raw_empty + RAW;               // [2] K of a tile converted
-  uint64_t* s_full = k_ready + 2;                    // [group][2] scores formed
-  uint64_t* pv_ready = s_full + 4;                   // [group][2] V of the tile converted and its weights written
-  uint64_t* pv_done = pv_ready + 4;                  // [group][2] product formed: weights (and scores) consumed
-  uint64_t* drain = pv_done + 4;                     // [3] of the issuing warps
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 3);
+  const uint32_t bars = smem_u32(smem + BAR);
+  const uint32_t k_full = bars;                      // [3] K of a tile converted
+  const uint32_t s_full = k_full + 8 * BUF;          // [3] scores formed (K consumed)
+  const uint32_t pv_ready = s_full + 8 * BUF;        // [3] V of the tile converted and its weights written
+  const uint32_t pv_done = pv_ready + 8 * BUF;       // [3] product formed: weights, scores and V consumed
+  const uint32_t s_free = pv_done + 8 * BUF;         // [2] scores read
+  const uint32_t o_free = s_free + 16;               // both accumulators read
+  const uint32_t q_ready = o_free + 8;               // the piece's queries lie in tensor memory
+  const uint32_t meet = q_ready + 8;                 // of the softmax warps
+  const uint32_t chunk_full = meet + 8;              // [RING]
+  const uint32_t chunk_empty = chunk_full + 8 * RING;                     // [RING]
+  const uint32_t raw_full = chunk_empty + 8 * RING;  // [converting warp][DEPTH]
+  const uint32_t drain = raw_full + 8 * 16 * DEPTH;  // [2] of the issuing warps
+  constexpr int N_BAR = 4 * BUF + 5 + 2 * RING + 16 * DEPTH + 2;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + BAR + 8 * N_BAR);
+  static_assert(8 * N_BAR + 8 <= SCAN - BAR, "");
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  Window* windows = reinterpret_cast<Window*>(smem + S::WINDOW);        // 64 bytes apart
-  int* pid = reinterpret_cast<int*>(smem + S::PAGES);
-  float* pks = reinterpret_cast<float*>(pid + WIN);
-  float* plv = pks + WIN;
+  Chunk* chunks = reinterpret_cast<Chunk*>(smem + CHUNKS);
   const int P = a.c.page, pshift = 31 - __clz(P);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rep = a.n_heads / a.c.n_kv;
 
-  const TreeShare share = tree_share<THREADS>(t, reinterpret_cast<int64_t*>(smem + S::SCAN));
+  const TreeShare share = tree_share<THREADS>(t, reinterpret_cast<int64_t*>(smem + SCAN));
   if (share.hi <= share.lo) return;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < RAW; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 8); }
-    for (int i = 0; i < 2; ++i) mbar_init(&k_ready[i], 4);
-    for (int i = 0; i < 4; ++i) { mbar_init(&s_full[i], 1); mbar_init(&pv_ready[i], 8); mbar_init(&pv_done[i], 1); }
-    for (int i = 0; i < 3; ++i) mbar_init(&drain[i], 1);
+    uint64_t* const bar = reinterpret_cast<uint64_t*>(smem + BAR);
+    for (int i = 0; i < N_BAR; ++i) {
+      const uint32_t at = bars + 8 * i;
+      mbar_init(&bar[i], at < s_full ? 4 : (at < pv_ready ? 1 : (at < pv_done ? 8 : (at < s_free ? 1 : (at < o_free ? 4 :
+                         (at < chunk_full ? 8 : (at < chunk_empty ? 1 : (at < raw_full ? 26 : 1))))))));
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc(tmem_holder, 512);
   tc_fence_before();
-  cta_sync();
+  __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  constexpr uint32_t O_COL = 256;                    // scores: group g, buffer b at column 128 g + 64 b; O: 256 + 128 g
+  // a role whose wait runs out sets the flag and leaves; those that wait for it follow.  All meet at the end
   auto fail = [&]() { omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; };
-  auto window = [&](int k) -> Window& { return *reinterpret_cast<Window*>(reinterpret_cast<uint8_t*>(windows) + (k & 1) * 64); };
-  // items (token tiles) of a group in a window, and the group and item of a tile
-  auto items_of = [](int tiles, bool dual, int g) { return dual ? tiles : (tiles + 1 - g) >> 1; };
+  auto chunk_at = [&](int k) -> Chunk& { return chunks[k % RING]; };
+  auto chunk_wait = [&](int k) { return soon(chunk_full + 8 * (k % RING), (k / RING) & 1); };
+  auto tiles_of = [](const Chunk& w) { return (w.t1 - w.t0 + TT - 1) / TT; };
 
-  // Every role: for each window the barrier that ends the one before, its set-up, the barrier that starts it, its tiles.  A
-  // role whose wait runs out sets the flag, which all see behind the next barrier.  J, N: tiles and items of the windows
-  // before, which give the phases.
-  // registers: 128 x 56 + 256 x 48 + 256 x 160 of the launch's 640 x 96
-  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  if (warp == 0) {
-    TreeWalk walk;
-    walk.start(t, share);
-    Window w;
-    w.t1 = 0; w.flags = LAST;
-    int J = 0;
-    for (int k = 0;; ++k) {
-      if (w.flags & LAST) {
-        if (walk.next(t, &w.p)) {
-          w.flags = FIRST | (TILES > 1 && w.p.R - w.p.r0 > BMR ? DUAL : 0);
-          w.t1 = w.p.t0;
-        } else {
-          w.flags = DONE;
-        }
-      } else {
-        w.flags &= ~FIRST;
-      }
-      if (!(w.flags & DONE)) {
-        w.t0 = w.t1;
-        w.t1 = min(w.p.t1, w.t0 + WIN * P);
-        if (w.t1 == w.p.t1) w.flags |= LAST;
-      }
-      if (lane == 0) window(k) = w;
-      cta_sync();
-      if ((w.flags & DONE) || *abort_flag) break;
-      cta_sync();
-      const int tiles = (w.t1 - w.t0 + TT - 1) / TT, box = min(P, TT), per = TT / box;
-      int i = 0;
-      for (; i < tiles; ++i) {
-        const int st = (J + i) % RAW;
-        // row of the pool of each box that holds tokens, one lane each (-1: none, or a page out of range)
-        const int tk = i * TT + lane * box, id = lane < per && tk < w.t1 - w.t0 ? pid[tk >> pshift] : -1;
-        const int row = id < 0 ? -1 : (id * a.c.n_kv + w.p.g) * P + (tk & (P - 1));
-        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, row >= 0)) * box * HD * 2;
-        if (!warp_wait(&raw_empty[st], (((J + i) / RAW) & 1) ^ 1)) { fail(); break; }
-        uint8_t* dst = smem + S::RAWS + st * RAW_BYTES;
-        if (elect_one()) mbar_expect_tx(&raw_full[st], bytes);
-        __syncwarp();
-        for (int b = 0; b < per; ++b) {
-          const int rb = __shfl_sync(0xffffffffu, row, b);
-          if (rb >= 0 && elect_one()) {
-            tma_load_3d(&tmK, &raw_full[st], dst + b * box * HD, 0, rb, 0);
-            tma_load_3d(&tmV, &raw_full[st], dst + TT * HD + b * box * HD, 0, rb, 0);
-          }
-        }
-        __syncwarp();
-      }
-      if (__any_sync(0xffffffffu, *abort_flag))      // no copy may land after this CTA has left
-        for (int j = max(0, i - RAW); j < i; ++j)
-          if (!wait_phase(&raw_full[(J + j) % RAW], ((J + j) / RAW) & 1)) break;
-      J += tiles;
-    }
-  } else if (warp == 1 || warp == 2) {
-    // ---------------- S of one group: the whole warp runs the loop, one lane issues ----------------
-    const int g = warp - 1;
-    constexpr uint32_t idS = idesc_f16(BMR, TT);
-    const uint64_t dk = sdesc(smem_u32(smem + S::CONV), 16, 1024);
-    int J = 0, N = 0;
-    for (int k = 0;; ++k) {
-      cta_sync();
-      const Window& w = window(k);
-      if ((w.flags & DONE) || *abort_flag) break;
-      cta_sync();
-      tc_fence_after();
-      const bool dual = w.flags & DUAL;
-      const int tiles = (w.t1 - w.t0 + TT - 1) / TT, items = items_of(tiles, dual, g);
-      const uint64_t dq = sdesc(smem_u32(smem + (dual ? g * Q_BYTES : 0)), 16, 1024);
-      for (int n = 0; n < items; ++n) {
-        const int j = J + (dual ? n : 2 * n + g), b = (N + n) & 1;
-        if (!warp_wait(&k_ready[j & 1], (j >> 1) & 1) || !warp_wait(&pv_done[2 * g + b], (((N + n) >> 1) & 1) ^ 1)) { fail(); break; }
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t k0 = dk + (uint64_t)((j & 1) * (OP_BYTES >> 4));
-#pragma unroll
-          for (int c = 0; c < HD / 16; ++c)
-            umma_bf16(tmem + g * 128 + b * TT, dq + (((c >> 2) * (BMR * 128) + (c & 3) * 32) >> 4),
-                      k0 + (((c >> 2) * HALF + (c & 3) * 32) >> 4), idS, c != 0);
-          umma_commit(&s_full[2 * g + b]);
-        }
-        __syncwarp();
-      }
-      J += tiles;
-      N += items;
-    }
-    if (*abort_flag) {                        // products in flight end before the tensor memory is released
-      if (elect_one()) umma_commit(&drain[g]);
-      wait_phase(&drain[g], 0);
-    }
-  } else if (warp == 3) {
-    // ---------------- P V of both groups ----------------
-    constexpr uint32_t idO = idesc_f16(BMR, HD) | (1u << 16);           // V is MN-major
-    const uint64_t dv = sdesc(smem_u32(smem + S::CONV + 2 * OP_BYTES), HALF, 1024);
-    int J = 0, N[2] = {0, 0};
-    bool some[2] = {false, false};            // the group's O holds tiles of this piece
-    for (int k = 0;; ++k) {
-      cta_sync();
-      const Window& w = window(k);
-      if ((w.flags & DONE) || *abort_flag) break;
-      if (w.flags & FIRST) some[0] = some[1] = false;
-      cta_sync();
-      tc_fence_after();
-      const bool dual = w.flags & DUAL;
-      const int tiles = (w.t1 - w.t0 + TT - 1) / TT;
+  // registers: 128 x 48 + 256 x 144 + 512 x 40 of the launch's 896 x 72
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 0) {
+      // ---------------- S: the whole warp runs the loop, one lane issues ----------------
+      constexpr uint32_t idS = idesc_f16(BMR, TT);
+      const uint64_t dk = sdesc(smem_u32(smem + K_CONV), 16, 1024);
+      Place at{0, 0};
+      int g = 0;                              // the tile's group
+      uint32_t q_ph = 0, read_ph = 0;
       bool ok = true;
-      for (int j = 0; j < tiles && ok; ++j) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          if (!dual && (j & 1) != g) continue;
-          const int n = N[g] + (dual ? j : j >> 1), b = n & 1;
-          ok = ok && warp_wait(&pv_ready[2 * g + b], (n >> 1) & 1);
+      for (int k = 0; ok; ++k) {
+        ok = chunk_wait(k);
+        if (!ok) break;
+        const Chunk& w = chunk_at(k);
+        if (w.flags & DONE) break;
+        const int tiles = tiles_of(w);
+        if (w.flags & FIRST) { ok = soon(q_ready, q_ph); q_ph ^= 1; }
+        for (int i = 0; i < tiles && ok; ++i) {
+          ok = soon(k_full + 8 * at.b, at.ph) && soon(s_free + 8 * g, read_ph ^ 1);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t v0 = dv + (uint64_t)(((J + j) & 1) * (OP_BYTES >> 4));
+            const uint64_t k0 = dk + (uint64_t)(at.b * (OP_BYTES >> 4));
 #pragma unroll
-            for (int c = 0; c < TT / 16; ++c)
-              umma_ts(tmem + O_COL + g * HD, tmem + g * 128 + b * TT + c * 8, v0 + ((c * 2048) >> 4), idO, some[g] || c != 0);
-            umma_commit(&pv_done[2 * g + b]);
+            for (int c = 0; c < HD / 16; ++c)
+              umma_ts(tmem + S_COL + g * TT, tmem + Q_COL + c * 8, k0 + (((c >> 2) * HALF + (c & 3) * 32) >> 4), idS, c != 0);
+            commit(s_full + 8 * at.b);
           }
-          some[g] = true;
           __syncwarp();
+          at.move(1);
+          read_ph ^= g;
+          g ^= 1;
         }
-      }
-      J += tiles;
-      for (int g = 0; g < 2; ++g) {           // a window ends with its products, so that the next one finds all free
-        const int items = items_of(tiles, dual, g);
-        N[g] += items;
-        if (ok && items > 0) ok = warp_wait(&pv_done[2 * g + ((N[g] - 1) & 1)], ((N[g] - 1) >> 1) & 1);
+        arrive(chunk_empty + 8 * (k % RING), lane);
       }
       if (!ok) fail();
-    }
-    if (*abort_flag) {
-      if (elect_one()) umma_commit(&drain[2]);
-      wait_phase(&drain[2], 0);
-    }
-  } else if (warp >= 8 && warp < 16) {
-    // ---------------- convert ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    const bool is_v = warp >= 12;
-    const int tid = threadIdx.x & 127, r = tid & 63, h = tid >> 6;      // token, half of its channels
-    const uint32_t x = r & 7, src0 = smem_u32(smem + S::RAWS) + (is_v ? TT * HD : 0) + r * HD;
-    const uint32_t dst0 = smem_u32(smem + S::CONV) + (is_v ? 2 * OP_BYTES : 0) + h * HALF + r * 128;
-    const uint64_t* freed = is_v ? pv_done : s_full;
-    int J = 0, N[2] = {0, 0};
-    for (int k = 0;; ++k) {
-      cta_sync();
-      const Window& w = window(k);
-      if ((w.flags & DONE) || *abort_flag) break;
-      const int np = (w.t1 - w.t0 + P - 1) >> pshift;
-      for (int i = threadIdx.x - 256; i < np; i += 256) attn_page(a, w.p.b, w.p.g, (w.t0 >> pshift) + i, pid + i, pks + i, plv + i);
-      cta_sync();
-      const bool dual = w.flags & DUAL;
-      const int tiles = (w.t1 - w.t0 + TT - 1) / TT;
-      for (int j = 0; j < tiles; ++j) {
-        const int rs = (J + j) % RAW, slot = (J + j) & 1;
-        if (!warp_wait(&raw_full[rs], ((J + j) / RAW) & 1)) { fail(); break; }
-        uint4 u[4];
+    } else if (warp == 1) {
+      // ---------------- P V ----------------
+      constexpr uint32_t idO = idesc_f16(BMR, HD) | (1u << 16);           // V is MN-major
+      const uint64_t dv = sdesc(smem_u32(smem + V_CONV), HALF, 1024);
+      Place at{0, 0};
+      int g = 0;                              // the tile's group
+      bool ok = true, some[2] = {false, false};                           // the group's O holds tiles of this piece
+      for (int k = 0; ok; ++k) {
+        ok = chunk_wait(k);
+        if (!ok) break;
+        const Chunk& w = chunk_at(k);
+        if (w.flags & DONE) break;
+        if (w.flags & FIRST) some[0] = some[1] = false;
+        const int tiles = tiles_of(w);
+        for (int i = 0; i < tiles && ok; ++i) {
+          ok = soon(pv_ready + 8 * at.b, at.ph);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t v0 = dv + (uint64_t)(at.b * (OP_BYTES >> 4));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) u[c] = lds128(src0 + rs * RAW_BYTES + (((4 * h + c) ^ x) << 4));
-        if (j > 1) {                          // the slot's last tile has been read
-          bool ok = true;
-          const int i = j - 2;
-#pragma unroll
-          for (int g = 0; g < 2; ++g)
-            if (dual || (i & 1) == g) {
-              const int n = N[g] + (dual ? i : i >> 1);
-              ok = ok && warp_wait(const_cast<uint64_t*>(&freed[2 * g + (n & 1)]), (n >> 1) & 1);
-            }
-          if (!ok) { fail(); break; }
+            for (int c = 0; c < TT / 16; ++c)
+              umma_ts(tmem + O_COL + g * HD, tmem + P_COL + g * 32 + c * 8, v0 + ((c * 2048) >> 4), idO,
+                      (g ? some[1] : some[0]) || c != 0);
+            commit(pv_done + 8 * at.b);
+          }
+          __syncwarp();
+          some[0] |= g == 0; some[1] |= g == 1;
+          at.move(1);
+          g ^= 1;
         }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) put16(dst0 + slot * OP_BYTES, c, x, u[c]);
-        fence_async_smem();                   // the converted tile -> visible to the tensor core
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&raw_empty[rs]);
-          if (!is_v) {
-            mbar_arrive(&k_ready[slot]);
-          } else {
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-              if (dual || (j & 1) == g) mbar_arrive(&pv_ready[2 * g + ((N[g] + (dual ? j : j >> 1)) & 1)]);
+        arrive(chunk_empty + 8 * (k % RING), lane);
+      }
+      if (!ok) fail();
+    } else if (warp == 2) {
+      // ---------------- the walk ----------------
+      TreeWalk walk;
+      walk.start(t, share);
+      TreePiece p;
+      int t1 = 0, flags = LAST;
+      for (int k = 0;; ++k) {
+        if (flags & LAST) {
+          flags = walk.next(t, &p) ? FIRST : DONE;
+          t1 = p.t0;
+        } else {
+          flags = 0;
+        }
+        const int t0 = t1;
+        if (!(flags & DONE)) {
+          t1 = min(p.t1, t0 + CHUNK);
+          if (t1 == p.t1) flags |= LAST;
+        }
+        if (!soon(chunk_empty + 8 * (k % RING), ((k / RING) & 1) ^ 1)) { fail(); break; }
+        Chunk& w = chunk_at(k);
+        if (!(flags & DONE)) {
+          const int np = (t1 - t0 + P - 1) >> pshift;
+          for (int i = lane; i < np; i += 32) {
+            int id;
+            float4 x;
+            attn_page(a, p.b, p.g, (t0 >> pshift) + i, &id, &x.x, &x.y);
+            x.z = __int_as_float(id < 0 ? -1 : (id * a.c.n_kv + p.g) * P);          // (below 2^31: attention_check)
+            x.w = 0.f;
+            w.page[i] = x;
           }
         }
+        if (flags & FIRST) {                  // the unit's queries to L2, by tokens
+          const int rep = a.n_heads / a.c.n_kv, i0 = p.r0 / rep, i1 = (min(p.R, p.r0 + BMR) + rep - 1) / rep;
+          for (int i = i0 + lane; i < i1; i += 32)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(a.Q + (int64_t)(p.row0 + i) * a.ldq + p.g * rep * HD)), "r"(rep * HD * 2) : "memory");
+        }
+        if (lane == 0) { w.p = p; w.t0 = t0; w.t1 = t1; w.flags = flags; }
+        arrive(chunk_full + 8 * (k % RING), lane);
+        if (flags & DONE) break;
       }
-      J += tiles;
-      for (int g = 0; g < 2; ++g) N[g] += items_of(tiles, dual, g);
+    }
+    // what is in flight ends before the tensor memory is released
+    __syncwarp();
+    if (warp < 2 && *abort_flag) {
+      if (elect_one()) commit(drain + 8 * warp);
+      soon(drain + 8 * warp, 0);
+    }
+  } else if (warp >= 12) {
+    // ---------------- convert ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    const int cw = warp - 12, set = cw >> 3, q = warp & 3;
+    const bool is_v = cw & 4;
+    // 16 codes of channels 16 c .. of tokens 16 q + r + 4 e.  The eight lanes of a load or store phase have the first half of
+    // one token's row and the second half of its neighbour's, whose swizzle differs in the lowest bit: eight
+    // 16-byte bank groups both times
+    const int r = (lane >> 2 & 1) | lane >> 4 << 1, c = (lane & 3) | ((lane >> 2 ^ lane >> 3) & 1) << 2;
+    const uint32_t dst0 = smem_u32(smem + (is_v ? V_CONV : K_CONV)) + (c >> 2) * HALF + (16 * q + r) * 128;
+    const uint32_t x0 = 2 * (c & 3) ^ r;      // chunk of the row, swizzled with r + 4 e
+    const uint8_t* const pool = is_v ? a.c.v : a.c.k;
+    const uint32_t slots = smem_u32(smem + RAW) + cw * (DEPTH * RAW_BYTES), mine = r * HD + c * 16;
+    const uint32_t full = is_v ? pv_ready : k_full, freed = is_v ? pv_done : s_full, got = raw_full + 8 * cw * DEPTH;
+    bool ok = true, done = false;
+    int k = 0, tiles = -1, i = set;           // the chunk fetched from, its tiles (-1: not looked at), the next one of this set's
+    int slot = 0, on_way = 0;                 // the slot to convert, tiles on their way
+    uint32_t ph = 0;
+    Place at{set, 0};
+    while (true) {
+      while (on_way < DEPTH && !done) {       // the next tiles' rows on their way
+        if (tiles < 0) {
+          // while a tile is on its way the next chunk is not waited for: it may come only once that tile's chunk is over
+          if (on_way == 0) ok = chunk_wait(k);
+          else if (!__all_sync(0xffffffffu, bar_test(chunk_full + 8 * (k % RING), (k / RING) & 1))) break;
+          if (!ok) break;
+          done = chunk_at(k).flags & DONE;
+          if (done) break;
+          tiles = tiles_of(chunk_at(k));
+        }
+        if (i >= tiles) {
+          arrive(chunk_empty + 8 * (k % RING), lane);
+          ++k;
+          i -= tiles;                         // of the next chunk
+          tiles = -1;
+          continue;
+        }
+        const Chunk& w = chunk_at(k);
+        const int tk = i * TT + 16 * q, at0 = tk < w.t1 - w.t0 ? __float_as_int(w.page[tk >> pshift].z) : -1, s = slot ^ on_way;
+        if (elect_one()) {
+          if (at0 < 0) {
+            bar_arrive(got + 8 * s);          // unseen, whatever the slot holds
+          } else {
+            fetch_bytes(slots + s * RAW_BYTES, pool + ((int64_t)at0 + (tk & (P - 1))) * HD, RAW_BYTES, got + 8 * s);
+          }
+        }
+        __syncwarp();
+        i += 2;
+        ++on_way;
+      }
+      if (!ok || on_way == 0) break;
+      ok = soon(got + 8 * slot, ph) && soon(freed + 8 * at.b, at.ph ^ 1);
+      if (!ok) break;
+      const uint32_t src = slots + mine + slot * RAW_BYTES, dst = dst0 + at.b * OP_BYTES;
+#pragma unroll 1
+      for (int e = 0; e < 4; e += 2) {
+        const uint4 u = lds128(src + e * 4 * HD), v = lds128(src + (e + 1) * 4 * HD);
+        const uint32_t to = dst + e * 4 * 128;
+        sts128(to + (x0 << 4), make_uint4(codes_lo(u.x), codes_hi(u.x), codes_lo(u.y), codes_hi(u.y)));
+        sts128(to + ((x0 ^ 1) << 4), make_uint4(codes_lo(u.z), codes_hi(u.z), codes_lo(u.w), codes_hi(u.w)));
+        sts128(to + 4 * 128 + ((x0 ^ 4) << 4), make_uint4(codes_lo(v.x), codes_hi(v.x), codes_lo(v.y), codes_hi(v.y)));
+        sts128(to + 4 * 128 + ((x0 ^ 5) << 4), make_uint4(codes_lo(v.z), codes_hi(v.z), codes_lo(v.w), codes_hi(v.w)));
+      }
+      slot ^= 1;
+      ph ^= slot == 0;
+      --on_way;
+      fence_async_smem();                     // the converted tile -> visible to the tensor core
+      arrive(full + 8 * at.b, lane);              // (and the slot has been read)
+      at.move(2);
+    }
+    if (!ok) {                                // no copy may land after this CTA has left
+      fail();
+      for (int s = slot; on_way > 0; --on_way, s ^= 1, ph ^= s == 0) soon(got + 8 * s, ph);
     }
   } else {
     // ---------------- softmax: one row per thread ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
-    constexpr int SPAN = BMR / CP, TW = TT / CP;              // rows held, tokens of a thread
-    const int sg = warp >= 16, qw = warp & 3, r = qw * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)(qw * 32) << 16), s_col = lanes + sg * 128;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    constexpr int SPAN = BMR / CP, TW = TT / CP, QT = TW / NQ;          // rows held, tokens of a thread, of them on a page
+    const int rep = a.n_heads / a.c.n_kv;
+    const int sg = warp >= 8, qw = warp & 3, r = qw * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(qw * 32) << 16), o_col = lanes + O_COL + sg * HD;
     const int w0 = r / SPAN * TW;                             // this copy's tokens of a tile
-    float m = ATTN_NOTHING, d = ATTN_NO_VALUE, l = 0.f;
-    int N = 0, n_piece = 0;                                   // items of the windows before, of the piece's
-    for (int k = 0;; ++k) {
-      cta_sync();
-      const Window& w = window(k);
-      if ((w.flags & DONE) || *abort_flag) break;
-      const bool dual = w.flags & DUAL;
-      const int start = w.p.len - w.p.nq, np = (w.t1 - w.t0 + P - 1) >> pshift;
-      if (w.flags & FIRST) {
-        // the query operand: fp16, K-major, 128-byte swizzle, two halves of 64 channels; a warp's rows in batches
-        m = ATTN_NOTHING; d = ATTN_NO_VALUE; l = 0.f;
-        n_piece = 0;
-        const SeqRows s{w.p.row0, w.p.nq, w.p.len, true};
-        const int held = TILES > 1 && dual ? 2 * BMR : SPAN;
-        const int wid = sg * 4 + qw;
-        for (int i0 = wid * 8; i0 < held; i0 += 64) {
-          uint2 u[8];
+    const uint32_t s_col = lanes + S_COL + sg * TT, p_col = lanes + P_COL + sg * 32;
+    uint32_t meet_ph = 0;
+    auto all_meet = [&]() { arrive(meet, lane); meet_ph ^= 1; return soon(meet, meet_ph ^ 1); };
+
+    // the piece's rows
+    float m = ATTN_NOTHING, d = ATTN_NO_VALUE, l = 0.f, f = 0.f;
+    int token = -1;                                           // its row of the packed arrays; -1: none
+    int J = 0;                                                // tiles before
+    auto queries = [&](const Chunk& w) {
+      // Rows in fp16 under a power of two, 16 lanes per row, through shared memory to the row's two threads, 64 channels each
+      constexpr int RW = SPAN / 8;
+      const int r0 = (sg * 4 + qw) * RW;
+      uint4 u[RW / 2];
+      {
+        int row = w.p.r0 + r0 + (lane >> 4), h = row % rep;
+        const __nv_bfloat16* from = a.Q + (int64_t)(w.p.row0 + row / rep) * a.ldq + w.p.g * rep * HD + 8 * (lane & 15);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) u[e] = attn_query_raw(a, s, w.p.g, rep, w.p.r0 + i0 + e, i0 + e < held ? w.p.R : 0, lane);
+        for (int e = 0; e < RW / 2; ++e) {
+          u[e] = row < w.p.R ? __ldg(reinterpret_cast<const uint4*>(from + h * HD)) : make_uint4(0, 0, 0, 0);
+          row += 2;
+          h += 2;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int i = i0 + e;
-            if (i >= held) break;
-            float v[4];
-            int sh;
-            attn_query_scaled(u[e], v, &sh);
-            const uint2 h = make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]));
-            const int tile = TILES > 1 ? i >> 7 : 0;
-            for (int rr = i & (BMR - 1); rr < BMR; rr += SPAN) {
-              uint8_t* row = smem + tile * Q_BYTES + (lane >> 4) * (BMR * 128) + rr * 128;
-              *reinterpret_cast<uint2*>(row + (((lane & 15) >> 1 ^ (rr & 7)) << 4) + (lane & 1) * 8) = h;
-              if (lane == 0) {
-                qs[tile * BMR + rr] = __uint_as_float((uint32_t)(127 - sh) << 23);
-                token[tile * BMR + rr] = w.p.row0 + min(w.p.r0 + i, w.p.R - 1) / rep;
-              }
-            }
-          }
+          for (int z = 0; z < 2; ++z)
+            if (h >= rep) { h -= rep; from += a.ldq; }
         }
-        fence_async_smem();
       }
-      cta_sync();
-      const int at = (dual ? sg * BMR : 0) + r;               // the thread's row of those held
-      const int row = w.p.r0 + (dual ? sg * BMR : 0) + (r & (SPAN - 1));
-      const bool mine = row < w.p.R, idle = __all_sync(0xffffffffu, !mine);
-      const float f = qs[at];
-      const uint32_t* const bits = a.seen + (int64_t)token[at] * a.words;
-      const int items = items_of((w.t1 - w.t0 + TT - 1) / TT, dual, sg);
-      bool ok = true;
-      for (int n = 0; n < items; ++n) {
-        // the 16-token quarters, each of one page: score factor, log2 of the value scale; the tokens that
-        // this row sees, as bits
-        const int j = dual ? n : 2 * n + sg, b = (N + n) & 1, t0 = w.t0 + j * TT + w0;
-        const uint32_t col = s_col + b * TT;
-        float fk[TW / 16], lv[TW / 16];
-        uint64_t seen = ~0ull;
-        bool whole = t0 + TW <= start;
-        if (!whole) seen = attn_window(bits, mine ? a.words : 0, w.p.nq, t0 - start);
+      if (!all_meet()) return false;                          // the stage has been read
+      const uint32_t rows = smem_u32(smem + STAGE);
+      float* const factor = reinterpret_cast<float*>(smem + ROW);
 #pragma unroll
-        for (int q = 0; q < TW / 16; ++q) {
-          const int pi = min((j * TT + w0 + 16 * q) >> pshift, np - 1);
-          fk[q] = pks[pi] * f;
-          lv[q] = plv[pi];
-          if (pid[pi] < 0) {
-            whole = false;
-            seen &= ~(0xffffull << (16 * q));
-          }
+      for (int e = 0; e < RW / 2; ++e) {
+        const uint32_t y[4] = {u[e].x, u[e].y, u[e].z, u[e].w};
+        uint32_t big = 0;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) big = max(big, max(y[z] << 16 & 0x7fffffffu, y[z] & 0x7fff0000u));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+        const int sh = big == 0 ? 0 : min(13 + 127 - (int)(big >> 23), 126), i = r0 + 2 * e + (lane >> 4);
+        const float up = __uint_as_float((uint32_t)(127 + sh) << 23);         // as attn_query_scaled
+        uint32_t z[4];
+#pragma unroll
+        for (int o = 0; o < 4; ++o) z[o] = pack_half2(__uint_as_float(y[o] << 16) * up, __uint_as_float(y[o] & 0xffff0000u) * up);
+        sts128(rows + i * 256 + (((lane & 15) ^ (i & 15)) << 4), make_uint4(z[0], z[1], z[2], z[3]));
+        if ((lane & 15) == 0) factor[i] = __uint_as_float((uint32_t)(127 - sh) << 23);
+      }
+      if (!all_meet()) return false;
+      const int i = r & (SPAN - 1), row = w.p.r0 + i;
+      token = row < w.p.R ? w.p.row0 + row / rep : -1;
+      f = factor[i];
+      // the scores of the piece before are all formed
+      if (J > 0 && !soon(s_full + 8 * ((J - 1) % BUF), ((J - 1) / BUF) & 1)) return false;
+#pragma unroll
+      for (int c = 8 * sg; c < 8 * sg + 8; c += 2) {
+        const uint4 x = lds128(rows + i * 256 + ((c ^ (i & 15)) << 4)), y = lds128(rows + i * 256 + (((c + 1) ^ (i & 15)) << 4));
+        const uint32_t z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        tmem_st8(lanes + Q_COL + c * 4, z);
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      tc_fence_before();
+      arrive(q_ready, lane);
+      return true;
+    };
+
+    // a tile's scores to weights
+    auto tile = [&](const Chunk& w, const int i, const int before, const int seen_all, const int np, const Place at) {
+      const Place prev = at.before();         // of the group's last tile (before the first: a phase that is over)
+      // score factor and log2 of the value scale of each page; the tokens that this row sees, as bits
+      const int o = i * TT + w0;
+      float fk[NQ], lv[NQ];
+      uint64_t seen = ~0ull;
+      bool whole = o + TW <= seen_all;
+      if (!whole) seen = attn_window(a.seen + (int64_t)max(token, 0) * a.words, token >= 0 ? a.words : 0, w.p.nq, o - seen_all);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const float4 pg = w.page[min((o + QT * q) >> pshift, np - 1)];
+        fk[q] = pg.x * f;
+        lv[q] = pg.y;
+        if (__float_as_int(pg.z) < 0) {
+          whole = false;
+          seen &= ~(((1ull << (QT - 1) << 1) - 1) << (QT * q));
         }
-        ok = warp_wait(&s_full[2 * sg + b], ((N + n) >> 1) & 1);
-        if (!ok) { fail(); break; }
-        tc_fence_after();
-        if (!idle) {
+      }
+      if (!soon(s_full + 8 * at.b, at.ph)) return false;
+      tc_fence_after();
+      if (__any_sync(0xffffffffu, token >= 0)) {
         float x[TW];
         if (TW == 16) {
-          tmem_ld16(col + w0, x);
+          tmem_ld16(s_col + w0, x);
         } else {
 #pragma unroll
-          for (int c = 0; c < TW; c += 32) tmem_ld32(col + w0 + c, x + c);
+          for (int c = 0; c < TW; c += 32) tmem_ld32_async(s_col + w0 + c, x + c);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+          for (int c = 0; c < TW; ++c) asm volatile("" : "+f"(x[c]));
         }
-        if (!whole) {
-          // what the row does not see: minus infinity under any positive factor.  A page without a token that it sees gets
+        tc_fence_before();
+        arrive(s_free + 8 * sg, lane);
+        if (!whole) {                         // what the row does not see
+#pragma unroll
+          for (int c = 0; c < TW; ++c)
+            if (!((seen >> c) & 1)) x[c] = -INFINITY;
+          // the unseen stay minus infinity under any positive factor.  A page without a token that the row sees gets
           // the factor 1 and no value scale, whatever it has; a factor of zero makes way for one that changes no score
 #pragma unroll
-          for (int q = 0; q < TW / 16; ++q) {
-            const uint32_t sb = (uint32_t)(seen >> (16 * q)) & 0xffffu;
-            if (sb == 0) { fk[q] = 1.f; lv[q] = -INFINITY; }
+          for (int q = 0; q < NQ; ++q) {
+            if ((seen >> (QT * q) & ((1ull << (QT - 1) << 1) - 1)) == 0) { fk[q] = 1.f; lv[q] = -INFINITY; }
             else if (fk[q] == 0.f) fk[q] = 1e-30f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!((sb >> i) & 1)) x[16 * q + i] = -INFINITY;
           }
         }
         // the row's largest score (factors are not negative), and how far it passes m + d with the value scale
-        float top = -INFINITY, far = -INFINITY, xm[TW / 16];
+        float top = -INFINITY, far = -INFINITY, xm[NQ];
 #pragma unroll
-        for (int q = 0; q < TW / 16; ++q) {
+        for (int q = 0; q < NQ; ++q) {
           float mx[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mx[i] = fmaxf(fmaxf(x[16 * q + i], x[16 * q + 4 + i]), fmaxf(x[16 * q + 8 + i], x[16 * q + 12 + i]));
-          const float mq = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          for (int c = 0; c < 4; ++c) mx[c] = x[QT * q + c];
+#pragma unroll
+          for (int c = 4; c + 8 <= QT; c += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], x[QT * q + c + e], x[QT * q + c + 4 + e]);
+          static_assert(QT % 8 == 0, "");
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], x[QT * q + QT - 4 + e]);
+          const float mq = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
           xm[q] = mq == -INFINITY ? -INFINITY : mq * fk[q];
           top = fmaxf(top, xm[q]);
           far = fmaxf(far, (xm[q] - m) + (lv[q] - d));
         }
+        // the weights and the accumulator of the group's last tile are done with
+        if (!soon(pv_done + 8 * prev.b, prev.ph)) return false;
+        tc_fence_after();
         if (__any_sync(0xffffffffu, top - m > ATTN_SLACK || far > ATTN_SLACK)) {
           const float mn = fmaxf(m, top), drop = m - mn;
           float dn = fmaxf(d + drop, ATTN_NO_VALUE);
 #pragma unroll
-          for (int q = 0; q < TW / 16; ++q) dn = fmaxf(dn, (xm[q] - mn) + lv[q]);
+          for (int q = 0; q < NQ; ++q) dn = fmaxf(dn, (xm[q] - mn) + lv[q]);
           const float grow = ex2((d - dn) + drop);
           l *= ex2(drop);
           m = mn;
           d = dn;
-          if (n_piece + n > 0) {              // O of the tiles before
-            const int last = N + n - 1;
-            ok = warp_wait(&pv_done[2 * sg + (last & 1)], (last >> 1) & 1);
-            if (!ok) { fail(); break; }
-            tc_fence_after();
+          if (before + i > 1) {               // O of the group's tiles before
 #pragma unroll 1
             for (int c = 0; c < HD; c += 16) {
               float v[16];
-              tmem_ld16(lanes + O_COL + sg * HD + c, v);
+              tmem_ld16(o_col + c, v);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] *= grow;
-              tmem_st8(lanes + O_COL + sg * HD + c, reinterpret_cast<const uint32_t(&)[8]>(v[0]));
-              tmem_st8(lanes + O_COL + sg * HD + c + 8, reinterpret_cast<const uint32_t(&)[8]>(v[8]));
+              for (int e = 0; e < 16; ++e) v[e] *= grow;
+              tmem_st8(o_col + c, reinterpret_cast<const uint32_t(&)[8]>(v[0]));
+              tmem_st8(o_col + c + 8, reinterpret_cast<const uint32_t(&)[8]>(v[8]));
             }
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           }
         }
-        // x fk - m below is one operation, whose exact product differs from the rounded one in m by up to
-        // 2^-25 |m|: scores of such size are rounded first
-        if (fabsf(m) > 1048576.f) {
+        // A weight is p = 2^(x fk - m) times c = 2^e for its page's value scale, l the sum of p.  Where e is moderate it goes
+        // into the exponent, and the sum is divided by c: one product less per pair.  e - m rounds to 2^-19 for
+        // |m| below 64; beyond, and for pages whose values vanish beside the others', p and c stay apart.
+        float e[NQ];
+        bool apart = fabsf(m) > 64.f;
 #pragma unroll
-          for (int q = 0; q < TW / 16; ++q) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[16 * q + i] *= fk[q];
-            fk[q] = 1.f;
-          }
+        for (int q = 0; q < NQ; ++q) {
+          e[q] = lv[q] - d + ATTN_SHIFT;
+          apart = apart || !(fabsf(e[q]) < 100.f);
         }
-        float2 ls = make_float2(0.f, 0.f), lt = ls;
-        const float2 nm = make_float2(-m, -m);
+        auto weights = [&](auto kind) {
+          constexpr bool together = decltype(kind)::value;
 #pragma unroll
-        for (int q = 0; q < TW / 16; ++q) {
-          uint32_t pw[8];
-          const float c = attn_factor(lv[q] - d + ATTN_SHIFT);
-          const float2 c2 = make_float2(c, c), f2 = make_float2(fk[q], fk[q]);
+          for (int q = 0; q < NQ; ++q) {
+            const float cq = together ? 0.f : attn_factor(e[q]), s = together ? e[q] - m : -m;
+            const float2 f2 = make_float2(fk[q], fk[q]), s2 = make_float2(s, s);
+            constexpr int BW = QT < 16 ? QT : 16;
+            float2 ls[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 u = omq_fma2(make_float2(x[16 * q + 2 * i], x[16 * q + 2 * i + 1]), f2, nm);
-            const float2 p = make_float2(ex2(u.x), ex2(u.y));
-            if (i & 1) lt = omq_add2(lt, p);
-            else ls = omq_add2(ls, p);
-            const float2 e = omq_mul2(p, c2);
-            pw[i] = pack_half2(e.x, e.y);
+            for (int h = 0; h < 4; ++h) ls[h] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int o = 0; o < QT; o += BW) {
+              float2 y[BW / 2];
+#pragma unroll
+              for (int h = 0; h < BW / 2; ++h) y[h] = omq_fma2(make_float2(x[QT * q + o + 2 * h], x[QT * q + o + 2 * h + 1]), f2, s2);
+#pragma unroll
+              for (int h = 0; h < BW / 2; ++h) y[h] = make_float2(ex2(y[h].x), ex2(y[h].y));
+#pragma unroll
+              for (int h = 0; h < BW / 2; ++h) ls[h & 3] = omq_add2(ls[h & 3], y[h]);
+              if (!together) {
+#pragma unroll
+                for (int h = 0; h < BW / 2; ++h) { y[h].x *= cq; y[h].y *= cq; }
+              }
+              uint32_t pw[8];
+#pragma unroll
+              for (int h = 0; h < BW / 2; ++h) pw[h] = pack_half2(y[h].x, y[h].y);
+              tmem_st8(p_col + (w0 + QT * q + o) / 2, pw);
+            }
+            ls[0] = omq_add2(omq_add2(ls[0], ls[1]), omq_add2(ls[2], ls[3]));
+            l = together ? fmaf(ls[0].x + ls[0].y, ex2(-e[q]), l) : l + (ls[0].x + ls[0].y);
           }
-          tmem_st8(col + w0 / 2 + 8 * q, pw);                 // to the scores' first 32 columns
-        }
-        ls = omq_add2(ls, lt);
-        l += ls.x + ls.y;
-        if (CP > 1) {                         // the other copies' tokens weigh nothing here
-          const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        };
+        if (!__any_sync(0xffffffffu, apart)) {
+          weights(std::true_type());
+        } else {
+          // x fk - m is one operation, whose exact product differs from the rounded one in m by up to 2^-25 |m|: scores of such
+          // size are rounded first
+          if (fabsf(m) > 1048576.f) {
 #pragma unroll
-          for (int c = 0; c < TT / 16; ++c)
-            if (c / (TW / 16) != r / SPAN) tmem_st8(col + 8 * c, zero);
+            for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+              for (int h = 0; h < QT; ++h) x[QT * q + h] *= fk[q];
+              fk[q] = 1.f;
+            }
+          }
+          weights(std::false_type());
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&pv_ready[2 * sg + b]);
+      } else {
+        arrive(s_free + 8 * sg, lane);
+        if (!soon(pv_done + 8 * prev.b, prev.ph)) return false;
       }
-      N += items;
-      n_piece += items;
-      if (!(w.flags & LAST)) continue;
+      tc_fence_before();
+      arrive(pv_ready + 8 * at.b, lane);
+      return true;
+    };
+
+    if (CP > 1) {                             // the other copies' tokens weigh nothing here
+      const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) tmem_st8(p_col + c, zero);
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+    }
+    uint32_t o_ph = 1;
+    Place at{sg, 0};                          // of the group's next tile
+    bool ok = chunk_wait(0);
+    if (ok && !(chunk_at(0).flags & DONE)) ok = queries(chunk_at(0));
+    for (int k = 0; ok; ++k) {
+      const Chunk& w = chunk_at(k);
+      if (w.flags & DONE) break;
+      const int first = (w.p.t1 - w.p.t0 + TT - 1) / TT;      // tiles of the piece
+      const int piece0 = (w.t0 - w.p.t0) / TT;                // its tiles before this chunk
+      const int J0 = J - piece0, tiles = tiles_of(w), seen_all = w.p.len - w.p.nq - w.t0, np = (w.t1 - w.t0 + P - 1) >> pshift;
+      if (w.flags & FIRST) {
+        m = ATTN_NOTHING; d = ATTN_NO_VALUE; l = 0.f;
+        ok = soon(o_free, o_ph);              // the piece before has read its accumulators
+        o_ph ^= 1;
+      }
+      for (int i = (J ^ sg) & 1; i < tiles && ok; i += 2) {
+        ok = tile(w, i, piece0, seen_all, np, at);
+        at.move(2);
+      }
+      J += tiles;
+      if (!ok) break;
+      if (!(w.flags & LAST)) { arrive(chunk_empty + 8 * (k % RING), lane); ok = chunk_wait(k + 1); continue; }
+      // what the piece's end needs of this piece's rows
+      const bool mine_now = token >= 0;
+      const int row = w.p.r0 + (r & (SPAN - 1));
+      // the next piece's queries, once this one's scores are all formed
+      ok = chunk_wait(k + 1);
+      if (ok && !(chunk_at(k + 1).flags & DONE)) ok = queries(chunk_at(k + 1));
+      if (!ok) break;
 
       // ---- the piece's end: O over the sum of weights, to the outputs or the partial results ----
-      if (ok && items > 0) {
-        const int last = N - 1;
-        ok = warp_wait(&pv_done[2 * sg + (last & 1)], (last >> 1) & 1);
-        if (!ok) fail();
+      const int n_a = (first + ((J0 & 1) == 0)) >> 1, n_b = first - n_a;  // tiles of the two groups
+      if (sg == 0 ? n_a > 0 : n_b > 0) {
+        const Place prev = at.before();
+        ok = soon(pv_done + 8 * prev.b, prev.ph);
+        if (!ok) break;
       }
       tc_fence_after();
-      float c0, c1 = 0.f, lse;
-      if (TILES > 1 && dual) {
-        const bool none = l == 0.f;                           // a NaN score is not an empty row
-        c0 = none ? 0.f : ex2(d - ATTN_SHIFT) / l;
-        lse = none ? -INFINITY : m + log2f(l);
-        if (none || n_piece == 0) c0 = 0.f;
-      } else {
-        refs[(sg * 3 + 0) * BMR + r] = m;
-        refs[(sg * 3 + 1) * BMR + r] = d;
-        refs[(sg * 3 + 2) * BMR + r] = l;
-        tc_fence_before();
-        group_sync(3, 256);                                   // both groups' references, and their products are done
-        tc_fence_after();
-        float mm = ATTN_NOTHING, dd = ATTN_NO_VALUE, L = 0.f;
-        for (int c = 0; c < CP; ++c)
+      float* const refs = reinterpret_cast<float*>(smem + REF);
+      refs[(sg * 3 + 0) * BMR + r] = m;
+      refs[(sg * 3 + 1) * BMR + r] = d;
+      refs[(sg * 3 + 2) * BMR + r] = l;
+      tc_fence_before();
+      ok = all_meet();                                        // both groups' references, and their products are done
+      if (!ok) break;
+      tc_fence_after();
+      float mm = ATTN_NOTHING, dd = ATTN_NO_VALUE, L = 0.f;
+      for (int c = 0; c < CP; ++c)
 #pragma unroll
-          for (int g = 0; g < 2; ++g) mm = fmaxf(mm, refs[g * 3 * BMR + c * SPAN + (r & (SPAN - 1))]);
-        for (int c = 0; c < CP; ++c)
+        for (int g = 0; g < 2; ++g) mm = fmaxf(mm, refs[g * 3 * BMR + c * SPAN + (r & (SPAN - 1))]);
+      for (int c = 0; c < CP; ++c)
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const int i = g * 3 * BMR + c * SPAN + (r & (SPAN - 1));
-            dd = fmaxf(dd, (refs[i] - mm) + refs[i + BMR]);
-            L += refs[i + 2 * BMR] * ex2(refs[i] - mm);
-          }
-        const bool none = L == 0.f;
-        const float c = none ? 0.f : ex2(dd - ATTN_SHIFT) / L;
-        c0 = none ? 0.f : c * ex2((refs[r] - mm) + refs[BMR + r] - dd);
-        c1 = none ? 0.f : c * ex2((refs[3 * BMR + r] - mm) + refs[4 * BMR + r] - dd);
-        lse = none ? -INFINITY : mm + log2f(L);
-      }
-      const int n_a = dual ? n_piece : (sg == 0 ? n_piece : (w.p.t1 - w.p.t0 + 2 * TT - 1) / (2 * TT));      // group 0's tiles
-      const int n_b = dual ? 0 : (w.p.t1 - w.p.t0 + TT - 1) / TT - n_a;
-      const int first = w.p.r0 + (dual ? sg * BMR : 0), rows = min(dual ? BMR : SPAN, w.p.R - first);
-      if (mine && (dual || sg == 0) && r < SPAN) {
-        if (w.p.part >= 0) t.pl[(int64_t)w.p.part * t.cost.rows + (dual ? sg * BMR : 0) + r] = lse;
+        for (int g = 0; g < 2; ++g) {
+          const int i = g * 3 * BMR + c * SPAN + (r & (SPAN - 1));
+          dd = fmaxf(dd, (refs[i] - mm) + refs[i + BMR]);
+          L += refs[i + 2 * BMR] * ex2(refs[i] - mm);
+        }
+      const bool none = L == 0.f;                             // a NaN score is not an empty row
+      const float c = none ? 0.f : ex2(dd - ATTN_SHIFT) / L;
+      const float c0 = none ? 0.f : c * ex2((refs[r] - mm) + refs[BMR + r] - dd);
+      const float c1 = none ? 0.f : c * ex2((refs[3 * BMR + r] - mm) + refs[4 * BMR + r] - dd);
+      const float lse = none ? -INFINITY : mm + log2f(L);
+      if (mine_now && sg == 0 && r < SPAN) {
+        if (w.p.part >= 0) t.pl[(int64_t)w.p.part * t.cost.rows + r] = lse;
         else if (a.lse) a.lse[(int64_t)(w.p.row0 + row / rep) * a.n_heads + w.p.g * rep + row % rep] = lse;
       }
-      // 64 channels at a time through shared memory (the queries' own tile: its last product is done), rows of 256 bytes
-      const uint32_t stage = smem_u32(dual ? smem + sg * Q_BYTES : (sg == 0 ? smem : smem + S::CONV));
-      for (int hf = dual ? 0 : sg; hf < (dual ? 2 : sg + 1); ++hf) {
+      // 64 channels of each group, 32 at a time through shared memory to rows of 128 bytes
+      constexpr int RO = SPAN / 4;                            // rows that a warp writes
+      const int q0 = qw * RO + (lane >> 3), rows = min(min(SPAN, w.p.R - w.p.r0), (qw + 1) * RO);
+      const uint32_t stage = smem_u32(smem + STAGE) + sg * (BMR * 128);
+      const int h0 = (w.p.r0 + q0) % rep, step_h = 4 % rep;
+      const int64_t to0 = (int64_t)(w.p.row0 + (w.p.r0 + q0) / rep) * a.ldo + w.p.g * rep * HD + 4 * (lane & 7), step = 4 / rep * a.ldo;
 #pragma unroll 1
-        for (int ch = 0; ch < 64; ch += 32) {
-          float v[32], u[32];
-          const uint32_t o = lanes + O_COL + hf * 64 + ch;
-          if (n_a > 0) tmem_ld32(o + (dual ? sg * HD : 0), v);
-          if (n_b > 0) tmem_ld32(o + HD, u);
+      for (int ch = sg * 64; ch < sg * 64 + 64; ch += 32) {
+        if (CP > 1 && (ch & 32)) ok = all_meet();             // the stage has been read
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+        for (int b = 0; b < 32; b += 16) {
+          float v[16], u[16];
+          const uint32_t o = lanes + O_COL + ch + b;
+          if (n_a > 0) tmem_ld16(o, v);
+          if (n_b > 0) tmem_ld16(o + HD, u);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
             const float y = n_a > 0 && c0 != 0.f ? v[i] * c0 : 0.f;
             v[i] = n_b > 0 && c1 != 0.f ? fmaf(u[i], c1, y) : y;
           }
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            sts128(stage + r * 256 + ((((ch + i) >> 2) ^ (r & 15)) << 4),
+          for (int i = 0; i < 16; i += 4)
+            sts128(stage + r * 128 + ((((b + i) >> 2) ^ (r & 7)) << 4),
                    make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
         }
-        group_sync(1 + sg, 128);
-        const int n_rows = *abort_flag ? 0 : rows;
-        for (int q = 2 * qw + (lane >> 4); q < n_rows; q += 8) {        // half a row per half warp
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (ch & 32) {                                        // the accumulators have been read
+          tc_fence_before();
+          arrive(o_free, lane);
+        }
+        if (CP > 1) ok = ok && all_meet();
+        else __syncwarp();
+        if (!ok) break;
+        int h = h0;
+        int64_t to = to0 + ch;
 #pragma unroll
-          for (int c = 0; c < CP; ++c) {
-            const int i = c * SPAN + q;
-            const uint4 y = lds128(stage + i * 256 + (((lane & 15) ^ (i & 15)) << 4));
-            o.x += __uint_as_float(y.x); o.y += __uint_as_float(y.y); o.z += __uint_as_float(y.z); o.w += __uint_as_float(y.w);
-          }
-          const int rw = first + q, ch = hf * 64 + 4 * (lane & 15);
-          if (w.p.part >= 0) {
-            *reinterpret_cast<float4*>(t.po + ((int64_t)w.p.part * t.cost.rows + (rw - w.p.r0)) * HD + ch) = o;
-          } else {
-            const int64_t to = (int64_t)(w.p.row0 + rw / rep) * a.ldo + (w.p.g * rep + rw % rep) * HD + ch;
-            if (a.Of) *reinterpret_cast<float4*>(a.Of + to) = o;
-            if (a.Ob) {
-              uint2 y;
-              __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&y);
-              h[0] = __floats2bfloat162_rn(o.x, o.y);
-              h[1] = __floats2bfloat162_rn(o.z, o.w);
-              *reinterpret_cast<uint2*>(a.Ob + to) = y;
+        for (int n = 0; n < RO / 4; ++n) {                    // a row per eight lanes
+          const int q = q0 + 4 * n;
+          if (q < rows) {
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < CP; ++c) {
+              const int i = c * SPAN + q;
+              const uint4 y = lds128(stage + i * 128 + (((lane & 7) ^ (i & 7)) << 4));
+              o.x += __uint_as_float(y.x); o.y += __uint_as_float(y.y); o.z += __uint_as_float(y.z); o.w += __uint_as_float(y.w);
+            }
+            if (w.p.part >= 0) {
+              *reinterpret_cast<float4*>(t.po + ((int64_t)w.p.part * t.cost.rows + q) * HD + ch + 4 * (lane & 7)) = o;
+            } else {
+              if (a.Of) *reinterpret_cast<float4*>(a.Of + to + h * HD) = o;
+              if (a.Ob) {
+                uint2 y;
+                __nv_bfloat162* b2 = reinterpret_cast<__nv_bfloat162*>(&y);
+                b2[0] = __floats2bfloat162_rn(o.x, o.y);
+                b2[1] = __floats2bfloat162_rn(o.z, o.w);
+                *reinterpret_cast<uint2*>(a.Ob + to + h * HD) = y;
+              }
             }
           }
+          to += step;
+          h += step_h;
+          if (h >= rep) { h -= rep; to += a.ldo; }
         }
-        group_sync(1 + sg, 128);
       }
-      tc_fence_before();
+      if (!ok) break;
+      arrive(chunk_empty + 8 * (k % RING), lane);
     }
+    if (!ok) fail();
   }
   tc_fence_before();
-  cta_sync();
+  __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
 }
 
-template <int CP, int TILES>
+template <int CP, int NQ>
 omq_status launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
-  auto kern = kv_attention_tree_tc_kernel<CP, TILES>;
+  auto kern = kv_attention_tree_tc_kernel<CP, NQ>;
   static std::atomic<uint64_t> allowed{0};
-  OMQ_TRY(omq_allow_smem(allowed, kern, Smem<TILES>::BYTES));
-  CUtensorMap tk, tv;
-  const omq_kv_cache& c = t.a.c;
-  const int64_t rows = (int64_t)c.n_pages * c.n_kv * c.page;
-  const int box = c.page < TT ? c.page : TT;
-  if (!omq_make_map_u8(&tk, c.k, HD, rows, HD, box, HD) || !omq_make_map_u8(&tv, c.v, HD, rows, HD, box, HD))
-    return OMQ_ERR_UNSUPPORTED;
-  kern<<<n_ctas, THREADS, Smem<TILES>::BYTES, st>>>(tk, tv, t);
+  OMQ_TRY(omq_allow_smem(allowed, kern, SMEM));
+  kern<<<n_ctas, THREADS, SMEM, st>>>(t);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
@@ -619,8 +776,8 @@ omq_status launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
 // By the most rows that a KV head has in the call.
 omq_status tree_tc_launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
   const int64_t rows = (int64_t)t.a.max_q * (t.a.n_heads / t.a.c.n_kv);
+  const int page = t.a.c.page;
   if (rows <= BMR / 4) return launch<4, 1>(st, t, n_ctas);
-  if (rows <= BMR / 2) return launch<2, 1>(st, t, n_ctas);
-  if (rows <= BMR) return launch<1, 1>(st, t, n_ctas);
-  return launch<1, 2>(st, t, n_ctas);
+  if (rows <= BMR / 2) return page >= 32 ? launch<2, 1>(st, t, n_ctas) : launch<2, 2>(st, t, n_ctas);
+  return page >= TT ? launch<1, 1>(st, t, n_ctas) : launch<1, 4>(st, t, n_ctas);
 }
