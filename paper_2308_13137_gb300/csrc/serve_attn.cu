@@ -506,33 +506,22 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = L == 0.f ? -INFINITY : ref + log2f(L);
 }
 
-// The same for the cut units of draft trees: partial results of the CTAs whose shares hold tokens of the row's unit, in
-// order of tokens
+// The same for the cut units of draft trees: a unit per blockIdx.x, its rows a warp each
 __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeArgs t) {
-  const AttnArgs& a = t.a;
-  const int b = blockIdx.y, lane = threadIdx.x & 31, rep = a.n_heads / a.c.n_kv;
-  const int idx = blockIdx.x * 8 + (threadIdx.x >> 5);
-  const TreeSeq q = tree_seq(t, b);
-  const int i = idx / a.n_heads, head = idx % a.n_heads;
-  if (i >= q.nq || q.slots == 0) return;
-  const int row = i * rep + head % rep, tile = row / t.cost.rows, w = tree_weight(t, q, tile);
-  const int64_t at = t.before[b] + (head / rep) * q.head + tile * q.full, end = at + t.cost.start + (int64_t)q.slots * w;
-  const int64_t total = t.work->total, n = t.work->n;
-  int c0 = (int)(((at + 1) * n - 1) / total), c1 = (int)((end * n - 1) / total);       // CTAs of its two ends
-  // the first ones may have no more than the unit's start
-  while (c0 < c1 && tree_slots(t, q, w, at, tree_border(total, n, c0 + 1)) == 0) ++c0;
-  if (c0 == c1) return;                                       // whole
-  const int64_t lo0 = tree_border(total, n, c0);
-  auto place = [&](int c) { return (int64_t)(2 * c + (c > c0 ? 0 : at >= lo0)) * t.cost.rows + row % t.cost.rows; };
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const TreeCut u = t.cut[blockIdx.x];
+  const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (u.parts == 0 || u.r0 + r >= u.R) return;
+  auto place = [&](int c) { return (int64_t)(c == 0 ? u.first : 2 * ((int)blockIdx.x + c)) * t.cost.rows + r; };
   float top = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, t.pl[place(c)]);
+  for (int c = lane; c < u.parts; c += 32) top = fmaxf(top, t.pl[place(c)]);
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
   const float ref = top == -INFINITY ? 0.f : top;
   float L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int c = c0; c <= c1; ++c) {
+  for (int c = 0; c < u.parts; ++c) {
     const int64_t k = place(c);
     const float f = ex2(t.pl[k] - ref);
     const float4 x = *reinterpret_cast<const float4*>(t.po + k * HD + 4 * lane);
@@ -540,7 +529,9 @@ __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeA
     o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
   }
   const float f = L == 0.f ? 0.f : 1.f / L;
-  write_row(a, q.row0 + i, head, lane, make_float4(o.x * f, o.y * f, o.z * f, o.w * f), L == 0.f ? -INFINITY : ref + log2f(L));
+  const int row = u.r0 + r;
+  write_row(t.a, u.row0 + row / t.rep, u.g * t.rep + row % t.rep, lane, make_float4(o.x * f, o.y * f, o.z * f, o.w * f),
+            L == 0.f ? -INFINITY : ref + log2f(L));
 }
 
 struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
@@ -611,12 +602,12 @@ TreePlan tree_plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   return p;
 }
 
-// partial results, the sequences' places, the whole
-size_t tree_workspace(const TreePlan& p, int64_t B, size_t* pl, size_t* before) {
+// partial results and what they belong to
+size_t tree_workspace(const TreePlan& p, size_t* pl, size_t* cut) {
   const size_t parts = (size_t)2 * p.ctas * p.cost.rows;
   *pl = parts * HD * sizeof(float);
-  *before = *pl + (parts * sizeof(float) + 255) / 256 * 256;
-  return *before + ((size_t)B * 8 + sizeof(TreeWork) + 255) / 256 * 256;
+  *cut = *pl + (parts * sizeof(float) + 255) / 256 * 256;
+  return *cut + ((size_t)p.ctas * sizeof(TreeCut) + 255) / 256 * 256;
 }
 
 omq_status attention_check(const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q, int32_t max_kv,
@@ -672,8 +663,8 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
 size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                             int32_t n_kv) {
   if (B <= 0 || total_q <= 0 || max_q <= 0 || max_kv <= 0 || n_kv <= 0 || n_heads <= 0 || n_heads % n_kv) return 0;
-  size_t pl, before;
-  return tree_workspace(tree_plan_of(B, max_q, max_kv, n_heads, n_kv), B, &pl, &before);
+  size_t pl, cut;
+  return tree_workspace(tree_plan_of(B, max_q, max_kv, n_heads, n_kv), &pl, &cut);
 }
 
 omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
@@ -685,19 +676,29 @@ omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache,
   OMQ_REQUIRE(omq_aligned4(seen), OMQ_ERR_ALIGN);
   OMQ_TRY(attention_check(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace));
   const TreePlan p = tree_plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
-  const int64_t pairs = (int64_t)max_q * n_heads;
-  OMQ_REQUIRE(pairs < (1ll << 31), OMQ_ERR_SHAPE);
-  size_t pl, before;
-  OMQ_REQUIRE(workspace && ws_bytes >= tree_workspace(p, cache->B, &pl, &before), OMQ_ERR_WORKSPACE);
+  const int rep = n_heads / cache->n_kv;
+  OMQ_REQUIRE((int64_t)max_q * rep <= 1 << 20, OMQ_ERR_SHAPE);
+  size_t pl, cut;
+  OMQ_REQUIRE(workspace && ws_bytes >= tree_workspace(p, &pl, &cut), OMQ_ERR_WORKSPACE);
   char* const ws = (char*)workspace;
   const TreeArgs t{AttnArgs{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
                             lse, nullptr, nullptr, 0, 1, 1, dev_status, seen, words},
-                   p.cost, p.min_share, (TreeWork*)(ws + before), (int64_t*)(ws + before + sizeof(TreeWork)), (float*)ws,
+                   p.cost, p.min_share, rep, (uint32_t)(((1ull << 32) + rep - 1) / rep), (TreeCut*)(ws + cut), (float*)ws,
                    (float*)(ws + pl)};
   cudaStream_t st = (cudaStream_t)stream;
   OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
                             : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));
-  kv_attention_tree_join_kernel<<<dim3((unsigned)((pairs + 7) / 8), cache->B), 256, 0, st>>>(t);
+  // launched beside the one before, whose end it waits for itself
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)p.ctas, (unsigned)(p.cost.rows / 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kv_attention_tree_join_kernel, t) != cudaSuccess) { cudaGetLastError(); return OMQ_ERR_CUDA; }
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }

@@ -15,15 +15,16 @@ constexpr int TREE_SLOT = 128;              // tokens: whole pages and whole til
 // those of up to `small` rows
 struct TreeCost { int rows, small, start, weight, weight_small; };
 
-struct TreeWork {                           // in the workspace, for the joining launch
-  int64_t total; int64_t n;
-};
+// In the workspace, for the joining launch: the cut unit whose first tokens a CTA has.  It lies in `parts` partial results:
+// `first`, then the first ones of the CTAs behind.  parts 0: none
+struct TreeCut { int row0, g, r0, R, first, parts; };
 
 struct TreeArgs {
   AttnArgs a;
   TreeCost cost;
   int64_t min_share;                        // of the line, per CTA
-  TreeWork* work; int64_t* before;          // [B] where each sequence starts on the line
+  int rep; uint32_t rep_inv;                // query heads per KV head, and 2^32 over it rounded up: row / rep for rows below 2^20
+  TreeCut* cut;                             // [n]
   float* po; float* pl;                     // partial results: [2 n][rows][128] and their log-sum-exp
 };
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& t, int b) {
   q.ok = s.ok && s.len <= t.a.max_kv && s.len <= 0x7ff00000;      // (rounded up without overflow)
   q.row0 = s.row0; q.nq = s.nq;
   q.len = q.ok ? s.len : 0;                                    // its rows read as empty
-  q.R = s.nq * (t.a.n_heads / t.a.c.n_kv);
+  q.R = s.nq * t.rep;
   q.tiles = (q.R + t.cost.rows - 1) / t.cost.rows;
   q.slots = (q.len + TREE_SLOT - 1) / TREE_SLOT;
   q.w_last = q.R - (q.tiles - 1) * t.cost.rows > t.cost.small ? t.cost.weight : t.cost.weight_small;
@@ -61,8 +62,8 @@ __device__ __forceinline__ int tree_slots(const TreeArgs& t, const TreeSeq& q, i
 __device__ __forceinline__ int64_t tree_border(int64_t total, int64_t n, int64_t c) { return total * c / n; }
 
 // Share of this CTA on the line: [lo, hi), and the sequence that lo lies in.  Block-wide, THREADS of it; `scratch` holds
-// THREADS / 32 + 4 numbers.  CTA 0 leaves the sequences' places for the joining launch.
-struct TreeShare { int64_t lo, hi, before; int b; };
+// THREADS / 32 + 4 numbers.
+struct TreeShare { int64_t lo, hi, before, total, n; int b; };
 template <int THREADS>
 __device__ __forceinline__ TreeShare tree_share(const TreeArgs& t, int64_t* scratch) {
   constexpr int NW = THREADS / 32;
@@ -95,14 +96,11 @@ __device__ __forceinline__ TreeShare tree_share(const TreeArgs& t, int64_t* scra
   };
   int64_t mine, end = 0;
   const bool once = t.a.c.B <= THREADS;
-  for (int base = 0; base < t.a.c.B; base += THREADS) {
-    end = scan(base, &mine);
-    if (blockIdx.x == 0 && base + (int)threadIdx.x < t.a.c.B) t.before[base + threadIdx.x] = end - mine;
-  }
+  for (int base = 0; base < t.a.c.B; base += THREADS) end = scan(base, &mine);
   const int64_t sum = total;
   const int64_t n = max((int64_t)1, min((int64_t)gridDim.x, sum / t.min_share));
-  if (blockIdx.x == 0 && threadIdx.x == 0) *t.work = TreeWork{sum, n};
-  TreeShare r{0, 0, 0, 0};
+  if (threadIdx.x == 0) t.cut[blockIdx.x].parts = 0;
+  TreeShare r{0, 0, 0, sum, n, 0};
   if (blockIdx.x >= n || sum == 0) return r;
   r.lo = tree_border(sum, n, blockIdx.x);
   r.hi = tree_border(sum, n, blockIdx.x + 1);
@@ -148,6 +146,10 @@ struct TreeWalk {
       const bool take = z > a || (q.slots == 0 && at >= s.lo);
       *p = TreePiece{s.b, q.row0, q.nq, q.len, q.R, g, tile * t.cost.rows, a * TREE_SLOT, min(q.len, z * TREE_SLOT),
                      a == 0 && z == q.slots ? -1 : (int)(2 * blockIdx.x + (at >= s.lo))};
+      if (take && p->part >= 0 && a == 0) {                   // the CTA that has the end: as many borders lie before it
+        const int last = (int)(((at + t.cost.start + (int64_t)q.slots * w) * s.n - 1) / s.total);
+        t.cut[blockIdx.x] = TreeCut{q.row0, g, tile * t.cost.rows, q.R, p->part, last - (int)blockIdx.x + 1};
+      }
       at += t.cost.start + (int64_t)q.slots * w;
       if (++tile == q.tiles) {
         tile = 0;

@@ -5,14 +5,17 @@
 // converted tiles in and the products' operands out.  So the queries and the weights, the A operands, lie in tensor
 // memory, and a tile of 64 tokens costs 768 cycles there (codes in and out, converted in and out), 517 on the tensor
 // cores, and its 16 KB of codes 725 from HBM.  Roles of the 28 warps:
-//   0, 1     issue S = Q K^T (128 x 64 x 128) and O += P V (128 x 128 x 64)
+//   0, 3     issue S = Q K^T (128 x 64 x 128), of one group each (an issue and the waits before it are 700 cycles)
+//   1        issues O += P V (128 x 128 x 64)
 //   2        walks the CTA's share: chunks of up to 1024 tokens, with the records of their pages
 //   4..11    softmax, a row per thread, two groups (even and odd tiles) with their own references, sums and accumulators:
 //            scores from tensor memory, weights in fp16 to columns of their own, so that the group's next scores are
 //            formed meanwhile
 //   12..27   convert K and V to fp16, two sets (even and odd tiles), from rings of their own that bulk copies fill.  K is
 //            read K-major, V MN-major, both from [half][64 tokens][128 bytes] swizzled tiles
-// Tile j's converted K and V lie in the places j % 3, its scores and weights in its group's.  Nothing stops between chunks or
+// Tile j's converted V lies in the place j % 3, its K in one of its group's two places, its scores and weights in its group's.
+// Barriers of what one warp does in order of tiles go by place; the scores of the two groups come in no order, so theirs
+// belong to a group (a phase may be waited for only when the one before it is known to be over).  Nothing stops between chunks or
 // pieces: the next piece's queries are written, and its scores formed, before the last one's output is.
 // No role may spill: local memory passes the small rest of the L1 here, and a tile whose softmax reloads a dozen registers takes
 // half again as long.
@@ -27,7 +30,7 @@ using namespace tc;
 constexpr int HD = ATTN_HD, BMR = 128, TT = 64;
 constexpr int HALF = TT * HD;                        // one 64-channel half of a converted tile: 64 rows x 128 bytes
 constexpr int OP_BYTES = 2 * HALF;
-constexpr int BUF = 3;                               // places of tiles
+constexpr int BUF = 3, KBUF = 4;                     // places of V and of K
 constexpr int CHUNK = 1024, PAGES = CHUNK / 16, RING = 8;      // tokens, pages at most of a chunk; chunks in flight
 constexpr int RAW_BYTES = 16 * HD, DEPTH = 2;        // a warp's share of a tile's codes, its two slots
 constexpr int THREADS = 896;
@@ -40,7 +43,7 @@ struct __align__(16) Chunk {                         // tokens [t0, t1) of a pie
   float4 page[PAGES];                                // score factor, log2 of the value scale, place of its rows in the pool (-1: none)
 };
 
-constexpr int K_CONV = 0, V_CONV = K_CONV + BUF * OP_BYTES, STAGE = V_CONV + BUF * OP_BYTES;
+constexpr int K_CONV = 0, V_CONV = K_CONV + KBUF * OP_BYTES, STAGE = V_CONV + BUF * OP_BYTES;
 constexpr int RAW = STAGE + BMR * HD * 2;            // the stage: queries in fp16, or 32 channels of O from each group
 constexpr int ROW = RAW + 16 * DEPTH * RAW_BYTES;    // factor of each row
 constexpr int REF = ROW + BMR * 4;                   // [group][m, d, l]
@@ -150,9 +153,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   uint8_t* const smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
   const AttnArgs& a = t.a;
   const uint32_t bars = smem_u32(smem + BAR);
-  const uint32_t k_full = bars;                      // [3] K of a tile converted
-  const uint32_t s_full = k_full + 8 * BUF;          // [3] scores formed (K consumed)
-  const uint32_t pv_ready = s_full + 8 * BUF;        // [3] V of the tile converted and its weights written
+  const uint32_t k_full = bars;                      // [4] K of a tile converted
+  const uint32_t s_full = k_full + 8 * KBUF;         // [4] scores formed (K consumed)
+  const uint32_t pv_ready = s_full + 8 * KBUF;       // [3] V of the tile converted and its weights written
   const uint32_t pv_done = pv_ready + 8 * BUF;       // [3] product formed: weights, scores and V consumed
   const uint32_t s_free = pv_done + 8 * BUF;         // [2] scores read
   const uint32_t o_free = s_free + 16;               // both accumulators read
@@ -161,8 +164,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   const uint32_t chunk_full = meet + 8;              // [RING]
   const uint32_t chunk_empty = chunk_full + 8 * RING;                     // [RING]
   const uint32_t raw_full = chunk_empty + 8 * RING;  // [converting warp][DEPTH]
-  const uint32_t drain = raw_full + 8 * 16 * DEPTH;  // [2] of the issuing warps
-  constexpr int N_BAR = 4 * BUF + 5 + 2 * RING + 16 * DEPTH + 2;
+  const uint32_t q_seen = raw_full + 8 * 16 * DEPTH; // both issuing warps have come to the piece
+  const uint32_t drain = q_seen + 8;  // [4] of the issuing warps
+  constexpr int N_BAR = 2 * KBUF + 2 * BUF + 5 + 2 * RING + 16 * DEPTH + 5;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + BAR + 8 * N_BAR);
   static_assert(8 * N_BAR + 8 <= SCAN - BAR, "");
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
@@ -177,7 +181,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     for (int i = 0; i < N_BAR; ++i) {
       const uint32_t at = bars + 8 * i;
       mbar_init(&bar[i], at < s_full ? 4 : (at < pv_ready ? 1 : (at < pv_done ? 8 : (at < s_free ? 1 : (at < o_free ? 4 :
-                         (at < chunk_full ? 8 : (at < chunk_empty ? 1 : (at < raw_full ? 26 : 1))))))));
+                         (at < chunk_full ? 8 : (at < chunk_empty ? 1 : (at < raw_full ? 27 : (at == q_seen ? 2 : 1)))))))));
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -196,13 +200,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   // registers: 128 x 48 + 256 x 144 + 512 x 40 of the launch's 896 x 72
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 0) {
-      // ---------------- S: the whole warp runs the loop, one lane issues ----------------
+    if (warp == 0 || warp == 3) {
+      // ---------------- S of one group: the whole warp runs the loop, one lane issues ----------------
       constexpr uint32_t idS = idesc_f16(BMR, TT);
       const uint64_t dk = sdesc(smem_u32(smem + K_CONV), 16, 1024);
-      Place at{0, 0};
-      int g = 0;                              // the tile's group
-      uint32_t q_ph = 0, read_ph = 0;
+      const int g = warp == 3;
+      int i = g, n = 0;                       // the next tile in the chunk, the group's tiles so far
+      uint32_t q_ph = 0;
       bool ok = true;
       for (int k = 0; ok; ++k) {
         ok = chunk_wait(k);
@@ -210,23 +214,27 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
         const Chunk& w = chunk_at(k);
         if (w.flags & DONE) break;
         const int tiles = tiles_of(w);
-        if (w.flags & FIRST) { ok = soon(q_ready, q_ph); q_ph ^= 1; }
-        for (int i = 0; i < tiles && ok; ++i) {
-          ok = soon(k_full + 8 * at.b, at.ph) && soon(s_free + 8 * g, read_ph ^ 1);
+        if (w.flags & FIRST) {                // (with a tile of it or without: a phase that nobody waits for can be missed)
+          ok = soon(q_ready, q_ph);
+          q_ph ^= 1;
+          arrive(q_seen, lane);
+        }
+        for (; i < tiles && ok; i += 2) {
+          const int b = 2 * g + (n & 1);
+          ok = soon(k_full + 8 * b, (n >> 1) & 1) && soon(s_free + 8 * g, (n & 1) ^ 1);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t k0 = dk + (uint64_t)(at.b * (OP_BYTES >> 4));
+            const uint64_t k0 = dk + (uint64_t)(b * (OP_BYTES >> 4));
 #pragma unroll
             for (int c = 0; c < HD / 16; ++c)
               umma_ts(tmem + S_COL + g * TT, tmem + Q_COL + c * 8, k0 + (((c >> 2) * HALF + (c & 3) * 32) >> 4), idS, c != 0);
-            commit(s_full + 8 * at.b);
+            commit(s_full + 8 * b);
           }
           __syncwarp();
-          at.move(1);
-          read_ph ^= g;
-          g ^= 1;
+          ++n;
         }
+        i -= tiles;                           // of the next chunk
         arrive(chunk_empty + 8 * (k % RING), lane);
       }
       if (!ok) fail();
@@ -296,7 +304,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
           }
         }
         if (flags & FIRST) {                  // the unit's queries to L2, by tokens
-          const int rep = a.n_heads / a.c.n_kv, i0 = p.r0 / rep, i1 = (min(p.R, p.r0 + BMR) + rep - 1) / rep;
+          const int rep = t.rep, i0 = p.r0 / rep, i1 = (min(p.R, p.r0 + BMR) + rep - 1) / rep;
           for (int i = i0 + lane; i < i1; i += 32)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(a.Q + (int64_t)(p.row0 + i) * a.ldq + p.g * rep * HD)), "r"(rep * HD * 2) : "memory");
         }
@@ -307,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     }
     // what is in flight ends before the tensor memory is released
     __syncwarp();
-    if (warp < 2 && *abort_flag) {
+    if (warp != 2 && *abort_flag) {
       if (elect_one()) commit(drain + 8 * warp);
       soon(drain + 8 * warp, 0);
     }
@@ -329,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     int k = 0, tiles = -1, i = set;           // the chunk fetched from, its tiles (-1: not looked at), the next one of this set's
     int slot = 0, on_way = 0;                 // the slot to convert, tiles on their way
     uint32_t ph = 0;
-    Place at{set, 0};
+    Place at{is_v ? set : 2 * set, 0};
     while (true) {
       while (on_way < DEPTH && !done) {       // the next tiles' rows on their way
         if (tiles < 0) {
@@ -365,7 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       ok = soon(got + 8 * slot, ph) && soon(freed + 8 * at.b, at.ph ^ 1);
       if (!ok) break;
       const uint32_t src = slots + mine + slot * RAW_BYTES, dst = dst0 + at.b * OP_BYTES;
-#pragma unroll 1
+#pragma unroll
       for (int e = 0; e < 4; e += 2) {
         const uint4 u = lds128(src + e * 4 * HD), v = lds128(src + (e + 1) * 4 * HD);
         const uint32_t to = dst + e * 4 * 128;
@@ -379,7 +387,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       --on_way;
       fence_async_smem();                     // the converted tile -> visible to the tensor core
       arrive(full + 8 * at.b, lane);              // (and the slot has been read)
-      at.move(2);
+      if (is_v) {
+        at.move(2);
+      } else {
+        at.b ^= 1;
+        at.ph ^= at.b == 2 * set;
+      }
     }
     if (!ok) {                                // no copy may land after this CTA has left
       fail();
@@ -389,7 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     // ---------------- softmax: one row per thread ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     constexpr int SPAN = BMR / CP, TW = TT / CP, QT = TW / NQ;          // rows held, tokens of a thread, of them on a page
-    const int rep = a.n_heads / a.c.n_kv;
+    const int rep = t.rep;
+    auto by_rep = [&](int row) { return rep == 1 ? row : (int)__umulhi((uint32_t)row, t.rep_inv); };            // row / rep
     const int sg = warp >= 8, qw = warp & 3, r = qw * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(qw * 32) << 16), o_col = lanes + O_COL + sg * HD;
     const int w0 = r / SPAN * TW;                             // this copy's tokens of a tile
@@ -401,14 +415,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     float m = ATTN_NOTHING, d = ATTN_NO_VALUE, l = 0.f, f = 0.f;
     int token = -1;                                           // its row of the packed arrays; -1: none
     int J = 0;                                                // tiles before
+    uint32_t seen_ph = 1;
     auto queries = [&](const Chunk& w) {
       // Rows in fp16 under a power of two, 16 lanes per row, through shared memory to the row's two threads, 64 channels each
       constexpr int RW = SPAN / 8;
       const int r0 = (sg * 4 + qw) * RW;
       uint4 u[RW / 2];
       {
-        int row = w.p.r0 + r0 + (lane >> 4), h = row % rep;
-        const __nv_bfloat16* from = a.Q + (int64_t)(w.p.row0 + row / rep) * a.ldq + w.p.g * rep * HD + 8 * (lane & 15);
+        int row = w.p.r0 + r0 + (lane >> 4);
+        const int tok = by_rep(row);
+        int h = row - tok * rep;
+        const __nv_bfloat16* from = a.Q + (int64_t)(w.p.row0 + tok) * a.ldq + w.p.g * rep * HD + 8 * (lane & 15);
 #pragma unroll
         for (int e = 0; e < RW / 2; ++e) {
           u[e] = row < w.p.R ? __ldg(reinterpret_cast<const uint4*>(from + h * HD)) : make_uint4(0, 0, 0, 0);
@@ -440,10 +457,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       }
       if (!all_meet()) return false;
       const int i = r & (SPAN - 1), row = w.p.r0 + i;
-      token = row < w.p.R ? w.p.row0 + row / rep : -1;
+      token = row < w.p.R ? w.p.row0 + by_rep(row) : -1;
       f = factor[i];
-      // the scores of the piece before are all formed
-      if (J > 0 && !soon(s_full + 8 * ((J - 1) % BUF), ((J - 1) / BUF) & 1)) return false;
+      // (the scores of the piece before are all formed: both groups have met here)
+      if (!soon(q_seen, seen_ph)) return false;
+      seen_ph ^= 1;
+      tc_fence_after();
 #pragma unroll
       for (int c = 8 * sg; c < 8 * sg + 8; c += 2) {
         const uint4 x = lds128(rows + i * 256 + ((c ^ (i & 15)) << 4)), y = lds128(rows + i * 256 + (((c + 1) ^ (i & 15)) << 4));
@@ -457,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     };
 
     // a tile's scores to weights
-    auto tile = [&](const Chunk& w, const int i, const int before, const int seen_all, const int np, const Place at) {
+    auto tile = [&](const Chunk& w, const int i, const int before, const int seen_all, const int np, const Place at, const int n) {
       const Place prev = at.before();         // of the group's last tile (before the first: a phase that is over)
       // score factor and log2 of the value scale of each page; the tokens that this row sees, as bits
       const int o = i * TT + w0;
@@ -475,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
           seen &= ~(((1ull << (QT - 1) << 1) - 1) << (QT * q));
         }
       }
-      if (!soon(s_full + 8 * at.b, at.ph)) return false;
+      if (!soon(s_full + 8 * (2 * sg + (n & 1)), (n >> 1) & 1)) return false;
       tc_fence_after();
       if (__any_sync(0xffffffffu, token >= 0)) {
         float x[TW];
@@ -620,6 +639,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     }
     uint32_t o_ph = 1;
     Place at{sg, 0};                          // of the group's next tile
+    int n = 0;                                // the group's tiles so far
     bool ok = chunk_wait(0);
     if (ok && !(chunk_at(0).flags & DONE)) ok = queries(chunk_at(0));
     for (int k = 0; ok; ++k) {
@@ -634,7 +654,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
         o_ph ^= 1;
       }
       for (int i = (J ^ sg) & 1; i < tiles && ok; i += 2) {
-        ok = tile(w, i, piece0, seen_all, np, at);
+        ok = tile(w, i, piece0, seen_all, np, at, n++);
         at.move(2);
       }
       J += tiles;
@@ -682,18 +702,27 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       const float lse = none ? -INFINITY : mm + log2f(L);
       if (mine_now && sg == 0 && r < SPAN) {
         if (w.p.part >= 0) t.pl[(int64_t)w.p.part * t.cost.rows + r] = lse;
-        else if (a.lse) a.lse[(int64_t)(w.p.row0 + row / rep) * a.n_heads + w.p.g * rep + row % rep] = lse;
+        else if (a.lse) a.lse[(int64_t)(w.p.row0 + by_rep(row)) * a.n_heads + w.p.g * rep + row - by_rep(row) * rep] = lse;
       }
-      // 64 channels of each group, 32 at a time through shared memory to rows of 128 bytes
+      // 64 channels of each group, 32 at a time: each thread its row's, or, with copies of a row to add up, through shared
+      // memory to rows of 128 bytes
       constexpr int RO = SPAN / 4;                            // rows that a warp writes
-      const int q0 = qw * RO + (lane >> 3), rows = min(min(SPAN, w.p.R - w.p.r0), (qw + 1) * RO);
+      const int q0 = CP == 1 ? r : qw * RO + (lane >> 3), rows = min(min(SPAN, w.p.R - w.p.r0), (qw + 1) * RO);
       const uint32_t stage = smem_u32(smem + STAGE) + sg * (BMR * 128);
-      const int h0 = (w.p.r0 + q0) % rep, step_h = 4 % rep;
-      const int64_t to0 = (int64_t)(w.p.row0 + (w.p.r0 + q0) / rep) * a.ldo + w.p.g * rep * HD + 4 * (lane & 7), step = 4 / rep * a.ldo;
+      const int tok0 = by_rep(w.p.r0 + q0), h0 = w.p.r0 + q0 - tok0 * rep;
+      auto put = [&](const float4& o, int64_t to) {
+        if (a.Of) *reinterpret_cast<float4*>(a.Of + to) = o;
+        if (a.Ob) {
+          uint2 y;
+          __nv_bfloat162* b2 = reinterpret_cast<__nv_bfloat162*>(&y);
+          b2[0] = __floats2bfloat162_rn(o.x, o.y);
+          b2[1] = __floats2bfloat162_rn(o.z, o.w);
+          *reinterpret_cast<uint2*>(a.Ob + to) = y;
+        }
+      };
 #pragma unroll 1
       for (int ch = sg * 64; ch < sg * 64 + 64; ch += 32) {
         if (CP > 1 && (ch & 32)) ok = all_meet();             // the stage has been read
-        __syncwarp();
 #pragma unroll
         for (int b = 0; b < 32; b += 16) {
           float v[16], u[16];
@@ -705,20 +734,45 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
             const float y = n_a > 0 && c0 != 0.f ? v[i] * c0 : 0.f;
             v[i] = n_b > 0 && c1 != 0.f ? fmaf(u[i], c1, y) : y;
           }
+          if (CP > 1) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            sts128(stage + r * 128 + ((((b + i) >> 2) ^ (r & 7)) << 4),
-                   make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
+            for (int i = 0; i < 16; i += 4)
+              sts128(stage + r * 128 + ((((b + i) >> 2) ^ (r & 7)) << 4),
+                     make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
+          } else if (mine_now) {
+            if (w.p.part >= 0) {
+              float* const to = t.po + ((int64_t)w.p.part * BMR + r) * HD + ch + b;
+#pragma unroll
+              for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            } else {
+              const int64_t to = (int64_t)(w.p.row0 + tok0) * a.ldo + (w.p.g * rep + h0) * HD + ch + b;
+              if (a.Of) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(a.Of + to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+              }
+              if (a.Ob) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 8) {
+                  uint4 y;
+                  __nv_bfloat162* b2 = reinterpret_cast<__nv_bfloat162*>(&y);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) b2[e] = __floats2bfloat162_rn(v[i + 2 * e], v[i + 2 * e + 1]);
+                  *reinterpret_cast<uint4*>(a.Ob + to + i) = y;
+                }
+              }
+            }
+          }
         }
         if (ch & 32) {                                        // the accumulators have been read
           tc_fence_before();
           arrive(o_free, lane);
         }
-        if (CP > 1) ok = ok && all_meet();
-        else __syncwarp();
+        if (CP == 1) continue;
+        ok = ok && all_meet();
         if (!ok) break;
         int h = h0;
-        int64_t to = to0 + ch;
+        int64_t to = (int64_t)(w.p.row0 + tok0) * a.ldo + w.p.g * rep * HD + ch + 4 * (lane & 7);
+        const int step_t = by_rep(4), step_h = 4 - step_t * rep;
 #pragma unroll
         for (int n = 0; n < RO / 4; ++n) {                    // a row per eight lanes
           const int q = q0 + 4 * n;
@@ -730,20 +784,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
               const uint4 y = lds128(stage + i * 128 + (((lane & 7) ^ (i & 7)) << 4));
               o.x += __uint_as_float(y.x); o.y += __uint_as_float(y.y); o.z += __uint_as_float(y.z); o.w += __uint_as_float(y.w);
             }
-            if (w.p.part >= 0) {
-              *reinterpret_cast<float4*>(t.po + ((int64_t)w.p.part * t.cost.rows + q) * HD + ch + 4 * (lane & 7)) = o;
-            } else {
-              if (a.Of) *reinterpret_cast<float4*>(a.Of + to + h * HD) = o;
-              if (a.Ob) {
-                uint2 y;
-                __nv_bfloat162* b2 = reinterpret_cast<__nv_bfloat162*>(&y);
-                b2[0] = __floats2bfloat162_rn(o.x, o.y);
-                b2[1] = __floats2bfloat162_rn(o.z, o.w);
-                *reinterpret_cast<uint2*>(a.Ob + to + h * HD) = y;
-              }
-            }
+            if (w.p.part >= 0) *reinterpret_cast<float4*>(t.po + ((int64_t)w.p.part * BMR + q) * HD + ch + 4 * (lane & 7)) = o;
+            else put(o, to + h * HD);
           }
-          to += step;
+          to += step_t * a.ldo;
           h += step_h;
           if (h >= rep) { h -= rep; to += a.ldo; }
         }
