@@ -6,12 +6,13 @@
 namespace {
 
 // ------------------------------------------------------------------------------------------------
-// omq_draft_tree: ancestors by pointer doubling.  After round k a node holds the bits of its 2^k nearest
-// ancestors and a jump to the next one; it takes over the bits and the jump of the node it jumps to.  So the chain of
-// dependent steps is log2(depth) long and not the depth.  One CTA per sequence, a thread per node, bits in shared
-// memory.  (A node whose bits grow in the same round passes on more than its 2^k ancestors: they are ancestors
-// of the reader too.)  Bound: the launch and the round trips to the parents and back.
+// omq_draft_tree: one CTA per sequence, a thread per node, bits in shared memory.  Depths by pointer doubling: after round k
+// a node has a jump over its 2^k nearest ancestors, so the chain of dependent steps is log2(depth) long.  The bits of
+// trees up to WALK deep are set by walking up, one word for each ancestor; those of deeper ones by doubling too: a
+// node takes over the bits of the node that it jumps to.  (A node whose bits grow in the same round passes on more than its 2^k
+// ancestors: they are ancestors of the reader too.)  Bound: the launch and the round trips to the parents and back.
 // ------------------------------------------------------------------------------------------------
+constexpr int WALK = 24;
 constexpr int MAX_NODES = 1024;
 
 struct NodeArgs {
@@ -37,21 +38,22 @@ __global__ void __launch_bounds__(MAX_NODES) draft_tree_kernel(const NodeArgs a)
   const int i = threadIdx.x, W = (a.max_q + 31) >> 5, ld = W | 1;      // an odd row length: no bank conflicts
   uint32_t* bits = tree_smem;                                            // [max_q][ld]
   int2* hop = reinterpret_cast<int2*>(bits + ((a.max_q * ld + 1) & ~1));    // [2][max_q]: jump, ancestors up to it
+  for (int k = i; k < (n * ld + 1) / 2; k += blockDim.x) reinterpret_cast<uint2*>(bits)[k] = make_uint2(0, 0);
+  int up = -1;
   if (i < n) {
-    int p = __ldg(a.parent + row0 + i);
-    if (p < -1 || p >= i) { omq_set_status(a.status, OMQ_ERR_INVALID_ARG); p = -1; }
-    for (int w = 0; w < W; ++w) bits[i * ld + w] = w == i >> 5 ? 1u << (i & 31) : 0u;
-    hop[i] = make_int2(p, p >= 0);
+    up = __ldg(a.parent + row0 + i);
+    if (up < -1 || up >= i) { omq_set_status(a.status, OMQ_ERR_INVALID_ARG); up = -1; }
+    hop[i] = make_int2(up, up >= 0);
   }
   __syncthreads();
-  int2 h = i < n ? hop[i] : make_int2(-1, 0);
-  for (int k = 0;; k ^= 1) {
+  int2 h = make_int2(up, up >= 0);
+  int k = 0;
+  for (;; k ^= 1) {
     const int2* const now = hop + k * a.max_q;
     int2* const next = hop + (k ^ 1) * a.max_q;
     bool more = false;
     if (i < n) {
       if (h.x >= 0) {
-        for (int w = 0; w <= h.x >> 5; ++w) bits[i * ld + w] |= bits[h.x * ld + w];
         const int2 j = now[h.x];
         h = make_int2(j.x, h.y + j.y);
         more = j.x >= 0;
@@ -61,9 +63,36 @@ __global__ void __launch_bounds__(MAX_NODES) draft_tree_kernel(const NodeArgs a)
     if (!__syncthreads_or(more)) break;
   }
   if (i < n) a.depth[row0 + i] = h.y;
-  for (int k = i; k < n * a.words; k += blockDim.x) {
-    const int r = k / a.words, w = k - r * a.words;
-    a.seen[(int64_t)row0 * a.words + k] = w < W ? bits[r * ld + w] : 0u;
+  uint32_t* const mine = bits + i * ld;
+  if (i < n) mine[i >> 5] = 1u << (i & 31);
+  // every thread has its last round's jumps behind it: the first array takes the parents again
+  if (i < n) hop[i].x = up;
+  if (!__syncthreads_or(i < n && h.y > WALK)) {
+    if (i < n)
+      for (int j = up; j >= 0; j = hop[j].x) mine[j >> 5] |= 1u << (j & 31);
+  } else {
+    int j = up;
+    for (k = 0;; k ^= 1) {
+      const int2* const now = hop + k * a.max_q;
+      int2* const next = hop + (k ^ 1) * a.max_q;
+      if (i < n) {
+        if (j >= 0) {
+          for (int w = 0; w <= j >> 5; ++w) mine[w] |= bits[j * ld + w];
+          j = now[j].x;
+        }
+        next[i].x = j;
+      }
+      if (!__syncthreads_or(i < n && j >= 0)) break;
+    }
+  }
+  __syncthreads();
+  // rows of `words` words, consecutive threads on consecutive words
+  const int step_r = blockDim.x / a.words, step_w = blockDim.x - step_r * a.words;
+  for (int r = i / a.words, w = i - r * a.words; r < n;) {
+    a.seen[((int64_t)row0 + r) * a.words + w] = w < W ? bits[r * ld + w] : 0u;
+    r += step_r;
+    w += step_w;
+    if (w >= a.words) { w -= a.words; ++r; }
   }
 }
 
@@ -90,7 +119,8 @@ size_t tree_smem_bytes(int max_q) {
 // its slice of the vocabulary (the second pass over a row finds it in L1), and the parts meet in CTA 0.  Every CTA
 // does what CTA 0 posts and decides nothing itself, so no input can make them disagree at a barrier.
 // ------------------------------------------------------------------------------------------------
-constexpr int VT = 256, VW = VT / 32;       // threads, warps
+constexpr int VT = 512, VW = VT / 32;       // threads, warps
+constexpr int BATCH = 4;                    // 128-token steps whose loads a warp has in flight
 constexpr int VMAX_CLUSTER = 8;
 constexpr int VMAX_V = 1 << 20;
 
@@ -106,12 +136,12 @@ __device__ __forceinline__ float probability(float p) { return fminf(fmaxf(p, 0.
 
 __device__ __forceinline__ float number(float u) { return fminf(fmaxf(u, 0.f), 0.99999994f); }  // in [0, 1)
 
-// p in [0, 1] times 2^60, truncated
+// p in [0, 1] times 2^60, truncated: the significand at 2^37, and back by 127 less the exponent
 __device__ __forceinline__ uint64_t fixed60(float p) {
-  const uint32_t b = __float_as_uint(p), e = b >> 23;
-  const uint64_t m = (b & 0x7fffffu) | 0x800000u;
-  const int s = (int)e - 90;
-  return s >= 0 ? m << s : (s > -24 ? m >> -s : 0ull);
+  const uint32_t b = __float_as_uint(p);
+  uint64_t w = (uint64_t)((b & 0x7fffffu) | 0x800000u) << 37;
+  asm("shr.u64 %0, %0, %1;" : "+l"(w) : "r"(127u - (b >> 23)));            // (64 and more: zero)
+  return w;
 }
 
 // a q times 2^60, truncated, for a = a52 2^-52: 88 bits of product and a shift; all ones when it passes 2^63
@@ -148,7 +178,6 @@ __device__ __forceinline__ float4 prob4(const void* row, int i, int n, bool wide
       if (i + k < n)
         v[k] = BF ? __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(row) + i + k)) : __ldg(static_cast<const float*>(row) + i + k);
   }
-  f.x = probability(f.x); f.y = probability(f.y); f.z = probability(f.z); f.w = probability(f.w);
   return f;
 }
 
@@ -161,27 +190,46 @@ enum { PASS = 0, DRAW = 1, DRAW_PASS = 2, DRAW_WHOLE = 3 };
 struct __align__(16) VerifySmem {
   Order order;
   uint64_t part[VMAX_CLUSTER];              // the CTAs' sums, in every CTA
-  uint64_t warp_sum[VW];
+  uint64_t warp_sum[VW], step_sum[VW];
   int32_t parent[MAX_NODES], token[MAX_NODES];
   float u[MAX_NODES], p[MAX_NODES], q[MAX_NODES];
   uint32_t gone[VMAX_V / VMAX_CLUSTER / 32];          // tokens of the slice that were rejected (no draft distribution)
 };
 
-// the weights of four tokens of the slice
-template <bool BF>
-__device__ __forceinline__ void weights4(const VerifyArgs& a, const VerifySmem& s, int64_t row, uint64_t a52, bool cut, int i,
-                                         int lo, int hi, uint64_t (&w)[4]) {
+// p and q of N x 128 tokens of a warp, four of each to a lane: all on their way before the first is used
+template <bool BF, int N>
+__device__ __forceinline__ void fetch(const VerifyArgs& a, int64_t row, bool both, int at, int hi, float4 (&p)[N], float4 (&q)[N]) {
   const char* const pr = static_cast<const char*>(a.P) + row * a.ldp * (BF ? 2 : 4);
-  const float4 p = prob4<BF>(pr, i, hi, a.wide);
-  w[0] = fixed60(p.x); w[1] = fixed60(p.y); w[2] = fixed60(p.z); w[3] = fixed60(p.w);
-  if (a52) {
-    const char* const qr = static_cast<const char*>(a.Q) + row * a.ldq * (BF ? 2 : 4);
-    const float4 q = prob4<BF>(qr, i, hi, a.wide);
-    const uint64_t d[4] = {scaled60(q.x, a52), scaled60(q.y, a52), scaled60(q.z, a52), scaled60(q.w, a52)};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = w[k] > d[k] ? w[k] - d[k] : 0ull;
+  for (int k = 0; k < N; ++k) p[k] = prob4<BF>(pr, at + 128 * k, hi, a.wide);
+  if (both) {
+    const char* const qr = static_cast<const char*>(a.Q) + row * a.ldq * (BF ? 2 : 4);
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = prob4<BF>(qr, at + 128 * k, hi, a.wide);
   }
-  if (cut) {
+}
+
+// the weights of four tokens of the slice
+__device__ __forceinline__ void weights4(const VerifySmem& s, const float4& p, const float4& q, uint64_t a52, bool cut, int i, int lo,
+                                         int hi, uint64_t (&w)[4]) {
+  w[0] = fixed60(probability(p.x)); w[1] = fixed60(probability(p.y)); w[2] = fixed60(probability(p.z)); w[3] = fixed60(probability(p.w));
+  if (a52) {
+    const float f[4] = {probability(q.x), probability(q.y), probability(q.z), probability(q.w)};
+    if (a52 == 1ull << 52) {                // a node's first rejection
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t d = fixed60(f[k]);
+        w[k] = w[k] > d ? w[k] - d : 0ull;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t d = scaled60(f[k], a52);
+        w[k] = w[k] > d ? w[k] - d : 0ull;
+      }
+    }
+  }
+  if (cut && i < hi) {
     const uint32_t g = s.gone[(i - lo) >> 5] >> ((i - lo) & 31);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -202,7 +250,7 @@ __device__ __forceinline__ void put64(uint64_t* at, int rank, int C, uint64_t v)
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(VT) verify_kernel(const VerifyArgs a, const int C) {
+__global__ void __launch_bounds__(VT, 2) verify_kernel(const VerifyArgs a, const int C) {
   __shared__ VerifySmem s;
   const int b = blockIdx.x / C, rank = blockIdx.x - b * C, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lo = min(a.V, rank * a.slice), hi = min(a.V, lo + a.slice);
@@ -308,10 +356,15 @@ __global__ void __launch_bounds__(VT) verify_kernel(const VerifyArgs a, const in
     while (true) {
       if (o.kind != DRAW) {
         uint64_t sum = 0;
-        for (int at = w_lo + 4 * lane; at < w_hi; at += 128) {
-          uint64_t w[4];
-          weights4<BF>(a, s, o.row, o.a52, cut, at, lo, w_hi, w);
-          sum += (w[0] + w[1]) + (w[2] + w[3]);
+        for (int at = w_lo + 4 * lane; at < w_hi; at += 128 * BATCH) {
+          float4 p[BATCH], q[BATCH];
+          fetch<BF, BATCH>(a, o.row, o.a52 != 0, at, w_hi, p, q);
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            uint64_t w[4];
+            weights4(s, p[k], q[k], o.a52, cut, at + 128 * k, lo, w_hi, w);
+            sum += (w[0] + w[1]) + (w[2] + w[3]);
+          }
         }
         sum = warp_sum64(sum);
         if (lane == 0) s.warp_sum[warp] = sum;
@@ -347,14 +400,41 @@ __global__ void __launch_bounds__(VT) verify_kernel(const VerifyArgs a, const in
       if (total == 0) { omq_set_status(a.status, OMQ_ERR_INVALID_ARG); tokens[o.count - 1] = 0; }
     }
     const uint64_t t = __umul64hi((uint64_t)((double)number(__ldg(a.u + row0)) * 18446744073709551616.0), total);
+    // the warp share that t falls into, if this CTA has it
     uint64_t run = before;
+    int own = -1;
+#pragma unroll
+    for (int k = 0; k < VW; ++k) {
+      if (own < 0 && t >= run && t - run < s.warp_sum[k]) own = k;
+      if (own < 0) run += s.warp_sum[k];
+    }
+    if (own < 0) return;
+    // a part of that share for each warp
+    const int part = share / VW;            // (a multiple of 4)
+    const int p_lo = min(hi, lo + own * share + warp * part), p_hi = min(hi, p_lo + part);
+    uint64_t sum = 0;
+    for (int at = p_lo + 4 * lane; at < p_hi; at += 128 * 2) {
+      float4 p[2], q[2];
+      fetch<BF, 2>(a, o.row, o.a52 != 0, at, p_hi, p, q);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint64_t w[4];
+        weights4(s, p[k], q[k], o.a52, cut, at + 128 * k, lo, p_hi, w);
+        sum += (w[0] + w[1]) + (w[2] + w[3]);
+      }
+    }
+    sum = warp_sum64(sum);
+    if (lane == 0) s.step_sum[warp] = sum;
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < VW; ++k)
-      if (k < warp) run += s.warp_sum[k];
-    if (t >= run && t - run < s.warp_sum[warp]) {
-      for (int base = w_lo; base < w_hi; base += 128) {
+      if (k < warp) run += s.step_sum[k];
+    if (t >= run && t - run < sum) {
+      for (int base = p_lo; base < p_hi; base += 128) {
+        float4 p[1], q[1];
         uint64_t w[4];
-        weights4<BF>(a, s, o.row, o.a52, cut, base + 4 * lane, lo, w_hi, w);
+        fetch<BF, 1>(a, o.row, o.a52 != 0, base + 4 * lane, p_hi, p, q);
+        weights4(s, p[0], q[0], o.a52, cut, base + 4 * lane, lo, p_hi, w);
         uint64_t in = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -400,13 +480,15 @@ __device__ __forceinline__ uint4 again16(uint4 u, float r) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// omq_kv_keep.  Place j of a sequence's drafted tokens takes the codes of node path[j], which lies at j or behind it, so
-// pages are settled in order: no place is written before what it held has been read.  A page's scale grows
-// where a token comes in from a page of larger values, and the codes of the page are rounded again then, as in the
-// append.  One CTA per (sequence, KV head, K or V, layer), eight threads per token.  Bound: the chain count -> path -> page ->
-// codes and the launch; every layer's cache is in one launch for that.
+// omq_kv_keep.  Place j of a sequence's drafted tokens takes the codes of node path[j], which lies at j or behind it, so in
+// order of j no place is written before what it held has been read.  A page's scale grows where a token comes in from a
+// page of larger values, and the codes of the page are rounded again then, as in the append; tokens that move within
+// the page are rounded like those that stay.  A warp per (sequence, KV head, K or V, layer), four tokens at a time, eight lanes
+// each; the CTA's eight warps share the path.  Bound: the chain of path, page, scale and codes; few registers and no barrier
+// between warps keep 64 of them on an SM (a CTA of four warps for each head, each with the moved tokens in
+// registers: 51.2 us for 64 sequences of 8 heads in 40 layers).
 // ------------------------------------------------------------------------------------------------
-constexpr int KT = 128, KGRP = KT / 8;      // threads, tokens per pass
+constexpr int KT = 256, KW = KT / 32;       // threads, warps
 constexpr int KEEP_LAYERS = 128;            // caches of a launch
 
 struct KeepCache {
@@ -420,29 +502,30 @@ struct KeepArgs {
   KeepCache c[L];
 };
 
-template <int L, int NP>
+template <int L>
 __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ KeepArgs<L> a) {
   __shared__ int32_t path[MAX_NODES];
-  __shared__ uint32_t red[KT / 32];
   const KeepCache& c = a.c[blockIdx.z];
-  const int b = blockIdx.y, g = blockIdx.x >> 1;
-  const bool is_v = blockIdx.x & 1;
-  const int P = a.page;
+  const int b = blockIdx.y, lane = threadIdx.x & 31, unit = blockIdx.x * KW + (threadIdx.x >> 5), g = unit >> 1;
+  const bool is_v = unit & 1;
+  const int P = a.page, shift = 31 - __clz(P);
+  const int32_t* const my_path = a.path + (int64_t)b * a.steps;
+  const int ahead = (int)threadIdx.x < a.steps ? __ldg(my_path + threadIdx.x) : 0;     // asked for beside the lengths
   int row0, nq;
   const bool rows = node_rows(a.cu_q, a.max_q, a.total_q, b, &row0, &nq);
   const int len = __ldg(c.kv_len + b), n = __ldg(a.count + b), start = len - nq;
   bool bad = !rows || n < 0 || n > a.steps || n > nq || (n > 0 && start < 0);
+  if (!bad) {
+    for (int j = threadIdx.x; j < n; j += KT) path[j] = j < KT ? ahead : __ldg(my_path + j);
+  }
+  __syncthreads();
   if (!bad)
-    for (int j = threadIdx.x; j < n; j += KT) {
-      const int p = __ldg(a.path + (int64_t)b * a.steps + j);
-      bad |= p >= nq || p < 0 || (j > 0 && __ldg(a.path + (int64_t)b * a.steps + j - 1) >= p);
-      path[j] = p;
-    }
+    for (int j = threadIdx.x; j < n; j += KT) bad |= path[j] >= nq || path[j] < 0 || (j > 0 && path[j - 1] >= path[j]);
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) omq_set_status(c.status, OMQ_ERR_INVALID_ARG);
     return;
   }
-  const int grp = threadIdx.x >> 3, lane8 = threadIdx.x & 7;
+  if (unit >= 2 * a.n_kv) return;
   uint8_t* const codes = is_v ? c.v : c.k;
   float* const scales = is_v ? c.v_scale : c.k_scale;
   auto page_id = [&](int pg) {
@@ -451,66 +534,75 @@ __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ Kee
     omq_set_status(c.status, OMQ_ERR_INVALID_ARG);
     return -1;
   };
+  const int sub = lane >> 3, at16 = 16 * (lane & 7);          // token of four, its bytes
   int j0 = 0;
   while (j0 < n && path[j0] == j0) ++j0;    // these lie where they belong
   while (j0 < n) {
-    const int pg = (start + j0) / P, j1 = min(n, (pg + 1) * P - start);
+    const int pg = (start + j0) >> shift, j1 = min(n, ((pg + 1) << shift) - start);
+    // four tokens' codes; whether they come from another page, and under which scale; nothing for one that stays, or whose page is
+    // out of range
+    auto get = [&](int j, uint4* u, float* from, bool* other) {
+      if (j >= j1 || path[j] == j) return false;
+      const int at = start + path[j], src = page_id(at >> shift);
+      if (src < 0) return false;
+      const int64_t head = (int64_t)src * a.n_kv + g;
+      *other = at >> shift != pg;
+      *u = *reinterpret_cast<const uint4*>(codes + (head * P + (at & (P - 1))) * 128 + at16);
+      *from = scales[head];
+      return true;
+    };
     const int id = page_id(pg);
-    const float before = id < 0 ? 0.f : scales[(int64_t)id * a.n_kv + g];
-    uint4 u[NP];
-    float from[NP];                         // scale of the token's page; negative: does not move
+    if (id < 0) { j0 = j1; continue; }
+    const int64_t head = (int64_t)id * a.n_kv + g;
+    uint8_t* const dst = codes + head * P * 128 + at16;
+    const float before = scales[head];
     uint32_t big = 0;
+    uint4 u0 = make_uint4(0, 0, 0, 0);
+    float from0 = 0.f;
+    bool other0 = false, got0 = false;
+    for (int jb = j0; jb < j1; jb += 4) {
+      uint4 u;
+      float from;
+      bool other;
+      const bool got = get(jb + sub, &u, &from, &other);
+      if (got && other) {
+        uint32_t top = 0;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int j = j0 + p * KGRP + grp;
-      from[p] = -1.f;
-      u[p] = make_uint4(0, 0, 0, 0);
-      if (j < j1 && id >= 0 && path[j] != j) {
-        const int at = start + path[j], src = at / P == pg ? id : page_id(at / P);
-        if (src >= 0) {
-          u[p] = *reinterpret_cast<const uint4*>(codes + (((int64_t)src * a.n_kv + g) * P + at % P) * 128 + 16 * lane8);
-          from[p] = at / P == pg ? before : scales[(int64_t)src * a.n_kv + g];
-          if (at / P != pg) {
-            int top = 0;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const uint32_t w = e < 4 ? u[p].x : (e < 8 ? u[p].y : (e < 12 ? u[p].z : u[p].w));
-              top = max(top, abs((int)((w >> (8 * (e & 3))) & 255u) - 128));
-            }
-            big = max(big, __float_as_uint(__fmul_rn((float)top, from[p])) & 0x7fffffffu);
-          }
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t w = e < 4 ? u.x : (e < 8 ? u.y : (e < 12 ? u.z : u.w));
+          top = max(top, (uint32_t)abs((int)((w >> (8 * (e & 3))) & 255u) - 128));
         }
+        big = max(big, __float_as_uint(__fmul_rn((float)top, from)) & 0x7fffffffu);
       }
+      if (jb == j0) { u0 = u; from0 = from; other0 = other; got0 = got; }
     }
     big = __reduce_max_sync(0xffffffffu, big);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = big;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < KT / 32; ++w) big = max(big, red[w]);
     const float want = __fdiv_rn(__uint_as_float(big), 127.f);
     const bool grows = !(before >= want) && before == before;
     const float after = grows ? want : before;
-    if (id >= 0) {
-      uint8_t* const dst = codes + ((int64_t)id * a.n_kv + g) * P * 128;
-      if (grows) {
-        const float r = __fdiv_rn(before, after);
-        for (int k = threadIdx.x; k < P * 8; k += KT) {
-          uint4* at = reinterpret_cast<uint4*>(dst) + k;
-          *at = again16(*at, r);
-        }
-        if (threadIdx.x == 0) scales[(int64_t)id * a.n_kv + g] = after;
+    if (grows) {
+      const float r = __fdiv_rn(before, after);
+      for (int k = sub; k < P; k += 4) {
+        uint4* at = reinterpret_cast<uint4*>(dst + k * 128);
+        *at = again16(*at, r);
       }
-      __syncthreads();                      // (id is the CTA's)
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int j = j0 + p * KGRP + grp;
-        if (from[p] >= 0.f || from[p] != from[p]) {
-          const float r = after > 0.f ? __fdiv_rn(from[p], after) : 0.f;
-          *reinterpret_cast<uint4*>(dst + (start + j - pg * P) * 128 + 16 * lane8) = again16(u[p], r);
-        }
-      }
+      if (lane == 0) scales[head] = after;
+      __syncwarp();
     }
-    __syncthreads();
+    for (int jb = j0; jb < j1; jb += 4) {
+      uint4 u = u0;
+      float from = from0;
+      bool other = other0, got = got0;
+      // (what moves within a page that grew has been rounded by now, but for the first four, read before)
+      if (jb > j0) got = get(jb + sub, &u, &from, &other);
+      if (got) {
+        const float r = after > 0.f ? __fdiv_rn(other || jb == j0 ? from : after, after) : 0.f;
+        u = again16(u, r);
+      }
+      __syncwarp();
+      if (got) *reinterpret_cast<uint4*>(dst + (start + jb + sub - (pg << shift)) * 128) = u;
+      __syncwarp();
+    }
     j0 = j1;
   }
 }
@@ -526,13 +618,7 @@ omq_status keep_launch(cudaStream_t st, const omq_kv_cache* const* caches, int32
     a.c[i] = KeepCache{c.k, c.v, c.k_scale, c.v_scale, c.page_table, c.kv_len, status ? status[i < n ? i : 0] : nullptr, c.n_pages,
                        c.max_pages};
   }
-  const dim3 grid(2 * a.n_kv, caches[0]->B, n);
-  switch (a.page) {
-    case 16: kv_keep_kernel<L, 1><<<grid, KT, 0, st>>>(a); break;
-    case 32: kv_keep_kernel<L, 2><<<grid, KT, 0, st>>>(a); break;
-    case 64: kv_keep_kernel<L, 4><<<grid, KT, 0, st>>>(a); break;
-    default: kv_keep_kernel<L, 8><<<grid, KT, 0, st>>>(a); break;
-  }
+  kv_keep_kernel<L><<<dim3((2 * a.n_kv + KW - 1) / KW, caches[0]->B, n), KT, 0, st>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
