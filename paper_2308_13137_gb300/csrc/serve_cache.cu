@@ -28,6 +28,7 @@ struct AppendArgs {
   const void* QKV; int64_t ld;
   const float2* rope; int n_pos; const float* sa;
   __nv_bfloat16* Qo; int64_t ldq; __nv_bfloat16 *Ko, *Vo; int64_t ldkv;
+  int kv_units;
   int32_t* status;
   const int32_t* depth;                // of the rows in their draft trees (TREE), or NULL
 };
@@ -74,36 +75,26 @@ template <bool BF, bool TREE>
 __device__ __forceinline__ void q_unit(const AppendArgs& a, const SeqRows& s, int unit) {
   const int grp = threadIdx.x >> 3, j = 8 * (threadIdx.x & 7);
   const int rep = a.n_heads / a.c.n_kv;
-  // every row's values are on their way before the first is turned
-  float x[QPASS][8], y[QPASS][8];
-  int i[QPASS], h[QPASS], pos[QPASS];
 #pragma unroll
   for (int p = 0; p < QPASS; ++p) {
     const int idx = (unit * QPASS + p) * GRP + grp;
-    i[p] = idx / a.n_heads;
-    h[p] = idx - i[p] * a.n_heads;
-    if (i[p] < s.nq) {
-      const int64_t row = s.row0 + i[p];
-      load8<BF>(a.QKV, row * a.ld + h[p] * HD + j, x[p]);
-      load8<BF>(a.QKV, row * a.ld + h[p] * HD + j + 64, y[p]);
-      pos[p] = position<TREE>(a, s, i[p]);
-    }
-  }
-#pragma unroll
-  for (int p = 0; p < QPASS; ++p) {
-    if (i[p] >= s.nq) return;
-    const int64_t row = s.row0 + i[p];
-    turn(a.rope, pos[p], j, x[p], y[p]);
+    const int i = idx / a.n_heads, h = idx - i * a.n_heads;
+    if (i >= s.nq) return;
+    const int64_t row = s.row0 + i;
+    float x[8], y[8];
+    load8<BF>(a.QKV, row * a.ld + h * HD + j, x);
+    load8<BF>(a.QKV, row * a.ld + h * HD + j + 64, y);
+    turn(a.rope, position<TREE>(a, s, i), j, x, y);
     if (a.sa) {
       float u[8], w[8];
-      load8<false>(a.sa, (h[p] / rep) * HD + j, u);
-      load8<false>(a.sa, (h[p] / rep) * HD + j + 64, w);
+      load8<false>(a.sa, (h / rep) * HD + j, u);
+      load8<false>(a.sa, (h / rep) * HD + j + 64, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { x[p][e] = __fdiv_rn(x[p][e], u[e]); y[p][e] = __fdiv_rn(y[p][e], w[e]); }
+      for (int e = 0; e < 8; ++e) { x[e] = __fdiv_rn(x[e], u[e]); y[e] = __fdiv_rn(y[e], w[e]); }
     }
-    __nv_bfloat16* o = a.Qo + row * a.ldq + h[p] * HD + j;
-    *reinterpret_cast<uint4*>(o) = pack_bf16x8(x[p]);
-    *reinterpret_cast<uint4*>(o + 64) = pack_bf16x8(y[p]);
+    __nv_bfloat16* o = a.Qo + row * a.ldq + h * HD + j;
+    *reinterpret_cast<uint4*>(o) = pack_bf16x8(x);
+    *reinterpret_cast<uint4*>(o + 64) = pack_bf16x8(y);
   }
 }
 
@@ -112,23 +103,42 @@ __device__ __forceinline__ float code_of(float v, float scale) {
   return fminf(fmaxf(rintf(__fdiv_rn(v, scale)), -127.f), 127.f);
 }
 
-// one (page of the call's, KV head, K or V); `red` is shared by the CTA's units
 template <bool BF, int NP, bool TREE>
-__device__ __forceinline__ void kv_unit(const AppendArgs& a, const SeqRows& s, int b, int unit, uint32_t (&red)[NT / 32]) {
+__global__ void __launch_bounds__(NT) kv_append_kernel(const AppendArgs a) {
+  __shared__ uint32_t red[NT / 32];
+  const int b = blockIdx.y;
+  const SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
   const int start = s.len - s.nq;                      // position of the first new token
+  if (!s.ok || (s.nq > 0 && (start < 0 || (TREE ? start >= a.n_pos : s.len > a.n_pos)))) {
+    if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
+    return;
+  }
+  if (s.nq == 0) return;
+  if ((int)blockIdx.x >= a.kv_units) {
+    q_unit<BF, TREE>(a, s, blockIdx.x - a.kv_units);
+    return;
+  }
   const int G = a.c.n_kv, P = a.c.page;
-  const bool is_v = unit & 1;
-  const int g = (unit >> 1) % G;
-  const int pg = start / P + (unit >> 1) / G;          // page of the sequence
+  const bool is_v = blockIdx.x & 1;
+  const int g = (blockIdx.x >> 1) % G;
+  const int pg = start / P + (blockIdx.x >> 1) / G;    // page of the sequence
+  if ((int64_t)pg * P >= s.len) return;
   const int id = pg < a.c.max_pages ? __ldg(a.c.page_table + (int64_t)b * a.c.max_pages + pg) : -1;
+  if (id < 0 || id >= a.c.n_pages) {
+    if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
+    return;
+  }
   const int kept = max(start - pg * P, 0);             // the page's tokens from before this call
   const int n_new = min(s.len, (pg + 1) * P) - pg * P - kept;
   const int grp = threadIdx.x >> 3, j = 8 * (threadIdx.x & 7);
+  const int64_t head = (int64_t)id * G + g;
+  float* scale_at = (is_v ? a.c.v_scale : a.c.k_scale) + head;
+  uint8_t* codes = (is_v ? a.c.v : a.c.k) + head * P * HD;
+  const float before = kept > 0 ? *scale_at : 0.f;
   const int64_t col = (int64_t)(a.n_heads + (is_v ? G : 0) + g) * HD + j;
 
-  // the rows are on their way while the page's id and scale are
   float x[NP][8], y[NP][8];
-  int at_pos[NP];
+  uint32_t big = 0;              // largest magnitude as its bits: ordered as the values, a NaN on top
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int i = p * GRP + grp;                 // new token of the page
@@ -137,25 +147,8 @@ __device__ __forceinline__ void kv_unit(const AppendArgs& a, const SeqRows& s, i
       const int64_t row = s.row0 + (pos - start);
       load8<BF>(a.QKV, row * a.ld + col, x[p]);
       load8<BF>(a.QKV, row * a.ld + col + 64, y[p]);
-      at_pos[p] = TREE && !is_v ? position<TREE>(a, s, pos - start) : pos;
-    }
-  }
-  if (id < 0 || id >= a.c.n_pages) {
-    if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
-    return;
-  }
-  const int64_t head = (int64_t)id * G + g;
-  float* scale_at = (is_v ? a.c.v_scale : a.c.k_scale) + head;
-  uint8_t* codes = (is_v ? a.c.v : a.c.k) + head * P * HD;
-  const float before = kept > 0 ? *scale_at : 0.f;
-
-  uint32_t big = 0;              // largest magnitude as its bits: ordered as the values, a NaN on top
-#pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    const int i = p * GRP + grp;
-    if (i < n_new) {
       if (!is_v) {
-        turn(a.rope, at_pos[p], j, x[p], y[p]);
+        turn(a.rope, TREE ? position<TREE>(a, s, pos - start) : pos, j, x[p], y[p]);
         if (a.sa) {
           float u[8], w[8];
           load8<false>(a.sa, g * HD + j, u);
@@ -169,7 +162,6 @@ __device__ __forceinline__ void kv_unit(const AppendArgs& a, const SeqRows& s, i
         big = max(big, max(__float_as_uint(x[p][e]) & 0x7fffffffu, __float_as_uint(y[p][e]) & 0x7fffffffu));
     }
   }
-  __syncthreads();                                     // the unit before has read `red`
   big = __reduce_max_sync(0xffffffffu, big);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = big;
   __syncthreads();
@@ -225,28 +217,6 @@ __device__ __forceinline__ void kv_unit(const AppendArgs& a, const SeqRows& s, i
   }
 }
 
-// A CTA's share of one sequence's units, those of the cache and then those of q: as many CTAs as the GPU holds a few times over,
-// so that a ragged batch launches none for rows that it does not have
-template <bool BF, int NP, bool TREE>
-__global__ void __launch_bounds__(NT, NP > 1 ? 2 : 3) kv_append_kernel(const AppendArgs a) {
-  __shared__ uint32_t red[NT / 32];
-  const int b = blockIdx.y;
-  const SeqRows s = seq_rows(a.c, a.cu_q, a.max_q, a.total_q, b);
-  const int start = s.len - s.nq;
-  if (!s.ok || (s.nq > 0 && (start < 0 || (TREE ? start >= a.n_pos : s.len > a.n_pos)))) {
-    if (threadIdx.x == 0) omq_set_status(a.status, OMQ_ERR_INVALID_ARG);
-    return;
-  }
-  if (s.nq == 0) return;
-  const int kv_units = 2 * a.c.n_kv * ((s.len - 1) / a.c.page - start / a.c.page + 1);
-  const int units = kv_units + (int)(((int64_t)s.nq * a.n_heads + QPASS * GRP - 1) / (QPASS * GRP));
-#pragma unroll 1
-  for (int u = blockIdx.x; u < units; u += gridDim.x) {
-    if (u < kv_units) kv_unit<BF, NP, TREE>(a, s, b, u, red);
-    else q_unit<BF, TREE>(a, s, u - kv_units);
-  }
-}
-
 template <bool BF, bool TREE>
 omq_status append_launch(cudaStream_t st, const AppendArgs& a, const dim3& grid) {
   if (a.c.page <= 32) kv_append_kernel<BF, 1, TREE><<<grid, NT, 0, st>>>(a);
@@ -274,13 +244,13 @@ omq_status append(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_
   OMQ_REQUIRE(!TREE || depth, OMQ_ERR_INVALID_ARG);
   OMQ_REQUIRE(omq_aligned4(depth), OMQ_ERR_ALIGN);
   AppendArgs a{*cache, total_q, max_q, cu_q, n_heads, QKV, ld, (const float2*)rope, n_pos, sa, (__nv_bfloat16*)Qo, ldq,
-               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, dev_status, depth};
+               (__nv_bfloat16*)Ko, (__nv_bfloat16*)Vo, ldkv, 0, dev_status, depth};
   const int64_t pages = ((int64_t)max_q + cache->page - 2) / cache->page + 1;    // that max_q tokens can touch
   const int64_t kv_units = 2 * pages * cache->n_kv;
   const int64_t q_units = ((int64_t)max_q * n_heads + QPASS * GRP - 1) / (QPASS * GRP);
   OMQ_REQUIRE(kv_units + q_units < (1ll << 31), OMQ_ERR_SHAPE);
-  const int64_t most = ((int64_t)omq_num_sms() * 9 + cache->B - 1) / cache->B;
-  const dim3 grid((unsigned)(kv_units + q_units < most ? kv_units + q_units : most), (unsigned)cache->B);
+  a.kv_units = (int)kv_units;
+  const dim3 grid((unsigned)(kv_units + q_units), (unsigned)cache->B);
   return dtype == OMQ_BF16 ? append_launch<true, TREE>((cudaStream_t)stream, a, grid)
                            : append_launch<false, TREE>((cudaStream_t)stream, a, grid);
 }

@@ -119,8 +119,8 @@ size_t tree_smem_bytes(int max_q) {
 // its slice of the vocabulary (the second pass over a row finds it in L1), and the parts meet in CTA 0.  Every CTA
 // does what CTA 0 posts and decides nothing itself, so no input can make them disagree at a barrier.
 // ------------------------------------------------------------------------------------------------
-constexpr int VT = 512, VW = VT / 32;       // threads, warps
-constexpr int BATCH = 4;                    // 128-token steps whose loads a warp has in flight
+constexpr int VT = 256, VW = VT / 32;       // threads, warps
+constexpr int BATCH = 2;                    // 128-token steps whose loads a warp has in flight
 constexpr int VMAX_CLUSTER = 8;
 constexpr int VMAX_V = 1 << 20;
 
@@ -136,23 +136,33 @@ __device__ __forceinline__ float probability(float p) { return fminf(fmaxf(p, 0.
 
 __device__ __forceinline__ float number(float u) { return fminf(fmaxf(u, 0.f), 0.99999994f); }  // in [0, 1)
 
-// p in [0, 1] times 2^60, truncated: the significand at 2^37, and back by 127 less the exponent
-__device__ __forceinline__ uint64_t fixed60(float p) {
-  const uint32_t b = __float_as_uint(p);
-  uint64_t w = (uint64_t)((b & 0x7fffffu) | 0x800000u) << 37;
+// a q times 2^60, truncated, for q in [0, 1] and a = a37 2^-37 below 8: 64 bits of product, at 2^37 of the significand, and back
+// by 127 less the exponent
+__device__ __forceinline__ uint64_t times60(float q, uint64_t a37) {
+  const uint32_t b = __float_as_uint(q), m = (b & 0x7fffffu) | 0x800000u;
+  uint64_t w = (uint64_t)m * (uint32_t)a37 + ((uint64_t)(m * (uint32_t)(a37 >> 32)) << 32);
   asm("shr.u64 %0, %0, %1;" : "+l"(w) : "r"(127u - (b >> 23)));            // (64 and more: zero)
   return w;
 }
+// p times 2^60, truncated
+__device__ __forceinline__ uint64_t fixed60(float p) {
+  uint64_t w = (uint64_t)((__float_as_uint(p) & 0x7fffffu) | 0x800000u) << 37;
+  asm("shr.u64 %0, %0, %1;" : "+l"(w) : "r"(127u - (__float_as_uint(p) >> 23)));
+  return w;
+}
 
-// a q times 2^60, truncated, for a = a52 2^-52: 88 bits of product and a shift; all ones when it passes 2^63
+// the same for a = a52 2^-52 of any size: 88 bits of product and a shift; all ones when it passes 2^63
 __device__ __forceinline__ uint64_t scaled60(float q, uint64_t a52) {
   const uint32_t b = __float_as_uint(q), e = b >> 23;
-  if (e == 0) return 0;
-  const uint32_t m = (b & 0x7fffffu) | 0x800000u;
+  const uint32_t m = e ? (b & 0x7fffffu) | 0x800000u : 0u;
   const uint64_t lo = (uint64_t)m * (uint32_t)a52, hi = (uint64_t)m * (uint32_t)(a52 >> 32) + (lo >> 32);   // hi : low half of lo
-  const int s = 142 - (int)e;               // right shift, 15 or more
-  if (s >= 32) return s >= 96 ? 0ull : hi >> (s - 32);
-  return hi >> (31 + s) ? ~0ull : (hi << (32 - s)) | ((uint32_t)lo >> s);
+  const int s = 142 - (int)e;               // right shift, 15 or more: of both words below 32, else of hi alone (64 and more: zero)
+  uint64_t far = hi, near = hi;
+  asm("shr.u64 %0, %0, %1;" : "+l"(far) : "r"((uint32_t)max(s - 32, 0)));
+  asm("shl.b64 %0, %0, %1;" : "+l"(near) : "r"((uint32_t)max(32 - s, 0)));
+  near |= (uint32_t)lo >> (s & 31);
+  if (hi >> min(31 + s, 63)) near = ~0ull;
+  return s >= 32 ? far : near;
 }
 
 __device__ __forceinline__ float prob_at(const void* base, bool bf, int64_t at) {
@@ -215,10 +225,10 @@ __device__ __forceinline__ void weights4(const VerifySmem& s, const float4& p, c
   w[0] = fixed60(probability(p.x)); w[1] = fixed60(probability(p.y)); w[2] = fixed60(probability(p.z)); w[3] = fixed60(probability(p.w));
   if (a52) {
     const float f[4] = {probability(q.x), probability(q.y), probability(q.z), probability(q.w)};
-    if (a52 == 1ull << 52) {                // a node's first rejection
+    if (a52 < 8ull << 52) {                 // (more only after eight rejections)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint64_t d = fixed60(f[k]);
+        const uint64_t d = times60(f[k], a52 >> 15);
         w[k] = w[k] > d ? w[k] - d : 0ull;
       }
     } else {
@@ -250,7 +260,7 @@ __device__ __forceinline__ void put64(uint64_t* at, int rank, int C, uint64_t v)
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(VT, 2) verify_kernel(const VerifyArgs a, const int C) {
+__global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const int C) {
   __shared__ VerifySmem s;
   const int b = blockIdx.x / C, rank = blockIdx.x - b * C, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lo = min(a.V, rank * a.slice), hi = min(a.V, lo + a.slice);
@@ -289,13 +299,13 @@ __global__ void __launch_bounds__(VT, 2) verify_kernel(const VerifyArgs a, const
   }
   sync();                                   // the nodes are there; every CTA runs, so its shared memory can be written
 
-  // ---- the walk: every warp of CTA 0 alike ----
+  // ---- the walk: one warp, since its tests are in double, of which an SM has few units ----
   int cur = 0, count = 1, i = 0;            // node, tokens with the new one, last child tested
   double A = 0.0, T = 1.0;
   bool fresh = false;                       // the last pass's sums are those of (cur, A)
   Order o;
   while (true) {
-    if (rank == 0) {
+    if (rank == 0 && warp == 0) {
       o = Order{n > 0 ? row0 + cur : -1, DRAW_WHOLE, 0, 0, 0ull};
       while (n > 0 && count < a.steps) {
         uint32_t m = 0;
@@ -390,7 +400,7 @@ __global__ void __launch_bounds__(VT, 2) verify_kernel(const VerifyArgs a, const
       sync();                               // every CTA has read the parts
     }
     if (o.kind == PASS) {
-      T = (double)total * (1.0 / 1152921504606846976.0);
+      if (rank == 0 && warp == 0) T = (double)total * (1.0 / 1152921504606846976.0);
       fresh = true;
       continue;
     }
