@@ -591,7 +591,7 @@ TreePlan tree_plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
     const int r = rows <= 8 ? 8 : 16;
     p.cost = TreeCost{r, r, 2, 1, 1};
   } else {
-    p.cost = TreeCost{ATTN_TC_ROWS, ATTN_TC_ROWS, 6, 1, 1};
+    p.cost = TreeCost{ATTN_TC_ROWS, ATTN_TC_ROWS, 4, 1, 1};
   }
   p.min_share = p.cost.start + 2 * p.cost.weight;             // 256 tokens
   // no more CTAs than there is work for by the bounds
