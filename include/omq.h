@@ -507,7 +507,7 @@ omq_status omq_selftest_qgemm_wait(omq_stream_t stream, int64_t M, int64_t N, in
  * dev_status, and the sequence (or page) is skipped: nothing of it is read or written in the pool. */
 typedef struct {
   uint8_t* k; uint8_t* v;            /* [n_pages, n_kv, page, 128] codes */
-  float* k_scale; float* v_scale;    /* [n_pages, n_kv] */
+  float* k_scale; float* v_scale;    /* [n_pages, n_kv], 4-byte aligned */
   const int32_t* page_table;         /* [B, max_pages] */
   const int32_t* kv_len;             /* [B] */
   int32_t n_pages, n_kv, page, max_pages, B;
@@ -577,7 +577,8 @@ omq_status omq_kv_append_tree(omq_stream_t stream, const omq_kv_cache* cache, in
 
 /* omq_kv_attention with other visible keys: row i of a sequence sees every key j < kv_len - rows, and key
  * kv_len - rows + k where bit k of its words in seen [total_q, words] is set (any bits, not only a tree's; those from
- * the sequence's number of rows on count for nothing).  All else as there. */
+ * the sequence's number of rows on count for nothing).  max_q n_heads / n_kv at most 2^20 (OMQ_ERR_SHAPE); a workspace is
+ * always needed.  All else as there. */
 omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
                                  const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
                                  const void* Q, int64_t ldq, float* Of, void* Ob, int64_t ldo, float* lse, void* workspace,

@@ -508,7 +508,6 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
 
 // The same for the cut units of draft trees: a unit per blockIdx.x, its rows a warp each
 __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeArgs t) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const TreeCut u = t.cut[blockIdx.x];
   const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
   if (u.parts == 0 || u.r0 + r >= u.R) return;
@@ -688,17 +687,7 @@ omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache,
   cudaStream_t st = (cudaStream_t)stream;
   OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
                             : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));
-  // launched beside the one before, whose end it waits for itself
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)p.ctas, (unsigned)(p.cost.rows / 8));
-  cfg.blockDim = dim3(256);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kv_attention_tree_join_kernel, t) != cudaSuccess) { cudaGetLastError(); return OMQ_ERR_CUDA; }
+  kv_attention_tree_join_kernel<<<dim3((unsigned)p.ctas, (unsigned)(p.cost.rows / 8)), 256, 0, st>>>(t);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }

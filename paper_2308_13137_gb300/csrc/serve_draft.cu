@@ -136,11 +136,14 @@ __device__ __forceinline__ float probability(float p) { return fminf(fmaxf(p, 0.
 
 __device__ __forceinline__ float number(float u) { return fminf(fmaxf(u, 0.f), 0.99999994f); }  // in [0, 1)
 
-// a q times 2^60, truncated, for q in [0, 1] and a = a37 2^-37 below 8: 64 bits of product, at 2^37 of the significand, and back
-// by 127 less the exponent
-__device__ __forceinline__ uint64_t times60(float q, uint64_t a37) {
-  const uint32_t b = __float_as_uint(q), m = (b & 0x7fffffu) | 0x800000u;
+// a q times 2^60, truncated, for q in [0, 1] and a = a52 2^-52 below 8: the product of significand and a52, less 15 bits, is
+// that for an exponent of 127 and has 64 bits; back by 127 less the exponent.  (a52's last 15 bits are zero after a node's first
+// rejection, a = 1)
+__device__ __forceinline__ uint64_t times60(float q, uint64_t a52) {
+  const uint32_t b = __float_as_uint(q), m = (b & 0x7fffffu) | 0x800000u, rest = (uint32_t)a52 & 0x7fffu;
+  const uint64_t a37 = a52 >> 15;
   uint64_t w = (uint64_t)m * (uint32_t)a37 + ((uint64_t)(m * (uint32_t)(a37 >> 32)) << 32);
+  if (rest) w += (uint64_t)m * rest >> 15;
   asm("shr.u64 %0, %0, %1;" : "+l"(w) : "r"(127u - (b >> 23)));            // (64 and more: zero)
   return w;
 }
@@ -228,7 +231,7 @@ __device__ __forceinline__ void weights4(const VerifySmem& s, const float4& p, c
     if (a52 < 8ull << 52) {                 // (more only after eight rejections)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint64_t d = times60(f[k], a52 >> 15);
+        const uint64_t d = times60(f[k], a52);
         w[k] = w[k] > d ? w[k] - d : 0ull;
       }
     } else {
