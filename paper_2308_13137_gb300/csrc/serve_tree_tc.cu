@@ -176,14 +176,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
 
   const TreeShare share = tree_share<THREADS>(t, reinterpret_cast<int64_t*>(smem + SCAN));
   if (share.hi <= share.lo) return;
-  if (threadIdx.x == 0) {
-    uint64_t* const bar = reinterpret_cast<uint64_t*>(smem + BAR);
-    for (int i = 0; i < N_BAR; ++i) {
-      const uint32_t at = bars + 8 * i;
-      mbar_init(&bar[i], at < s_full ? 4 : (at < pv_ready ? 1 : (at < pv_done ? 8 : (at < s_free ? 1 : (at < o_free ? 4 :
-                         (at < chunk_full ? 8 : (at < chunk_empty ? 1 : (at < raw_full ? 27 : (at == q_seen ? 2 : 1)))))))));
-    }
-    *abort_flag = 0;
+  if (threadIdx.x < N_BAR) {                  // (one thread after the other's barrier: 170 cycles each)
+    const uint32_t at = bars + 8 * threadIdx.x;
+    const uint32_t count = at < s_full ? 4 : (at < pv_ready ? 1 : (at < pv_done ? 8 : (at < s_free ? 1 : (at < o_free ? 4 :
+                           (at < chunk_full ? 8 : (at < chunk_empty ? 1 : (at < raw_full ? 27 : (at == q_seen ? 2 : 1))))))));
+    mbar_init(reinterpret_cast<uint64_t*>(smem + BAR) + threadIdx.x, count);
+    if (threadIdx.x == 0) *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc(tmem_holder, 512);
@@ -292,6 +290,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
         }
         if (!soon(chunk_empty + 8 * (k % RING), ((k / RING) & 1) ^ 1)) { fail(); break; }
         Chunk& w = chunk_at(k);
+        if (flags & FIRST) {                  // the unit's queries to L2, by tokens
+          const int rep = t.rep, i0 = p.r0 / rep, i1 = (min(p.R, p.r0 + BMR) + rep - 1) / rep;
+          for (int i = i0 + lane; i < i1; i += 32)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(a.Q + (int64_t)(p.row0 + i) * a.ldq + p.g * rep * HD)), "r"(rep * HD * 2) : "memory");
+        }
         if (!(flags & DONE)) {
           const int np = (t1 - t0 + P - 1) >> pshift;
           for (int i = lane; i < np; i += 32) {
@@ -302,11 +305,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
             x.w = 0.f;
             w.page[i] = x;
           }
-        }
-        if (flags & FIRST) {                  // the unit's queries to L2, by tokens
-          const int rep = t.rep, i0 = p.r0 / rep, i1 = (min(p.R, p.r0 + BMR) + rep - 1) / rep;
-          for (int i = i0 + lane; i < i1; i += 32)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(a.Q + (int64_t)(p.row0 + i) * a.ldq + p.g * rep * HD)), "r"(rep * HD * 2) : "memory");
         }
         if (lane == 0) { w.p = p; w.t0 = t0; w.t1 = t1; w.flags = flags; }
         arrive(chunk_full + 8 * (k % RING), lane);
