@@ -158,7 +158,6 @@ __global__ void __launch_bounds__(W * 32, 2)
     b = p.b; g = p.g; r0 = p.r0; R = p.R; part = p.part;
     start = p.len - p.nq;
     t_begin = p.t0; t_end = p.t1;
-    if (threadIdx.x == 0) pieces->more[piece ^ 1] = pieces->walk.next(args, &pieces->piece[piece ^ 1]);
   }
 
   // ---- query fragments and row factors; page records of the tokens (of WIN pages at a time) ----
@@ -168,6 +167,43 @@ __global__ void __launch_bounds__(W * 32, 2)
   };
   const int first_end = TREE ? min(t_end, t_begin + WIN * P) : t_end;
   records(t_begin, first_end);
+  // this warp's ring: its n-th tile of a window is tile warp + n W, in the slots one after another
+  constexpr int DEPTH = S::DEPTH;
+  uint64_t* wfull = full + warp * DEPTH;
+  const uint32_t ring = smem_u32(smem + warp * DEPTH * TILE_BYTES);
+  auto fill = [&](const int n, const int slot) {              // the converged warp; one lane issues
+    const int t = (warp + n * W) * TILE, id = pid[t >> pshift];
+    uint8_t* dst = smem + (warp * DEPTH + slot) * TILE_BYTES;
+    const int row = (id * a.c.n_kv + g) * P + (t & (P - 1));
+    if (elect_one()) {
+      if (id < 0) {
+        mbar_arrive(&wfull[slot]);                            // its tokens read as unseen
+      } else {
+        mbar_expect_tx(&wfull[slot], TILE_BYTES);
+        tma_load_3d(&tmK, &wfull[slot], dst, 0, row, 0);
+        tma_load_3d(&tmV, &wfull[slot], dst + TILE * HD, 0, row, 0);
+      }
+    }
+    __syncwarp();
+  };
+
+  auto tiles_of = [&](int from, int to, int* tiles) {         // of a window, and this warp's
+    *tiles = to > from ? (to - from + TILE - 1) / TILE : 0;
+    return *tiles > warp ? (*tiles - warp + W - 1) / W : 0;
+  };
+  auto fill_first = [&](int from, int to) {
+    int tiles;
+    const int mine = tiles_of(from, to, &tiles), filled = min(DEPTH, mine);
+    for (int n = 0; n < filled; ++n) fill(n, slot + n < DEPTH ? slot + n : slot + n - DEPTH);
+    return filled;
+  };
+  int filled = 0;
+  if constexpr (TREE) {                                       // the first tiles are on their way while the queries are laid out
+    __syncthreads();
+    filled = fill_first(t_begin, first_end);
+    // (the next piece's walk, by a thread whose warp has the fewest tiles)
+    if (threadIdx.x == (W - 1) * 32) pieces->more[piece ^ 1] = pieces->walk.next(args, &pieces->piece[piece ^ 1]);
+  }
   for (int r = warp; r < ROWS; r += W) {
     const int row = r0 + r;
     float v[4];
@@ -196,26 +232,6 @@ __global__ void __launch_bounds__(W * 32, 2)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[nt][i][e] = 0.f;
   }
-
-  // this warp's ring: its n-th tile of a window is tile warp + n W, in the slots one after another
-  constexpr int DEPTH = S::DEPTH;
-  uint64_t* wfull = full + warp * DEPTH;
-  const uint32_t ring = smem_u32(smem + warp * DEPTH * TILE_BYTES);
-  auto fill = [&](const int n, const int slot) {              // the converged warp; one lane issues
-    const int t = (warp + n * W) * TILE, id = pid[t >> pshift];
-    uint8_t* dst = smem + (warp * DEPTH + slot) * TILE_BYTES;
-    const int row = (id * a.c.n_kv + g) * P + (t & (P - 1));
-    if (elect_one()) {
-      if (id < 0) {
-        mbar_arrive(&wfull[slot]);                            // its tokens read as unseen
-      } else {
-        mbar_expect_tx(&wfull[slot], TILE_BYTES);
-        tma_load_3d(&tmK, &wfull[slot], dst, 0, row, 0);
-        tma_load_3d(&tmV, &wfull[slot], dst + TILE * HD, 0, row, 0);
-      }
-    }
-    __syncwarp();
-  };
 
   {
     const uint2* qfw = qf + lane;
@@ -346,9 +362,9 @@ __global__ void __launch_bounds__(W * 32, 2)
     };
 
     for (int from = t_begin, to = first_end;;) {
-      const int tiles = to > from ? (to - from + TILE - 1) / TILE : 0, mine = tiles > warp ? (tiles - warp + W - 1) / W : 0;
-      int filled = min(DEPTH, mine);
-      for (int n = 0; n < filled; ++n) fill(n, slot + n < DEPTH ? slot + n : slot + n - DEPTH);
+      int tiles;
+      const int mine = tiles_of(from, to, &tiles);
+      if (!TREE || from != t_begin) filled = fill_first(from, to);
       int n = 0;
       for (; n < mine; ++n) {
         if (!warp_wait(&wfull[slot], turn)) {
