@@ -478,6 +478,11 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
 // 16 codes under a scale that is 1 / r of theirs
 __device__ __forceinline__ uint4 again16(uint4 u, float r) {
   uint32_t* w = reinterpret_cast<uint32_t*>(&u);
+  if (r == 1.f) {                           // all whole numbers already: only the clamp of code 0
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __vmaxu4(w[k], 0x01010101u);
+    return u;
+  }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     uint32_t o = 0;
