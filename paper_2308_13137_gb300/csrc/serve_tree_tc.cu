@@ -195,9 +195,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   auto chunk_wait = [&](int k) { return soon(chunk_full + 8 * (k % RING), (k / RING) & 1); };
   auto tiles_of = [](const Chunk& w) { return (w.t1 - w.t0 + TT - 1) / TT; };
 
-  // registers: 128 x 48 + 256 x 144 + 512 x 40 of the launch's 896 x 72
+  // registers: 128 x 56 + 256 x 144 + 512 x 40 of the launch's 896 x 72; with copies of rows 128 x 56 + 256 x 120 + 512 x 48
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (CP > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 3) {
       // ---------------- S of one group: the whole warp runs the loop, one lane issues ----------------
       constexpr uint32_t idS = idesc_f16(BMR, TT);
@@ -319,7 +320,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     }
   } else if (warp >= 12) {
     // ---------------- convert ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (CP > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     const int cw = warp - 12, set = cw >> 3, q = warp & 3;
     const bool is_v = cw & 4;
     // 16 codes of channels 16 c .. of tokens 16 q + r + 4 e.  The eight lanes of a load or store phase have the first half of
@@ -398,7 +400,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     }
   } else {
     // ---------------- softmax: one row per thread ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    if (CP > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     constexpr int SPAN = BMR / CP, TW = TT / CP, QT = TW / NQ;          // rows held, tokens of a thread, of them on a page
     const int rep = t.rep;
     auto by_rep = [&](int row) { return rep == 1 ? row : (int)__umulhi((uint32_t)row, t.rep_inv); };            // row / rep
