@@ -597,21 +597,19 @@ omq_status attn_launch(cudaStream_t st, const A& args, dim3 grid) {
   return OMQ_OK;
 }
 
-// Draft trees: rows of a unit, CTAs, and what the units cost (serve_tree.cuh)
+// Draft trees: rows of a unit, CTAs, and what the units cost (serve_tree.cuh).  A unit of up to 16 rows takes this file's form,
+// at two CTAs per SM, larger ones the tcgen05 tiles.  The start of a unit there (queries, first tiles, output) is 4 slots of
+// 128 tokens: with 2, 6, 10 and 16 instead 64 sequences of up to 4099 tokens and 104 rows, 141 us, take up to 16 us more.  A
+// CTA gets no less than half a start and a slot (a whole start and two: 6 sequences of 948 tokens and 126 rows 34.8 us, not 31.5).
 struct TreePlan { TreeCost cost; int64_t min_share; int ctas; };
 TreePlan tree_plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
   const int64_t rows = (int64_t)max_q * (n_heads / n_kv);
   TreePlan p;
-  if (rows <= 16) {
-    const int r = rows <= 8 ? 8 : 16;
-    p.cost = TreeCost{r, r, 2, 1, 1};
-  } else {
-    p.cost = TreeCost{ATTN_TC_ROWS, ATTN_TC_ROWS, 4, 1, 1};
-  }
-  p.min_share = p.cost.start / 2 + p.cost.weight;            // (a start and 256 tokens: 6 sequences of 948 tokens, 126 rows, 34.8 us, and 31.5)
+  p.cost = rows <= 8 ? TreeCost{8, 2} : (rows <= 16 ? TreeCost{16, 2} : TreeCost{ATTN_TC_ROWS, 4});
+  p.min_share = p.cost.start / 2 + 1;
   // no more CTAs than there is work for by the bounds
   const int64_t units = B * n_kv * ((rows + p.cost.rows - 1) / p.cost.rows), slots = ((int64_t)max_kv + TREE_SLOT - 1) / TREE_SLOT;
-  const int64_t most = units * (p.cost.start + slots * p.cost.weight) / p.min_share + 1;
+  const int64_t most = units * (p.cost.start + slots) / p.min_share + 1;
   const int64_t ctas = omq_num_sms() * (rows <= 16 ? 2ll : 1ll);
   p.ctas = (int)(most < ctas ? most : ctas);
   return p;

@@ -10,7 +10,8 @@ namespace {
 // a node has a jump over its 2^k nearest ancestors, so the chain of dependent steps is log2(depth) long.  The bits of
 // trees up to WALK deep are set by walking up, one word for each ancestor; those of deeper ones by doubling too: a
 // node takes over the bits of the node that it jumps to.  (A node whose bits grow in the same round passes on more than its 2^k
-// ancestors: they are ancestors of the reader too.)  Bound: the launch and the round trips to the parents and back.
+// ancestors: they are ancestors of the reader too.)  Bound: the launch and the round trips to the parents and back: 4.1 us
+// for one tree, of which the launch is nearly all, 8.2 us for 384 of 509 nodes (by doubling throughout 10.2).
 // ------------------------------------------------------------------------------------------------
 constexpr int WALK = 24;
 constexpr int MAX_NODES = 1024;
@@ -118,6 +119,11 @@ size_t tree_smem_bytes(int max_q) {
 // walk that accepts first children touches shared memory only.  For a pass it posts (row, a) to all CTAs, each sums
 // its slice of the vocabulary (the second pass over a row finds it in L1), and the parts meet in CTA 0.  Every CTA
 // does what CTA 0 posts and decides nothing itself, so no input can make them disagree at a barrier.
+//
+// Bound: the passes of the longest walk, one after the other, each a read of the row (from the caches after the first), 30
+// integer instructions per token, and two cluster barriers: 2 us and 2.5 for 32000 tokens, 6 and 2.5 for 128256.  64
+// sequences of up to 15 rows, 128256 tokens, 41 us; one of 26 rows, 32000 tokens, 10 to 22 us by the length of its walk.  All
+// clusters of 64 sequences are resident (four CTAs per SM, hence the registers); CTAs of 512 threads, in two waves, 61 us.
 // ------------------------------------------------------------------------------------------------
 constexpr int VT = 256, VW = VT / 32;       // threads, warps
 constexpr int BATCH = 2;                    // 128-token steps whose loads a warp has in flight
@@ -503,8 +509,8 @@ __device__ __forceinline__ uint4 again16(uint4 u, float r) {
 // page of larger values, and the codes of the page are rounded again then, as in the append; tokens that move within
 // the page are rounded like those that stay.  A warp per (sequence, KV head, K or V, layer), four tokens at a time, eight lanes
 // each; the CTA's eight warps share the path.  Bound: the chain of path, page, scale and codes; few registers and no barrier
-// between warps keep 64 of them on an SM (a CTA of four warps for each head, each with the moved tokens in
-// registers: 51.2 us for 64 sequences of 8 heads in 40 layers).
+// between warps keep 40 of them on an SM: 64 sequences of 8 heads in 40 layers 17.8 us, one of 32 heads in 32 layers 8 (a CTA of
+// four warps for each head, with the moved tokens in registers, 51.2 us).
 // ------------------------------------------------------------------------------------------------
 constexpr int KT = 256, KW = KT / 32;       // threads, warps
 constexpr int KEEP_LAYERS = 128;            // caches of a launch

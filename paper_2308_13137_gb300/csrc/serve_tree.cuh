@@ -3,7 +3,7 @@
 // A unit of work is (sequence, KV head, a tile of its query rows); it goes over all of the sequence's tokens, whose number
 // only the device knows.  Sequences differ in length by orders of magnitude, so a grid of units leaves most SMs
 // waiting for the longest ones.  Here the units lie one after another on a line, each as long as it costs (its
-// start, then a weight per 128 tokens), and CTA c of n takes the c-th n-th of the line, cutting units where they lie
+// start, then one per 128 tokens), and CTA c of n takes the c-th n-th of the line, cutting units where they lie
 // across a border.  A unit that one CTA has whole is written straight away; of a cut one each CTA leaves a partial result,
 // and the joining launch adds them in order of tokens.
 #pragma once
@@ -11,9 +11,8 @@
 
 constexpr int TREE_SLOT = 128;              // tokens: whole pages and whole tiles of both forms
 
-// what a unit costs: start + 128-token slots times a weight; units of up to `rows` query rows, with another weight for
-// those of up to `small` rows
-struct TreeCost { int rows, small, start, weight, weight_small; };
+// query rows of a unit, at most, and what its start costs, in 128-token slots
+struct TreeCost { int rows, start; };
 
 // In the workspace, for the joining launch: the cut unit whose first tokens a CTA has.  It lies in `parts` partial results:
 // `first`, then the first ones of the CTAs behind.  parts 0: none
@@ -31,8 +30,7 @@ struct TreeArgs {
 struct TreeSeq {
   int row0, nq, len, R, tiles, slots;       // R: query rows of a KV head, in `tiles` units
   bool ok;
-  int64_t full, head;                       // cost of a unit that is not the last of its head, of all units of a head
-  int w_last;
+  int64_t unit, head;                       // cost of a unit, of all units of a head
 };
 
 __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& t, int b) {
@@ -44,20 +42,15 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& t, int b) {
   q.R = s.nq * t.rep;
   q.tiles = (q.R + t.cost.rows - 1) / t.cost.rows;
   q.slots = (q.len + TREE_SLOT - 1) / TREE_SLOT;
-  q.w_last = q.R - (q.tiles - 1) * t.cost.rows > t.cost.small ? t.cost.weight : t.cost.weight_small;
-  q.full = t.cost.start + (int64_t)q.slots * t.cost.weight;
-  q.head = q.tiles > 0 ? (q.tiles - 1) * q.full + t.cost.start + (int64_t)q.slots * q.w_last : 0;
+  q.unit = t.cost.start + (int64_t)q.slots;
+  q.head = q.tiles * q.unit;
   return q;
 }
 
-// the unit `tile` of a head, at `at` on the line: its weight
-__device__ __forceinline__ int tree_weight(const TreeArgs& t, const TreeSeq& q, int tile) {
-  return tile == q.tiles - 1 ? q.w_last : t.cost.weight;
-}
-// slots of it that lie before x on the line
-__device__ __forceinline__ int tree_slots(const TreeArgs& t, const TreeSeq& q, int w, int64_t at, int64_t x) {
+// slots of the unit at `at` on the line that lie before x
+__device__ __forceinline__ int tree_slots(const TreeArgs& t, const TreeSeq& q, int64_t at, int64_t x) {
   const int64_t k = x - at - t.cost.start;
-  return k <= 0 ? 0 : (k >= (int64_t)q.slots * w ? q.slots : (int)((uint32_t)k / (uint32_t)w));    // (slots below 2^24)
+  return k <= 0 ? 0 : (k >= q.slots ? q.slots : (int)k);
 }
 __device__ __forceinline__ int64_t tree_border(int64_t total, int64_t n, int64_t c) { return total * c / n; }
 
@@ -136,21 +129,20 @@ struct TreeWalk {
     q = tree_seq(t, s.b);
     const int64_t k = s.lo - s.before;
     g = (int)(k / q.head);
-    tile = (int)min((int64_t)q.tiles - 1, (k - g * q.head) / q.full);
-    at = s.before + g * q.head + tile * q.full;
+    tile = (int)((k - g * q.head) / q.unit);
+    at = s.before + g * q.head + tile * q.unit;
   }
   __device__ __forceinline__ bool next(const TreeArgs& t, TreePiece* p) {
     while (at < s.hi && s.hi > s.lo) {
-      const int w = tree_weight(t, q, tile);
-      const int a = tree_slots(t, q, w, at, s.lo), z = tree_slots(t, q, w, at, s.hi);
+      const int a = tree_slots(t, q, at, s.lo), z = tree_slots(t, q, at, s.hi);
       const bool take = z > a || (q.slots == 0 && at >= s.lo);
       *p = TreePiece{s.b, q.row0, q.nq, q.len, q.R, g, tile * t.cost.rows, a * TREE_SLOT, min(q.len, z * TREE_SLOT),
                      a == 0 && z == q.slots ? -1 : (int)(2 * blockIdx.x + (at >= s.lo))};
       if (take && p->part >= 0 && a == 0) {                   // the CTA that has the end: as many borders lie before it
-        const int last = (int)(((at + t.cost.start + (int64_t)q.slots * w) * s.n - 1) / s.total);
+        const int last = (int)(((at + q.unit) * s.n - 1) / s.total);
         t.cut[blockIdx.x] = TreeCut{q.row0, g, tile * t.cost.rows, q.R, p->part, last - (int)blockIdx.x + 1};
       }
-      at += t.cost.start + (int64_t)q.slots * w;
+      at += q.unit;
       if (++tile == q.tiles) {
         tile = 0;
         if (++g == t.a.c.n_kv) {
