@@ -590,12 +590,11 @@ __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ Kee
       bool other;
       const bool got = get(jb + sub, &u, &from, &other);
       if (got && other) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const uint32_t w = e < 4 ? u.x : (e < 8 ? u.y : (e < 12 ? u.z : u.w));
-          top = max(top, (uint32_t)abs((int)((w >> (8 * (e & 3))) & 255u) - 128));
-        }
+        // largest |code - 128|, four bytes at a time
+        uint32_t four = __vmaxu4(__vmaxu4(__vabsdiffu4(u.x, 0x80808080u), __vabsdiffu4(u.y, 0x80808080u)),
+                                 __vmaxu4(__vabsdiffu4(u.z, 0x80808080u), __vabsdiffu4(u.w, 0x80808080u)));
+        four = __vmaxu4(four, four >> 16);
+        const uint32_t top = max(four & 255u, four >> 8 & 255u);
         big = max(big, __float_as_uint(__fmul_rn((float)top, from)) & 0x7fffffffu);
       }
       if (jb == j0) { u0 = u; from0 = from; other0 = other; got0 = got; }

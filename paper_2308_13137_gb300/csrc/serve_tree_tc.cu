@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   const uint32_t k_full = bars;                      // [4] K of a tile converted
   const uint32_t s_full = k_full + 8 * KBUF;         // [4] scores formed (K consumed)
   const uint32_t pv_ready = s_full + 8 * KBUF;       // [3] V of the tile converted and its weights written
-  const uint32_t pv_done = pv_ready + 8 * BUF;       // [3] product formed: weights, scores and V consumed
+  const uint32_t pv_done = pv_ready + 8 * BUF;       // [3] product formed: weights and V consumed
   const uint32_t s_free = pv_done + 8 * BUF;         // [2] scores read
   const uint32_t o_free = s_free + 16;               // both accumulators read
   const uint32_t q_ready = o_free + 8;               // the piece's queries lie in tensor memory
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   const uint32_t chunk_empty = chunk_full + 8 * RING;                     // [RING]
   const uint32_t raw_full = chunk_empty + 8 * RING;  // [converting warp][DEPTH]
   const uint32_t q_seen = raw_full + 8 * 16 * DEPTH; // both issuing warps have come to the piece
-  const uint32_t drain = q_seen + 8;  // [4] of the issuing warps
+  const uint32_t drain = q_seen + 8;                 // [4] of the issuing warps
   constexpr int N_BAR = 2 * KBUF + 2 * BUF + 5 + 2 * RING + 16 * DEPTH + 5;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + BAR + 8 * N_BAR);
   static_assert(8 * N_BAR + 8 <= SCAN - BAR, "");
@@ -202,8 +202,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
 
   // registers: 128 x 56 + 256 x 144 + 512 x 40 of the launch's 896 x 72; with copies of rows 128 x 56 + 256 x 120 + 512 x 48
   if (warp < 4) {
-    if (CP > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 3) {
       // ---------------- S of one group: the whole warp runs the loop, one lane issues ----------------
       constexpr uint32_t idS = idesc_f16(BMR, TT);
@@ -391,7 +390,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       ph ^= slot == 0;
       --on_way;
       fence_async_smem();                     // the converted tile -> visible to the tensor core
-      arrive(full + 8 * at.b, lane);              // (and the slot has been read)
+      arrive(full + 8 * at.b, lane);          // (and the slot has been read)
       if (is_v) {
         at.move(2);
       } else {
