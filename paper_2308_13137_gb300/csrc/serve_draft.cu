@@ -507,10 +507,11 @@ __device__ __forceinline__ uint4 again16(uint4 u, float r) {
 // omq_kv_keep.  Place j of a sequence's drafted tokens takes the codes of node path[j], which lies at j or behind it, so in
 // order of j no place is written before what it held has been read.  A page's scale grows where a token comes in from a
 // page of larger values, and the codes of the page are rounded again then, as in the append; tokens that move within
-// the page are rounded like those that stay.  A warp per (sequence, KV head, K or V, layer), four tokens at a time, eight lanes
+// the page are rounded like those that stay.  A warp per (sequence, KV head, layer), four tokens' K and V at a time, eight lanes
 // each; the CTA's eight warps share the path.  Bound: the chain of path, page, scale and codes; few registers and no barrier
-// between warps keep 40 of them on an SM: 64 sequences of 8 heads in 40 layers 17.8 us, one of 32 heads in 32 layers 8 (a CTA of
-// four warps for each head, with the moved tokens in registers, 51.2 us).
+// between warps keep 32 of them on an SM: 64 sequences of 8 heads in 40 layers 13.4 us, one of 32 heads in 32 layers 7.7.  (A CTA
+// of four warps for each head and each of K and V, with the moved tokens in registers, 51.2 us; a warp for each 17.8, bound by
+// the instructions around the moves.)
 // ------------------------------------------------------------------------------------------------
 constexpr int KT = 256, KW = KT / 32;       // threads, warps
 constexpr int KEEP_LAYERS = 128;            // caches of a launch
@@ -530,8 +531,7 @@ template <int L>
 __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ KeepArgs<L> a) {
   __shared__ int32_t path[MAX_NODES];
   const KeepCache& c = a.c[blockIdx.z];
-  const int b = blockIdx.y, lane = threadIdx.x & 31, unit = blockIdx.x * KW + (threadIdx.x >> 5), g = unit >> 1;
-  const bool is_v = unit & 1;
+  const int b = blockIdx.y, lane = threadIdx.x & 31, g = blockIdx.x * KW + (threadIdx.x >> 5);
   const int P = a.page, shift = 31 - __clz(P);
   const int32_t* const my_path = a.path + (int64_t)b * a.steps;
   const int ahead = (int)threadIdx.x < a.steps ? __ldg(my_path + threadIdx.x) : 0;     // asked for beside the lengths
@@ -549,9 +549,9 @@ __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ Kee
     if (threadIdx.x == 0) omq_set_status(c.status, OMQ_ERR_INVALID_ARG);
     return;
   }
-  if (unit >= 2 * a.n_kv) return;
-  uint8_t* const codes = is_v ? c.v : c.k;
-  float* const scales = is_v ? c.v_scale : c.k_scale;
+  if (g >= a.n_kv) return;
+  uint8_t* const codes[2] = {c.k, c.v};
+  float* const scales[2] = {c.k_scale, c.v_scale};
   auto page_id = [&](int pg) {
     const int id = pg < c.max_pages ? __ldg(c.page_table + (int64_t)b * c.max_pages + pg) : -1;
     if (id >= 0 && id < c.n_pages) return id;
@@ -563,67 +563,85 @@ __global__ void __launch_bounds__(KT) kv_keep_kernel(const __grid_constant__ Kee
   while (j0 < n && path[j0] == j0) ++j0;    // these lie where they belong
   while (j0 < n) {
     const int pg = (start + j0) >> shift, j1 = min(n, ((pg + 1) << shift) - start);
-    // four tokens' codes; whether they come from another page, and under which scale; nothing for one that stays, or whose page is
-    // out of range
-    auto get = [&](int j, uint4* u, float* from, bool* other) {
+    // four tokens' codes of K and V; whether they come from another page, and under which scales; nothing for one that stays, or
+    // whose page is out of range
+    auto get = [&](int j, uint4 (&u)[2], float (&from)[2], bool* other) {
       if (j >= j1 || path[j] == j) return false;
       const int at = start + path[j], src = page_id(at >> shift);
       if (src < 0) return false;
-      const int64_t head = (int64_t)src * a.n_kv + g;
+      const int64_t head = (int64_t)src * a.n_kv + g, place = (head * P + (at & (P - 1))) * 128 + at16;
       *other = at >> shift != pg;
-      *u = *reinterpret_cast<const uint4*>(codes + (head * P + (at & (P - 1))) * 128 + at16);
-      *from = scales[head];
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        u[v] = *reinterpret_cast<const uint4*>(codes[v] + place);
+        from[v] = scales[v][head];
+      }
       return true;
     };
     const int id = page_id(pg);
     if (id < 0) { j0 = j1; continue; }
-    const int64_t head = (int64_t)id * a.n_kv + g;
-    uint8_t* const dst = codes + head * P * 128 + at16;
-    const float before = scales[head];
-    uint32_t big = 0;
-    uint4 u0 = make_uint4(0, 0, 0, 0);
-    float from0 = 0.f;
+    const int64_t head = (int64_t)id * a.n_kv + g, dst = head * P * 128 + at16;
+    const float before[2] = {scales[0][head], scales[1][head]};
+    uint32_t big[2] = {0, 0};
+    uint4 u0[2];
+    float from0[2];
     bool other0 = false, got0 = false;
     for (int jb = j0; jb < j1; jb += 4) {
-      uint4 u;
-      float from;
+      uint4 u[2];
+      float from[2];
       bool other;
-      const bool got = get(jb + sub, &u, &from, &other);
+      const bool got = get(jb + sub, u, from, &other);
       if (got && other) {
-        // largest |code - 128|, four bytes at a time
-        uint32_t four = __vmaxu4(__vmaxu4(__vabsdiffu4(u.x, 0x80808080u), __vabsdiffu4(u.y, 0x80808080u)),
-                                 __vmaxu4(__vabsdiffu4(u.z, 0x80808080u), __vabsdiffu4(u.w, 0x80808080u)));
-        four = __vmaxu4(four, four >> 16);
-        const uint32_t top = max(four & 255u, four >> 8 & 255u);
-        big = max(big, __float_as_uint(__fmul_rn((float)top, from)) & 0x7fffffffu);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {       // largest |code - 128|, four bytes at a time
+          uint32_t four = __vmaxu4(__vmaxu4(__vabsdiffu4(u[v].x, 0x80808080u), __vabsdiffu4(u[v].y, 0x80808080u)),
+                                   __vmaxu4(__vabsdiffu4(u[v].z, 0x80808080u), __vabsdiffu4(u[v].w, 0x80808080u)));
+          four = __vmaxu4(four, four >> 16);
+          const uint32_t top = max(four & 255u, four >> 8 & 255u);
+          big[v] = max(big[v], __float_as_uint(__fmul_rn((float)top, from[v])) & 0x7fffffffu);
+        }
       }
-      if (jb == j0) { u0 = u; from0 = from; other0 = other; got0 = got; }
-    }
-    big = __reduce_max_sync(0xffffffffu, big);
-    const float want = __fdiv_rn(__uint_as_float(big), 127.f);
-    const bool grows = !(before >= want) && before == before;
-    const float after = grows ? want : before;
-    if (grows) {
-      const float r = __fdiv_rn(before, after);
-      for (int k = sub; k < P; k += 4) {
-        uint4* at = reinterpret_cast<uint4*>(dst + k * 128);
-        *at = again16(*at, r);
+      if (jb == j0) {
+        other0 = other; got0 = got;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) { u0[v] = u[v]; from0[v] = from[v]; }
       }
-      if (lane == 0) scales[head] = after;
-      __syncwarp();
     }
+    float after[2];
+    bool any = false;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const float want = __fdiv_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, big[v])), 127.f);
+      const bool grows = !(before[v] >= want) && before[v] == before[v];
+      after[v] = grows ? want : before[v];
+      if (grows) {
+        const float r = __fdiv_rn(before[v], after[v]);
+        for (int k = sub; k < P; k += 4) {
+          uint4* at = reinterpret_cast<uint4*>(codes[v] + dst + k * 128);
+          *at = again16(*at, r);
+        }
+        if (lane == 0) scales[v][head] = after[v];
+        any = true;
+      }
+    }
+    if (any) __syncwarp();
     for (int jb = j0; jb < j1; jb += 4) {
-      uint4 u = u0;
-      float from = from0;
+      uint4 u[2] = {u0[0], u0[1]};
+      float from[2] = {from0[0], from0[1]};
       bool other = other0, got = got0;
       // (what moves within a page that grew has been rounded by now, but for the first four, read before)
-      if (jb > j0) got = get(jb + sub, &u, &from, &other);
+      if (jb > j0) got = get(jb + sub, u, from, &other);
       if (got) {
-        const float r = after > 0.f ? __fdiv_rn(other || jb == j0 ? from : after, after) : 0.f;
-        u = again16(u, r);
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+          u[v] = again16(u[v], after[v] > 0.f ? __fdiv_rn(other || jb == j0 ? from[v] : after[v], after[v]) : 0.f);
       }
       __syncwarp();
-      if (got) *reinterpret_cast<uint4*>(dst + (start + jb + sub - (pg << shift)) * 128) = u;
+      if (got) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+          *reinterpret_cast<uint4*>(codes[v] + dst + (start + jb + sub - (pg << shift)) * 128) = u[v];
+      }
       __syncwarp();
     }
     j0 = j1;
@@ -641,7 +659,7 @@ omq_status keep_launch(cudaStream_t st, const omq_kv_cache* const* caches, int32
     a.c[i] = KeepCache{c.k, c.v, c.k_scale, c.v_scale, c.page_table, c.kv_len, status ? status[i < n ? i : 0] : nullptr, c.n_pages,
                        c.max_pages};
   }
-  kv_keep_kernel<L><<<dim3((2 * a.n_kv + KW - 1) / KW, caches[0]->B, n), KT, 0, st>>>(a);
+  kv_keep_kernel<L><<<dim3((a.n_kv + KW - 1) / KW, caches[0]->B, n), KT, 0, st>>>(a);
   OMQ_LAUNCH_CHECK();
   return OMQ_OK;
 }
