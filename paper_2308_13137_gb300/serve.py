@@ -170,8 +170,9 @@ class Verified(NamedTuple):
 def draft_tree(parent, cu_q=None, max_q: Optional[int] = None, out: Optional[DraftTree] = None, status=None) -> DraftTree:
     """Depths and visible rows of trees of drafted tokens (omq_draft_tree), once per step for all layers.  parent: int32,
     the row of every row's parent within its sequence (before its own; -1 at row 0); [rows] with cu_q and max_q, or
-    [B, n] for n rows of every sequence.  out: a DraftTree whose depth and seen are filled.  status: an int32 device word
-    that is set where a parent is out of range (a KVCache's serves)."""
+    [B, n] for n rows of every sequence.  out: a DraftTree whose depth and seen are filled; its parent, cu_q and max_q may be
+    another step's, and what comes back has this call's.  status: an int32 device word that is set where a parent is out of
+    range (a KVCache's serves)."""
     if cu_q is None:
         _need(parent.dim() == 2 and (max_q is None or max_q == parent.shape[1]), "parent: [B, n] without cu_q")
         max_q, parent = parent.shape[1], parent.reshape(-1)
@@ -183,7 +184,15 @@ def draft_tree(parent, cu_q=None, max_q: Optional[int] = None, out: Optional[Dra
     code = _calls.draft_tree(parent, cu_q, max_q, out.depth, out.seen, status)
     if code:
         _lib.check("omq_draft_tree", code)
+    if out.max_q != max_q or not _same(out.parent, parent) or not _same(out.cu_q, cu_q):
+        out = DraftTree(parent, out.depth, out.seen, cu_q, max_q)
     return out
+
+
+def _same(a: Optional[torch.Tensor], b: Optional[torch.Tensor]) -> bool:
+    """The same int32 values in the same place, whichever tensor objects name them (b has passed the call's checks)."""
+    return a is b or (a is not None and b is not None and a.data_ptr() == b.data_ptr() and a.shape == b.shape and
+                      a.dtype == b.dtype and a.device == b.device and a.is_contiguous())
 
 
 def _rows_of(tree: Optional[DraftTree], cu_q, max_q):
