@@ -601,7 +601,8 @@ size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t 
  *   for a sequence without rows); out_tokens [B, steps]: the accepted tokens and, at count - 1, the new one, -1 behind.
  * Sums are exact (64-bit fixed point, terms truncated to 2^-60): the same numbers on every run and split.
  * A parent or token out of range sets OMQ_ERR_INVALID_ARG in dev_status, and that row is nobody's child; a new token for
- * which no weight is left in P either sets it and is 0.  V at most 2^20. */
+ * which no weight is left in P either sets it and is 0.  So does one from weights R that add up to 8 or more (of a row far
+ * from adding up to one); where they do after a rejection, the row's other children are not tested.  V at most 2^20. */
 omq_status omq_verify_drafts(omq_stream_t stream, int32_t B, int32_t total_q, int32_t max_q, const int32_t* cu_q,
                              const int32_t* parent, const int32_t* tokens, int64_t V, const void* P, const void* Q,
                              int32_t dtype, int64_t ldp, int64_t ldq, const float* u, int32_t steps, int32_t* out_tokens,

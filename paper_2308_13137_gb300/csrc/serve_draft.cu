@@ -113,7 +113,7 @@ size_t tree_smem_bytes(int max_q) {
 // The outcome is whole numbers, and a comparison next to its border must not depend on the order of a sum: terms
 // are taken in 64-bit fixed point (2^-60, truncated), sums are exact, and the scalar tests are in double.  The new token is
 // the first index whose running sum passes floor(u S): the 64-bit formula's, unless u S lies within V 2^-60 of a
-// running sum.
+// running sum.  Sums of 8 and more, which only rows that are far from adding up to one can have, are marked and reported, not held.
 //
 // A cluster of CTAs per sequence.  CTA 0 walks: every node's p(x) and q(x) are fetched at the start, all at once, so a
 // walk that accepts first children touches shared memory only.  For a pass it posts (row, a) to all CTAs, each sums
@@ -256,10 +256,18 @@ __device__ __forceinline__ void weights4(const VerifySmem& s, const float4& p, c
   }
 }
 
+// A sum of weights that comes to 8 (2^63) or more keeps its top bit from there on, whatever is added: 2^63 - 1 and a term of up
+// to 2^63 do not pass 64 bits, and a sum with the bit is not looked at further.
+constexpr uint64_t HEAVY = 1ull << 63;
+__device__ __forceinline__ uint64_t add_held(uint64_t a, uint64_t b) { return (a + b) | ((a | b) & HEAVY); }
+
+// of a warp, in digits of 24 bits and the 16 above them: three reductions (five steps of marked sums of
+// shuffled values cost 64 x 128256 up to 1.5 us)
 __device__ __forceinline__ uint64_t warp_sum64(uint64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+  const uint64_t low = ((uint64_t)__reduce_add_sync(0xffffffffu, (uint32_t)(v >> 24) & 0xffffffu) << 24) +
+                       __reduce_add_sync(0xffffffffu, (uint32_t)v & 0xffffffu);
+  const uint32_t top = __reduce_add_sync(0xffffffffu, (uint32_t)(v >> 48)) + (uint32_t)(low >> 48);
+  return (low & 0xffffffffffffull) | (uint64_t)top << 48 | (top >> 15 ? HEAVY : 0ull);
 }
 
 // to this CTA's shared variable and its like in the other CTAs of the cluster
@@ -316,7 +324,7 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
   while (true) {
     if (rank == 0 && warp == 0) {
       o = Order{n > 0 ? row0 + cur : -1, DRAW_WHOLE, 0, 0, 0ull};
-      while (n > 0 && count < a.steps) {
+      while (n > 0 && count < a.steps && T >= 0.0) {         // (below zero: a row without a sum, see below)
         uint32_t m = 0;
         int base = (i + 1) & ~31;
         for (; base < n && !m; base += 32) {
@@ -375,6 +383,8 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
     while (true) {
       if (o.kind != DRAW) {
         uint64_t sum = 0;
+        uint32_t high = 0;                  // of all sums so far: a batch adds 2^63 at most
+        static_assert(BATCH <= 2, "");
         for (int at = w_lo + 4 * lane; at < w_hi; at += 128 * BATCH) {
           float4 p[BATCH], q[BATCH];
           fetch<BF, BATCH>(a, o.row, o.a52 != 0, at, w_hi, p, q);
@@ -384,14 +394,15 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
             weights4(s, p[k], q[k], o.a52, cut, at + 128 * k, lo, w_hi, w);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
           }
+          high |= (uint32_t)(sum >> 32);
         }
-        sum = warp_sum64(sum);
+        sum = warp_sum64(sum | ((uint64_t)high << 32 & HEAVY));
         if (lane == 0) s.warp_sum[warp] = sum;
         __syncthreads();
         if (threadIdx.x < C) {
           uint64_t mine = 0;
 #pragma unroll
-          for (int k = 0; k < VW; ++k) mine += s.warp_sum[k];
+          for (int k = 0; k < VW; ++k) mine = add_held(mine, s.warp_sum[k]);
           put64(&s.part[rank], threadIdx.x, C, mine);
         }
         sync();
@@ -399,7 +410,7 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
       total = before = 0;
       for (int k = 0; k < C; ++k) {
         if (k < rank) before += s.part[k];
-        total += s.part[k];
+        total = add_held(total, s.part[k]);
       }
       if (total != 0 || o.kind == PASS || o.kind == DRAW_WHOLE) break;
       // nothing is left of the weights (rows that do not sum to one): the new token comes from p as it is
@@ -408,16 +419,21 @@ __global__ void __launch_bounds__(VT, 4) verify_kernel(const VerifyArgs a, const
       cut = false;
       sync();                               // every CTA has read the parts
     }
+    const bool heavy = total & HEAVY;       // the weights add up to 8 or more: no distribution, and no sum to draw from
     if (o.kind == PASS) {
-      if (rank == 0 && warp == 0) T = (double)total * (1.0 / 1152921504606846976.0);
+      if (rank == 0 && warp == 0) {
+        T = heavy ? -1.0 : (double)total * (1.0 / 1152921504606846976.0);
+        if (heavy) A = 0.0;                 // p itself is posted next, and adds up to no less
+      }
       fresh = true;
       continue;
     }
     // ---- the new token: the first one whose running sum passes floor(u total) ----
     if (rank == 0 && threadIdx.x == 0) {
       a.out_count[b] = o.count;
-      if (total == 0) { omq_set_status(a.status, OMQ_ERR_INVALID_ARG); tokens[o.count - 1] = 0; }
+      if (total == 0 || heavy) { omq_set_status(a.status, OMQ_ERR_INVALID_ARG); tokens[o.count - 1] = 0; }
     }
+    if (heavy) return;
     const uint64_t t = __umul64hi((uint64_t)((double)number(__ldg(a.u + row0)) * 18446744073709551616.0), total);
     // the warp share that t falls into, if this CTA has it
     uint64_t run = before;
