@@ -586,6 +586,14 @@ omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache,
 size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t max_q, int32_t max_kv, int32_t n_heads,
                                             int32_t n_kv);
 
+/* Failure-detection self-test of that call for more than 16 query rows per KV head, as omq_selftest_bounded_wait: O fp32, every
+ * wait bounded by wait_limit_ns (1e3 .. 1e9; counted in tries).  withhold: the chunk of up to 1024 tokens of each CTA's share
+ * that never comes, so that the waits for it run out, *dev_status becomes OMQ_ERR_TIMEOUT and O is unspecified; -1: none. */
+omq_status omq_selftest_tree_wait(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                                  const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
+                                  const void* Q, int64_t ldq, float* O, int64_t ldo, void* workspace, size_t ws_bytes,
+                                  uint64_t wait_limit_ns, int32_t withhold, int32_t* dev_status);
+
 /* Drafted tokens against the target's probabilities, from given random numbers; the outcome is distributed as
  * tokens drawn from the target.  The walk starts at row 0.  At a row with weights R (first its row of P) and T = 1,
  * its children are tested in order: child c with token x = tokens[c] is accepted, and the walk goes on there, when

@@ -138,6 +138,7 @@ _SIGS = {
     "omq_kv_append_tree": (I32, [P, P, I32, I32, P, P, I32, P, I32, I64, P, I32, P, P, I64, P, P, I64, P]),
     "omq_kv_attention_tree": (I32, [P, P, I32, I32, P, P, I32, I32, I32, P, I64, P, P, I64, P, P, SZ, P]),
     "omq_kv_attention_tree_workspace_size": (SZ, [I32, I32, I32, I32, I32, I32]),
+    "omq_selftest_tree_wait": (I32, [P, P, I32, I32, P, P, I32, I32, I32, P, I64, P, I64, P, SZ, ctypes.c_uint64, I32, P]),
     "omq_verify_drafts": (I32, [P, I32, I32, I32, P, P, P, I64, P, P, I32, I64, I64, P, I32, P, P, P, P]),
     "omq_kv_keep": (I32, [P, P, P, I32, I32, I32, P, P, I32, P]),
     "omq_stream_status": (I32, [P, P, POINTER(c_int32)]),
@@ -439,6 +440,14 @@ def omq_kv_attention_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) ->
 
 def omq_kv_attention_tree_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv) -> int:
     return lib().omq_kv_attention_tree_workspace_size(B, total_q, max_q, max_kv, n_heads, n_kv)
+
+
+def omq_selftest_tree_wait(cache, total_q, max_q, cu_q, seen, words, max_kv, n_heads, Q, O, workspace, wait_limit_ns, withhold,
+                           dev_status, stream=None):
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    check("omq_selftest_tree_wait", lib().omq_selftest_tree_wait(
+        stream_handle(stream), ctypes.byref(cache), total_q, max_q, ptr(cu_q), ptr(seen), words, max_kv, n_heads, ptr(Q),
+        n_heads * 128, ptr(O), n_heads * 128, ptr(workspace), ws_bytes, int(wait_limit_ns), int(withhold), ptr(dev_status)))
 
 
 def omq_stream_status(dev_status, stream=None) -> int:

@@ -637,6 +637,32 @@ omq_status attention_check(const omq_kv_cache* cache, int32_t total_q, int32_t m
   return OMQ_OK;
 }
 
+omq_status attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q, const int32_t* cu_q,
+                          const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads, const void* Q, int64_t ldq, float* Of,
+                          void* Ob, int64_t ldo, float* lse, void* workspace, size_t ws_bytes, uint32_t tries, int withhold,
+                          int32_t* dev_status) {
+  OMQ_REQUIRE(seen, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(max_q > 0 && words >= (max_q - 1) / 32 + 1, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(omq_aligned4(seen), OMQ_ERR_ALIGN);
+  OMQ_TRY(attention_check(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace));
+  const TreePlan p = tree_plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
+  const int rep = n_heads / cache->n_kv;
+  OMQ_REQUIRE((int64_t)max_q * rep <= 1 << 20, OMQ_ERR_SHAPE);
+  size_t pl, cut;
+  OMQ_REQUIRE(workspace && ws_bytes >= tree_workspace(p, &pl, &cut), OMQ_ERR_WORKSPACE);
+  char* const ws = (char*)workspace;
+  const TreeArgs t{AttnArgs{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
+                            lse, nullptr, nullptr, 0, 1, 1, dev_status, seen, words},
+                   p.cost, p.min_share, rep, (uint32_t)(((1ull << 32) + rep - 1) / rep), (TreeCut*)(ws + cut), (float*)ws,
+                   (float*)(ws + pl), tries, withhold};
+  cudaStream_t st = (cudaStream_t)stream;
+  OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
+                            : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));
+  kv_attention_tree_join_kernel<<<dim3((unsigned)p.ctas, (unsigned)(p.cost.rows / 8)), 256, 0, st>>>(t);
+  OMQ_LAUNCH_CHECK();
+  return OMQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -684,26 +710,22 @@ omq_status omq_kv_attention_tree(omq_stream_t stream, const omq_kv_cache* cache,
                                  const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
                                  const void* Q, int64_t ldq, float* Of, void* Ob, int64_t ldo, float* lse, void* workspace,
                                  size_t ws_bytes, int32_t* dev_status) {
-  OMQ_REQUIRE(seen, OMQ_ERR_INVALID_ARG);
-  OMQ_REQUIRE(max_q > 0 && words >= (max_q - 1) / 32 + 1, OMQ_ERR_SHAPE);
-  OMQ_REQUIRE(omq_aligned4(seen), OMQ_ERR_ALIGN);
-  OMQ_TRY(attention_check(cache, total_q, max_q, cu_q, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace));
-  const TreePlan p = tree_plan_of(cache->B, max_q, max_kv, n_heads, cache->n_kv);
-  const int rep = n_heads / cache->n_kv;
-  OMQ_REQUIRE((int64_t)max_q * rep <= 1 << 20, OMQ_ERR_SHAPE);
-  size_t pl, cut;
-  OMQ_REQUIRE(workspace && ws_bytes >= tree_workspace(p, &pl, &cut), OMQ_ERR_WORKSPACE);
-  char* const ws = (char*)workspace;
-  const TreeArgs t{AttnArgs{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
-                            lse, nullptr, nullptr, 0, 1, 1, dev_status, seen, words},
-                   p.cost, p.min_share, rep, (uint32_t)(((1ull << 32) + rep - 1) / rep), (TreeCut*)(ws + cut), (float*)ws,
-                   (float*)(ws + pl)};
-  cudaStream_t st = (cudaStream_t)stream;
-  OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
-                            : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));
-  kv_attention_tree_join_kernel<<<dim3((unsigned)p.ctas, (unsigned)(p.cost.rows / 8)), 256, 0, st>>>(t);
-  OMQ_LAUNCH_CHECK();
-  return OMQ_OK;
+  return attention_tree(stream, cache, total_q, max_q, cu_q, seen, words, max_kv, n_heads, Q, ldq, Of, Ob, ldo, lse, workspace,
+                        ws_bytes, TREE_ORDINARY, -1, dev_status);
+}
+
+// Failure-detection self-test: the tcgen05 form with every wait bounded by wait_limit_ns, and optionally without one of the
+// chunks that its roles share, so that their waits for it run out.
+omq_status omq_selftest_tree_wait(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
+                                  const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,
+                                  const void* Q, int64_t ldq, float* O, int64_t ldo, void* workspace, size_t ws_bytes,
+                                  uint64_t wait_limit_ns, int32_t withhold, int32_t* dev_status) {
+  OMQ_REQUIRE(cache && cache->n_kv > 0 && n_heads > 0 && max_q > 0, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE((int64_t)max_q * (n_heads / cache->n_kv) > 16, OMQ_ERR_SHAPE);
+  OMQ_REQUIRE(withhold >= -1, OMQ_ERR_INVALID_ARG);
+  OMQ_REQUIRE(wait_limit_ns >= 1000ull && wait_limit_ns <= OMQ_WAIT_LIMIT_NS, OMQ_ERR_INVALID_ARG);
+  return attention_tree(stream, cache, total_q, max_q, cu_q, seen, words, max_kv, n_heads, Q, ldq, O, nullptr, ldo, nullptr, workspace,
+                        ws_bytes, tree_tries(wait_limit_ns), withhold, dev_status);
 }
 
 }  // extern "C"

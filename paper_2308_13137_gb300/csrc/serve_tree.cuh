@@ -10,6 +10,9 @@
 #include "serve_attn.cuh"
 
 constexpr int TREE_SLOT = 128;              // tokens: whole pages and whole tiles of both forms
+// limit of a wait of the tcgen05 form, in tries (wait_tries)
+constexpr uint32_t tree_tries(uint64_t limit_ns) { return (uint32_t)(limit_ns / 1300u); }
+constexpr uint32_t TREE_TRIES = tree_tries(OMQ_WAIT_LIMIT_NS), TREE_ORDINARY = ~0u;
 
 // query rows of a unit, at most, and what its start costs, in 128-token slots
 struct TreeCost { int rows, start; };
@@ -25,6 +28,8 @@ struct TreeArgs {
   int rep; uint32_t rep_inv;                // query heads per KV head, and 2^32 over it rounded up: row / rep for rows below 2^20
   TreeCut* cut;                             // [n]
   float* po; float* pl;                     // partial results: [2 n][rows][128] and their log-sum-exp
+  uint32_t tries;                           // self-test of the tcgen05 form: limit of a wait (else TREE_ORDINARY),
+  int withhold;                             // and the chunk of each share that never comes (-1: none)
 };
 
 struct TreeSeq {

@@ -81,10 +81,10 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
 // A converged warp's bounded wait.  The phase is mostly over already: a test costs 50 cycles, a wait 120.  A try without a time
 // hint suspends the warp for 1.3 us at most and costs one instruction; with a hint it is a loop of polls, and those of
 // this kernel's 28 warps were more than half of all its instructions.
-__device__ __forceinline__ bool soon(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool wait_tries(uint32_t bar, uint32_t parity, uint32_t tries) {
   bool ok = bar_test(bar, parity);
   for (uint32_t i = 0; !__all_sync(0xffffffffu, ok); ++i) {
-    if (i == (uint32_t)(OMQ_WAIT_LIMIT_NS / 1300u)) return false;
+    if (i == tries) return false;
     uint32_t p;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -151,8 +151,9 @@ struct Place {
   __device__ __forceinline__ Place before() const { return b >= 2 ? Place{b - 2, ph} : Place{b + BUF - 2, ph ^ 1}; }      // of tile j - 2
 };
 
-// CP: copies of a row (serve_attn_tc.cu); NQ: pages (at most) that a softmax thread's 64 / CP tokens of a tile lie on
-template <int CP, int NQ>
+// CP: copies of a row (serve_attn_tc.cu); NQ: pages (at most) that a softmax thread's 64 / CP tokens of a tile lie on; TEST: the
+// waits' limit and the chunk that never comes are the self-test's (a limit from memory, 16 x 64 rows 210 us in place of 207)
+template <int CP, int NQ, bool TEST>
 __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const TreeArgs t) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
@@ -196,6 +197,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   const uint32_t tmem = *tmem_holder;
   // a role whose wait runs out sets the flag and leaves; those that wait for it follow.  All meet at the end
   auto fail = [&]() { omq_set_status(a.status, OMQ_ERR_TIMEOUT); *abort_flag = 1; };
+  auto soon = [&](uint32_t bar, uint32_t parity) { return wait_tries(bar, parity, TEST ? t.tries : TREE_TRIES); };
+  // for what is in flight when a role leaves, whatever the limit of its waits
+  auto landed = [&](uint32_t bar, uint32_t parity) { return wait_tries(bar, parity, TREE_TRIES); };
   auto chunk_at = [&](int k) -> Chunk& { return chunks[k % RING]; };
   auto chunk_wait = [&](int k) { return soon(chunk_full + 8 * (k % RING), (k / RING) & 1); };
   auto tiles_of = [](const Chunk& w) { return (w.t1 - w.t0 + TT - 1) / TT; };
@@ -293,6 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
           t1 = min(p.t1, t0 + CHUNK);
           if (t1 == p.t1) flags |= LAST;
         }
+        if (TEST && k == t.withhold) break;   // this chunk never comes
         if (!soon(chunk_empty + 8 * (k % RING), ((k / RING) & 1) ^ 1)) { fail(); break; }
         Chunk& w = chunk_at(k);
         if (flags & FIRST) {                  // the unit's queries to L2, by tokens
@@ -316,11 +321,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
         if (flags & DONE) break;
       }
     }
-    // what is in flight ends before the tensor memory is released
+    // The products end before the tensor memory is released.  (Without a condition: a wait of another role may run out, and
+    // end the CTA, after this one has issued all it had.)
     __syncwarp();
-    if (warp != 2 && *abort_flag) {
+    if (warp != 2) {
       if (elect_one()) commit(drain + 8 * warp);
-      soon(drain + 8 * warp, 0);
+      landed(drain + 8 * warp, 0);
     }
   } else if (warp >= 12) {
     // ---------------- convert ----------------
@@ -400,7 +406,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
     }
     if (!ok) {                                // no copy may land after this CTA has left
       fail();
-      for (int s = slot; on_way > 0; --on_way, s ^= 1, ph ^= s == 0) soon(got + 8 * s, ph);
+      for (int s = slot; on_way > 0; --on_way, s ^= 1, ph ^= s == 0) landed(got + 8 * s, ph);
     }
   } else {
     // ---------------- softmax: one row per thread ----------------
@@ -810,9 +816,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
   }
 }
 
-template <int CP, int NQ>
+template <int CP, int NQ, bool TEST>
 omq_status launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
-  auto kern = kv_attention_tree_tc_kernel<CP, NQ>;
+  auto kern = kv_attention_tree_tc_kernel<CP, NQ, TEST>;
   static std::atomic<uint64_t> allowed{0};
   OMQ_TRY(omq_allow_smem(allowed, kern, SMEM));
   kern<<<n_ctas, THREADS, SMEM, st>>>(t);
@@ -820,13 +826,18 @@ omq_status launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
   return OMQ_OK;
 }
 
-}  // namespace
-
 // By the most rows that a KV head has in the call.
-omq_status tree_tc_launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
+template <bool TEST>
+omq_status launch_form(cudaStream_t st, const TreeArgs& t, int n_ctas) {
   const int64_t rows = (int64_t)t.a.max_q * (t.a.n_heads / t.a.c.n_kv);
   const int page = t.a.c.page;
-  if (rows <= BMR / 4) return launch<4, 1>(st, t, n_ctas);
-  if (rows <= BMR / 2) return page >= 32 ? launch<2, 1>(st, t, n_ctas) : launch<2, 2>(st, t, n_ctas);
-  return page >= TT ? launch<1, 1>(st, t, n_ctas) : launch<1, 4>(st, t, n_ctas);
+  if (rows <= BMR / 4) return launch<4, 1, TEST>(st, t, n_ctas);
+  if (rows <= BMR / 2) return page >= 32 ? launch<2, 1, TEST>(st, t, n_ctas) : launch<2, 2, TEST>(st, t, n_ctas);
+  return page >= TT ? launch<1, 1, TEST>(st, t, n_ctas) : launch<1, 4, TEST>(st, t, n_ctas);
+}
+
+}  // namespace
+
+omq_status tree_tc_launch(cudaStream_t st, const TreeArgs& t, int n_ctas) {
+  return t.tries != TREE_ORDINARY ? launch_form<true>(st, t, n_ctas) : launch_form<false>(st, t, n_ctas);
 }
