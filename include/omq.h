@@ -587,7 +587,7 @@ size_t omq_kv_attention_tree_workspace_size(int32_t B, int32_t total_q, int32_t 
                                             int32_t n_kv);
 
 /* Failure-detection self-test of that call for more than 16 query rows per KV head, as omq_selftest_bounded_wait: O fp32, every
- * wait bounded by wait_limit_ns (1e3 .. 1e9; counted in tries).  withhold: the chunk of up to 1024 tokens of each CTA's share
+ * wait bounded by wait_limit_ns (1e3 .. 1e9; counted in tries of about 4 us).  withhold: the chunk of up to 1024 tokens of each CTA's share
  * that never comes, so that the waits for it run out, *dev_status becomes OMQ_ERR_TIMEOUT and O is unspecified; -1: none. */
 omq_status omq_selftest_tree_wait(omq_stream_t stream, const omq_kv_cache* cache, int32_t total_q, int32_t max_q,
                                   const int32_t* cu_q, const uint32_t* seen, int32_t words, int32_t max_kv, int32_t n_heads,

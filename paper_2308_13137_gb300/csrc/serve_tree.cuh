@@ -10,8 +10,8 @@
 #include "serve_attn.cuh"
 
 constexpr int TREE_SLOT = 128;              // tokens: whole pages and whole tiles of both forms
-// limit of a wait of the tcgen05 form, in tries (wait_tries)
-constexpr uint32_t tree_tries(uint64_t limit_ns) { return (uint32_t)(limit_ns / 1300u); }
+// limit of a wait of the tcgen05 form, in tries of 3.8 us (wait_tries); one that came back at once would still leave it 10 ms
+constexpr uint32_t tree_tries(uint64_t limit_ns) { return (uint32_t)(limit_ns / 4000u); }
 constexpr uint32_t TREE_TRIES = tree_tries(OMQ_WAIT_LIMIT_NS), TREE_ORDINARY = ~0u;
 
 // query rows of a unit, at most, and what its start costs, in 128-token slots

@@ -88,6 +88,16 @@ def test_roles_that_give_up_anywhere(cuda_lib, heads, n_kv, n, page):
     assert TIMEOUT in codes[:10]                             # without a try, the first chunk is not there yet
 
 
+def test_the_librarys_own_limit(cuda_lib):
+    """A withheld chunk under the limit of ordinary calls: two waits one after another at most."""
+    run = _Run(8, 1, 8, 32)
+    want = run.ordinary()
+    code, took = run(1_000_000_000, 0)
+    print(f"a wait that nothing ends: {took:.3f} s")
+    assert code == TIMEOUT and 0.05 < took < 2.5
+    assert torch.equal(run.ordinary(), want)
+
+
 def test_refusals(cuda_lib):
     from paper_2308_13137_gb300 import _lib
     run = _Run(8, 1, 8, 32)
