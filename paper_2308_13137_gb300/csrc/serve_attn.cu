@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(W * 32, 2)
         if (part >= 0) {
           const int64_t at = (int64_t)part * ROWS + row - r0;
           *reinterpret_cast<float4*>(args.po + at * HD + 4 * lane) = o;
-          if (lane == 0) args.pl[at] = lse;
+          if (lane == 0) args.pl[at] = attn_part(mm, L);
           continue;
         }
       }
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeA
   if (u.parts == 0 || u.r0 + r >= u.R) return;
   auto place = [&](int c) { return (int64_t)(c == 0 ? u.first : 2 * ((int)blockIdx.x + c)) * t.cost.rows + r; };
   float top = -INFINITY;
-  for (int c = lane; c < u.parts; c += 32) top = fmaxf(top, t.pl[place(c)]);
+  for (int c = lane; c < u.parts; c += 32) top = fmaxf(top, t.pl[place(c)].x);
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
   const float ref = top == -INFINITY ? 0.f : top;
@@ -538,7 +538,8 @@ __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeA
 #pragma unroll 4
   for (int c = 0; c < u.parts; ++c) {
     const int64_t k = place(c);
-    const float f = ex2(t.pl[k] - ref);
+    const float2 l = t.pl[k];
+    const float f = ex2((l.x - ref) + l.y);
     const float4 x = *reinterpret_cast<const float4*>(t.po + k * HD + 4 * lane);
     L += f;
     o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
@@ -619,7 +620,7 @@ TreePlan tree_plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
 size_t tree_workspace(const TreePlan& p, size_t* pl, size_t* cut) {
   const size_t parts = (size_t)2 * p.ctas * p.cost.rows;
   *pl = parts * HD * sizeof(float);
-  *cut = *pl + (parts * sizeof(float) + 255) / 256 * 256;
+  *cut = *pl + (parts * sizeof(float2) + 255) / 256 * 256;
   return *cut + ((size_t)p.ctas * sizeof(TreeCut) + 255) / 256 * 256;
 }
 
@@ -654,7 +655,7 @@ omq_status attention_tree(omq_stream_t stream, const omq_kv_cache* cache, int32_
   const TreeArgs t{AttnArgs{*cache, total_q, max_q, cu_q, max_kv, n_heads, (const __nv_bfloat16*)Q, ldq, Of, (__nv_bfloat16*)Ob, ldo,
                             lse, nullptr, nullptr, 0, 1, 1, dev_status, seen, words},
                    p.cost, p.min_share, rep, (uint32_t)(((1ull << 32) + rep - 1) / rep), (TreeCut*)(ws + cut), (float*)ws,
-                   (float*)(ws + pl), tries, withhold};
+                   (float2*)(ws + pl), tries, withhold};
   cudaStream_t st = (cudaStream_t)stream;
   OMQ_TRY((p.cost.rows == 8 ? attn_launch<1>(st, t, dim3(p.ctas))
                             : (p.cost.rows == 16 ? attn_launch<2>(st, t, dim3(p.ctas)) : tree_tc_launch(st, t, p.ctas))));

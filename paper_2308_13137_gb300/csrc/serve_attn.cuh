@@ -94,6 +94,15 @@ __device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s,
   attn_query_scaled(attn_query_raw(a, s, g, rep, row, rows, lane), v, sh);
 }
 
+// Log-sum-exp of a part of a row's tokens (reference m, sum L), and what its rounding to fp32 left out.  Parts are weighed by
+// 2^ of it: from 4096 on the rounding would count beside the fp16 weights' 2^-11, and at 2^24 a part of ten tokens with the top
+// score would weigh what a part of one does.  Below, the rest is taken as nothing.
+__device__ __forceinline__ float2 attn_part(float m, float L) {
+  if (L == 0.f) return make_float2(-INFINITY, 0.f);           // (a NaN score is not an empty row)
+  const float lg = log2f(L), lse = m + lg;
+  return make_float2(lse, fabsf(lse) < 4096.f ? 0.f : lg - (lse - m));
+}
+
 // page record i of a chunk that starts at page `first`: id (-1 and the status word where it is out of range),
 // key scale times log2(e) / sqrt(128), log2 of the value scale
 __device__ __forceinline__ void attn_page(const AttnArgs& a, int b, int g, int page, int* id_out, float* ks, float* lv) {

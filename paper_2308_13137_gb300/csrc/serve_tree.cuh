@@ -27,7 +27,7 @@ struct TreeArgs {
   int64_t min_share;                        // of the line, per CTA
   int rep; uint32_t rep_inv;                // query heads per KV head, and 2^32 over it rounded up: row / rep for rows below 2^20
   TreeCut* cut;                             // [n]
-  float* po; float* pl;                     // partial results: [2 n][rows][128] and their log-sum-exp
+  float* po; float2* pl;                    // partial results: [2 n][rows][128] and their log-sum-exp (attn_part)
   uint32_t tries;                           // self-test of the tcgen05 form: limit of a wait (else TREE_ORDINARY),
   int withhold;                             // and the chunk of each share that never comes (-1: none)
 };

@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
       const float c1 = none ? 0.f : c * ex2((refs[3 * BMR + r] - mm) + refs[4 * BMR + r] - dd);
       const float lse = none ? -INFINITY : mm + log2f(L);
       if (mine_now && sg == 0 && r < SPAN) {
-        if (w.p.part >= 0) t.pl[(int64_t)w.p.part * t.cost.rows + r] = lse;
+        if (w.p.part >= 0) t.pl[(int64_t)w.p.part * t.cost.rows + r] = attn_part(mm, L);
         else if (a.lse) a.lse[(int64_t)(w.p.row0 + by_rep(row)) * a.n_heads + w.p.g * rep + row - by_rep(row) * rep] = lse;
       }
       // 64 channels of each group, 32 at a time: each thread its row's, or, with copies of a row to add up, through shared
