@@ -133,6 +133,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+  return a;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+  return a;
+}
 
 // eight 32-bit columns from registers into tensor memory (warp-collective; not waited for)
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
@@ -575,16 +583,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
             }
           }
         }
-        // A weight is p = 2^(x fk - m) times c = 2^e for its page's value scale, l the sum of p.  Where e is moderate it goes
-        // into the exponent, and the sum is divided by c: one product less per pair.  e - m rounds to 2^-19 for
-        // |m| below 64; beyond, and for pages whose values vanish beside the others', p and c stay apart.
+        // A weight is p = 2^(x fk - m) times c = 2^e for its page's value scale, l the sum of p.  Where e and m are moderate c goes
+        // into the exponent, and the sum is divided by it: one product less per pair.  e - m and the exponents that count, those
+        // near e, round to 2^-19 below 64; beyond (large scores, pages whose values vanish beside the others') p and c stay apart.
         float e[NQ];
-        bool apart = fabsf(m) > 64.f;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          e[q] = lv[q] - d + ATTN_SHIFT;
-          apart = apart || !(fabsf(e[q]) < 100.f);
-        }
+        for (int q = 0; q < NQ; ++q) e[q] = lv[q] - d + ATTN_SHIFT;
+        float lo = e[0], hi = e[0];           // (a NaN stays)
+#pragma unroll
+        for (int q = 1; q < NQ; ++q) { lo = min_nan(lo, e[q]); hi = max_nan(hi, e[q]); }
+        const bool apart = !(lo > fmaxf(m, 0.f) - 64.f && hi < fminf(m, 0.f) + 64.f);
         auto weights = [&](auto kind) {
           constexpr bool together = decltype(kind)::value;
 #pragma unroll

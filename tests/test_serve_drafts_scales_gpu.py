@@ -1,8 +1,7 @@
 """Attention of draft trees where scores and value scales are far apart (omq_kv_attention_tree), against float64: the
-causal attention's hard inputs in all forms of the trees' kernels."""
+causal attention's hard inputs in all forms of the trees' kernels, and the log-sum-exp beside pages of vanishing values."""
 import math
 
-import numpy as np
 import pytest
 import torch
 
@@ -75,6 +74,33 @@ def test_scores_of_any_size(cuda_lib, heads, n, page, v_scale, size):
     # and beside ordinary scores: half of the pages have keys next to zero
     c.k_scale[: 10] = 2.0 ** -100
     _check(c, heads, CHAIN(n), q)
+
+
+@pytest.mark.parametrize("heads,n", ROWS)
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("low", [-20, -50, -75, -90, -100, -120])
+def test_log_sum_exp_beside_vanishing_values(cuda_lib, heads, n, page, low):
+    """Half of the pages have scores of 35 to 61 (in bits) and values of the order 2^low, the others 2 less and ordinary values.
+    The value scales are no part of the log-sum-exp: it holds to the roundings of its own size, however far the scales lie apart.
+
+    Scores are whole numbers times a power of two and the constant log2(e) / sqrt(128), which lies within 1e-8 of its
+    value in fp32 (9.1e-9, relative).  Roundings of 2^-19 (numbers from 32 to 64): a score, the log-sum-exp of a part of the tokens,
+    and of the row; where a page's factor is in the exponent, that factor less the reference, and the exponent.  The logarithm, the
+    exponentials and the sums: 2^-20."""
+    worst = 0.0
+    for i, code in enumerate((80, 108, 110, 112, 80, 71, 97, 119) * 3):
+        c = S._cache(10, page, seed=i, tail=3)
+        c.k_scale.fill_(2.0 ** -5)
+        c.v_scale.fill_(1.0)
+        for p in range(0, 10, 2):
+            c.k[S._at(c, p)] = 128 + code
+            c.k[S._at(c, p + 1)] = 128 + code - 4
+            c.v_scale[S._at(c, p)] = 2.0 ** low * (1 + i / 24)
+        q = torch.ones(n, heads * 128, device="cuda").to(BF16)
+        _, lse, _, L, _ = _run(c, heads, STAR(n), q)
+        worst = max(worst, float((lse - L).abs().max()))
+    together = abs(low) < 50                  # the factor of a page, low + 10, and that less the reference lie below 64
+    assert worst <= (5 if together else 3) * 2.0 ** -19 + 2.0 ** -20 + 1e-8 * 64, worst
 
 
 @pytest.mark.parametrize("drawn", [True, False])
