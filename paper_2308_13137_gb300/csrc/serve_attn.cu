@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(W * 32, 2)
       if (!TREE && a.n_split > 1) {
         const int64_t at = (tok * a.n_heads + head) * a.n_split + split;
         *reinterpret_cast<float4*>(a.wo + at * HD + 4 * lane) = o;
-        if (lane == 0) a.wl[at] = lse;
+        if (lane == 0) a.wl[at] = attn_part(mm, L);
       } else {
         if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
         if (a.Ob) {
@@ -483,8 +483,31 @@ __device__ __forceinline__ void write_row(const AttnArgs& a, int64_t tok, int he
   if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = lse;
 }
 
-// O = sum_s O_s 2^(lse_s - lse) over the splits that hold keys of the row, in split order; one warp per
-// (row, head)
+// O = sum_c O_c 2^(lse_c - lse) over a row's n parts in their order; a warp, four channels per lane
+template <class Place>
+__device__ __forceinline__ void join_row(int n, const float* po, const float2* pl, const Place& place, int lane, float4* out, float* lse) {
+  float top = -INFINITY;
+  for (int c = lane; c < n; c += 32) top = fmaxf(top, pl[place(c)].x);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int c = 0; c < n; ++c) {
+    const int64_t k = place(c);
+    const float2 l = pl[k];
+    const float f = ex2((l.x - ref) + l.y);
+    const float4 x = *reinterpret_cast<const float4*>(po + k * HD + 4 * lane);
+    L += f;
+    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+  }
+  const float f = L == 0.f ? 0.f : 1.f / L;
+  *out = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+  *lse = L == 0.f ? -INFINITY : ref + log2f(L);
+}
+
+// the splits that hold keys of the row; one warp per (row, head)
 __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 31;
   const int idx = blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -493,61 +516,24 @@ __global__ void __launch_bounds__(256) kv_attention_join_kernel(const AttnArgs a
   const int i = idx / a.n_heads, head = idx % a.n_heads;
   if (i >= s.nq) return;
   const int seen = max(0, min(s.len, s.len - s.nq + i + 1));
-  const int nv = (seen + a.chunk - 1) / a.chunk;
   const int64_t tok = s.row0 + i, at = (tok * a.n_heads + head) * a.n_split;
-  float top = -INFINITY;
-  for (int k = lane; k < nv; k += 32) top = fmaxf(top, a.wl[at + k]);
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int k = 0; k < nv; ++k) {
-    const float c = ex2(a.wl[at + k] - ref);
-    const float4 x = *reinterpret_cast<const float4*>(a.wo + (at + k) * HD + 4 * lane);
-    L += c;
-    o.x = fmaf(x.x, c, o.x); o.y = fmaf(x.y, c, o.y); o.z = fmaf(x.z, c, o.z); o.w = fmaf(x.w, c, o.w);
-  }
-  const float c = L == 0.f ? 0.f : 1.f / L;
-  o.x *= c; o.y *= c; o.z *= c; o.w *= c;
-  if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
-  if (a.Ob) {
-    uint2 u;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
-    h[0] = __floats2bfloat162_rn(o.x, o.y);
-    h[1] = __floats2bfloat162_rn(o.z, o.w);
-    *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
-  }
-  if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = L == 0.f ? -INFINITY : ref + log2f(L);
+  float4 o;
+  float lse;
+  join_row((seen + a.chunk - 1) / a.chunk, a.wo, a.wl, [&](int c) { return at + c; }, lane, &o, &lse);
+  write_row(a, tok, head, lane, o, lse);
 }
 
-// The same for the cut units of draft trees: a unit per blockIdx.x, its rows a warp each
+// the cut units of draft trees: a unit per blockIdx.x, its rows a warp each
 __global__ void __launch_bounds__(256) kv_attention_tree_join_kernel(const TreeArgs t) {
   const TreeCut u = t.cut[blockIdx.x];
   const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
   if (u.parts == 0 || u.r0 + r >= u.R) return;
-  auto place = [&](int c) { return (int64_t)(c == 0 ? u.first : 2 * ((int)blockIdx.x + c)) * t.cost.rows + r; };
-  float top = -INFINITY;
-  for (int c = lane; c < u.parts; c += 32) top = fmaxf(top, t.pl[place(c)].x);
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int c = 0; c < u.parts; ++c) {
-    const int64_t k = place(c);
-    const float2 l = t.pl[k];
-    const float f = ex2((l.x - ref) + l.y);
-    const float4 x = *reinterpret_cast<const float4*>(t.po + k * HD + 4 * lane);
-    L += f;
-    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
-  }
-  const float f = L == 0.f ? 0.f : 1.f / L;
   const int row = u.r0 + r;
-  write_row(t.a, u.row0 + row / t.rep, u.g * t.rep + row % t.rep, lane, make_float4(o.x * f, o.y * f, o.z * f, o.w * f),
-            L == 0.f ? -INFINITY : ref + log2f(L));
+  float4 o;
+  float lse;
+  join_row(u.parts, t.po, t.pl, [&](int c) { return (int64_t)(c == 0 ? u.first : 2 * ((int)blockIdx.x + c)) * t.cost.rows + r; }, lane, &o,
+           &lse);
+  write_row(t.a, u.row0 + row / t.rep, u.g * t.rep + row % t.rep, lane, o, lse);
 }
 
 struct Plan { int form, row_tiles, chunk, n_split; };   // form: rows per CTA, 8 or 16 (this file) or 128 (tcgen05)
@@ -577,7 +563,7 @@ Plan plan_of(int64_t B, int max_q, int max_kv, int n_heads, int n_kv) {
 size_t plan_workspace(const Plan& p, int64_t total_q, int64_t n_heads) {
   if (p.n_split <= 1) return 0;
   const size_t parts = (size_t)total_q * n_heads * p.n_split;
-  return parts * HD * sizeof(float) + (parts * sizeof(float) + 255) / 256 * 256;
+  return parts * HD * sizeof(float) + (parts * sizeof(float2) + 255) / 256 * 256;
 }
 
 template <int NT, class A>
@@ -686,7 +672,7 @@ omq_status omq_kv_attention(omq_stream_t stream, const omq_kv_cache* cache, int3
              lse, nullptr, nullptr, p.chunk, p.n_split, p.row_tiles, dev_status, nullptr, 0};
   if (p.n_split > 1) {
     a.wo = (float*)workspace;
-    a.wl = a.wo + (size_t)total_q * n_heads * p.n_split * HD;
+    a.wl = (float2*)(a.wo + (size_t)total_q * n_heads * p.n_split * HD);
   }
   cudaStream_t st = (cudaStream_t)stream;
   const dim3 grid(p.n_split * cache->n_kv * p.row_tiles, cache->B);

@@ -29,7 +29,7 @@ struct AttnArgs {
   int total_q, max_q; const int32_t* cu_q; int max_kv, n_heads;
   const __nv_bfloat16* Q; int64_t ldq;
   float* Of; __nv_bfloat16* Ob; int64_t ldo; float* lse;
-  float* wo; float* wl;                     // partial results of the splits (n_split > 1)
+  float* wo; float2* wl;                    // partial results of the splits (n_split > 1) and their log-sum-exp (attn_part)
   int chunk, n_split, row_tiles;
   int32_t* status;
   const uint32_t* seen; int words;          // draft trees (serve_tree.cuh): bits of the newest tokens that each row sees

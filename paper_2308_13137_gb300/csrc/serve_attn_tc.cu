@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int row = r0 + r;
         const int64_t at = (s.row0 + row / rep) * a.n_heads + g * rep + row % rep;
         const float lse = none ? -INFINITY : mm + log2f(L);
-        if (a.n_split > 1) a.wl[at * a.n_split + split] = lse;
+        if (a.n_split > 1) a.wl[at * a.n_split + split] = attn_part(mm, L);
         else if (a.lse) a.lse[at] = lse;
       }
 #pragma unroll 1
