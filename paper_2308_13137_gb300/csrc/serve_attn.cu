@@ -87,6 +87,19 @@ constexpr int PIECES_BYTES = (sizeof(Pieces) + 15) / 16 * 16, WIN = 256;
 __host__ __device__ __forceinline__ const AttnArgs& attn_args(const AttnArgs& a) { return a; }
 __host__ __device__ __forceinline__ const AttnArgs& attn_args(const TreeArgs& t) { return t.a; }
 
+// a row of the outputs, four channels per lane
+__device__ __forceinline__ void write_row(const AttnArgs& a, int64_t tok, int head, int lane, const float4& o, float lse) {
+  if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
+  if (a.Ob) {
+    uint2 u;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
+    h[0] = __floats2bfloat162_rn(o.x, o.y);
+    h[1] = __floats2bfloat162_rn(o.z, o.w);
+    *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
+  }
+  if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = lse;
+}
+
 // A = TreeArgs: the rows of draft trees, on CTAs that share all sequences' tokens (serve_tree.cuh); else a CTA has one chunk of
 // one sequence's tokens
 template <int NT, class A>
@@ -451,15 +464,7 @@ __global__ void __launch_bounds__(W * 32, 2)
         *reinterpret_cast<float4*>(a.wo + at * HD + 4 * lane) = o;
         if (lane == 0) a.wl[at] = attn_part(mm, L);
       } else {
-        if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
-        if (a.Ob) {
-          uint2 u;
-          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
-          h[0] = __floats2bfloat162_rn(o.x, o.y);
-          h[1] = __floats2bfloat162_rn(o.z, o.w);
-          *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
-        }
-        if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = lse;
+        write_row(a, tok, head, lane, o, lse);
       }
     }
   }
@@ -468,19 +473,6 @@ __global__ void __launch_bounds__(W * 32, 2)
   __syncthreads();
   if (*abort_flag) break;
   }
-}
-
-// a row of the outputs, four channels per lane
-__device__ __forceinline__ void write_row(const AttnArgs& a, int64_t tok, int head, int lane, const float4& o, float lse) {
-  if (a.Of) *reinterpret_cast<float4*>(a.Of + tok * a.ldo + head * HD + 4 * lane) = o;
-  if (a.Ob) {
-    uint2 u;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&u);
-    h[0] = __floats2bfloat162_rn(o.x, o.y);
-    h[1] = __floats2bfloat162_rn(o.z, o.w);
-    *reinterpret_cast<uint2*>(a.Ob + tok * a.ldo + head * HD + 4 * lane) = u;
-  }
-  if (a.lse && lane == 0) a.lse[tok * a.n_heads + head] = lse;
 }
 
 // O = sum_c O_c 2^(lse_c - lse) over a row's n parts in their order; a warp, four channels per lane

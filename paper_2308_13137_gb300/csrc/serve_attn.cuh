@@ -68,15 +68,13 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Four channels (4 lane ..) of query row `row` of KV head g as bf16, or zeros
-__device__ __forceinline__ uint2 attn_query_raw(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane) {
-  if (row >= rows) return make_uint2(0, 0);
-  return __ldg(reinterpret_cast<const uint2*>(a.Q + (int64_t)(s.row0 + row / rep) * a.ldq + (g * rep + row % rep) * ATTN_HD + 4 * lane));
-}
-
-// The same times 2^*sh: the power of two that puts the row's largest magnitude in [2^13, 2^14) (capped where 2^sh
-// would overflow).  Warp-collective.
-__device__ __forceinline__ void attn_query_scaled(const uint2& u, float (&v)[4], int* sh) {
+// Four channels (4 lane ..) of query row `row` of KV head g (zeros from `rows` on) times 2^*sh: the power of two that puts the
+// row's largest magnitude in [2^13, 2^14) (capped where 2^sh would overflow).  Warp-collective.
+__device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane,
+                                            float (&v)[4], int* sh) {
+  uint2 u = make_uint2(0, 0);
+  if (row < rows)
+    u = __ldg(reinterpret_cast<const uint2*>(a.Q + (int64_t)(s.row0 + row / rep) * a.ldq + (g * rep + row % rep) * ATTN_HD + 4 * lane));
   v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
   v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
   uint32_t big = 0;
@@ -87,11 +85,6 @@ __device__ __forceinline__ void attn_query_scaled(const uint2& u, float (&v)[4],
   const float up = __uint_as_float((uint32_t)(127 + *sh) << 23);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= up;
-}
-
-__device__ __forceinline__ void attn_query4(const AttnArgs& a, const SeqRows& s, int g, int rep, int row, int rows, int lane,
-                                            float (&v)[4], int* sh) {
-  attn_query_scaled(attn_query_raw(a, s, g, rep, row, rows, lane), v, sh);
 }
 
 // Log-sum-exp of a part of a row's tokens (reference m, sum L), and what its rounding to fp32 left out.  Parts are weighed by
