@@ -122,8 +122,9 @@ size_t tree_smem_bytes(int max_q) {
 //
 // Bound: the passes of the longest walk, one after the other, each a read of the row (from the caches after the first), 30
 // integer instructions per token, and two cluster barriers: 2 us and 2.5 for 32000 tokens, 6 and 2.5 for 128256.  64
-// sequences of up to 15 rows, 128256 tokens, 41 us; one of 26 rows, 32000 tokens, 10 to 22 us by the length of its walk.  All
-// clusters of 64 sequences are resident (four CTAs per SM, hence the registers); CTAs of 512 threads, in two waves, 61 us.
+// sequences of up to 15 rows, 128256 tokens, 35 to 46 us (bf16 41 to 54), one of 26 rows, 32000 tokens, 10 to 25 us, by the length of
+// the longest walk; with chosen drafts (one pass per sequence at most) 20 and 10 to 12 us.  All clusters of 64 sequences are
+// resident (four CTAs per SM, hence the registers); CTAs of 512 threads, in two waves, 61 us.
 // ------------------------------------------------------------------------------------------------
 constexpr int VT = 256, VW = VT / 32;       // threads, warps
 constexpr int BATCH = 2;                    // 128-token steps whose loads a warp has in flight
@@ -525,9 +526,11 @@ __device__ __forceinline__ uint4 again16(uint4 u, float r) {
 // page of larger values, and the codes of the page are rounded again then, as in the append; tokens that move within
 // the page are rounded like those that stay.  A warp per (sequence, KV head, layer), four tokens' K and V at a time, eight lanes
 // each; the CTA's eight warps share the path.  Bound: the chain of path, page, scale and codes; few registers and no barrier
-// between warps keep 32 of them on an SM: 64 sequences of 8 heads in 40 layers 13.4 us, one of 32 heads in 32 layers 7.7.  (A CTA
-// of four warps for each head and each of K and V, with the moved tokens in registers, 51.2 us; a warp for each 17.8, bound by
-// the instructions around the moves.)
+// between warps keep 32 of them on an SM: 64 sequences of 8 heads in 40 layers, 34 to 55 tokens of which move, 13.4 us, one of 32
+// heads in 32 layers (none or one moves) 4.1 to 8.  (A CTA of four warps for each head and each of K and V, with the moved tokens in
+// registers, 51.2 us; a warp for each 17.8, bound by the instructions around the moves.)  Where seven tokens of every sequence come
+// from other pages to both sides of a page's end: 34.8 and 10.2 us; where both pages grow, 203 and 59 us, since one warp rounds a
+// page's K and V (745 MB and 71 MB in all: 112 and 11 us).
 // ------------------------------------------------------------------------------------------------
 constexpr int KT = 256, KW = KT / 32;       // threads, warps
 constexpr int KEEP_LAYERS = 128;            // caches of a launch

@@ -15,15 +15,18 @@
 //            read K-major, V MN-major, both from [half][64 tokens][128 bytes] swizzled tiles
 // Tile j's converted V lies in the place j % 3, its K in one of its group's two places, its scores and weights in its group's.
 // Barriers of what one warp does in order of tiles go by place; the scores of the two groups come in no order, so theirs
-// belong to a group (a phase may be waited for only when the one before it is known to be over).  Nothing stops between chunks or
-// pieces: the next piece's queries are written, and its scores formed, before the last one's output is.
-// Bound: the softmax warps, two per scheduler: 64 scores of a row take 345 cycles of a scheduler in a loop of their own (the
-// exponentials alone 267), and with the conversion (210), the maximum (80) and the hand-offs a tile of 128 rows takes 1250; with
-// copies of rows (32 or 16 scores per thread) the hand-offs, about 1000.  A piece costs about 13000 cycles beside its tiles (queries,
-// joining, output), which short sequences feel.  Measured: 16 sequences of up to 8192 tokens, 512 rows on each of 8 KV heads, 208 us,
-// 0.82 PFLOP/s; 64 of up to 4099 tokens, up to 104 rows, 137 us; 4 of up to 131072 tokens, 32 rows, 192 us, 4.4 TB/s.
-// No role may spill much: local memory passes the small rest of the L1 here, and a tile whose softmax reloads a dozen registers
-// takes half again as long.  Two threads per row (16 softmax warps): 290 us where one took 265, bound by issue.
+// belong to a group (a phase may be waited for only when the one before it is known to be over).  Chunks of a piece follow one
+// another without a stop; between pieces the next one's queries are written, and its first scores formed, before the last one's
+// output is, by the softmax warps themselves.
+// Time: a tile of 128 rows takes 1250 cycles.  Of these a scheduler issues for 635 (64 scores of its two softmax warps' rows 345,
+// the exponentials alone 267; the maximum 80; the conversion 210) and shared memory works for 768; the rest are waits between the
+// roles, a latency and no limit of the chip.  With copies of rows (32 or 16 scores per thread) a tile takes about 1000.  A piece costs about
+// 13000 cycles beside its tiles (queries, joining, output), which short sequences feel.  Measured: 16 sequences of up to 8192 tokens,
+// 512 rows on each of 8 KV heads, 209 us, 0.82 PFLOP/s (235 us with pages of 16 tokens); 64 of up to 4099 tokens, up to 104 rows,
+// 137 us; 16 of up to 8192, 64 rows, 57 us; 4 of up to 131072 tokens, 32 rows, 190 us, 4.4 TB/s, and 64 rows, 168 us.
+// No role may spill much: local memory passes the small rest of the L1 here, and a softmax that reloads a dozen registers in every
+// tile took half again as long.  What is spilled now: 84 bytes with four pages per tile, 28 with one, 4 with copies of rows.  Two threads per
+// row (16 softmax warps): 290 us where one took 265, bound by issue.
 #include <type_traits>
 
 #include "serve_tree.cuh"
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_attention_tree_tc_kernel(const 
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
         const int sh = big == 0 ? 0 : min(13 + 127 - (int)(big >> 23), 126), i = r0 + 2 * e + (lane >> 4);
-        const float up = __uint_as_float((uint32_t)(127 + sh) << 23);         // as attn_query_scaled
+        const float up = __uint_as_float((uint32_t)(127 + sh) << 23);         // as attn_query4
         uint32_t z[4];
 #pragma unroll
         for (int o = 0; o < 4; ++o) z[o] = pack_half2(__uint_as_float(y[o] << 16) * up, __uint_as_float(y[o] & 0xffff0000u) * up);
