@@ -253,7 +253,8 @@ def verify_drafts(tree: DraftTree, tokens, probs, u, draft_probs=None, steps: Op
     distribution after every row; draft_probs, of the same type: the one from which a row's children were drawn, or
     None where they were chosen (the likeliest, say); u [rows] fp32: uniform numbers in [0, 1), a drafted row's for its test
     and row 0's for the new token.  steps: columns of the outputs, the most rows of a path (default: max_q).
-    status: an int32 device word that is set where a parent or token is out of range (a KVCache's serves)."""
+    status: an int32 device word that is set where a parent or token is out of range, or a row that the new token would be
+    drawn from adds up to nothing or to 8 and more (a KVCache's serves)."""
     if out is None:
         B = tree.cu_q.shape[0] - 1 if tree.cu_q is not None else tree.parent.shape[0] // tree.max_q
         n = tree.max_q if steps is None else steps
